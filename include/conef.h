@@ -53,9 +53,11 @@ enum {
 enum { CONEF_Q_IDENTITY = 0, CONEF_Q_RANDK = 1, CONEF_Q_LOWRANK = 2, CONEF_Q_RANDBLOCK = 3 };
 /* error compressor C (Alg. 2 line 9; Sec. 4.2) */
 enum { CONEF_C_IDENTITY = 0, CONEF_C_INT8 = 1, CONEF_C_INT4 = 2, CONEF_C_COUNTSKETCH = 3,
-       CONEF_C_ROWSKETCH = 4, CONEF_C_STOCHQUANT = 5 };
+       CONEF_C_ROWSKETCH = 4, CONEF_C_STOCHQUANT = 5, CONEF_C_MX4 = 6, CONEF_C_MX4_STOCHASTIC = 7 };
 enum { CONEF_SCALE_FP32 = 0, CONEF_SCALE_FP16 = 1 };
 /* message kinds */
+/* element types of the matrix operators */
+enum { CONEF_F32 = 0, CONEF_BF16 = 1, CONEF_F16 = 2 };
 enum { CONEF_MSG_VALUES = 0, CONEF_MSG_P = 1, CONEF_MSG_Q = 2, CONEF_MSG_DENSE1D = 3 };
 
 #define CONEF_MAX_WORKERS 64
@@ -124,6 +126,14 @@ typedef struct {
  * as int8 when s <= 127, else int16.  The uniform variate of (worker i, tensor,
  * step t, element j) is the top 24 bits of the library's 64-bit hash of j in
  * the stream (mix64(seed + i + 1), tensor, t), times 2^-24.
+ * mx4, mx4-stochastic (a 4-bit float per element, see conef_mx4_quantise): the
+ * row-major flattening of a tensor is quantised like one row of that many
+ * elements, rounded to nearest even, or stochastically by the numbers that
+ * conef_mx4_quantise draws for (seed, worker i, tensor, t).  State: two
+ * elements to a byte, then a scale byte per block of 32; `block` and
+ * scale_dtype are not read.  Unlike the other codes, a residual that is
+ * infinite or NaN makes its whole block NaN, in this step's state and, where
+ * its elements are not all sent, in those after it.  iconef has to be 0.
  * cs_chunk (count sketch only; 0 = off): the sketch of Sec. 4.2.2 applied to
  * runs of a tensor, one level below the paper's layer-wise use.  A tensor of
  * d elements is cut into nc = max(1, floor(d / cs_chunk)) runs of cs_chunk
@@ -341,6 +351,61 @@ int conef_randk_indices_noalloc(uint64_t seed, int64_t tensor, int64_t step, int
 enum { CONEF_SELECT_HALF = 4 };
 int conef_randk_indices_noalloc_select(uint64_t seed, int64_t tensor, int64_t step, int64_t d, int64_t k,
                                        int how, uint32_t *idx_out /* DEVICE */, conef_stream stream);
+
+/* ---- matrix operators: counter-based draws, dropout, microscaled 4-bit floats ----
+ *
+ * (The paper has no counterpart to these: they are what a training step does around the exchange of
+ * gradients, on the same random streams and in the same kind of code as the error state.)
+ *
+ * A matrix argument is DEVICE memory: rows of `cols` elements of type CONEF_F32, CONEF_BF16 or CONEF_F16, `ld`
+ * elements apart (ld >= cols where there is more than one row), aligned to its elements.  Sides and ld are below 2^31
+ * (CONEF_ERR_UNSUPPORTED).  Sides of zero are allowed; nothing is launched for them.  What lies
+ * between a row's end and the next row is neither read nor written.  No call allocates or synchronises; all may be captured into a graph.
+ *
+ * conef_draw names a set of random numbers.  Its stream is that of the step's own draws, with key mix64(seed +
+ * worker + 1), tensor and step; element (r, c) of a matrix of C columns has, in the stream's hash of 2 (r ceil(C/4) +
+ * floor(c/4)) (dropout) or of that + 1 (rounding), the 16 bits from 16 (c mod 4) on as its number u in 0..65535.
+ * So the numbers depend on the draw, the number of columns and the element's place alone, and a
+ * backward pass that names the draw of the forward pass has its numbers again. */
+typedef struct {
+    uint64_t seed;
+    int64_t worker, tensor, step; /* >= 0 */
+} conef_draw;
+
+/* Dropout: out = x 65536 / (65536 - f) where u >= f = rint(65536 p), else 0, plus add (of the same type) unless that is
+ * NULL; in fp32 with one rounding of the product and sum, then one to the type.  0 <= p <= 1.  A dropped element is
+ * not read into the result, be it NaN.  The gradient of x is the same call on the gradient of out (add = NULL), that of
+ * add is the gradient of out.  out may be x or add (with the same ld), else it does not overlap them. */
+int conef_dropout(const void *x, const void *add, void *out, int dtype, int64_t rows, int64_t cols, int64_t x_ld,
+                  int64_t add_ld, int64_t out_ld, double p, const conef_draw *draw /* HOST */, conef_stream stream);
+
+/* A matrix in microscaled 4-bit floats (the OCP format MXFP4): blocks of 32 consecutive elements of a row, the last of a row
+ * may be short; each element a sign and one of 0, 0.5, 1, 1.5, 2, 3, 4, 6; a scale 2^E per block.  codes: for
+ * each row ceil(cols/32) times 16 bytes, element 2q in the low and 2q + 1 in the high half of byte q, zero past the row's
+ * end.  scales: bytes E + 127 (255: NaN) in tiles of 128 rows by 4 blocks; row r, block b has byte
+ * 512 ((r/128) ceil(cols/128) + b/4) + 16 (r mod 32) + 4 (r mod 128 / 32) + b mod 4; those of rows and blocks that do not exist are zero.
+ * Both are DEVICE memory, 16-byte aligned, of the sizes that conef_mx4_bytes gives. */
+int conef_mx4_bytes(int64_t rows, int64_t cols, size_t *code_bytes /* HOST out */, size_t *scale_bytes /* HOST out */);
+
+/* Quantise x: its rows into (codes, scales), and / or the rows of its transpose (cols x rows, blocks along x's columns)
+ * into (codes_t, scales_t); a form not asked for is NULL.  E is the least, not below -127, for which no element is above
+ * 6 2^E; a block that holds an infinity or a NaN has scale 255 and codes 0.  Elements are rounded to nearest even, or
+ * (stochastic) up where floor(65536 f + 1/2) + u >= 65536, f the part of the step between the two values next to it that it lies
+ * above the smaller one in size: off by 2^-17 at most from the unbiased probability.  With p > 0 what is quantised is x behind
+ * the dropout above (rounded to fp32 once).  Both forms round an element by the same number.  draw may be NULL where
+ * nothing is drawn. */
+int conef_mx4_quantise(const void *x, int dtype, int64_t rows, int64_t cols, int64_t ld, double p, int stochastic,
+                       const conef_draw *draw /* HOST */, void *codes, void *scales, void *codes_t, void *scales_t,
+                       conef_stream stream);
+/* The values of a form, code 2^E, rounded to the type (in fp32 they are exact below 2^128, and infinite there: x above 1.75 2^127 in size
+ * is rounded to that). */
+int conef_mx4_dequantise(const void *codes, const void *scales, int64_t rows, int64_t cols, void *out, int dtype, int64_t ld,
+                         conef_stream stream);
+/* out[i][j] = sum over c < k of A[i][c] B[j][c] for forms A (m x k) and B (n x k), accumulated in fp32 and rounded once to the
+ * type.  The bytes past a row's end and the scales of rows and blocks that do not exist have to be zero, as conef_mx4_quantise
+ * leaves them.  k = 0 gives zeros. */
+int conef_mx4_matmul(const void *a_codes, const void *a_scales, int64_t m, const void *b_codes, const void *b_scales, int64_t n,
+                     int64_t k, void *out, int dtype, int64_t ld, conef_stream stream);
 
 #ifdef __cplusplus
 }

@@ -16,6 +16,8 @@ from typing import Dict, List, Optional, Sequence, Tuple
 
 import numpy as np
 
+from oracle import mx4_oracle
+
 _HERE = os.path.dirname(os.path.abspath(__file__))
 _SRC = os.path.join(_HERE, "conef_oracle.c")
 _LIB = os.path.join(_HERE, "libconef_oracle.so")
@@ -374,7 +376,7 @@ class QCfg:
 @dataclass
 class CCfg:
     """Error compressor C (Alg. 2 line 9)."""
-    kind: str = "int8"             # 'identity' | 'int8' | 'int4' | 'countsketch' | 'rowsketch' | 'stochquant'
+    kind: str = "int8"             # 'identity' | 'int8' | 'int4' | 'countsketch' | 'rowsketch' | 'stochquant' | 'mx4' | 'mx4-stochastic'
     block: int = 256
     scale_dtype: str = "fp32"      # 'fp32' | 'fp16'
     cs_rows: int = 5               # v
@@ -489,6 +491,8 @@ class ConEFOracle:
         if k == "stochquant":
             return {"levels": np.zeros(d, np.int16),
                     "scales": np.zeros((d + self.c.block - 1) // self.c.block, np.float32)}
+        if k in ("mx4", "mx4-stochastic"):
+            return {"codes": np.zeros(d, np.uint8), "scales": np.zeros((d + 31) // 32, np.uint8)}
         if k == "rowsketch":
             size = self.c.cs_rows * self.w_of(l) * self.tensors[l][1]
             if self.c.scale_dtype == "fp16":     # the sketch itself in binary16
@@ -506,6 +510,8 @@ class ConEFOracle:
             return quant_decode(st["codes"], st["scales"], self.d_of(l), self.c.block, self._bits())
         if k == "stochquant":
             return stochquant_decode(st["levels"], st["scales"], self.c.block)
+        if k in ("mx4", "mx4-stochastic"):
+            return mx4_oracle.decode(st["codes"][None], st["scales"][None])[0].astype(np.float32)
         if k == "rowsketch":
             n, m, _ = self.tensors[l]
             if "T16" in st:
@@ -554,6 +560,10 @@ class ConEFOracle:
             rnd = uniform24(self.c.seed, i, l, t, r.size)
             lv, sc = stochquant_encode(r, rnd, self.c.block, self.c.levels)
             store[i][l] = {"levels": lv, "scales": sc}
+        elif k in ("mx4", "mx4-stochastic"):
+            u = mx4_oracle.numbers(self.c.seed, i, l, t, 1, r.size, mx4_oracle.ROUNDING) if k == "mx4-stochastic" else None
+            codes, scales = mx4_oracle.encode(r[None].astype(np.float64), u)
+            store[i][l] = {"codes": codes[0], "scales": scales[0]}
         elif k == "identity":
             store[i][l] = {"e": r.copy()}
         elif k in ("int8", "int4"):

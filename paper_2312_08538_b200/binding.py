@@ -7,9 +7,10 @@ fallback.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes as C
 import os
-from typing import Dict, List, Optional, Sequence, Tuple
+from typing import Dict, List, NamedTuple, Optional, Sequence, Tuple, Union
 
 import torch
 
@@ -21,7 +22,8 @@ ERR_INVALID_ARG, ERR_BAD_PHASE, ERR_WORKSPACE_TOO_SMALL, ERR_UNSUPPORTED, ERR_CU
     ERR_TOO_LARGE = -1, -2, -3, -4, -5, -6, -7
 NOALLOC_MAX_ELEMS = 1 << 24
 Q_IDENTITY, Q_RANDK, Q_LOWRANK, Q_RANDBLOCK = 0, 1, 2, 3
-C_IDENTITY, C_INT8, C_INT4, C_COUNTSKETCH, C_ROWSKETCH, C_STOCHQUANT = 0, 1, 2, 3, 4, 5
+C_IDENTITY, C_INT8, C_INT4, C_COUNTSKETCH, C_ROWSKETCH, C_STOCHQUANT, C_MX4, C_MX4_STOCHASTIC = 0, 1, 2, 3, 4, 5, 6, 7
+F32, BF16, F16 = 0, 1, 2
 SCALE_FP32, SCALE_FP16 = 0, 1
 MSG_VALUES, MSG_P, MSG_Q, MSG_DENSE1D = 0, 1, 2, 3
 SELECT_NORMAL, SELECT_MISS, SELECT_FULL, SELECT_STALE, SELECT_HALF = 0, 1, 2, 3, 4
@@ -34,7 +36,8 @@ EXPORTS = ["conef_workspace_bytes", "conef_init", "conef_step", "conef_reduce_me
            "conef_set_fast_path", "conef_set_select", "conef_set_total_workers", "conef_error_string", "conef_randk_indices_noalloc",
            "conef_randk_indices_noalloc_select",
            "conef_get_error_step", "conef_set_error_step", "conef_set_fused", "conef_fused_info",
-           "conef_get_fused_q"]
+           "conef_get_fused_q",
+           "conef_dropout", "conef_mx4_bytes", "conef_mx4_quantise", "conef_mx4_dequantise", "conef_mx4_matmul"]
 
 
 class conef_tensor(C.Structure):
@@ -50,6 +53,11 @@ class conef_c_cfg(C.Structure):
     _fields_ = [("kind", C.c_int32), ("block", C.c_int32), ("scale_dtype", C.c_int32),
                 ("cs_rows", C.c_int32), ("cs_col_div", C.c_int64), ("seed", C.c_uint64),
                 ("beta", C.c_float), ("levels", C.c_int32), ("iconef", C.c_int32), ("cs_chunk", C.c_int32)]
+
+
+class Draw(C.Structure):
+    """A set of counter-based random numbers (conef_draw): seed, worker, tensor, step."""
+    _fields_ = [("seed", C.c_uint64), ("worker", C.c_int64), ("tensor", C.c_int64), ("step", C.c_int64)]
 
 
 def _load() -> C.CDLL:
@@ -93,6 +101,11 @@ def _load() -> C.CDLL:
     L.conef_get_fused_q.argtypes = [vp, i32, i32, C.POINTER(vp)]
     L.conef_randk_indices_noalloc.argtypes = [C.c_uint64, i64, i64, i64, i64, vp, vp]
     L.conef_randk_indices_noalloc_select.argtypes = [C.c_uint64, i64, i64, i64, i64, i32, vp, vp]
+    L.conef_dropout.argtypes = [vp, vp, vp, i32, i64, i64, i64, i64, i64, C.c_double, C.POINTER(Draw), vp]
+    L.conef_mx4_bytes.argtypes = [i64, i64, C.POINTER(C.c_size_t), C.POINTER(C.c_size_t)]
+    L.conef_mx4_quantise.argtypes = [vp, i32, i64, i64, i64, C.c_double, i32, C.POINTER(Draw), vp, vp, vp, vp, vp]
+    L.conef_mx4_dequantise.argtypes = [vp, vp, i64, i64, vp, i32, i64, vp]
+    L.conef_mx4_matmul.argtypes = [vp, vp, i64, vp, vp, i64, i64, vp, i32, i64, vp]
     L.conef_error_string.argtypes = [i32]
     L.conef_error_string.restype = C.c_char_p
     return L
@@ -114,7 +127,7 @@ def _check(code: int, where: str) -> None:
 
 _QK = {"identity": Q_IDENTITY, "randk": Q_RANDK, "lowrank": Q_LOWRANK, "randblock": Q_RANDBLOCK}
 _CK = {"identity": C_IDENTITY, "int8": C_INT8, "int4": C_INT4, "countsketch": C_COUNTSKETCH,
-       "rowsketch": C_ROWSKETCH, "stochquant": C_STOCHQUANT}
+       "rowsketch": C_ROWSKETCH, "stochquant": C_STOCHQUANT, "mx4": C_MX4, "mx4-stochastic": C_MX4_STOCHASTIC}
 
 
 def make_tensors(tensors: Sequence[Tuple[int, int, int]]):
@@ -171,6 +184,164 @@ def conef_randk_indices_noalloc_select(seed: int, tensor: int, step: int, d: int
     assert idx_out.is_cuda and idx_out.element_size() == 4 and idx_out.numel() >= k and idx_out.is_contiguous()
     _check(lib.conef_randk_indices_noalloc_select(int(seed), int(tensor), int(step), int(d), int(k), int(how), idx_out.data_ptr(),
                                                   _stream_handle(stream)), "conef_randk_indices_noalloc_select")
+
+
+# ---- matrix operators: dropout, microscaled 4-bit floats
+#
+# The last dimension of a tensor is a matrix' columns, those before it are its rows; a row's elements are adjacent, and rows
+# are evenly spaced (a slice of columns is taken as it is, other strides are refused).  Work is enqueued on `stream` (default:
+# the current stream of the tensors' device), on which outputs are allocated too.
+
+_ELEM = {torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16}
+
+
+def _refuse(where: str, why: str) -> None:
+    raise ConEFError(ERR_INVALID_ARG, f"{where}: {why}")
+
+
+def _matrix(x: torch.Tensor, where: str, name: str = "x") -> Tuple[int, int, int]:
+    """(rows, cols, elements from row to row) of a tensor."""
+    if not x.is_cuda:
+        _refuse(where, f"{name} has to be on a GPU")
+    if x.dtype not in _ELEM:
+        _refuse(where, f"{name} has to be float32, bfloat16 or float16")
+    shape = x.shape
+    if len(shape) == 0:
+        _refuse(where, f"{name} has no dimension")
+    cols = shape[-1]
+    rows = shape[0] if len(shape) == 2 else x.numel() // cols if cols else shape[:-1].numel()
+    if x.is_contiguous():
+        return rows, cols, cols
+    stride = x.stride()
+    if cols > 1 and stride[-1] != 1:
+        _refuse(where, f"the elements of a row of {name} are not adjacent")
+    ld, expect = cols, None
+    for size, step in zip(reversed(shape[:-1]), reversed(stride[:-1])):
+        if size == 1:
+            continue
+        if expect is None:
+            ld = step
+        elif step != expect:
+            _refuse(where, f"the rows of {name} are not evenly spaced")
+        expect = step * size
+    if rows > 1 and ld < cols:
+        _refuse(where, f"the rows of {name} overlap")
+    return rows, cols, ld
+
+
+_NOTHING = contextlib.nullcontext()
+
+
+def _on(device: torch.device, stream: Optional[torch.cuda.Stream]):
+    """The tensors' device and the caller's stream as the current ones, where they are not."""
+    if stream is not None:
+        return torch.cuda.stream(stream)
+    return _NOTHING if device.index == torch._C._cuda_getDevice() else torch.cuda.device(device)
+
+
+def _same_device(where: str, device: torch.device, stream: Optional[torch.cuda.Stream], *tensors: torch.Tensor) -> None:
+    for t in tensors:
+        if t.device != device:
+            _refuse(where, "the tensors are on different devices")
+    if stream is not None and stream.device != device:
+        _refuse(where, "the stream belongs to another device than the tensors")
+
+
+def dropout(x: torch.Tensor, p: float, draw: Draw, add: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None,
+            stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
+    """x behind a dropout with probability p (a multiple of 2^-16), plus `add`.  The mask comes from `draw` and is not stored:
+    the gradient of x is this call on the gradient of the result, with the same draw and without `add`."""
+    rows, cols, ld = _matrix(x, "dropout")
+    add_ld = out_ld = cols
+    for t, name in ((add, "add"), (out, "out")):
+        if t is not None and (t.shape != x.shape or t.dtype != x.dtype):
+            _refuse("dropout", f"{name} differs from x in shape or type")
+    if add is not None:
+        add_ld = _matrix(add, "dropout", "add")[2]
+    if out is not None:
+        out_ld = _matrix(out, "dropout", "out")[2]
+    device = x.device
+    _same_device("dropout", device, stream, *(t for t in (add, out) if t is not None))
+    with _on(device, stream):
+        if out is None:
+            out = torch.empty(x.shape, dtype=x.dtype, device=device)
+        _check(lib.conef_dropout(x.data_ptr(), None if add is None else add.data_ptr(), out.data_ptr(), _ELEM[x.dtype], rows, cols, ld, add_ld,
+                                 out_ld, p, draw, _stream_handle(None)), "conef_dropout")
+    return out
+
+
+class MX4(NamedTuple):
+    """A rows x cols matrix in microscaled 4-bit floats, as conef_mx4_quantise leaves it: flat or shaped uint8 tensors."""
+    rows: int
+    cols: int
+    codes: torch.Tensor
+    scales: torch.Tensor
+
+
+def _mx4_sizes(rows: int, cols: int) -> Tuple[int, int]:
+    return rows * ((cols + 31) // 32) * 16, (rows + 127) // 128 * ((cols + 127) // 128) * 512
+
+
+def _mx4_check(a: MX4, where: str) -> None:
+    if a.rows < 0 or a.cols < 0:
+        _refuse(where, "a size is negative")
+    for t, size, name in zip((a.codes, a.scales), _mx4_sizes(a.rows, a.cols), ("codes", "scales")):
+        if not t.is_cuda or t.dtype != torch.uint8 or not t.is_contiguous() or t.numel() != size:
+            _refuse(where, f"the {name} of a {a.rows} x {a.cols} form are {size} contiguous uint8 on a GPU")
+
+
+def mx4_quantise(x: torch.Tensor, forms: str = "rows", stochastic: bool = False, p: float = 0.0, draw: Optional[Draw] = None,
+                 stream: Optional[torch.cuda.Stream] = None) -> Union[MX4, Tuple[MX4, MX4]]:
+    """x in microscaled 4-bit floats: forms = "rows", "cols" (the form of x's transpose) or "both" (a pair, from one reading of x).
+    With p > 0 what is quantised is dropout(x, p, draw)."""
+    rows, cols, ld = _matrix(x, "mx4_quantise")
+    if forms not in ("rows", "cols", "both"):
+        _refuse("mx4_quantise", "forms has to be rows, cols or both")
+    device = x.device
+    _same_device("mx4_quantise", device, stream)
+    with _on(device, stream):
+        def form(r: int, c: int) -> MX4:
+            code_bytes, scale_bytes = _mx4_sizes(r, c)
+            return MX4(r, c, torch.empty(code_bytes, dtype=torch.uint8, device=device), torch.empty(scale_bytes, dtype=torch.uint8, device=device))
+        a = form(rows, cols) if forms != "cols" else None
+        t = form(cols, rows) if forms != "rows" else None
+        ptr = [None if f is None else v.data_ptr() for f in (a, t) for v in ((f.codes, f.scales) if f else (None, None))]
+        if rows and cols:
+            _check(lib.conef_mx4_quantise(x.data_ptr(), _ELEM[x.dtype], rows, cols, ld, p, int(bool(stochastic)), draw, *ptr, _stream_handle(None)),
+                   "conef_mx4_quantise")
+    return (a, t) if forms == "both" else a if t is None else t
+
+
+def mx4_dequantise(a: MX4, dtype: torch.dtype = torch.float32, stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
+    """The values of a form, rows x cols."""
+    _mx4_check(a, "mx4_dequantise")
+    if dtype not in _ELEM:
+        _refuse("mx4_dequantise", "dtype has to be float32, bfloat16 or float16")
+    device = a.codes.device
+    _same_device("mx4_dequantise", device, stream, a.scales)
+    with _on(device, stream):
+        out = torch.empty(a.rows, a.cols, dtype=dtype, device=device)
+        _check(lib.conef_mx4_dequantise(a.codes.data_ptr(), a.scales.data_ptr(), a.rows, a.cols, out.data_ptr(), _ELEM[dtype], a.cols,
+                                        _stream_handle(None)), "conef_mx4_dequantise")
+    return out
+
+
+def mx4_matmul(a: MX4, b: MX4, dtype: torch.dtype = torch.bfloat16, stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
+    """a b^T (a.rows x b.rows): rows of both against each other.  With Y = X W^T for activations X (tokens x in) and weights W
+    (out x in), dX = dY W takes the form of W's transpose, dW = dY^T X those of dY's and X's transposes."""
+    _mx4_check(a, "mx4_matmul")
+    _mx4_check(b, "mx4_matmul")
+    if a.cols != b.cols:
+        _refuse("mx4_matmul", f"rows of {a.cols} against rows of {b.cols}")
+    if dtype not in _ELEM:
+        _refuse("mx4_matmul", "dtype has to be float32, bfloat16 or float16")
+    device = a.codes.device
+    _same_device("mx4_matmul", device, stream, a.scales, b.codes, b.scales)
+    with _on(device, stream):
+        out = torch.empty(a.rows, b.rows, dtype=dtype, device=device)
+        _check(lib.conef_mx4_matmul(a.codes.data_ptr(), a.scales.data_ptr(), a.rows, b.codes.data_ptr(), b.scales.data_ptr(), b.rows, a.cols,
+                                    out.data_ptr(), _ELEM[dtype], b.rows, _stream_handle(None)), "conef_mx4_matmul")
+    return out
 
 
 class ConEF:

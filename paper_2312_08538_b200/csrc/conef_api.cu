@@ -13,6 +13,8 @@
 #include "conef_internal.h"
 #include "conef_kernels.cuh"
 #include "conef_hash.cuh"
+#include "conef_elem.cuh"
+#include "conef_mx4.cuh"
 #include "conef_randk.cuh"
 #include "conef_rowsketch.cuh"
 #include "conef_apply.cuh"
@@ -139,7 +141,7 @@ int make_plan(const conef_tensor *tensors, int n_tensors, int n_workers, const c
         return CONEF_ERR_UNSUPPORTED;
     if (q->kind < CONEF_Q_IDENTITY || q->kind > CONEF_Q_RANDBLOCK)
         return CONEF_ERR_INVALID_ARG;
-    if (c->kind < CONEF_C_IDENTITY || c->kind > CONEF_C_STOCHQUANT)
+    if (c->kind < CONEF_C_IDENTITY || c->kind > CONEF_C_MX4_STOCHASTIC)
         return CONEF_ERR_INVALID_ARG;
     if (!(c->beta >= 0.f && c->beta < 1.f) || c->iconef < 0 || c->iconef > 2)
         return CONEF_ERR_INVALID_ARG;
@@ -175,6 +177,9 @@ int make_plan(const conef_tensor *tensors, int n_tensors, int n_workers, const c
             return CONEF_ERR_INVALID_ARG;
         unit = b;
     }
+    const bool mx4 = c->kind == CONEF_C_MX4 || c->kind == CONEF_C_MX4_STOCHASTIC;
+    if (mx4)
+        unit = kMx4Block;
     if (c->kind == CONEF_C_ROWSKETCH) {
         if (c->scale_dtype != CONEF_SCALE_FP32 && c->scale_dtype != CONEF_SCALE_FP16)
             return CONEF_ERR_INVALID_ARG;
@@ -265,7 +270,9 @@ int make_plan(const conef_tensor *tensors, int n_tensors, int n_workers, const c
             switch (c->kind) {
             case CONEF_C_IDENTITY: L.a_bytes = L.d * 4; break;
             case CONEF_C_INT8: L.a_bytes = L.d; break;
-            case CONEF_C_INT4: L.a_bytes = (L.d + 1) / 2; break;
+            case CONEF_C_INT4:
+            case CONEF_C_MX4:
+            case CONEF_C_MX4_STOCHASTIC: L.a_bytes = (L.d + 1) / 2; break;
             case CONEF_C_STOCHQUANT: L.a_bytes = L.d * (c->levels > 127 ? 2 : 1); break;
             case CONEF_C_ROWSKETCH:
                 L.w = L.rows / c->cs_col_div < 1 ? 1 : L.rows / c->cs_col_div;
@@ -283,9 +290,9 @@ int make_plan(const conef_tensor *tensors, int n_tensors, int n_workers, const c
                 L.a_bytes = (int64_t)c->cs_rows * L.w * 4;
             }
             state_off += (int64_t)align_up((size_t)L.a_bytes);
-            if (c->kind == CONEF_C_INT8 || c->kind == CONEF_C_INT4 || c->kind == CONEF_C_STOCHQUANT) {
+            if (c->kind == CONEF_C_INT8 || c->kind == CONEF_C_INT4 || c->kind == CONEF_C_STOCHQUANT || mx4) {
                 L.b_off = state_off;
-                L.b_bytes = L.nunits * (c->kind == CONEF_C_STOCHQUANT ? 4 : scale_bytes);
+                L.b_bytes = L.nunits * (c->kind == CONEF_C_STOCHQUANT ? 4 : mx4 ? 1 : scale_bytes);
                 state_off += (int64_t)align_up((size_t)L.b_bytes);
             }
             if (c->iconef == 1) {   // the second state q (Alg. 3), laid out like the first
@@ -793,6 +800,8 @@ int launch_flat(conef_ctx *ctx, DevView V, cudaStream_t s, int table = T_FLAT)
     case CONEF_C_INT8: k_flat<QK, CONEF_C_INT8><<<grid, kFlatThreads, 0, s>>>(V); break;
     case CONEF_C_INT4: k_flat<QK, CONEF_C_INT4><<<grid, kFlatThreads, 0, s>>>(V); break;
     case CONEF_C_STOCHQUANT: k_flat<QK, CONEF_C_STOCHQUANT><<<grid, kFlatThreads, 0, s>>>(V); break;
+    case CONEF_C_MX4:
+    case CONEF_C_MX4_STOCHASTIC: k_flat<QK, CONEF_C_MX4><<<grid, kFlatThreads, 0, s>>>(V); break;
     default: k_flat<QK, CONEF_C_COUNTSKETCH><<<grid, kFlatThreads, 0, s>>>(V); break;
     }
     LAUNCH_CHECK(ctx);
@@ -832,6 +841,8 @@ int launch_pass1(conef_ctx *ctx, DevView V, cudaStream_t s, int table = T_P1)
     case CONEF_C_INT4: k_lr_pass1<CONEF_C_INT4><<<grid, 256, 0, s>>>(V); break;
     case CONEF_C_ROWSKETCH: k_lr_pass1<CONEF_C_ROWSKETCH><<<grid, 256, 0, s>>>(V); break;
     case CONEF_C_STOCHQUANT: k_lr_pass1<CONEF_C_STOCHQUANT><<<grid, 256, 0, s>>>(V); break;
+    case CONEF_C_MX4:
+    case CONEF_C_MX4_STOCHASTIC: k_lr_pass1<CONEF_C_MX4><<<grid, 256, 0, s>>>(V); break;
     default: k_lr_pass1<CONEF_C_COUNTSKETCH><<<grid, 256, 0, s>>>(V); break;
     }
     LAUNCH_CHECK(ctx);
@@ -851,6 +862,8 @@ int launch_pass2(conef_ctx *ctx, DevView V, cudaStream_t s, int table = T_P2)
     case CONEF_C_INT4: k_lr_pass2<CONEF_C_INT4><<<grid, kP2ColsPerCta, 0, s>>>(V); break;
     case CONEF_C_ROWSKETCH: k_lr_pass2<CONEF_C_ROWSKETCH><<<grid, kP2ColsPerCta, 0, s>>>(V); break;
     case CONEF_C_STOCHQUANT: k_lr_pass2<CONEF_C_STOCHQUANT><<<grid, kP2ColsPerCta, 0, s>>>(V); break;
+    case CONEF_C_MX4:
+    case CONEF_C_MX4_STOCHASTIC: k_lr_pass2<CONEF_C_MX4><<<grid, kP2ColsPerCta, 0, s>>>(V); break;
     default: k_lr_pass2<CONEF_C_COUNTSKETCH><<<grid, kP2ColsPerCta, 0, s>>>(V); break;
     }
     LAUNCH_CHECK(ctx);
@@ -1155,6 +1168,14 @@ int launch_randk_select(conef_ctx *ctx, const DevView &V, cudaStream_t s)
 }
 
 }  // namespace
+
+int conef::launched(cudaError_t e, const char *what)
+{
+    if (e == cudaSuccess)
+        return CONEF_OK;
+    g_last_cuda_error = std::string(what) + ": " + cudaGetErrorString(e);
+    return CONEF_ERR_CUDA;
+}
 
 extern "C" {
 
@@ -1697,6 +1718,8 @@ int conef_decompress_error(conef_ctx *ctx, int worker, float *out, conef_stream 
     case CONEF_C_INT4: k_decompress<CONEF_C_INT4><<<n, 256, 0, s>>>(V, worker, out); break;
     case CONEF_C_ROWSKETCH: k_decompress<CONEF_C_ROWSKETCH><<<n, 256, 0, s>>>(V, worker, out); break;
     case CONEF_C_STOCHQUANT: k_decompress<CONEF_C_STOCHQUANT><<<n, 256, 0, s>>>(V, worker, out); break;
+    case CONEF_C_MX4:
+    case CONEF_C_MX4_STOCHASTIC: k_decompress<CONEF_C_MX4><<<n, 256, 0, s>>>(V, worker, out); break;
     default: k_decompress<CONEF_C_COUNTSKETCH><<<n, 256, 0, s>>>(V, worker, out); break;
     }
     LAUNCH_CHECK(ctx);

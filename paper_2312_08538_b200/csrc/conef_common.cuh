@@ -7,6 +7,7 @@
 
 #include "conef_internal.h"
 #include "conef_hash.cuh"
+#include "conef_mx4.cuh"
 
 namespace conef {
 
@@ -382,6 +383,10 @@ __device__ __forceinline__ float decode_elem(const DevView &V, const LayerDesc &
     if (CK == CONEF_C_STOCHQUANT) {
         const int c = V.sq_wide ? (int)((const short *)(st + L.a_off))[j] : (int)((const signed char *)(st + L.a_off))[j];
         return __fmul_rn((float)c, ((const float *)(st + L.b_off))[j / (uint32_t)L.unit]);
+    }
+    if (CK == CONEF_C_MX4) {
+        const uint32_t code = (uint32_t)(st + L.a_off)[j >> 1] >> (4 * (j & 1u)) & 0xFu;
+        return __fmul_rn(mx4_value(code), mx4_pow((st + L.b_off)[j / (uint32_t)kMx4Block]));
     }
     if (CK == CONEF_C_ROWSKETCH) {
         // row sketch: median over sketch rows of s_i(a) * T_i[h_i(a)][b]; buckets and signs of

@@ -245,6 +245,22 @@ __global__ void __launch_bounds__(kFlatThreads) k_flat(const __grid_constant__ D
                         ((signed char *)(st + L.a_off))[j] = (signed char)c;
                 }
             }
+        } else if (CK == CONEF_C_MX4) {
+            // (a block has as many elements as a warp has lanes)
+            const uint32_t byte = mx4_scale(__reduce_max_sync(0xffffffffu, __float_as_uint(val[0]) & 0x7FFFFFFFu));
+            const float v = __fmul_rn(val[0], mx4_inv(byte));
+            uint32_t code;
+            if (V.ckind == CONEF_C_MX4_STOCHASTIC) {
+                const uint64_t stc = draw_stream(V.seed_c, worker, li, V.step);
+                code = mx4_stochastic(v, draw_of(draw_word(stc, base >> 2, kDrawRounding), base));
+            } else
+                code = mx4_nearest2(v, 0.f) & 0xFu;
+            code = byte == kMx4Nan ? 0u : code;
+            code |= __shfl_down_sync(0xffffffffu, code, 1) << 4;
+            if (lane == 0)
+                (st + L.b_off)[unit] = (uint8_t)byte;
+            if (base < d && !(lane & 1))
+                (st + L.a_off)[base >> 1] = (uint8_t)code;
         } else if (CK == CONEF_C_COUNTSKETCH) {
             float *S = (float *)(V.state_new + worker * V.state_stride + L.a_off);
 #pragma unroll
