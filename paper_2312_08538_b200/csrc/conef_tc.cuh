@@ -1,0 +1,126 @@
+// Inline PTX for the fifth-generation tensor cores: barriers in shared memory, asynchronous copies of tiles, tensor memory and the
+// block-scaled product of 4-bit floats.
+#pragma once
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+namespace conef {
+namespace tc {
+
+__device__ __forceinline__ uint32_t saddr(const void *p) { return (uint32_t)__cvta_generic_to_shared(p); }
+
+// ------------------------------------------------------------------ barriers
+__device__ __forceinline__ void bar_init(uint64_t *bar, uint32_t count) { asm volatile("mbarrier.init.shared.b64 [%0], %1;" ::"r"(saddr(bar)), "r"(count) : "memory"); }
+__device__ __forceinline__ void bar_arrive(uint64_t *bar) { asm volatile("mbarrier.arrive.shared.b64 _, [%0];" ::"r"(saddr(bar)) : "memory"); }
+__device__ __forceinline__ void bar_expect(uint64_t *bar, uint32_t bytes)
+{
+    asm volatile("mbarrier.arrive.expect_tx.shared.b64 _, [%0], %1;" ::"r"(saddr(bar)), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ bool bar_try(uint64_t *bar, uint32_t parity)
+{
+    uint32_t ok;
+    asm volatile("{\n\t.reg .pred q;\n\tmbarrier.try_wait.parity.shared.b64 q, [%1], %2;\n\tselp.u32 %0, 1, 0, q;\n\t}" : "=r"(ok) : "r"(saddr(bar)), "r"(parity) : "memory");
+    return ok != 0;
+}
+__device__ __forceinline__ uint64_t nanoseconds()
+{
+    uint64_t t;
+    asm volatile("mov.u64 %0, %globaltimer;" : "=l"(t));
+    return t;
+}
+// Waits for a phase, for two seconds at most (a product takes milliseconds): past that, or once another warp's wait has
+// run out, *dead is set and the answer is no.
+constexpr uint64_t kLimit = 2000000000ull;
+__device__ __forceinline__ bool bar_wait(uint64_t *bar, uint32_t parity, volatile int *dead)
+{
+    if (bar_try(bar, parity))
+        return true;
+    const uint64_t t0 = nanoseconds();
+    for (;;) {
+        for (int i = 0; i < 64; ++i)
+            if (bar_try(bar, parity))
+                return true;
+        if (*dead)
+            return false;
+        if (nanoseconds() - t0 > kLimit) {
+            *dead = 1;
+            return false;
+        }
+    }
+}
+// ... of copies or products in flight that nobody will use: the same limit, whatever *dead says
+__device__ __forceinline__ void bar_drain(uint64_t *bar, uint32_t parity)
+{
+    const uint64_t t0 = nanoseconds();
+    while (!bar_try(bar, parity) && nanoseconds() - t0 <= kLimit) {
+    }
+}
+
+// ------------------------------------------------------------------ asynchronous copies into shared memory
+__device__ __forceinline__ void tile_load(void *dst, const void *map, int x, int y, uint64_t *bar)
+{
+    asm volatile("cp.async.bulk.tensor.2d.shared::cta.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(saddr(dst)), "l"(map),
+                 "r"(x), "r"(y), "r"(saddr(bar))
+                 : "memory");
+}
+__device__ __forceinline__ void bulk_load(void *dst, const void *src, uint32_t bytes, uint64_t *bar)
+{
+    asm volatile("cp.async.bulk.shared::cta.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(saddr(dst)), "l"(src), "r"(bytes), "r"(saddr(bar))
+                 : "memory");
+}
+
+// ------------------------------------------------------------------ tensor memory
+__device__ __forceinline__ void tmem_alloc(uint32_t *where, uint32_t columns)   // a whole warp
+{
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(saddr(where)), "r"(columns) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+}
+__device__ __forceinline__ void tmem_free(uint32_t at, uint32_t columns)   // the same warp
+{
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(at), "r"(columns) : "memory");
+}
+__device__ __forceinline__ void fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+// 32 columns of the warp's 32 lanes
+__device__ __forceinline__ void tmem_load32(uint32_t at, uint32_t (&v)[32])
+{
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, %17, %18, %19, %20, %21, "
+                 "%22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
+                 : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]), "=r"(v[8]), "=r"(v[9]), "=r"(v[10]),
+                   "=r"(v[11]), "=r"(v[12]), "=r"(v[13]), "=r"(v[14]), "=r"(v[15]), "=r"(v[16]), "=r"(v[17]), "=r"(v[18]), "=r"(v[19]), "=r"(v[20]),
+                   "=r"(v[21]), "=r"(v[22]), "=r"(v[23]), "=r"(v[24]), "=r"(v[25]), "=r"(v[26]), "=r"(v[27]), "=r"(v[28]), "=r"(v[29]), "=r"(v[30]),
+                   "=r"(v[31])
+                 : "r"(at));
+}
+__device__ __forceinline__ void tmem_load_wait() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+
+// ------------------------------------------------------------------ products
+// Descriptor of an operand in shared memory, rows of 128 bytes along k, eight rows to a 1024-byte group, 16-byte pieces exchanged
+// within a group as the tile copy with the 128-byte pattern leaves them
+__device__ __forceinline__ uint64_t desc_rows128(const void *p)
+{
+    return (uint64_t)((saddr(p) & 0x3FFFFu) >> 4) | (1ull << 16) | (64ull << 32) | (1ull << 46) | (2ull << 61);
+}
+// ... of 32 rows of 16 bytes, one behind the other (a tile of scales)
+__device__ __forceinline__ uint64_t desc_scales(const void *p)
+{
+    return (uint64_t)((saddr(p) & 0x3FFFFu) >> 4) | (1ull << 16) | (8ull << 32) | (1ull << 46);
+}
+// 512 bytes into four columns, the 32 rows to the lanes of each of the four warps
+__device__ __forceinline__ void scales_copy(uint32_t at, uint64_t desc) { asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(at), "l"(desc) : "memory"); }
+
+// 4-bit floats with power-of-two scales, 128 rows of A, n of B (a multiple of 8 up to 256), both along k
+__device__ __forceinline__ uint32_t mx4_instruction(uint32_t n) { return (1u << 7) | (1u << 10) | ((n >> 3) << 17) | (1u << 23) | (8u << 24); }
+// 64 elements along k; `half`: which two of the four scales in a column's word are theirs
+__device__ __forceinline__ void mx4_product(uint32_t d, uint64_t a, uint64_t b, uint32_t instruction, uint32_t half, uint32_t sa, uint32_t sb, bool add)
+{
+    instruction |= (half << 5) | (half << 30);   // (scale number 0 or 2, of B and of A)
+    asm volatile("{\n\t.reg .pred q;\n\tsetp.ne.u32 q, %6, 0;\n\ttcgen05.mma.cta_group::1.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%4], [%5], q;\n\t}" ::"r"(d),
+                 "l"(a), "l"(b), "r"(instruction), "r"(sa), "r"(sb), "r"((uint32_t)add)
+                 : "memory");
+}
+// the barrier is told when all that this thread has issued is done
+__device__ __forceinline__ void commit(uint64_t *bar) { asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(saddr(bar)) : "memory"); }
+
+}  // namespace tc
+}  // namespace conef
