@@ -18,7 +18,8 @@ namespace conef {
 constexpr int kMmM = 128, kMmK = 256;                    // rows of A per tile, elements of k per stage
 constexpr int kMmEpilogue = 8, kMmThreads = (kMmEpilogue + 2) * 32;
 constexpr int kMmMaxStages = 6;
-constexpr uint32_t kMmColumns = 512, kMmScaleColumn = 256;   // tensor memory: the sums, then 32 columns of scales per stage (24 used)
+// tensor memory, all of it, so from column 0 on: the sums, then 32 columns of scales per stage (24 used)
+constexpr uint32_t kMmColumns = 512, kMmScaleColumn = 256;
 
 struct MmArgs {
     const uint8_t *as, *bs;      // scales
@@ -109,8 +110,6 @@ __global__ void __launch_bounds__(kMmThreads, 1) k_mx4_matmul(const __grid_const
     tc::fence_after();
     grid_release();
     grid_wait();
-    const uint32_t tmem = S.tmem;
-
     if (warp == kMmEpilogue) {
         if (lane == 0) {
             uint32_t s = 0, phase = 0, armed = 0;
@@ -144,41 +143,47 @@ __global__ void __launch_bounds__(kMmThreads, 1) k_mx4_matmul(const __grid_const
         }
         __syncwarp();
     } else if (warp == kMmEpilogue + 1) {
-        if (lane == 0) {
-            const uint32_t instruction = tc::mx4_instruction(P.bn);
-            uint32_t s = 0, phase = 0, turn = 0;
-            bool ok = true;
-            for (uint32_t tile = blockIdx.x; ok && tile < P.n_tiles; tile += gridDim.x, turn ^= 1u) {
-                const uint32_t n0 = tile / P.tiles_m * P.bn;
-                const uint32_t shift = (n0 & 127u) >> 5;   // columns of the first tile of scales ahead of row n0
-                if (!(ok = tc::bar_wait(&S.taken, turn ^ 1u, dead)))
+        const uint32_t e = tc::elect(), instruction = tc::mx4_instruction(P.bn);
+        const uint32_t a0 = tc::desc_low(ring), b0 = a0 + kMmM * 8, sc0 = b0 + P.bn * 8, step16 = stage_bytes >> 4;
+        uint32_t s = 0, phase = 0, turn = 0;
+        bool ok = true;
+        for (uint32_t tile = blockIdx.x; ok && tile < P.n_tiles; tile += gridDim.x, turn ^= 1u) {
+            const uint32_t n0 = tile / P.tiles_m * P.bn;
+            const uint32_t shift = (n0 & 127u) >> 5;   // columns of the first tile of scales ahead of row n0
+            if (!(ok = tc::bar_wait(&S.taken, turn ^ 1u, dead)))
+                break;
+            tc::fence_after();
+            for (uint32_t ks = 0; ks < P.stages_k; ++ks) {
+                if (!(ok = tc::bar_wait(&S.full[s], phase, dead)))
                     break;
                 tc::fence_after();
-                for (uint32_t ks = 0; ks < P.stages_k; ++ks) {
-                    if (!(ok = tc::bar_wait(&S.full[s], phase, dead)))
-                        break;
-                    tc::fence_after();
-                    const uint8_t *st = ring + s * stage_bytes, *sc = st + kMmM * 128 + P.bn * 128;
-                    const uint32_t steps = min(P.k64 - ks * 4u, 4u), sa = tmem + kMmScaleColumn + s * 32u, sb = sa + 8u;
-                    for (uint32_t t = 0; t * 2 < steps; ++t) {
-                        tc::scales_copy(sa + 4 * t, tc::desc_scales(sc + 512 * t));
-                        for (uint32_t r = 0; r < scale_rows; ++r)
-                            tc::scales_copy(sb + 8 * t + 4 * r, tc::desc_scales(sc + 1024 * (1 + r) + 512 * t));
+                const uint32_t steps = P.k64 - ks * 4u, sa = kMmScaleColumn + s * 32u, sb = sa + 8u;
+                const uint32_t a = a0 + s * step16, b = b0 + s * step16, sc = sc0 + s * step16;
+#pragma unroll
+                for (uint32_t t = 0; t < 2; ++t)
+                    if (2 * t < steps) {
+                        tc::scales_copy(e, sa + 4 * t, sc + 32 * t);
+                        tc::scales_copy(e, sb + 8 * t, sc + 64 + 32 * t);
+                        if (scale_rows > 1)
+                            tc::scales_copy(e, sb + 8 * t + 4, sc + 128 + 32 * t);
                     }
-                    const uint64_t da = tc::desc_rows128(st), db = tc::desc_rows128(st + kMmM * 128);
-                    for (uint32_t c = 0; c < steps; ++c)
-                        tc::mx4_product(tmem, da + 2 * c, db + 2 * c, instruction, c & 1u, sa + 4 * (c >> 1), sb + 8 * (c >> 1) + shift, ks + c > 0);
-                    tc::commit(&S.empty[s]);
-                    if (++s == P.stages)
-                        s = 0, phase ^= 1u;
+#pragma unroll
+                for (uint32_t t = 0; t < 2; ++t) {
+                    if (2 * t < steps)
+                        tc::mx4_product<0>(e, 0, a + 4 * t, b + 4 * t, instruction, sa + 4 * t, sb + 8 * t + shift, ks + t);
+                    if (2 * t + 1 < steps)
+                        tc::mx4_product<1>(e, 0, a + 4 * t + 2, b + 4 * t + 2, instruction, sa + 4 * t, sb + 8 * t + shift, 1);
                 }
-                if (ok)
-                    tc::commit(&S.sums);
+                tc::commit(e, &S.empty[s]);
+                if (++s == P.stages)
+                    s = 0, phase ^= 1u;
             }
-            if (!ok) {   // products in flight end before tensor memory is given back
-                tc::commit(&S.drain);
-                tc::bar_drain(&S.drain, 0);
-            }
+            if (ok)
+                tc::commit(e, &S.sums);
+        }
+        if (!ok) {   // products in flight end before tensor memory is given back
+            tc::commit(e, &S.drain);
+            tc::bar_drain(&S.drain, 0);
         }
         __syncwarp();
     } else {
@@ -201,7 +206,7 @@ __global__ void __launch_bounds__(kMmThreads, 1) k_mx4_matmul(const __grid_const
 #pragma unroll
                     for (uint32_t g = 0; g < 2; ++g)
                         if (2 * h + g < groups)
-                            tc::tmem_load32(tmem + ((uint32_t)(warp & 3) << 21) + c0 + (2 * h + g) * 32, v[g]);
+                            tc::tmem_load32(((uint32_t)(warp & 3) << 21) + c0 + (2 * h + g) * 32, v[g]);
                     tc::tmem_load_wait();
                     if (h == 1) {
                         tc::fence_before();
@@ -244,7 +249,7 @@ __global__ void __launch_bounds__(kMmThreads, 1) k_mx4_matmul(const __grid_const
     __syncthreads();
     tc::fence_after();
     if (warp == 0)
-        tc::tmem_free(tmem, kMmColumns);
+        tc::tmem_free(0, kMmColumns);
 }
 
 // ------------------------------------------------------------------ host

@@ -95,32 +95,44 @@ __device__ __forceinline__ void tmem_load32(uint32_t at, uint32_t (&v)[32])
 __device__ __forceinline__ void tmem_load_wait() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
 
 // ------------------------------------------------------------------ products
-// Descriptor of an operand in shared memory, rows of 128 bytes along k, eight rows to a 1024-byte group, 16-byte pieces exchanged
-// within a group as the tile copy with the 128-byte pattern leaves them
-__device__ __forceinline__ uint64_t desc_rows128(const void *p)
+// These are issued by one lane of a warp that runs as a whole: with the loop inside a branch for that lane every operand had to be moved to the
+// uniform registers that the instructions take, and a product of 128 cycles took 265 to issue.
+__device__ __forceinline__ uint32_t elect()
 {
-    return (uint64_t)((saddr(p) & 0x3FFFFu) >> 4) | (1ull << 16) | (64ull << 32) | (1ull << 46) | (2ull << 61);
+    uint32_t e;
+    asm volatile("{\n\t.reg .pred q;\n\telect.sync _|q, 0xffffffff;\n\tselp.u32 %0, 1, 0, q;\n\t}" : "=r"(e));
+    return e;
 }
-// ... of 32 rows of 16 bytes, one behind the other (a tile of scales)
-__device__ __forceinline__ uint64_t desc_scales(const void *p)
-{
-    return (uint64_t)((saddr(p) & 0x3FFFFu) >> 4) | (1ull << 16) | (8ull << 32) | (1ull << 46);
-}
+// Low word of the descriptor of an operand in shared memory (its address in 16 bytes), and the high words: rows of 128 bytes along k, eight
+// to a 1024-byte group, 16-byte pieces exchanged within a group as the tile copy with the 128-byte pattern leaves them;
+// 32 rows of 16 bytes, one behind the other (a tile of scales)
+__device__ __forceinline__ uint32_t desc_low(const void *p) { return ((saddr(p) & 0x3FFFFu) >> 4) | (1u << 16); }
+constexpr uint32_t kDescRows128 = 64u | (1u << 14) | (2u << 29), kDescScales = 8u | (1u << 14);
 // 512 bytes into four columns, the 32 rows to the lanes of each of the four warps
-__device__ __forceinline__ void scales_copy(uint32_t at, uint64_t desc) { asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(at), "l"(desc) : "memory"); }
+__device__ __forceinline__ void scales_copy(uint32_t e, uint32_t at, uint32_t low)
+{
+    asm volatile("{\n\t.reg .pred e;\n\t.reg .b64 s;\n\tsetp.ne.u32 e, %0, 0;\n\tmov.b64 s, {%2, %3};\n\t"
+                 "@e tcgen05.cp.cta_group::1.32x128b.warpx4 [%1], s;\n\t}" ::"r"(e), "r"(at), "r"(low), "r"(kDescScales)
+                 : "memory");
+}
 
 // 4-bit floats with power-of-two scales, 128 rows of A, n of B (a multiple of 8 up to 256), both along k
 __device__ __forceinline__ uint32_t mx4_instruction(uint32_t n) { return (1u << 7) | (1u << 10) | ((n >> 3) << 17) | (1u << 23) | (8u << 24); }
-// 64 elements along k; `half`: which two of the four scales in a column's word are theirs
-__device__ __forceinline__ void mx4_product(uint32_t d, uint64_t a, uint64_t b, uint32_t instruction, uint32_t half, uint32_t sa, uint32_t sb, bool add)
+// 64 elements along k; HALF: which two of the four scales in a column's word are theirs (number 0 or 2, of B and of A)
+template <int HALF>
+__device__ __forceinline__ void mx4_product(uint32_t e, uint32_t d, uint32_t a, uint32_t b, uint32_t instruction, uint32_t sa, uint32_t sb, uint32_t add)
 {
-    instruction |= (half << 5) | (half << 30);   // (scale number 0 or 2, of B and of A)
-    asm volatile("{\n\t.reg .pred q;\n\tsetp.ne.u32 q, %6, 0;\n\ttcgen05.mma.cta_group::1.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%4], [%5], q;\n\t}" ::"r"(d),
-                 "l"(a), "l"(b), "r"(instruction), "r"(sa), "r"(sb), "r"((uint32_t)add)
+    asm volatile("{\n\t.reg .pred q, e;\n\t.reg .b64 a, b;\n\tsetp.ne.u32 e, %0, 0;\n\tsetp.ne.u32 q, %7, 0;\n\tmov.b64 a, {%2, %8};\n\tmov.b64 b, {%3, %8};\n\t"
+                 "@e tcgen05.mma.cta_group::1.kind::mxf4.block_scale.scale_vec::2X [%1], a, b, %4, [%5], [%6], q;\n\t}" ::"r"(e),
+                 "r"(d), "r"(a), "r"(b), "r"(instruction | (uint32_t)(HALF << 5) | ((uint32_t)HALF << 30)), "r"(sa), "r"(sb), "r"(add), "r"(kDescRows128)
                  : "memory");
 }
-// the barrier is told when all that this thread has issued is done
-__device__ __forceinline__ void commit(uint64_t *bar) { asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(saddr(bar)) : "memory"); }
+// the barrier is told when all that this lane has issued is done
+__device__ __forceinline__ void commit(uint32_t e, uint64_t *bar)
+{
+    asm volatile("{\n\t.reg .pred e;\n\tsetp.ne.u32 e, %0, 0;\n\t@e tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%1];\n\t}" ::"r"(e), "r"(saddr(bar))
+                 : "memory");
+}
 
 }  // namespace tc
 }  // namespace conef
