@@ -256,6 +256,27 @@ inline cudaError_t launch_cluster(void (*kernel)(P...), int tiles, int cluster_s
     return cudaLaunchKernelEx(&cfg, kernel, static_cast<A &&>(args)...);
 }
 
+// ... of at most 8 CTAs, with dynamic shared memory
+template <class... P, class... A>
+inline cudaError_t launch_cluster(void (*kernel)(P...), int tiles, int cluster_size, int threads, cudaStream_t s, size_t smem, A &&...args)
+{
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)(tiles * cluster_size), 1, 1);
+    cfg.blockDim = dim3((unsigned)threads, 1, 1);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = s;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = (unsigned)cluster_size;
+    attr[0].val.clusterDim.y = 1;
+    attr[0].val.clusterDim.z = 1;
+    attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[1].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 2;
+    return cudaLaunchKernelEx(&cfg, kernel, static_cast<A &&>(args)...);
+}
+
 // Opt a kernel in to `bytes` of dynamic shared memory, once per device and kernel: `done` is the
 // caller's per-kernel record (largest size set so far on each device).  Sizes up to the default
 // 48 KB need no call.

@@ -16,89 +16,107 @@
 namespace conef {
 
 constexpr int kMmM = 128, kMmK = 256;                    // rows of A per tile, elements of k per stage
-constexpr int kMmEpilogue = 8, kMmThreads = (kMmEpilogue + 2) * 32;
+constexpr int kMmEpilogue = 16, kMmThreads = (kMmEpilogue + 2) * 32;   // (four warps per 64 columns)
 constexpr int kMmMaxStages = 6;
-// tensor memory, all of it, so from column 0 on: the sums, then 32 columns of scales per stage (24 used)
-constexpr uint32_t kMmColumns = 512, kMmScaleColumn = 256;
+constexpr uint32_t kMmSmem = 226 * 1024;                 // of a CTA's 227 KB, beside the barriers
+// tensor memory, all of it, so from column 0 on: the sums, then the scales of each stage, two tiles along k of 4 (A) and 8 columns (B)
+constexpr uint32_t kMmColumns = 512, kMmScaleColumns = 24;
 
 struct MmArgs {
-    const uint8_t *as, *bs;      // scales
+    const uint8_t *as, *bs;      // scales (a single CTA's)
     int64_t m, n, ld;
     uint32_t k64, stages_k;      // steps of 64 and of kMmK elements along k
     uint32_t tiles;              // tiles of scales along k
     uint32_t b_rows;             // ... of 128 rows of B
-    uint32_t bn, tiles_m;
+    uint32_t bn, tiles_m, tiles_n;
     uint32_t n_tiles, stages;
+    uint32_t tiled;              // outputs go by tiled copies
+    uint32_t sums, scale_column; // sets of sums in tensor memory, and the first column of scales
+};
+struct MmMaps {
+    CUtensorMap a, b, out;       // (out: where it is `tiled`)
+    CUtensorMap as, bs;          // of scales, for pairs, whose copies have to tell the leader's barrier
 };
 
-// stage: A 128 x 128 bytes, B bn x 128 bytes, then 1024 bytes of scales per 128 rows (two tiles along k)
+// stage: A 128 x 128 bytes, B bn x 128 bytes (of a pair: half), then 1024 bytes of scales per 128 rows (two tiles along k)
 __host__ __device__ inline uint32_t mm_scale_rows(uint32_t bn) { return bn > 128 ? 2 : 1; }
-__host__ __device__ inline uint32_t mm_stage_bytes(uint32_t bn) { return kMmM * 128 + bn * 128 + 1024 * (1 + mm_scale_rows(bn)); }
-constexpr uint32_t kMmStaging = kMmEpilogue * 32 * 33 * 4;   // per warp 32 x 32 outputs where rows are stored piece by piece
+__host__ __device__ inline uint32_t mm_stage_bytes(uint32_t bn, bool pair) { return kMmM * 128 + bn * (pair ? 64 : 128) + 1024 * (1 + mm_scale_rows(bn)); }
+inline uint32_t mm_staging(uint32_t bn) { return bn / 16 * 4096; }   // per storing warp 32 rows of 128 bytes, where outputs are turned from a row per lane
+
+// Tiles are taken in bands of kMmBand along m, so that what runs at a time is about as high as wide (8192 x 6400 x 1600, pairs of 256 columns: in bands
+// of 8 and of 4 53 us, of one 59, in one band of all 55.6; with 192 columns 47.6 to 48.8)
+constexpr uint32_t kMmBand = 8;
+struct MmTile {
+    uint32_t m, n;
+};
+__device__ __forceinline__ MmTile mm_tile(const MmArgs &P, uint32_t tile)
+{
+    const uint32_t band = tile / (kMmBand * P.tiles_n), in = tile - band * kMmBand * P.tiles_n, high = min(kMmBand, P.tiles_m - band * kMmBand);
+    return {band * kMmBand + in % high, in / high};
+}
 
 struct MmShared {
-    uint64_t full[kMmMaxStages], empty[kMmMaxStages], sums, taken, drain;
+    uint64_t full[kMmMaxStages], empty[kMmMaxStages], sums[2], taken[2], drain;
     uint32_t tmem;
     int dead;
 };
 
+// 16 bytes of outputs from the sums of a row
 template <class T>
-__device__ __forceinline__ void store32(T *out, const uint32_t (&v)[32]);   // 32 outputs of a row, 32-byte aligned
-__device__ __forceinline__ void store_v8(void *p, const uint32_t *w)
+__device__ __forceinline__ uint4 pack16(const uint32_t *v);
+template <>
+__device__ __forceinline__ uint4 pack16<float>(const uint32_t *v)
 {
-    asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]), "r"(w[4]), "r"(w[5]), "r"(w[6]),
-                 "r"(w[7])
-                 : "memory");
+    return make_uint4(v[0], v[1], v[2], v[3]);
+}
+template <class F>
+__device__ __forceinline__ uint4 pack16_short(const uint32_t *v, F pack)
+{
+    uint4 w;
+    w.x = pack(__uint_as_float(v[0]), __uint_as_float(v[1]));
+    w.y = pack(__uint_as_float(v[2]), __uint_as_float(v[3]));
+    w.z = pack(__uint_as_float(v[4]), __uint_as_float(v[5]));
+    w.w = pack(__uint_as_float(v[6]), __uint_as_float(v[7]));
+    return w;
 }
 template <>
-__device__ __forceinline__ void store32<float>(float *out, const uint32_t (&v)[32])
+__device__ __forceinline__ uint4 pack16<__nv_bfloat16>(const uint32_t *v)
 {
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-        store_v8(out + 8 * i, v + 8 * i);
-}
-template <class H2, class F>
-__device__ __forceinline__ void store32_short(void *out, const uint32_t (&v)[32], F pack)
-{
-    uint32_t w[16];
-#pragma unroll
-    for (int i = 0; i < 16; ++i) {
-        const H2 h = pack(__uint_as_float(v[2 * i]), __uint_as_float(v[2 * i + 1]));
-        w[i] = *(const uint32_t *)&h;
-    }
-    store_v8(out, w);
-    store_v8((uint8_t *)out + 32, w + 8);
+    return pack16_short(v, [](float a, float b) {
+        const __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
+        return *(const uint32_t *)&h;
+    });
 }
 template <>
-__device__ __forceinline__ void store32<__nv_bfloat16>(__nv_bfloat16 *out, const uint32_t (&v)[32])
+__device__ __forceinline__ uint4 pack16<__half>(const uint32_t *v)
 {
-    store32_short<__nv_bfloat162>(out, v, [](float a, float b) { return __floats2bfloat162_rn(a, b); });
-}
-template <>
-__device__ __forceinline__ void store32<__half>(__half *out, const uint32_t (&v)[32])
-{
-    store32_short<__half2>(out, v, [](float a, float b) { return __floats2half2_rn(a, b); });
+    return pack16_short(v, [](float a, float b) {
+        const __half2 h = __floats2half2_rn(a, b);
+        return *(const uint32_t *)&h;
+    });
 }
 
-template <class T>
-__global__ void __launch_bounds__(kMmThreads, 1) k_mx4_matmul(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
-                                                              const __grid_constant__ MmArgs P, T *out)
+template <class T, bool PAIR>
+__global__ void __launch_bounds__(kMmThreads, 1) k_mx4_matmul(const __grid_constant__ MmMaps maps, const __grid_constant__ MmArgs P, T *out)
 {
     extern __shared__ __align__(1024) uint8_t mm_smem[];
     __shared__ MmShared S;
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const uint32_t stage_bytes = mm_stage_bytes(P.bn), scale_rows = mm_scale_rows(P.bn);
+    const int warp = __shfl_sync(0xffffffffu, (int)(threadIdx.x >> 5), 0), lane = threadIdx.x & 31;   // (known to be the same in all lanes)
+    const uint32_t stage_bytes = mm_stage_bytes(P.bn, PAIR), scale_rows = mm_scale_rows(P.bn), b_bytes = P.bn * (PAIR ? 64u : 128u);
+    const uint32_t rank = PAIR ? blockIdx.x & 1u : 0u, first = PAIR ? blockIdx.x / 2 : blockIdx.x, step = PAIR ? gridDim.x / 2 : gridDim.x;
     uint8_t *const ring = mm_smem + ((1024u - (tc::saddr(mm_smem) & 1023u)) & 1023u);
     volatile int *const dead = &S.dead;
     if (warp == 0) {
-        tc::tmem_alloc(&S.tmem, kMmColumns);
+        tc::tmem_alloc<PAIR>(&S.tmem, kMmColumns);
         if (lane == 0) {
             for (int i = 0; i < kMmMaxStages; ++i) {
                 tc::bar_init(&S.full[i], 1);
                 tc::bar_init(&S.empty[i], 1);
             }
-            tc::bar_init(&S.sums, 1);
-            tc::bar_init(&S.taken, kMmEpilogue);
+            for (int i = 0; i < 2; ++i) {
+                tc::bar_init(&S.sums[i], 1);
+                tc::bar_init(&S.taken[i], P.bn / 16 * (PAIR ? 2 : 1));
+            }
             tc::bar_init(&S.drain, 1);
             S.dead = 0;
             asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -107,149 +125,180 @@ __global__ void __launch_bounds__(kMmThreads, 1) k_mx4_matmul(const __grid_const
         tc::fence_before();
     }
     __syncthreads();
+    if (PAIR)
+        tc::cluster_sync();   // the other CTA's barriers exist
     tc::fence_after();
     grid_release();
     grid_wait();
+
     if (warp == kMmEpilogue) {
-        if (lane == 0) {
-            uint32_t s = 0, phase = 0, armed = 0;
-            bool ok = true;
-            for (uint32_t tile = blockIdx.x; ok && tile < P.n_tiles; tile += gridDim.x) {
-                const uint32_t tm = tile % P.tiles_m, tn = tile / P.tiles_m;
-                const uint32_t n0 = tn * P.bn;
-                const uint8_t *as = P.as + (size_t)tm * P.tiles * 512;
-                for (uint32_t ks = 0; ks < P.stages_k; ++ks) {
-                    if (!(ok = tc::bar_wait(&S.empty[s], phase ^ 1u, dead)))
-                        break;
-                    uint8_t *st = ring + s * stage_bytes;
-                    const uint32_t scale_bytes = min(P.tiles - ks * 2u, 2u) * 512u;
-                    tc::bar_expect(&S.full[s], kMmM * 128 + P.bn * 128 + scale_bytes * (1 + scale_rows));
-                    tc::tile_load(st, &map_a, ks * 128, tm * kMmM, &S.full[s]);
-                    tc::tile_load(st + kMmM * 128, &map_b, ks * 128, n0, &S.full[s]);
-                    uint8_t *sc = st + kMmM * 128 + P.bn * 128;
-                    tc::bulk_load(sc, as + ks * 1024u, scale_bytes, &S.full[s]);
-                    for (uint32_t r = 0; r < scale_rows; ++r)   // (rows past the last tile, whose products nobody stores: the last one's)
-                        tc::bulk_load(sc + 1024 * (1 + r), P.bs + ((size_t)min(n0 / 128 + r, P.b_rows - 1) * P.tiles + ks * 2) * 512, scale_bytes, &S.full[s]);
-                    ++armed;
-                    if (++s == P.stages)
-                        s = 0, phase ^= 1u;
+        const uint32_t ring0 = tc::saddr(ring);
+        uint32_t s = 0, phase = 0, armed = 0;
+        bool ok = true;
+        for (uint32_t tile = first; ok && tile < P.n_tiles; tile += step) {
+            const MmTile at = mm_tile(P, tile);
+            const uint32_t tm = at.m * (PAIR ? 2 : 1) + rank, n0 = at.n * P.bn;   // (tm in 128 rows)
+            const uint8_t *as = P.as + (size_t)tm * P.tiles * 512;
+            for (uint32_t ks = 0; ks < P.stages_k; ++ks) {
+                if (!(ok = tc::bar_wait(&S.empty[s], phase ^ 1u, dead)))
+                    break;
+                if (tc::elect()) {
+                    const uint32_t st = ring0 + s * stage_bytes, sc = st + kMmM * 128 + b_bytes;
+                    if constexpr (PAIR) {
+                        // (what does not exist of rows and tiles of scales is filled with zeros)
+                        const uint32_t bar = tc::leaders(&S.full[s]);
+                        if (rank == 0)
+                            tc::bar_expect(&S.full[s], 2 * stage_bytes);
+                        tc::tile_load_pair(st, &maps.a, ks * 128, tm * kMmM, bar);
+                        tc::tile_load_pair(st + kMmM * 128, &maps.b, ks * 128, n0 + rank * (P.bn / 2), bar);
+                        tc::tile_load_pair(sc, &maps.as, ks * 256, tm, bar);
+                        tc::tile_load_pair(sc + 1024, &maps.bs, ks * 256, n0 / 128, bar);
+                    } else {
+                        const uint32_t scale_bytes = min(P.tiles - ks * 2u, 2u) * 512u;
+                        tc::bar_expect(&S.full[s], kMmM * 128 + b_bytes + scale_bytes * (1 + scale_rows));
+                        tc::tile_load(st, &maps.a, ks * 128, tm * kMmM, &S.full[s]);
+                        tc::tile_load(st + kMmM * 128, &maps.b, ks * 128, n0, &S.full[s]);
+                        tc::bulk_load(sc, as + ks * 1024u, scale_bytes, &S.full[s]);
+                        for (uint32_t r = 0; r < scale_rows; ++r)   // (rows past the last tile, whose products nobody stores: the last one's)
+                            tc::bulk_load(sc + 1024 * (1 + r), P.bs + ((size_t)min(n0 / 128 + r, P.b_rows - 1) * P.tiles + ks * 2) * 512, scale_bytes, &S.full[s]);
+                    }
                 }
+                ++armed;
+                if (++s == P.stages)
+                    s = 0, phase ^= 1u;
             }
-            if (!ok)   // copies in flight end before the CTA does
-                for (uint32_t i = 0; i < P.stages && i < armed; ++i) {
-                    const uint32_t at = (armed - 1 - i) % P.stages;
-                    tc::bar_drain(&S.full[at], ((armed - 1 - i) / P.stages) & 1u);
-                }
         }
+        if (!ok && rank == 0)   // copies in flight (of both CTAs, which end together) end before the CTA does
+            for (uint32_t i = 0; i < P.stages && i < armed; ++i)
+                tc::bar_drain(&S.full[(armed - 1 - i) % P.stages], ((armed - 1 - i) / P.stages) & 1u);
         __syncwarp();
     } else if (warp == kMmEpilogue + 1) {
-        const uint32_t e = tc::elect(), instruction = tc::mx4_instruction(P.bn);
-        const uint32_t a0 = tc::desc_low(ring), b0 = a0 + kMmM * 8, sc0 = b0 + P.bn * 8, step16 = stage_bytes >> 4;
-        uint32_t s = 0, phase = 0, turn = 0;
+        const uint32_t instruction = tc::mx4_instruction<PAIR>(P.bn);
+        const uint32_t a0 = tc::desc_low(ring), b0 = a0 + kMmM * 8, sc0 = b0 + b_bytes / 16, step16 = stage_bytes >> 4;
+        uint32_t s = 0, phase = 0, set = 0, turn = 0;
         bool ok = true;
-        for (uint32_t tile = blockIdx.x; ok && tile < P.n_tiles; tile += gridDim.x, turn ^= 1u) {
-            const uint32_t n0 = tile / P.tiles_m * P.bn;
+        for (uint32_t tile = rank ? P.n_tiles : first; ok && tile < P.n_tiles; tile += step) {
+            const uint32_t n0 = mm_tile(P, tile).n * P.bn, d = set * P.bn;
             const uint32_t shift = (n0 & 127u) >> 5;   // columns of the first tile of scales ahead of row n0
-            if (!(ok = tc::bar_wait(&S.taken, turn ^ 1u, dead)))
+            if (!(ok = tc::bar_wait(&S.taken[set], turn ^ 1u, dead)))
                 break;
             tc::fence_after();
             for (uint32_t ks = 0; ks < P.stages_k; ++ks) {
                 if (!(ok = tc::bar_wait(&S.full[s], phase, dead)))
                     break;
                 tc::fence_after();
-                const uint32_t steps = P.k64 - ks * 4u, sa = kMmScaleColumn + s * 32u, sb = sa + 8u;
-                const uint32_t a = a0 + s * step16, b = b0 + s * step16, sc = sc0 + s * step16;
+                if (tc::elect()) {
+                    const uint32_t steps = P.k64 - ks * 4u, sa = P.scale_column + s * kMmScaleColumns, sb = sa + 8u;
+                    const uint32_t a = a0 + s * step16, b = b0 + s * step16, sc = sc0 + s * step16;
 #pragma unroll
-                for (uint32_t t = 0; t < 2; ++t)
-                    if (2 * t < steps) {
-                        tc::scales_copy(e, sa + 4 * t, sc + 32 * t);
-                        tc::scales_copy(e, sb + 8 * t, sc + 64 + 32 * t);
-                        if (scale_rows > 1)
-                            tc::scales_copy(e, sb + 8 * t + 4, sc + 128 + 32 * t);
+                    for (uint32_t t = 0; t < 2; ++t)
+                        if (2 * t < steps) {
+                            tc::scales_copy<PAIR>(sa + 4 * t, sc + 32 * t);
+                            tc::scales_copy<PAIR>(sb + 8 * t, sc + 64 + 32 * t);
+                            if (scale_rows > 1)
+                                tc::scales_copy<PAIR>(sb + 8 * t + 4, sc + 128 + 32 * t);
+                        }
+#pragma unroll
+                    for (uint32_t t = 0; t < 2; ++t) {
+                        if (2 * t < steps)
+                            tc::mx4_product<PAIR, 0>(d, a + 4 * t, b + 4 * t, instruction, sa + 4 * t, sb + 8 * t + shift, ks + t);
+                        if (2 * t + 1 < steps)
+                            tc::mx4_product<PAIR, 1>(d, a + 4 * t + 2, b + 4 * t + 2, instruction, sa + 4 * t, sb + 8 * t + shift, 1);
                     }
-#pragma unroll
-                for (uint32_t t = 0; t < 2; ++t) {
-                    if (2 * t < steps)
-                        tc::mx4_product<0>(e, 0, a + 4 * t, b + 4 * t, instruction, sa + 4 * t, sb + 8 * t + shift, ks + t);
-                    if (2 * t + 1 < steps)
-                        tc::mx4_product<1>(e, 0, a + 4 * t + 2, b + 4 * t + 2, instruction, sa + 4 * t, sb + 8 * t + shift, 1);
+                    tc::commit<PAIR>(&S.empty[s]);
                 }
-                tc::commit(e, &S.empty[s]);
                 if (++s == P.stages)
                     s = 0, phase ^= 1u;
             }
-            if (ok)
-                tc::commit(e, &S.sums);
+            if (ok && tc::elect())
+                tc::commit<PAIR>(&S.sums[set]);
+            if (++set == P.sums)
+                set = 0, turn ^= 1u;
         }
         if (!ok) {   // products in flight end before tensor memory is given back
-            tc::commit(e, &S.drain);
+            if (tc::elect())
+                tc::commit<PAIR>(&S.drain);
+            __syncwarp();
             tc::bar_drain(&S.drain, 0);
         }
         __syncwarp();
     } else {
-        uint32_t turn = 0;
+        // sums of 32 rows (a lane each) and 64 columns
+        constexpr int PER = 16 / sizeof(T), PASS = 128 / sizeof(T);   // outputs in 16 and in 128 bytes
+        uint32_t set = 0, turn = 0;
         bool ok = true;
-        const uint32_t half = P.bn / 2, c0 = (warp >> 2) * half, groups = half / 32;
-        const bool wide = ((P.ld * sizeof(T)) | (uintptr_t)out) % 32 == 0;
-        float(*stage)[33] = (float(*)[33])(ring + P.stages * stage_bytes) + warp * 32;
-        for (uint32_t tile = blockIdx.x; tile < P.n_tiles; tile += gridDim.x, turn ^= 1u) {
-            const int64_t row0 = (int64_t)(tile % P.tiles_m) * kMmM + (warp & 3) * 32, col0 = (int64_t)(tile / P.tiles_m) * P.bn + c0;
-            ok = ok && tc::bar_wait(&S.sums, turn, dead);
-            ok = __all_sync(0xffffffffu, ok);
-            if (ok)
+        const uint32_t c0 = (uint32_t)(warp >> 2) * 64;
+        const uint32_t staging = tc::saddr(ring) + P.stages * stage_bytes + warp * 4096;
+        float *const turned = (float *)(ring + P.stages * stage_bytes + warp * 4096);
+        for (uint32_t tile = c0 < P.bn ? first : P.n_tiles; tile < P.n_tiles; tile += step) {
+            const MmTile at = mm_tile(P, tile);
+            const int64_t row0 = ((int64_t)at.m * (PAIR ? 2 : 1) + rank) * kMmM + (warp & 3) * 32, col0 = (int64_t)at.n * P.bn + c0;
+            ok = ok && tc::bar_wait(&S.sums[set], turn, dead);
+            uint32_t v[64];
+            if (ok) {
                 tc::fence_after();
-            // 64 columns at a time: with all 128 of a warp in registers the kernel spilled
-#pragma unroll
-            for (uint32_t h = 0; h < 2; ++h) {
-                uint32_t v[2][32];
-                if (ok) {
-#pragma unroll
-                    for (uint32_t g = 0; g < 2; ++g)
-                        if (2 * h + g < groups)
-                            tc::tmem_load32(((uint32_t)(warp & 3) << 21) + c0 + (2 * h + g) * 32, v[g]);
-                    tc::tmem_load_wait();
-                    if (h == 1) {
-                        tc::fence_before();
-                        __syncwarp();
-                        if (lane == 0)
-                            tc::bar_arrive(&S.taken);
-                    }
-                } else {   // a wait ran out: what was not computed is NaN
-#pragma unroll
-                    for (uint32_t g = 0; g < 2; ++g)
-#pragma unroll
-                        for (int i = 0; i < 32; ++i)
-                            v[g][i] = 0x7FFFFFFFu;
+                const uint32_t sums = ((uint32_t)(warp & 3) << 21) + set * P.bn + c0;
+                tc::tmem_load32(sums, *(uint32_t(*)[32])v);
+                tc::tmem_load32(sums + 32, *(uint32_t(*)[32])(v + 32));
+                tc::tmem_load_wait();
+                tc::fence_before();
+                __syncwarp();
+                if (lane == 0) {
+                    if (PAIR)
+                        tc::bar_arrive_at(tc::leaders(&S.taken[set]));
+                    else
+                        tc::bar_arrive(&S.taken[set]);
                 }
+            } else {   // a wait ran out: what was not computed is NaN
 #pragma unroll
-                for (uint32_t g = 0; g < 2; ++g) {
-                    const int64_t col = col0 + (2 * h + g) * 32;
-                    if (2 * h + g < groups && col < P.n) {
-                        if (wide && col + 32 <= P.n) {
-                            if (row0 + lane < P.m)
-                                store32<T>(out + (row0 + lane) * P.ld + col, v[g]);
-                        } else {
-                            // lanes hold rows: turned in shared memory, so that a warp stores 32 outputs of a row
+                for (int i = 0; i < 64; ++i)
+                    v[i] = 0x7FFFFFFFu;
+            }
+            if (row0 < P.m && P.tiled) {
 #pragma unroll
-                            for (int i = 0; i < 32; ++i)
-                                stage[lane][i] = __uint_as_float(v[g][i]);
-                            __syncwarp();
-                            const int rows = (int)max((int64_t)0, min((int64_t)32, P.m - row0));
-                            if (col + lane < P.n)
-                                for (int r = 0; r < rows; ++r)
-                                    out[(row0 + r) * P.ld + col + lane] = from_f32<T>(stage[r][lane]);
-                            __syncwarp();
-                        }
+                for (int c = 0; c < 64; c += PASS) {
+                    if (lane == 0)
+                        tc::store_wait_read();
+                    __syncwarp();
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        const uint4 w = pack16<T>(v + c + i * PER);
+                        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(staging + lane * 128 + ((i ^ (lane & 7)) << 4)), "r"(w.x), "r"(w.y), "r"(w.z), "r"(w.w) : "memory");
                     }
+                    tc::store_fence();
+                    __syncwarp();
+                    if (lane == 0 && col0 + c < P.n)
+                        tc::tile_store(&maps.out, staging, (uint32_t)(col0 + c), (uint32_t)row0);
+                }
+            } else if (row0 < P.m) {
+                // a warp stores 32 outputs of a row
+                const int rows = (int)min((int64_t)32, P.m - row0);
+#pragma unroll
+                for (int c = 0; c < 64; c += 32) {
+#pragma unroll
+                    for (int i = 0; i < 32; ++i)
+                        turned[lane * 32 + (i ^ lane)] = __uint_as_float(v[c + i]);
+                    __syncwarp();
+                    if (col0 + c + lane < P.n)
+                        for (int r = 0; r < rows; ++r)
+                            out[(row0 + r) * P.ld + col0 + c + lane] = from_f32<T>(turned[r * 32 + (lane ^ r)]);
+                    __syncwarp();
                 }
             }
+            if (++set == P.sums)
+                set = 0, turn ^= 1u;
         }
+        if (lane == 0)
+            tc::store_wait();
+        __syncwarp();
     }
     tc::fence_before();
     __syncthreads();
+    if (PAIR)
+        tc::cluster_sync();   // neither CTA tells a barrier of one that has ended
     tc::fence_after();
     if (warp == 0)
-        tc::tmem_free(0, kMmColumns);
+        tc::tmem_free<PAIR>(0, kMmColumns);
 }
 
 // ------------------------------------------------------------------ host
@@ -267,33 +316,46 @@ static EncodeTiled encode_tiled()
     }();
     return f;
 }
-// `rows` rows of codes, copied in tiles of 128 bytes by `box` rows; what lies past either end is zero
-static bool codes_map(CUtensorMap *map, const void *codes, int64_t rows, int64_t row_bytes, uint32_t box)
+// Rows of `row_bytes` bytes, `ld` apart, as elements of `type`, copied in tiles of `width` elements by `box` rows; what lies past either end is read as
+// zero and not written
+static bool encode(CUtensorMap *map, CUtensorMapDataType type, int elem, const void *p, int64_t rows, int64_t row_bytes, int64_t ld, uint32_t width, uint32_t box)
 {
-    const cuuint64_t dims[2] = {(cuuint64_t)row_bytes, (cuuint64_t)rows}, strides[1] = {(cuuint64_t)row_bytes};
-    const cuuint32_t tile[2] = {128, box}, steps[2] = {1, 1};
-    return encode_tiled() && encode_tiled()(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, (void *)codes, dims, strides, tile, steps, CU_TENSOR_MAP_INTERLEAVE_NONE,
-                                            CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+    const cuuint64_t dims[2] = {(cuuint64_t)(row_bytes / elem), (cuuint64_t)rows}, strides[1] = {(cuuint64_t)ld};
+    const cuuint32_t tile[2] = {width, box}, steps[2] = {1, 1};
+    return encode_tiled() && encode_tiled()(map, type, 2, (void *)p, dims, strides, tile, steps, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                                            width * elem == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                                            CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-// Columns per tile: the width whose waves of tiles over the SMs cost least, a tile's cost taken as its width and 64 columns
-// more for what does not depend on it
-static uint32_t mm_columns(int64_t m, int64_t n)
+// Columns per tile, and whether pairs of CTAs take tiles of 256 rows: the choice whose waves of tiles over the SMs take least.  Nanoseconds per wave from
+// 8192 x 6400 by 1600 and by 4096: what a step of 64 along k takes (128, 192, 256 columns: single CTAs 53, 69, 91, pairs 52, 62, 76; full rate
+// would be 35, 52, 70), and what does not depend on k (pairs 950, 1300, and 2460 where tensor memory has room for one set of sums only).
+// Single CTAs and pairs there: 64.4, 54.1, 52.3 us and 54.6, 47.8, 52.9 us.
+struct MmChoice {
+    uint32_t bn;
+    bool pair;
+};
+static MmChoice mm_choice(int64_t m, int64_t n, int64_t k)
 {
-    const int64_t tiles_m = (m + kMmM - 1) / kMmM;
+    static const int per_step[2][4] = {{45, 53, 69, 91}, {45, 52, 62, 76}}, per_tile[4] = {700, 1000, 1350, 2400};
+    MmChoice best = {0, false};
     int64_t least = 0;
-    uint32_t best = 0;
-    for (uint32_t bn = 256; bn >= 64; bn -= 64) {
-        const int64_t cost = (tiles_m * ((n + bn - 1) / bn) + kPlanSMs - 1) / kPlanSMs * (bn + 64);
-        if (!best || cost < least)
-            best = bn, least = cost;
-    }
+    for (int pair = 0; pair < 2; ++pair)
+        for (uint32_t bn = 64; bn <= 256; bn += 64) {
+            const int64_t rows = pair ? 2 * kMmM : kMmM, sets = pair ? kPlanSMs / 2 : kPlanSMs;
+            const int64_t waves = ((m + rows - 1) / rows * ((n + bn - 1) / bn) + sets - 1) / sets;
+            const int64_t cost = waves * ((k + 63) / 64 * per_step[pair][bn / 64 - 1] + per_tile[bn / 64 - 1]);
+            if (!best.bn || cost < least)
+                best = {bn, pair != 0}, least = cost;
+        }
     return best;
 }
 
-template <class T>
-static int matmul(const uint8_t *a, const uint8_t *as, int64_t m, const uint8_t *b, const uint8_t *bs, int64_t n, int64_t k, T *out, int64_t ld, cudaStream_t s)
+template <class T, bool PAIR>
+static int matmul(const uint8_t *a, const uint8_t *as, int64_t m, const uint8_t *b, const uint8_t *bs, int64_t n, int64_t k, T *out, int64_t ld, uint32_t bn,
+                  cudaStream_t s)
 {
+    constexpr int64_t kRows = PAIR ? 2 * kMmM : kMmM;
     MmArgs P;
     P.as = as;
     P.bs = bs;
@@ -304,25 +366,41 @@ static int matmul(const uint8_t *a, const uint8_t *as, int64_t m, const uint8_t 
     P.stages_k = (uint32_t)((k + kMmK - 1) / kMmK);
     P.tiles = (uint32_t)mx4_scale_tiles(k);
     P.b_rows = (uint32_t)((n + 127) / 128);
-    P.bn = mm_columns(m, n);
-    P.tiles_m = (uint32_t)((m + kMmM - 1) / kMmM);
-    const int64_t tiles = (int64_t)P.tiles_m * ((n + P.bn - 1) / P.bn);
+    P.bn = bn;
+    P.tiles_m = (uint32_t)((m + kRows - 1) / kRows);
+    const int64_t tiles = (int64_t)P.tiles_m * ((n + bn - 1) / bn);
     if (tiles >= (1ll << 32) - kPlanSMs)
         return CONEF_ERR_UNSUPPORTED;
+    P.tiles_n = (uint32_t)((n + bn - 1) / bn);
     P.n_tiles = (uint32_t)tiles;
-    // (the staging is left out where no store needs it)
-    const bool wide = n % 32 == 0 && ((ld * sizeof(T)) | (uintptr_t)out) % 32 == 0;
-    const uint32_t room = 224 * 1024 - 1024 - (wide ? 0 : kMmStaging);
-    P.stages = std::min<uint32_t>({(uint32_t)kMmMaxStages, room / mm_stage_bytes(P.bn), std::max(2u, P.stages_k)});
-    CUtensorMap map_a, map_b;
-    const int64_t row_bytes = mx4_blocks(k) * 16;
-    if (!codes_map(&map_a, a, m, row_bytes, kMmM) || !codes_map(&map_b, b, n, row_bytes, P.bn))
+    // tensor memory: two sets of sums where that leaves room for the scales
+    P.sums = bn <= 192 ? 2 : 1;
+    P.scale_column = P.sums * bn > 256 ? 384 : 256;
+    const uint32_t stage_bytes = mm_stage_bytes(bn, PAIR);
+    const uint32_t room = kMmSmem - 1024 - mm_staging(bn);
+    P.stages = std::min<uint32_t>({(uint32_t)kMmMaxStages, (kMmColumns - P.scale_column) / kMmScaleColumns, room / stage_bytes, std::max(2u, P.stages_k)});
+    P.tiled = (((uint64_t)ld * sizeof(T)) | (uintptr_t)out) % 16 == 0;
+    MmMaps maps;
+    const int64_t row_bytes = mx4_blocks(k) * 16, scale_bytes = (int64_t)P.tiles * 512;
+    bool ok = encode(&maps.a, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, a, m, row_bytes, row_bytes, 128, kMmM) &&
+              encode(&maps.b, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, b, n, row_bytes, row_bytes, 128, PAIR ? bn / 2 : bn);
+    if (P.tiled)
+        ok = ok && encode(&maps.out, sizeof(T) == 4 ? CU_TENSOR_MAP_DATA_TYPE_UINT32 : CU_TENSOR_MAP_DATA_TYPE_UINT16, sizeof(T), out, m, n * (int64_t)sizeof(T),
+                          (m > 1 ? ld : (n + 7) / 8 * 8) * (int64_t)sizeof(T), 128 / sizeof(T), 32);
+    if (PAIR)
+        ok = ok && encode(&maps.as, CU_TENSOR_MAP_DATA_TYPE_UINT32, 4, as, (m + 127) / 128, scale_bytes, scale_bytes, 256, 1) &&
+             encode(&maps.bs, CU_TENSOR_MAP_DATA_TYPE_UINT32, 4, bs, P.b_rows, scale_bytes, scale_bytes, 256, mm_scale_rows(bn));
+    if (!ok)
         return launched(cudaErrorInvalidValue, "conef_mx4_matmul: tensor map");
-    const size_t smem = 1024 + (size_t)P.stages * mm_stage_bytes(P.bn) + (wide ? 0 : kMmStaging);
+    const size_t smem = 1024 + (size_t)P.stages * stage_bytes + mm_staging(bn);
     static int done[64];
-    cudaError_t e = opt_in_smem(k_mx4_matmul<T>, 224 * 1024, done);
-    if (e == cudaSuccess)
-        e = launch(k_mx4_matmul<T>, dim3(std::min<uint32_t>(P.n_tiles, kPlanSMs)), kMmThreads, smem, s, map_a, map_b, P, out);
+    cudaError_t e = opt_in_smem(k_mx4_matmul<T, PAIR>, kMmSmem, done);
+    if (e == cudaSuccess) {
+        if (PAIR)
+            e = launch_cluster(k_mx4_matmul<T, PAIR>, (int)std::min<uint32_t>(P.n_tiles, kPlanSMs / 2), 2, kMmThreads, s, smem, maps, P, out);
+        else
+            e = launch(k_mx4_matmul<T, PAIR>, dim3(std::min<uint32_t>(P.n_tiles, kPlanSMs)), kMmThreads, smem, s, maps, P, out);
+    }
     return launched(e, "conef_mx4_matmul");
 }
 
@@ -351,7 +429,8 @@ extern "C" int conef_mx4_matmul(const void *a_codes, const void *a_scales, int64
                         "conef_mx4_matmul");
     return with_elem(dtype, [&](auto t) {
         using T = decltype(t);
-        return matmul<T>((const uint8_t *)a_codes, (const uint8_t *)a_scales, m, (const uint8_t *)b_codes, (const uint8_t *)b_scales, n, k, (T *)out, ld,
-                         (cudaStream_t)stream);
+        const MmChoice c = mm_choice(m, n, k);
+        return (c.pair ? matmul<T, true> : matmul<T, false>)((const uint8_t *)a_codes, (const uint8_t *)a_scales, m, (const uint8_t *)b_codes,
+                                                             (const uint8_t *)b_scales, n, k, (T *)out, ld, c.bn, (cudaStream_t)stream);
     });
 }

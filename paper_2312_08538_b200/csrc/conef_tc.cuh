@@ -9,6 +9,16 @@ namespace tc {
 
 __device__ __forceinline__ uint32_t saddr(const void *p) { return (uint32_t)__cvta_generic_to_shared(p); }
 
+// Copies and products are issued by the one lane that this says, of a warp whose control flow is the same for all lanes as far as the
+// compiler can see (conditions by votes, counters from parameters): under a test of the lane's number, or with a loop that ends on what a lane
+// found, every operand took a move to the uniform registers that the instructions read, and a product of 128 cycles took 265 to issue.
+__device__ __forceinline__ bool elect()
+{
+    uint32_t e;
+    asm volatile("{\n\t.reg .pred q;\n\telect.sync _|q, 0xffffffff;\n\tselp.u32 %0, 1, 0, q;\n\t}" : "=r"(e));
+    return e != 0;
+}
+
 // ------------------------------------------------------------------ barriers
 __device__ __forceinline__ void bar_init(uint64_t *bar, uint32_t count) { asm volatile("mbarrier.init.shared.b64 [%0], %1;" ::"r"(saddr(bar)), "r"(count) : "memory"); }
 __device__ __forceinline__ void bar_arrive(uint64_t *bar) { asm volatile("mbarrier.arrive.shared.b64 _, [%0];" ::"r"(saddr(bar)) : "memory"); }
@@ -28,25 +38,21 @@ __device__ __forceinline__ uint64_t nanoseconds()
     asm volatile("mov.u64 %0, %globaltimer;" : "=l"(t));
     return t;
 }
-// Waits for a phase, for two seconds at most (a product takes milliseconds): past that, or once another warp's wait has
+// A warp waits for a phase, for two seconds at most (a product takes milliseconds): past that, or once another warp's wait has
 // run out, *dead is set and the answer is no.
 constexpr uint64_t kLimit = 2000000000ull;
 __device__ __forceinline__ bool bar_wait(uint64_t *bar, uint32_t parity, volatile int *dead)
 {
-    if (bar_try(bar, parity))
-        return true;
-    const uint64_t t0 = nanoseconds();
-    for (;;) {
-        for (int i = 0; i < 64; ++i)
-            if (bar_try(bar, parity))
-                return true;
-        if (*dead)
-            return false;
-        if (nanoseconds() - t0 > kLimit) {
-            *dead = 1;
-            return false;
+    bool there = bar_try(bar, parity);
+    if (!there) {
+        const uint64_t t0 = nanoseconds();
+        for (int i = 1; !there && !*dead; ++i) {
+            there = bar_try(bar, parity);
+            if (!there && i % 64 == 0 && nanoseconds() - t0 > kLimit)
+                *dead = 1;
         }
     }
+    return __all_sync(0xffffffffu, there);
 }
 // ... of copies or products in flight that nobody will use: the same limit, whatever *dead says
 __device__ __forceinline__ void bar_drain(uint64_t *bar, uint32_t parity)
@@ -56,28 +62,69 @@ __device__ __forceinline__ void bar_drain(uint64_t *bar, uint32_t parity)
     }
 }
 
-// ------------------------------------------------------------------ asynchronous copies into shared memory
-__device__ __forceinline__ void tile_load(void *dst, const void *map, int x, int y, uint64_t *bar)
+// ------------------------------------------------------------------ pairs of CTAs (a cluster of two; the even rank leads)
+__device__ __forceinline__ void cluster_sync()
 {
-    asm volatile("cp.async.bulk.tensor.2d.shared::cta.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(saddr(dst)), "l"(map),
-                 "r"(x), "r"(y), "r"(saddr(bar))
+    asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+    asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+__device__ __forceinline__ uint32_t leaders(const void *p)   // the leader's copy of a variable in shared memory
+{
+    uint32_t r;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, 0;" : "=r"(r) : "r"(saddr(p)));
+    return r;
+}
+__device__ __forceinline__ void bar_arrive_at(uint32_t bar) { asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory"); }
+
+// ------------------------------------------------------------------ asynchronous copies into shared memory
+__device__ __forceinline__ void tile_load(uint32_t dst, const void *map, uint32_t x, uint32_t y, uint64_t *bar)
+{
+    asm volatile("cp.async.bulk.tensor.2d.shared::cta.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(dst), "l"(map), "r"(x), "r"(y),
+                 "r"(saddr(bar))
                  : "memory");
 }
-__device__ __forceinline__ void bulk_load(void *dst, const void *src, uint32_t bytes, uint64_t *bar)
+__device__ __forceinline__ void bulk_load(uint32_t dst, const void *src, uint32_t bytes, uint64_t *bar)
 {
-    asm volatile("cp.async.bulk.shared::cta.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(saddr(dst)), "l"(src), "r"(bytes), "r"(saddr(bar))
+    asm volatile("cp.async.bulk.shared::cta.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(src), "r"(bytes), "r"(saddr(bar)) : "memory");
+}
+// ... of a CTA of a pair, into its own memory; the leader's barrier is told
+__device__ __forceinline__ void tile_load_pair(uint32_t dst, const void *map, uint32_t x, uint32_t y, uint32_t bar)
+{
+    asm volatile("cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(dst), "l"(map), "r"(x),
+                 "r"(y), "r"(bar)
                  : "memory");
 }
 
-// ------------------------------------------------------------------ tensor memory
+// ... and out of it: one thread stores a tile that the warp wrote (store_fence by each writer, then a barrier), and waits until the memory
+// may be written again, or until all its stores have ended
+__device__ __forceinline__ void store_fence() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
+__device__ __forceinline__ void tile_store(const void *map, uint32_t src, uint32_t x, uint32_t y)
+{
+    asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.tile.bulk_group [%0, {%2, %3}], [%1];" ::"l"(map), "r"(src), "r"(x), "r"(y) : "memory");
+    asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+}
+__device__ __forceinline__ void store_wait_read() { asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory"); }
+__device__ __forceinline__ void store_wait() { asm volatile("cp.async.bulk.wait_group 0;" ::: "memory"); }
+
+// ------------------------------------------------------------------ tensor memory (PAIR: by both CTAs)
+template <bool PAIR>
 __device__ __forceinline__ void tmem_alloc(uint32_t *where, uint32_t columns)   // a whole warp
 {
-    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(saddr(where)), "r"(columns) : "memory");
-    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    if constexpr (PAIR) {
+        asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(saddr(where)), "r"(columns) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+    } else {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(saddr(where)), "r"(columns) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
 }
+template <bool PAIR>
 __device__ __forceinline__ void tmem_free(uint32_t at, uint32_t columns)   // the same warp
 {
-    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(at), "r"(columns) : "memory");
+    if constexpr (PAIR)
+        asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(at), "r"(columns) : "memory");
+    else
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(at), "r"(columns) : "memory");
 }
 __device__ __forceinline__ void fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
@@ -95,43 +142,49 @@ __device__ __forceinline__ void tmem_load32(uint32_t at, uint32_t (&v)[32])
 __device__ __forceinline__ void tmem_load_wait() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
 
 // ------------------------------------------------------------------ products
-// These are issued by one lane of a warp that runs as a whole: with the loop inside a branch for that lane every operand had to be moved to the
-// uniform registers that the instructions take, and a product of 128 cycles took 265 to issue.
-__device__ __forceinline__ uint32_t elect()
-{
-    uint32_t e;
-    asm volatile("{\n\t.reg .pred q;\n\telect.sync _|q, 0xffffffff;\n\tselp.u32 %0, 1, 0, q;\n\t}" : "=r"(e));
-    return e;
-}
 // Low word of the descriptor of an operand in shared memory (its address in 16 bytes), and the high words: rows of 128 bytes along k, eight
 // to a 1024-byte group, 16-byte pieces exchanged within a group as the tile copy with the 128-byte pattern leaves them;
 // 32 rows of 16 bytes, one behind the other (a tile of scales)
 __device__ __forceinline__ uint32_t desc_low(const void *p) { return ((saddr(p) & 0x3FFFFu) >> 4) | (1u << 16); }
 constexpr uint32_t kDescRows128 = 64u | (1u << 14) | (2u << 29), kDescScales = 8u | (1u << 14);
-// 512 bytes into four columns, the 32 rows to the lanes of each of the four warps
-__device__ __forceinline__ void scales_copy(uint32_t e, uint32_t at, uint32_t low)
+// 512 bytes into four columns, the 32 rows to the lanes of each of the four warps; PAIR: by each CTA from its own shared memory
+template <bool PAIR>
+__device__ __forceinline__ void scales_copy(uint32_t at, uint32_t low)
 {
-    asm volatile("{\n\t.reg .pred e;\n\t.reg .b64 s;\n\tsetp.ne.u32 e, %0, 0;\n\tmov.b64 s, {%2, %3};\n\t"
-                 "@e tcgen05.cp.cta_group::1.32x128b.warpx4 [%1], s;\n\t}" ::"r"(e), "r"(at), "r"(low), "r"(kDescScales)
-                 : "memory");
+    const uint64_t desc = (uint64_t)kDescScales << 32 | low;
+    if constexpr (PAIR)
+        asm volatile("tcgen05.cp.cta_group::2.32x128b.warpx4 [%0], %1;" ::"r"(at), "l"(desc) : "memory");
+    else
+        asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(at), "l"(desc) : "memory");
 }
 
-// 4-bit floats with power-of-two scales, 128 rows of A, n of B (a multiple of 8 up to 256), both along k
-__device__ __forceinline__ uint32_t mx4_instruction(uint32_t n) { return (1u << 7) | (1u << 10) | ((n >> 3) << 17) | (1u << 23) | (8u << 24); }
+// 4-bit floats with power-of-two scales, 128 rows of A (PAIR: of each CTA), n of B (a multiple of 16 up to 256; PAIR: half of them with each
+// CTA, the scales of all with both), both along k
+template <bool PAIR>
+__device__ __forceinline__ uint32_t mx4_instruction(uint32_t n) { return (1u << 7) | (1u << 10) | ((n >> 3) << 17) | (1u << 23) | ((PAIR ? 16u : 8u) << 24); }
 // 64 elements along k; HALF: which two of the four scales in a column's word are theirs (number 0 or 2, of B and of A)
-template <int HALF>
-__device__ __forceinline__ void mx4_product(uint32_t e, uint32_t d, uint32_t a, uint32_t b, uint32_t instruction, uint32_t sa, uint32_t sb, uint32_t add)
+template <bool PAIR, int HALF>
+__device__ __forceinline__ void mx4_product(uint32_t d, uint32_t a, uint32_t b, uint32_t instruction, uint32_t sa, uint32_t sb, uint32_t add)
 {
-    asm volatile("{\n\t.reg .pred q, e;\n\t.reg .b64 a, b;\n\tsetp.ne.u32 e, %0, 0;\n\tsetp.ne.u32 q, %7, 0;\n\tmov.b64 a, {%2, %8};\n\tmov.b64 b, {%3, %8};\n\t"
-                 "@e tcgen05.mma.cta_group::1.kind::mxf4.block_scale.scale_vec::2X [%1], a, b, %4, [%5], [%6], q;\n\t}" ::"r"(e),
-                 "r"(d), "r"(a), "r"(b), "r"(instruction | (uint32_t)(HALF << 5) | ((uint32_t)HALF << 30)), "r"(sa), "r"(sb), "r"(add), "r"(kDescRows128)
-                 : "memory");
+    const uint64_t da = (uint64_t)kDescRows128 << 32 | a, db = (uint64_t)kDescRows128 << 32 | b;
+    instruction |= (uint32_t)(HALF << 5) | ((uint32_t)HALF << 30);
+    if constexpr (PAIR)
+        asm volatile("{\n\t.reg .pred q;\n\tsetp.ne.u32 q, %6, 0;\n\ttcgen05.mma.cta_group::2.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%4], [%5], q;\n\t}" ::"r"(d),
+                     "l"(da), "l"(db), "r"(instruction), "r"(sa), "r"(sb), "r"(add)
+                     : "memory");
+    else
+        asm volatile("{\n\t.reg .pred q;\n\tsetp.ne.u32 q, %6, 0;\n\ttcgen05.mma.cta_group::1.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%4], [%5], q;\n\t}" ::"r"(d),
+                     "l"(da), "l"(db), "r"(instruction), "r"(sa), "r"(sb), "r"(add)
+                     : "memory");
 }
-// the barrier is told when all that this lane has issued is done
-__device__ __forceinline__ void commit(uint32_t e, uint64_t *bar)
+// the barrier (PAIR: that of each CTA) is told when all that this lane has issued is done
+template <bool PAIR>
+__device__ __forceinline__ void commit(uint64_t *bar)
 {
-    asm volatile("{\n\t.reg .pred e;\n\tsetp.ne.u32 e, %0, 0;\n\t@e tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%1];\n\t}" ::"r"(e), "r"(saddr(bar))
-                 : "memory");
+    if constexpr (PAIR)
+        asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(saddr(bar)), "h"((uint16_t)3) : "memory");
+    else
+        asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(saddr(bar)) : "memory");
 }
 
 }  // namespace tc
