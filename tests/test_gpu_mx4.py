@@ -117,6 +117,25 @@ def test_dropout_in_place_and_into_the_residual(b, dtype):
         assert torch.equal(x2, y)
 
 
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("front", [1, 2, 3, 5, 7])
+@pytest.mark.parametrize("rows,cols", [(40, 33), (3, 1301), (200, 5), (50, 2), (9, 64), (1, 1000), (2000, 130)])
+def test_dropout_of_arrays_that_begin_off_a_boundary(b, dtype, front, rows, cols):
+    x, r = matrix(rows, cols, dtype), matrix(rows, cols, dtype, 1)
+
+    def moved(t, by):
+        whole = torch.full((t.numel() + by + 9,), 7.0, dtype=dtype, device="cuda")
+        whole[by:by + t.numel()] = t.reshape(-1)
+        return whole[by:by + t.numel()].view(rows, cols), whole
+
+    (xs, _), (rs, _), (ys, whole) = moved(x, front), moved(r, front), moved(x, front)
+    check_dropout(b.dropout(xs, 0.3, draw(b), add=rs, out=ys), x, 0.3, r)
+    assert (whole[:front] == 7).all() and (whole[front + rows * cols:] == 7).all()
+    check_dropout(b.dropout(xs, 0.3, draw(b), out=ys), x, 0.3)
+    assert (whole[:front] == 7).all() and (whole[front + rows * cols:] == 7).all()
+    check_dropout(b.dropout(xs, 0.3, draw(b), add=r), x, 0.3, r)       # (each off by something else)
+
+
 def test_dropout_takes_any_leading_dimensions(b):
     x = matrix(24, 50, torch.bfloat16)
     want = b.dropout(x, 0.2, draw(b))
