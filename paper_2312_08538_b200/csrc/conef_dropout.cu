@@ -77,24 +77,6 @@ __global__ void __launch_bounds__(kDropThreads) k_dropout_flat(const T *x, const
 // lane's is that of a warp's next step).  Where a row ends among them, it hashes all that it needs.  `shift` is the number of elements by which the array begins behind a 16-byte boundary.
 // 60000 x 1301 in fp32: a warp per row, edges element by element, 134 us; this 100 (6.2 TB/s), without the last lanes' exchange 118.  In bf16, which
 // is bound by the hashes' instructions, 88 and 76 us.
-struct Divider {   // division of 32-bit numbers by `by` > 1, rounding down: high word of x m, corrected for m's 33rd bit
-    uint32_t by, m, shift;
-};
-static Divider divider(uint32_t by)
-{
-    Divider d;
-    d.by = by;
-    d.shift = 0;
-    while ((1ull << (d.shift + 1)) < by)   // 2^shift < by <= 2^(shift + 1)
-        ++d.shift;
-    d.m = (uint32_t)((((1ull << (d.shift + 1)) - by) << 32) / by + 1);
-    return d;
-}
-__device__ __forceinline__ uint32_t divide(uint32_t x, const Divider &d)
-{
-    const uint32_t h = __umulhi(x, d.m);
-    return (h + ((x - h) >> 1)) >> d.shift;
-}
 template <class T, bool ADD, int U>
 __global__ void __launch_bounds__(kDropThreads) k_dropout_array(const T *x, const T *add, T *out, uint32_t n, uint32_t shift, const Divider width, uint64_t base,
                                                                 const Dropout drop)

@@ -71,6 +71,24 @@ struct Vec16<__half> {
     static __device__ __forceinline__ uint4 pack(const float (&f)[8]) { return make_uint4(pack2(f[0], f[1]), pack2(f[2], f[3]), pack2(f[4], f[5]), pack2(f[6], f[7])); }
 };
 
+struct Divider {   // division of 32-bit numbers by `by`, above 1, rounding down: high word of x m, corrected for m's 33rd bit
+    uint32_t by, m, shift;
+};
+inline Divider divider(uint32_t by)
+{
+    Divider d;
+    d.by = by;
+    d.shift = 0;
+    while ((1ull << (d.shift + 1)) < by)   // 2^shift < by <= 2^(shift + 1)
+        ++d.shift;
+    d.m = (uint32_t)((((1ull << (d.shift + 1)) - by) << 32) / by + 1);
+    return d;
+}
+__device__ __forceinline__ uint32_t divide(uint32_t x, const Divider &d)
+{
+    const uint32_t h = __umulhi(x, d.m);
+    return (h + ((x - h) >> 1)) >> d.shift;
+}
 inline size_t elem_bytes(int dtype) { return dtype == CONEF_F32 ? 4 : 2; }
 // calls f with a value of the type; f returns a code
 template <class F>
@@ -93,6 +111,21 @@ inline int check_matrix(const void *p, int dtype, int64_t rows, int64_t cols, in
     return CONEF_OK;
 }
 inline int check_draw(const conef_draw *d) { return !d || d->worker < 0 || d->tensor < 0 || d->step < 0 ? CONEF_ERR_INVALID_ARG : CONEF_OK; }
+
+// 32 bytes, aligned to that
+__device__ __forceinline__ void load32(const void *p, uint32_t (&w)[8])
+{
+    asm volatile("ld.global.cs.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                 : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]), "=r"(w[4]), "=r"(w[5]), "=r"(w[6]), "=r"(w[7])
+                 : "l"(p)
+                 : "memory");
+}
+__device__ __forceinline__ void store32(void *p, const uint32_t (&w)[8])
+{
+    asm volatile("st.global.cs.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]), "r"(w[4]), "r"(w[5]), "r"(w[6]),
+                 "r"(w[7])
+                 : "memory");
+}
 
 // the code of a call's launches; what CUDA says is kept for conef_error_string (conef_api.cu)
 int launched(cudaError_t e, const char *what);

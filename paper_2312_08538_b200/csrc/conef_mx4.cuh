@@ -35,16 +35,44 @@ __device__ __forceinline__ uint32_t mx4_nearest2(float lo, float hi)
     asm("{\n\t.reg .b8 t;\n\tcvt.rn.satfinite.e2m1x2.f32 t, %1, %2;\n\tcvt.u32.u8 %0, t;\n\t}" : "=r"(r) : "f"(hi), "f"(lo));
     return r;
 }
-// Code of one scaled element rounded up where floor(65536 f + 1/2) + u >= 65536, f the part of a step that it lies
-// above the code below it and u its number.  From 1 on the codes are the leading bits of the float; below 1 they are evenly spaced
-// like those of [1, 2), and 1 is added, rounded towards zero: the comparison is with a multiple of 2^-17 and
-// sees no bit that this drops.
-__device__ __forceinline__ uint32_t mx4_stochastic(float v, uint32_t u)
+// codes of eight scaled elements, nearest even, the first in the low four bits
+__device__ __forceinline__ uint32_t mx4_nearest8(const float *v)
 {
-    const uint32_t bits = __float_as_uint(v), mag = bits & 0x7FFFFFFFu;
-    const bool small = mag < 0x3F800000u;
-    const uint32_t y = __float_as_uint(__fadd_rz(__uint_as_float(mag), small ? 1.f : 0.f));
-    return ((y + (u << 6) + 32u) >> 22) - (small ? 254u : 252u) + ((bits >> 28) & 8u);
+    uint32_t r;
+    asm("{\n\t.reg .b8 a, b, c, d;\n\tcvt.rn.satfinite.e2m1x2.f32 a, %2, %1;\n\tcvt.rn.satfinite.e2m1x2.f32 b, %4, %3;\n\t"
+        "cvt.rn.satfinite.e2m1x2.f32 c, %6, %5;\n\tcvt.rn.satfinite.e2m1x2.f32 d, %8, %7;\n\tmov.b32 %0, {a, b, c, d};\n\t}"
+        : "=r"(r)
+        : "f"(v[0]), "f"(v[1]), "f"(v[2]), "f"(v[3]), "f"(v[4]), "f"(v[5]), "f"(v[6]), "f"(v[7]));
+    return r;
+}
+// Code of one scaled element rounded up where floor(65536 f + 1/2) + u >= 65536, f the part of a step that it lies
+// above the code below it and u its number, given as noise = 64 u + 32.  Times 2^-126 the smallest normal value, 1, becomes fp32's own
+// and the evenly spaced codes below it fp32's subnormals, so that the code is the leading bits of the float throughout and f the 22 that follow; rounded
+// towards zero, since the comparison is with a multiple of 32 in them and sees no bit that this drops.
+__device__ __forceinline__ uint32_t mx4_stochastic(float v, uint32_t noise)
+{
+    const uint32_t t = __float_as_uint(__fmul_rz(v, 0x1p-126f)) + noise;
+    return ((t >> 22) & 7u) | ((t >> 28) & 8u);   // (bits 25 to 30 are zero)
+}
+// the noise of the four columns of a word
+__device__ __forceinline__ void mx4_noise4(uint64_t word, uint32_t (&noise)[4])
+{
+    const uint32_t lo = (uint32_t)word, hi = (uint32_t)(word >> 32);
+    noise[0] = (lo << 6 & 0x3FFFC0u) | 32u;
+    noise[1] = (lo >> 10 & 0x3FFFC0u) | 32u;
+    noise[2] = (hi << 6 & 0x3FFFC0u) | 32u;
+    noise[3] = (hi >> 10 & 0x3FFFC0u) | 32u;
+}
+// ... of eight scaled elements by two words
+__device__ __forceinline__ uint32_t mx4_stochastic8(const float *v, uint64_t w0, uint64_t w1)
+{
+    uint32_t n[2][4], r = 0;
+    mx4_noise4(w0, n[0]);
+    mx4_noise4(w1, n[1]);
+#pragma unroll
+    for (int q = 7; q >= 0; --q)
+        r = r * 16u + mx4_stochastic(v[q], n[q >> 2][q & 3]);
+    return r;
 }
 // values of two codes (low four bits first), still to be scaled
 __device__ __forceinline__ float2 mx4_values2(uint32_t byte)
@@ -52,6 +80,20 @@ __device__ __forceinline__ float2 mx4_values2(uint32_t byte)
     uint32_t h;
     asm("{\n\t.reg .b8 t;\n\tcvt.u8.u32 t, %1;\n\tcvt.rn.f16x2.e2m1x2 %0, t;\n\t}" : "=r"(h) : "r"(byte));
     return __half22float2(*(const __half2 *)&h);
+}
+// ... of eight codes
+__device__ __forceinline__ void mx4_values8(uint32_t w, float (&v)[8])
+{
+    uint32_t h[4];
+    asm("{\n\t.reg .b8 a, b, c, d;\n\tmov.b32 {a, b, c, d}, %4;\n\tcvt.rn.f16x2.e2m1x2 %0, a;\n\tcvt.rn.f16x2.e2m1x2 %1, b;\n\t"
+        "cvt.rn.f16x2.e2m1x2 %2, c;\n\tcvt.rn.f16x2.e2m1x2 %3, d;\n\t}"
+        : "=r"(h[0]), "=r"(h[1]), "=r"(h[2]), "=r"(h[3])
+        : "r"(w));
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const float2 f = __half22float2(*(const __half2 *)&h[i]);
+        v[2 * i] = f.x, v[2 * i + 1] = f.y;
+    }
 }
 __device__ __forceinline__ float mx4_value(uint32_t code)   // one code
 {
