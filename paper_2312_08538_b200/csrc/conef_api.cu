@@ -356,7 +356,7 @@ int make_plan(const conef_tensor *tensors, int n_tensors, int n_workers, const c
                 P.msg_elems[CONEF_MSG_VALUES] += L.k;
                 // the tuned fused step: Alg. 2 and iConEF-v1 on every shape; iConEF-v2 on whole 8-element
                 // groups with 16-byte accesses
-                const bool fv = (c->kind == CONEF_C_INT8 || c->kind == CONEF_C_INT4 ||
+                const bool fv = (c->kind == CONEF_C_INT8 || c->kind == CONEF_C_INT4 || mx4 ||
                                  (c->kind == CONEF_C_STOCHQUANT && c->levels <= 127)) && c->beta == 0.f &&
                                 (c->iconef == 0 || c->kind != CONEF_C_STOCHQUANT) && L.d < (1ll << 31) &&
                                 (c->iconef != 2 || (L.d % 8 == 0 && L.g_off % 4 == 0));
@@ -1387,7 +1387,7 @@ int conef_step(conef_ctx *ctx, int64_t step, const float *const *grads, int phas
         if (!fv && !csk)
             return launch_flat<QK>(ctx, V, s);
         if (fv) {
-            const int half = ctx->c.kind == CONEF_C_STOCHQUANT ? 0 : V.scale_half;
+            const int half = ctx->c.kind == CONEF_C_INT8 || ctx->c.kind == CONEF_C_INT4 ? V.scale_half : 0;
             CK_CUDA(ctx->c.iconef == 2 ? flatvec_launch(QK, ctx->c.kind, half, V, table_ptr(ctx, T_FV), tiles_of(ctx, T_FV), s)
                                        : flat16_launch(QK, ctx->c.kind, half, V, table_ptr(ctx, T_FV), tiles_of(ctx, T_FV), s));
             LAUNCH_CHECK(ctx);
@@ -1707,8 +1707,10 @@ int conef_decompress_error(conef_ctx *ctx, int worker, float *out, conef_stream 
         ctx->draw_step[ctx->ev_cur] = V.ev_step;
     }
     const int ck = ctx->c.kind;
-    if (ctx->c.iconef != 2 && (ck == CONEF_C_INT8 || ck == CONEF_C_INT4 || (ck == CONEF_C_STOCHQUANT && ctx->c.levels <= 127))) {
-        decode_launch(ctx->plan.dec_batch, ck == CONEF_C_INT4, ctx->c.iconef == 1, V, table_ptr(ctx, T_DECODE), tiles_of(ctx, T_DECODE), worker, out, s);
+    if (ctx->c.iconef != 2 && (ck == CONEF_C_INT8 || ck == CONEF_C_INT4 || (ck == CONEF_C_STOCHQUANT && ctx->c.levels <= 127) ||
+                                   ck == CONEF_C_MX4 || ck == CONEF_C_MX4_STOCHASTIC)) {
+        const int code = ck == CONEF_C_INT4 ? DEC_INT4 : ck == CONEF_C_MX4 || ck == CONEF_C_MX4_STOCHASTIC ? DEC_MX4 : DEC_INT8;
+        decode_launch(ctx->plan.dec_batch, code, ctx->c.iconef == 1, V, table_ptr(ctx, T_DECODE), tiles_of(ctx, T_DECODE), worker, out, s);
         LAUNCH_CHECK(ctx);
         return CONEF_OK;
     }
@@ -1718,8 +1720,6 @@ int conef_decompress_error(conef_ctx *ctx, int worker, float *out, conef_stream 
     case CONEF_C_INT4: k_decompress<CONEF_C_INT4><<<n, 256, 0, s>>>(V, worker, out); break;
     case CONEF_C_ROWSKETCH: k_decompress<CONEF_C_ROWSKETCH><<<n, 256, 0, s>>>(V, worker, out); break;
     case CONEF_C_STOCHQUANT: k_decompress<CONEF_C_STOCHQUANT><<<n, 256, 0, s>>>(V, worker, out); break;
-    case CONEF_C_MX4:
-    case CONEF_C_MX4_STOCHASTIC: k_decompress<CONEF_C_MX4><<<n, 256, 0, s>>>(V, worker, out); break;
     default: k_decompress<CONEF_C_COUNTSKETCH><<<n, 256, 0, s>>>(V, worker, out); break;
     }
     LAUNCH_CHECK(ctx);

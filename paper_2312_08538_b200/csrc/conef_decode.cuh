@@ -1,4 +1,4 @@
-// The stored error expanded to fp32 (Alg. 2 line 5's decode alone) for the quantised states: int8, int4,
+// The stored error expanded to fp32 (Alg. 2 line 5's decode alone) for the quantised states: int8, int4, microscaled 4-bit floats,
 // stochastic levels in one byte, and the sum of the two states of iConEF-v1.
 //
 // HBM-bound: the codes in, 4 bytes per element out.  A thread takes four consecutive elements (one
@@ -20,10 +20,17 @@ constexpr int kDecTile = dec_tile(kDecBatch);
 // 1.93, 2.30; 1 M 2.38, 2.38; 2 M 3.03, 3.36 (int4 the same within 0.2).
 inline int dec_batch(int64_t elements) { return elements < (int64_t)dec_tile(kDecBatch) * kPlanSMs * 4 ? 1 : kDecBatch; }
 
+// how a state is coded: two codes to a byte in all but the first
+enum { DEC_INT8 = 0, DEC_INT4 = 1, DEC_MX4 = 2 };
 // four codes, element 0 in the low bits, times the scale; each product is rounded once
-template <bool INT4>
+template <int CODE>
 __device__ __forceinline__ float4 decode4(uint32_t w, float s)
 {
+    constexpr bool INT4 = CODE == DEC_INT4;
+    if (CODE == DEC_MX4) {
+        const float2 a = mx4_values2(w & 0xFFu), b = mx4_values2(w >> 8 & 0xFFu);
+        return make_float4(__fmul_rn(a.x, s), __fmul_rn(a.y, s), __fmul_rn(b.x, s), __fmul_rn(b.y, s));
+    }
     constexpr float off = INT4 ? 8388616.f : 8388736.f;   // 2^23 + the bias that makes codes non-negative
     w ^= INT4 ? 0x8888u : 0x80808080u;
     float v[4];
@@ -35,11 +42,12 @@ __device__ __forceinline__ float4 decode4(uint32_t w, float s)
     return make_float4(v[0], v[1], v[2], v[3]);
 }
 
-template <bool INT4, bool SECOND, int BATCH>
+template <int CODE, bool SECOND, int BATCH>
 __global__ void __launch_bounds__(kDecThreads) k_decode(const __grid_constant__ DevView V, const int32_t *__restrict__ pfx,
                                                         int worker, float *__restrict__ out)
 {
     constexpr int kTile = dec_tile(BATCH);
+    constexpr bool NIBBLES = CODE != DEC_INT8;
     grid_release();
     const int li = find_layer(pfx, V.n_layers, blockIdx.x);
     const LayerDesc &L = V.layers[li];
@@ -47,6 +55,7 @@ __global__ void __launch_bounds__(kDecThreads) k_decode(const __grid_constant__ 
     const uint8_t *__restrict__ codes[2] = {st + L.a_off, st + L.a2_off};
     const uint8_t *__restrict__ scales[2] = {st + L.b_off, st + L.b2_off};
     const bool half = V.scale_half && V.ckind != CONEF_C_STOCHQUANT;
+    auto scale = [&](const uint8_t *b, uint32_t blk) { return CODE == DEC_MX4 ? mx4_pow(b[blk]) : load_scale(b, blk, half); };
     const int shift = 31 - __clz(L.unit);
     const uint32_t d = (uint32_t)L.d, j0 = (blockIdx.x - pfx[li]) * (uint32_t)kTile;
     float *__restrict__ o = out + L.e_off;
@@ -60,14 +69,14 @@ __global__ void __launch_bounds__(kDecThreads) k_decode(const __grid_constant__ 
 #pragma unroll
             for (int u = 0; u < BATCH; ++u) {
                 const uint32_t j = j0 + (u * kDecThreads + threadIdx.x) * 4;
-                w[x][u] = INT4 ? (uint32_t)__ldcs((const unsigned short *)(codes[x] + j / 2)) : __ldcs((const uint32_t *)(codes[x] + j));
-                s[x][u] = load_scale(scales[x], j >> shift, half);
+                w[x][u] = NIBBLES ? (uint32_t)__ldcs((const unsigned short *)(codes[x] + j / 2)) : __ldcs((const uint32_t *)(codes[x] + j));
+                s[x][u] = scale(scales[x], j >> shift);
             }
 #pragma unroll
         for (int u = 0; u < BATCH; ++u) {
-            float4 e = decode4<INT4>(w[0][u], s[0][u]);
+            float4 e = decode4<CODE>(w[0][u], s[0][u]);
             if (SECOND) {   // e~ + q
-                const float4 q = decode4<INT4>(w[1][u], s[1][u]);
+                const float4 q = decode4<CODE>(w[1][u], s[1][u]);
                 e = make_float4(__fadd_rn(e.x, q.x), __fadd_rn(e.y, q.y), __fadd_rn(e.z, q.z), __fadd_rn(e.w, q.w));
             }
             __stcs((float4 *)(o + j0) + u * kDecThreads + threadIdx.x, e);
@@ -75,8 +84,8 @@ __global__ void __launch_bounds__(kDecThreads) k_decode(const __grid_constant__ 
         return;
     }
     auto one = [&](int x, uint32_t j) {
-        const uint32_t w = INT4 ? codes[x][j >> 1] >> (4 * (j & 1u)) : codes[x][j];
-        return decode4<INT4>(INT4 ? w & 0xFu : w, load_scale(scales[x], j >> shift, half)).x;
+        const uint32_t w = NIBBLES ? codes[x][j >> 1] >> (4 * (j & 1u)) : codes[x][j];
+        return decode4<CODE>(NIBBLES ? w & 0xFu : w, scale(scales[x], j >> shift)).x;
     };
     if (((uintptr_t)(o + j0) & 15) == 0) {   // a tensor's last tile
         for (uint32_t q = threadIdx.x * 4; q + 4 <= n; q += kDecThreads * 4) {
@@ -84,8 +93,8 @@ __global__ void __launch_bounds__(kDecThreads) k_decode(const __grid_constant__ 
             float4 e[2];
 #pragma unroll
             for (int x = 0; x < (SECOND ? 2 : 1); ++x)
-                e[x] = decode4<INT4>(INT4 ? (uint32_t)__ldcs((const unsigned short *)(codes[x] + j / 2)) : __ldcs((const uint32_t *)(codes[x] + j)),
-                                     load_scale(scales[x], j >> shift, half));
+                e[x] = decode4<CODE>(NIBBLES ? (uint32_t)__ldcs((const unsigned short *)(codes[x] + j / 2)) : __ldcs((const uint32_t *)(codes[x] + j)),
+                                     scale(scales[x], j >> shift));
             if (SECOND)
                 e[0] = make_float4(__fadd_rn(e[0].x, e[1].x), __fadd_rn(e[0].y, e[1].y), __fadd_rn(e[0].z, e[1].z), __fadd_rn(e[0].w, e[1].w));
             __stcs((float4 *)(o + j), e[0]);
@@ -109,20 +118,21 @@ __global__ void __launch_bounds__(kDecThreads) k_decode(const __grid_constant__ 
 }
 
 template <int BATCH>
-inline void decode_launch_batch(bool int4, bool second, const DevView &V, const int32_t *pfx, int tiles, int worker, float *out,
+inline void decode_launch_batch(int code, bool second, const DevView &V, const int32_t *pfx, int tiles, int worker, float *out,
                                 cudaStream_t s)
 {
-    auto *k = int4 ? (second ? k_decode<true, true, BATCH> : k_decode<true, false, BATCH>)
-                   : (second ? k_decode<false, true, BATCH> : k_decode<false, false, BATCH>);
+    auto *k = code == DEC_MX4    ? k_decode<DEC_MX4, false, BATCH>
+              : code == DEC_INT4 ? (second ? k_decode<DEC_INT4, true, BATCH> : k_decode<DEC_INT4, false, BATCH>)
+                                 : (second ? k_decode<DEC_INT8, true, BATCH> : k_decode<DEC_INT8, false, BATCH>);
     launch(k, dim3(tiles), kDecThreads, 0, s, V, pfx, worker, out);
 }
-inline void decode_launch(int batch, bool int4, bool second, const DevView &V, const int32_t *pfx, int tiles, int worker, float *out,
+inline void decode_launch(int batch, int code, bool second, const DevView &V, const int32_t *pfx, int tiles, int worker, float *out,
                           cudaStream_t s)
 {
     if (batch == 1)
-        decode_launch_batch<1>(int4, second, V, pfx, tiles, worker, out, s);
+        decode_launch_batch<1>(code, second, V, pfx, tiles, worker, out, s);
     else
-        decode_launch_batch<kDecBatch>(int4, second, V, pfx, tiles, worker, out, s);
+        decode_launch_batch<kDecBatch>(code, second, V, pfx, tiles, worker, out, s);
 }
 
 }  // namespace conef

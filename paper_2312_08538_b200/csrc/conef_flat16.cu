@@ -30,7 +30,9 @@ cudaError_t flat16_launch(int qkind, int ckind, int half, const DevView &V, cons
     CONEF_F16_CASE(QV, CONEF_C_INT8, true, 1)    \
     CONEF_F16_CASE(QV, CONEF_C_INT4, false, 1)   \
     CONEF_F16_CASE(QV, CONEF_C_INT4, true, 1)    \
-    CONEF_F16_CASE(QV, CONEF_C_STOCHQUANT, false, 0)
+    CONEF_F16_CASE(QV, CONEF_C_STOCHQUANT, false, 0) \
+    CONEF_F16_CASE(QV, CONEF_C_MX4, false, 0)        \
+    CONEF_F16_CASE(QV, CONEF_C_MX4_STOCHASTIC, false, 0)
     CONEF_F16_Q(CONEF_Q_IDENTITY)
     CONEF_F16_Q(CONEF_Q_RANDK)
     CONEF_F16_Q(CONEF_Q_RANDBLOCK)

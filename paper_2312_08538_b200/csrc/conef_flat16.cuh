@@ -1,5 +1,5 @@
 // Tuned fused step for Q in {identity, random-k, random-block-k} with an int8 / int4 error state, or the
-// stochastic quantiser of Eq. 6 with at most 127 levels (Alg. 2 lines 5, 6, 9 in one kernel): decode,
+// stochastic quantiser of Eq. 6 with at most 127 levels, or microscaled 4-bit floats (Alg. 2 lines 5, 6, 9 in one kernel): decode,
 // p = eta g + e, message, residual, block absmax, requantise, store in place.  ICO = 1 is iConEF-v1
 // (Alg. 3): a second state q of the same kind is decoded beside the first, p = (eta g + e~) + q, and the
 // store has a second round, q = C(r - decode(e~)).  Takes every size and every 4-byte alignment of the
@@ -42,10 +42,13 @@ __host__ __device__ constexpr int f16_ctas(int ico) { return ico == 1 ? 4 : 3; }
 // free of bank conflicts.
 __host__ __device__ constexpr uint32_t f16_slot(uint32_t p) { return p ^ ((p >> 3) & 3u); }
 
+__host__ __device__ constexpr bool f16_mx4(int ck) { return ck == CONEF_C_MX4 || ck == CONEF_C_MX4_STOCHASTIC; }
+__host__ __device__ constexpr bool f16_nibbles(int ck) { return ck == CONEF_C_INT4 || f16_mx4(ck); }   // two codes to a byte
+
 // a warp's stage
 template <int CK, int ICO>
 struct alignas(128) F16Stage {
-    static constexpr int CB = CK == CONEF_C_INT4 ? kF16Chunk / 2 : kF16Chunk;   // bytes of codes
+    static constexpr int CB = f16_nibbles(CK) ? kF16Chunk / 2 : kF16Chunk;   // bytes of codes
     float4 g[kF16Chunk / 4 + 8];                     // 129 pieces used
     uint8_t codes[ICO == 1 ? 2 : 1][CB];
     // what a lane copies as words: random-k's bitmap words, their offsets (two per word) and the tile's
@@ -116,10 +119,10 @@ __device__ __forceinline__ void pack_codes(const uint32_t (&t)[16], uint32_t (&w
 template <int QK, int CK, bool HALF, int ICO>
 __global__ void __launch_bounds__(kF16Threads, f16_ctas(ICO)) k_flat16(const __grid_constant__ DevView V, const int32_t *__restrict__ pfx)
 {
-    constexpr bool INT4 = CK == CONEF_C_INT4;
+    constexpr bool INT4 = f16_nibbles(CK), MX4 = f16_mx4(CK);
     constexpr int DK = CK == CONEF_C_STOCHQUANT ? CONEF_C_INT8 : CK;   // levels decode like int8 codes
     constexpr int kF16Ring = f16_ring(ICO);
-    constexpr int NW = INT4 ? 2 : 4, SB = HALF ? 2 : 4, NS = ICO == 1 ? 2 : 1;
+    constexpr int NW = INT4 ? 2 : 4, SB = MX4 ? 1 : HALF ? 2 : 4, NS = ICO == 1 ? 2 : 1;
     using Stage = F16Stage<CK, ICO>;
     extern __shared__ __align__(128) uint8_t f16_smem[];
     grid_release();
@@ -240,6 +243,8 @@ __global__ void __launch_bounds__(kF16Threads, f16_ctas(ICO)) k_flat16(const __g
     auto scale_of = [&](const Stage &S, int x) {
         const uint32_t b = (uint32_t)(lane * 16) >> shift;
         const uint32_t *sc = S.aux + SC0 + x * nsc;
+        if (MX4)
+            return mx4_pow(((const uint8_t *)sc)[b]);
         if (HALF)
             return __half2float(__ushort_as_half(((const unsigned short *)sc)[b]));
         return __uint_as_float(sc[b]);
@@ -254,7 +259,7 @@ __global__ void __launch_bounds__(kF16Threads, f16_ctas(ICO)) k_flat16(const __g
                 s2 = scale_of(S, 1);
         }
         // transmitted coordinates
-        uint32_t members = 0, slot = 0;
+        uint32_t members = 0, sent = 0, slot = 0;
         if (QK == CONEF_Q_RANDK) {
             const uint32_t word = S.aux[kF16AuxSel + (lane >> 1)], sh = (lane & 1) * 16u;
             members = (word >> sh) & 0xFFFFu;   // (no bits past the tensor)
@@ -269,6 +274,7 @@ __global__ void __launch_bounds__(kF16Threads, f16_ctas(ICO)) k_flat16(const __g
             }
         }
         if (QK != CONEF_Q_IDENTITY) {
+            sent = members;
             float *gf = (float *)S.g;
             while (members) {
                 const uint32_t q = (uint32_t)__ffs(members) - 1u;
@@ -283,12 +289,15 @@ __global__ void __launch_bounds__(kF16Threads, f16_ctas(ICO)) k_flat16(const __g
                         uint8_t *cp = &S.codes[x][e >> 1];
                         const uint32_t byte = *cp, at = 4u * (e & 1u);
                         code = (int)(((byte >> at) & 0xFu) ^ 8u) - 8;
+                        if (MX4)
+                            err[x] = __fmul_rn(mx4_value((byte >> at) & 0xFu), s1);
                         *cp = (uint8_t)(byte & ~(0xFu << at));
                     } else {
                         code = (int)(signed char)S.codes[x][e];
                         S.codes[x][e] = 0;
                     }
-                    err[x] = __fmul_rn((float)code, x ? s2 : s1);
+                    if (!MX4)
+                        err[x] = __fmul_rn((float)code, x ? s2 : s1);
                 }
                 float p = __fmaf_rn(lr, *gp, err[0]);   // Alg. 2 line 5
                 if (ICO == 1)
@@ -345,12 +354,22 @@ __global__ void __launch_bounds__(kF16Threads, f16_ctas(ICO)) k_flat16(const __g
                     const uint4 v = *(const uint4 *)(S.codes[x] + lane * 16);
                     w[0] = v.x; w[1] = v.y; w[NW - 2] = v.z; w[NW - 1] = v.w;
                 }
-                code_floats<INT4>(w, t);
+                float val[MX4 ? 16 : 1];
+                if constexpr (MX4) {
+                    mx4_values8(w[0], *(float(*)[8])val);
+                    mx4_values8(w[1], *(float(*)[8])(val + 8));
+                } else {
+                    code_floats<INT4>(w, t);
+                }
                 const float sx = x ? s2 : s1;
                 const f32x2 sx2 = pk2(sx, sx);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
-                    const f32x2 e2 = mul2(add2(pk2u(t[2 * i], t[2 * i + 1]), off2), sx2);   // float(code) * scale
+                    f32x2 e2;   // the code's value times the scale
+                    if constexpr (MX4)
+                        e2 = mul2(pk2(val[2 * i], val[2 * i + 1]), sx2);
+                    else
+                        e2 = mul2(add2(pk2u(t[2 * i], t[2 * i + 1]), off2), sx2);
                     if (x == 0) {
                         p2[i] = fma2(lr2, g2[i], e2);        // Alg. 2 line 5
                     } else {
@@ -366,6 +385,11 @@ __global__ void __launch_bounds__(kF16Threads, f16_ctas(ICO)) k_flat16(const __g
 #pragma unroll
         for (int i = 0; i < 8; ++i)
             upk2(p2[i], r[2 * i], r[2 * i + 1]);
+        if (MX4 && QK != CONEF_Q_IDENTITY && sent && s1 != s1) {   // (a block of NaN: what was sent is zero all the same)
+#pragma unroll
+            for (int q = 0; q < 16; ++q)
+                r[q] = (sent >> q) & 1u ? 0.f : r[q];
+        }
         if (QK == CONEF_Q_IDENTITY) {   // everything is sent, nothing is left
             if (left == 16u && ((uintptr_t)(msg + base) & 15) == 0) {
 #pragma unroll
@@ -389,15 +413,36 @@ __global__ void __launch_bounds__(kF16Threads, f16_ctas(ICO)) k_flat16(const __g
             float amax = 0.f;
 #pragma unroll
             for (int q = 0; q < 16; ++q)
-                amax = fmaxf(amax, fabsf(r[q]));
+                amax = MX4 ? absmax_nan(amax, r[q]) : fmaxf(amax, fabsf(r[q]));
+            if (MX4) {
+                amax = absmax_nan(amax, __shfl_xor_sync(0xffffffffu, amax, 1));
+            } else {
 #pragma unroll
-            for (int o = 8; o >= 1; o >>= 1)
-                if (lpb > o)
-                    amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, o));
-            float s, inv;
+                for (int o = 8; o >= 1; o >>= 1)
+                    if (lpb > o)
+                        amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, o));
+            }
+            float s = 0.f, inv;
             unsigned short hb = 0;
             uint32_t w[NW], t[16];
-            if constexpr (CK == CONEF_C_STOCHQUANT) {
+            uint32_t byte = 0;
+            if constexpr (MX4) {
+                byte = mx4_scale(__float_as_uint(amax));
+                inv = mx4_inv(byte);
+#pragma unroll
+                for (int q = 0; q < 16; ++q)
+                    r[q] = __fmul_rn(r[q], inv);
+                if constexpr (CK == CONEF_C_MX4_STOCHASTIC) {
+                    const uint64_t z = draw_base(draw_stream(V.seed_c, worker, li, V.step), kDrawRounding) + kDrawStep * (uint64_t)(base >> 2);
+                    w[0] = mx4_stochastic8(r, mix64(z), mix64(z + kDrawStep));
+                    w[1] = mx4_stochastic8(r + 8, mix64(z + 2 * kDrawStep), mix64(z + 3 * kDrawStep));
+                } else {
+                    w[0] = mx4_nearest8(r);
+                    w[1] = mx4_nearest8(r + 8);
+                }
+                w[0] = byte == kMx4Nan ? 0u : w[0];
+                w[1] = byte == kMx4Nan ? 0u : w[1];
+            } else if constexpr (CK == CONEF_C_STOCHQUANT) {
                 // Eq. 6 with the block's max-norm: level floor(u) or floor(u) + 1, up with probability
                 // u - floor(u); the variate of (worker, tensor, step, element) from a counter-based stream
                 const float lv = (float)V.levels;
@@ -446,10 +491,13 @@ __global__ void __launch_bounds__(kF16Threads, f16_ctas(ICO)) k_flat16(const __g
                 for (int q = 0; q < 16; ++q)   // (scalar: see above)
                     t[q] = __float_as_uint(__fadd_rn(__uint_as_float(t[q]), 12582912.0f));
             }
-            pack_codes<INT4>(t, w);
+            if constexpr (!MX4)
+                pack_codes<INT4>(t, w);
             if (left) {
                 if ((lane & (lpb - 1)) == 0) {
-                    if (HALF)
+                    if (MX4)
+                        scales[x][base >> shift] = (uint8_t)byte;
+                    else if (HALF)
                         ((unsigned short *)scales[x])[base >> shift] = hb;
                     else
                         ((float *)scales[x])[base >> shift] = s;

@@ -94,8 +94,7 @@ __global__ void __launch_bounds__(kQThreads) k_mx4_rows(const T *x, const __grid
         for (int q = 0; q < 8; ++q)
             v[i][q] = __fmul_rn(v[i][q], inv);
         uint32_t code = STOCH ? mx4_stochastic8(v[i], mix64(A.rounding + kDrawStep * group), mix64(A.rounding + kDrawStep * (group + 1))) : mx4_nearest8(v[i]);
-        const int64_t left = A.cols - ((int64_t)block[i] * 32 + part * 8);   // (elements that do not exist: their numbers could round a zero up)
-        code = byte == kMx4Nan || left <= 0 ? 0u : left < 8 ? code & ((1u << (4 * (int)left)) - 1u) : code;
+        code = byte == kMx4Nan ? 0u : code;   // (elements that do not exist are zero, which no number rounds up)
         if (u0 + i * (kQThreads / 4) < units) {
             const bool there = row[i] < A.rows && block[i] < blocks;
             if (part == 0)
@@ -211,8 +210,7 @@ __global__ void __launch_bounds__(kBothWarps * 32) k_mx4_both(const T *x, const 
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     code[i] = STOCH ? mx4_stochastic8(v + 8 * i, word[STOCH ? 2 * i : 0], word[STOCH ? 2 * i + 1 : 0]) : mx4_nearest8(v + 8 * i);
-                    const int64_t left = A.cols - (c0 + 8 * i);
-                    code[i] = byte == kMx4Nan || left <= 0 ? 0u : left < 8 ? code[i] & ((1u << (4 * (int)left)) - 1u) : code[i];
+                    code[i] = byte == kMx4Nan ? 0u : code[i];
                 }
                 A.scales[mx4_scale_at(r, c0 >> 5, scale_tiles)] = (uint8_t)(r < A.rows ? byte : 0u);
                 if (r < A.rows)
@@ -255,8 +253,7 @@ __global__ void __launch_bounds__(kBothWarps * 32) k_mx4_both(const T *x, const 
                 } else {
                     code[i] = mx4_nearest8(v + 8 * i);
                 }
-                const int64_t left = A.rows - (r0 + 8 * i);
-                code[i] = byte == kMx4Nan || left <= 0 ? 0u : left < 8 ? code[i] & ((1u << (4 * (int)left)) - 1u) : code[i];
+                code[i] = byte == kMx4Nan ? 0u : code[i];
             }
             A.scales_t[mx4_scale_at(ct, r0 >> 5, scale_tiles_t)] = (uint8_t)(ct < A.cols ? byte : 0u);
             if (ct < A.cols)
