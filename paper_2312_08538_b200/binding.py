@@ -239,6 +239,11 @@ def _on(device: torch.device, stream: Optional[torch.cuda.Stream]):
     return _NOTHING if device.index == torch._C._cuda_getDevice() else torch.cuda.device(device)
 
 
+def _plain(x: torch.Tensor, stream: Optional[torch.cuda.Stream]) -> bool:
+    """Whether a call is for the current device and stream, and on whole rows one behind the other."""
+    return stream is None and x.is_cuda and x.is_contiguous() and x.dtype in _ELEM and x.dim() > 0 and x.get_device() == torch._C._cuda_getDevice()
+
+
 def _same_device(where: str, device: torch.device, stream: Optional[torch.cuda.Stream], *tensors: torch.Tensor) -> None:
     for t in tensors:
         if t.device != device:
@@ -251,6 +256,14 @@ def dropout(x: torch.Tensor, p: float, draw: Draw, add: Optional[torch.Tensor] =
             stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
     """x behind a dropout with probability p (a multiple of 2^-16), plus `add`.  The mask comes from `draw` and is not stored:
     the gradient of x is this call on the gradient of the result, with the same draw and without `add`."""
+    if add is None and out is None and _plain(x, stream):   # (what follows, without what it need not ask: a third of a small call's host time)
+        cols = x.shape[-1]
+        out = torch.empty_like(x)
+        rc = lib.conef_dropout(x.data_ptr(), None, out.data_ptr(), _ELEM[x.dtype], x.numel() // cols if cols else 0, cols, cols, cols, cols, p, draw,
+                               _stream_handle(None))
+        if rc:
+            _check(rc, "conef_dropout")
+        return out
     rows, cols, ld = _matrix(x, "dropout")
     add_ld = out_ld = cols
     for t, name in ((add, "add"), (out, "out")):
@@ -264,7 +277,7 @@ def dropout(x: torch.Tensor, p: float, draw: Draw, add: Optional[torch.Tensor] =
     _same_device("dropout", device, stream, *(t for t in (add, out) if t is not None))
     with _on(device, stream):
         if out is None:
-            out = torch.empty(x.shape, dtype=x.dtype, device=device)
+            out = torch.empty_like(x, memory_format=torch.contiguous_format)
         _check(lib.conef_dropout(x.data_ptr(), None if add is None else add.data_ptr(), out.data_ptr(), _ELEM[x.dtype], rows, cols, ld, add_ld,
                                  out_ld, p, draw, _stream_handle(None)), "conef_dropout")
     return out
@@ -283,11 +296,18 @@ def _mx4_sizes(rows: int, cols: int) -> Tuple[int, int]:
 
 
 def _mx4_check(a: MX4, where: str) -> None:
-    if a.rows < 0 or a.cols < 0:
+    rows, cols, codes, scales = a
+    if rows < 0 or cols < 0:
         _refuse(where, "a size is negative")
-    for t, size, name in zip((a.codes, a.scales), _mx4_sizes(a.rows, a.cols), ("codes", "scales")):
-        if not t.is_cuda or t.dtype != torch.uint8 or not t.is_contiguous() or t.numel() != size:
-            _refuse(where, f"the {name} of a {a.rows} x {a.cols} form are {size} contiguous uint8 on a GPU")
+    for t, size, name in ((codes, rows * ((cols + 31) // 32) * 16, "codes"), (scales, (rows + 127) // 128 * ((cols + 127) // 128) * 512, "scales")):
+        if t.numel() != size or t.dtype is not torch.uint8 or not t.is_cuda or not t.is_contiguous():
+            _refuse(where, f"the {name} of a {rows} x {cols} form are {size} contiguous uint8 on a GPU")
+
+
+def _form(rows: int, cols: int, device: torch.device) -> MX4:
+    """A form to be written."""
+    code_bytes, scale_bytes = _mx4_sizes(rows, cols)
+    return MX4(rows, cols, torch.empty(code_bytes, dtype=torch.uint8, device=device), torch.empty(scale_bytes, dtype=torch.uint8, device=device))
 
 
 def mx4_quantise(x: torch.Tensor, forms: str = "rows", stochastic: bool = False, p: float = 0.0, draw: Optional[Draw] = None,
@@ -298,17 +318,17 @@ def mx4_quantise(x: torch.Tensor, forms: str = "rows", stochastic: bool = False,
     if forms not in ("rows", "cols", "both"):
         _refuse("mx4_quantise", "forms has to be rows, cols or both")
     device = x.device
-    _same_device("mx4_quantise", device, stream)
+    if stream is not None:
+        _same_device("mx4_quantise", device, stream)
     with _on(device, stream):
-        def form(r: int, c: int) -> MX4:
-            code_bytes, scale_bytes = _mx4_sizes(r, c)
-            return MX4(r, c, torch.empty(code_bytes, dtype=torch.uint8, device=device), torch.empty(scale_bytes, dtype=torch.uint8, device=device))
-        a = form(rows, cols) if forms != "cols" else None
-        t = form(cols, rows) if forms != "rows" else None
-        ptr = [None if f is None else v.data_ptr() for f in (a, t) for v in ((f.codes, f.scales) if f else (None, None))]
+        a = _form(rows, cols, device) if forms != "cols" else None
+        t = _form(cols, rows, device) if forms != "rows" else None
         if rows and cols:
-            _check(lib.conef_mx4_quantise(x.data_ptr(), _ELEM[x.dtype], rows, cols, ld, p, int(bool(stochastic)), draw, *ptr, _stream_handle(None)),
-                   "conef_mx4_quantise")
+            rc = lib.conef_mx4_quantise(x.data_ptr(), _ELEM[x.dtype], rows, cols, ld, p, 1 if stochastic else 0, draw, a.codes.data_ptr() if a else None,
+                                        a.scales.data_ptr() if a else None, t.codes.data_ptr() if t else None, t.scales.data_ptr() if t else None,
+                                        _stream_handle(None))
+            if rc:
+                _check(rc, "conef_mx4_quantise")
     return (a, t) if forms == "both" else a if t is None else t
 
 

@@ -1707,10 +1707,13 @@ int conef_decompress_error(conef_ctx *ctx, int worker, float *out, conef_stream 
         ctx->draw_step[ctx->ev_cur] = V.ev_step;
     }
     const int ck = ctx->c.kind;
-    if (ctx->c.iconef != 2 && (ck == CONEF_C_INT8 || ck == CONEF_C_INT4 || (ck == CONEF_C_STOCHQUANT && ctx->c.levels <= 127) ||
-                                   ck == CONEF_C_MX4 || ck == CONEF_C_MX4_STOCHASTIC)) {
-        const int code = ck == CONEF_C_INT4 ? DEC_INT4 : ck == CONEF_C_MX4 || ck == CONEF_C_MX4_STOCHASTIC ? DEC_MX4 : DEC_INT8;
-        decode_launch(ctx->plan.dec_batch, code, ctx->c.iconef == 1, V, table_ptr(ctx, T_DECODE), tiles_of(ctx, T_DECODE), worker, out, s);
+    if (ck == CONEF_C_MX4 || ck == CONEF_C_MX4_STOCHASTIC) {
+        decode_mx4_launch(ctx->plan.dec_batch, V, table_ptr(ctx, T_DECODE), tiles_of(ctx, T_DECODE), worker, out, s);
+        LAUNCH_CHECK(ctx);
+        return CONEF_OK;
+    }
+    if (ctx->c.iconef != 2 && (ck == CONEF_C_INT8 || ck == CONEF_C_INT4 || (ck == CONEF_C_STOCHQUANT && ctx->c.levels <= 127))) {
+        decode_launch(ctx->plan.dec_batch, ck == CONEF_C_INT4, ctx->c.iconef == 1, V, table_ptr(ctx, T_DECODE), tiles_of(ctx, T_DECODE), worker, out, s);
         LAUNCH_CHECK(ctx);
         return CONEF_OK;
     }

@@ -1,4 +1,4 @@
-// The stored error expanded to fp32 (Alg. 2 line 5's decode alone) for the quantised states: int8, int4, microscaled 4-bit floats,
+// The stored error expanded to fp32 (Alg. 2 line 5's decode alone) for the quantised states: int8, int4, microscaled 4-bit floats (at the end),
 // stochastic levels in one byte, and the sum of the two states of iConEF-v1.
 //
 // HBM-bound: the codes in, 4 bytes per element out.  A thread takes four consecutive elements (one
@@ -8,6 +8,7 @@
 // fp16: one element at a time in each thread took 564 us per worker (1.7 TB/s), this takes 159 us (6.0 TB/s).
 #pragma once
 #include "conef_common.cuh"
+#include "conef_elem.cuh"
 
 namespace conef {
 
@@ -20,17 +21,10 @@ constexpr int kDecTile = dec_tile(kDecBatch);
 // 1.93, 2.30; 1 M 2.38, 2.38; 2 M 3.03, 3.36 (int4 the same within 0.2).
 inline int dec_batch(int64_t elements) { return elements < (int64_t)dec_tile(kDecBatch) * kPlanSMs * 4 ? 1 : kDecBatch; }
 
-// how a state is coded: two codes to a byte in all but the first
-enum { DEC_INT8 = 0, DEC_INT4 = 1, DEC_MX4 = 2 };
 // four codes, element 0 in the low bits, times the scale; each product is rounded once
-template <int CODE>
+template <bool INT4>
 __device__ __forceinline__ float4 decode4(uint32_t w, float s)
 {
-    constexpr bool INT4 = CODE == DEC_INT4;
-    if (CODE == DEC_MX4) {
-        const float2 a = mx4_values2(w & 0xFFu), b = mx4_values2(w >> 8 & 0xFFu);
-        return make_float4(__fmul_rn(a.x, s), __fmul_rn(a.y, s), __fmul_rn(b.x, s), __fmul_rn(b.y, s));
-    }
     constexpr float off = INT4 ? 8388616.f : 8388736.f;   // 2^23 + the bias that makes codes non-negative
     w ^= INT4 ? 0x8888u : 0x80808080u;
     float v[4];
@@ -42,12 +36,11 @@ __device__ __forceinline__ float4 decode4(uint32_t w, float s)
     return make_float4(v[0], v[1], v[2], v[3]);
 }
 
-template <int CODE, bool SECOND, int BATCH>
+template <bool INT4, bool SECOND, int BATCH>
 __global__ void __launch_bounds__(kDecThreads) k_decode(const __grid_constant__ DevView V, const int32_t *__restrict__ pfx,
                                                         int worker, float *__restrict__ out)
 {
     constexpr int kTile = dec_tile(BATCH);
-    constexpr bool NIBBLES = CODE != DEC_INT8;
     grid_release();
     const int li = find_layer(pfx, V.n_layers, blockIdx.x);
     const LayerDesc &L = V.layers[li];
@@ -55,7 +48,6 @@ __global__ void __launch_bounds__(kDecThreads) k_decode(const __grid_constant__ 
     const uint8_t *__restrict__ codes[2] = {st + L.a_off, st + L.a2_off};
     const uint8_t *__restrict__ scales[2] = {st + L.b_off, st + L.b2_off};
     const bool half = V.scale_half && V.ckind != CONEF_C_STOCHQUANT;
-    auto scale = [&](const uint8_t *b, uint32_t blk) { return CODE == DEC_MX4 ? mx4_pow(b[blk]) : load_scale(b, blk, half); };
     const int shift = 31 - __clz(L.unit);
     const uint32_t d = (uint32_t)L.d, j0 = (blockIdx.x - pfx[li]) * (uint32_t)kTile;
     float *__restrict__ o = out + L.e_off;
@@ -69,14 +61,14 @@ __global__ void __launch_bounds__(kDecThreads) k_decode(const __grid_constant__ 
 #pragma unroll
             for (int u = 0; u < BATCH; ++u) {
                 const uint32_t j = j0 + (u * kDecThreads + threadIdx.x) * 4;
-                w[x][u] = NIBBLES ? (uint32_t)__ldcs((const unsigned short *)(codes[x] + j / 2)) : __ldcs((const uint32_t *)(codes[x] + j));
-                s[x][u] = scale(scales[x], j >> shift);
+                w[x][u] = INT4 ? (uint32_t)__ldcs((const unsigned short *)(codes[x] + j / 2)) : __ldcs((const uint32_t *)(codes[x] + j));
+                s[x][u] = load_scale(scales[x], j >> shift, half);
             }
 #pragma unroll
         for (int u = 0; u < BATCH; ++u) {
-            float4 e = decode4<CODE>(w[0][u], s[0][u]);
+            float4 e = decode4<INT4>(w[0][u], s[0][u]);
             if (SECOND) {   // e~ + q
-                const float4 q = decode4<CODE>(w[1][u], s[1][u]);
+                const float4 q = decode4<INT4>(w[1][u], s[1][u]);
                 e = make_float4(__fadd_rn(e.x, q.x), __fadd_rn(e.y, q.y), __fadd_rn(e.z, q.z), __fadd_rn(e.w, q.w));
             }
             __stcs((float4 *)(o + j0) + u * kDecThreads + threadIdx.x, e);
@@ -84,8 +76,8 @@ __global__ void __launch_bounds__(kDecThreads) k_decode(const __grid_constant__ 
         return;
     }
     auto one = [&](int x, uint32_t j) {
-        const uint32_t w = NIBBLES ? codes[x][j >> 1] >> (4 * (j & 1u)) : codes[x][j];
-        return decode4<CODE>(NIBBLES ? w & 0xFu : w, scale(scales[x], j >> shift)).x;
+        const uint32_t w = INT4 ? codes[x][j >> 1] >> (4 * (j & 1u)) : codes[x][j];
+        return decode4<INT4>(INT4 ? w & 0xFu : w, load_scale(scales[x], j >> shift, half)).x;
     };
     if (((uintptr_t)(o + j0) & 15) == 0) {   // a tensor's last tile
         for (uint32_t q = threadIdx.x * 4; q + 4 <= n; q += kDecThreads * 4) {
@@ -93,8 +85,8 @@ __global__ void __launch_bounds__(kDecThreads) k_decode(const __grid_constant__ 
             float4 e[2];
 #pragma unroll
             for (int x = 0; x < (SECOND ? 2 : 1); ++x)
-                e[x] = decode4<CODE>(NIBBLES ? (uint32_t)__ldcs((const unsigned short *)(codes[x] + j / 2)) : __ldcs((const uint32_t *)(codes[x] + j)),
-                                     scale(scales[x], j >> shift));
+                e[x] = decode4<INT4>(INT4 ? (uint32_t)__ldcs((const unsigned short *)(codes[x] + j / 2)) : __ldcs((const uint32_t *)(codes[x] + j)),
+                                     load_scale(scales[x], j >> shift, half));
             if (SECOND)
                 e[0] = make_float4(__fadd_rn(e[0].x, e[1].x), __fadd_rn(e[0].y, e[1].y), __fadd_rn(e[0].z, e[1].z), __fadd_rn(e[0].w, e[1].w));
             __stcs((float4 *)(o + j), e[0]);
@@ -117,22 +109,74 @@ __global__ void __launch_bounds__(kDecThreads) k_decode(const __grid_constant__ 
     }
 }
 
+// Microscaled 4-bit floats.  A thread takes eight elements at a time, those that fill 32 aligned bytes of the output wherever that begins: its codes are cut
+// out of two words, its scales are those of two blocks at most.  A tile has as many such pieces as the one above has elements of eight, the last one
+// may have one more; pieces over a tensor's ends are stored element by element.  Layers of a transformer, an odd one among them, 13.6 M elements:
+// where the output begins off a boundary, element by element took 33 us per worker, this takes 14.4 (4.3 TB/s).
 template <int BATCH>
-inline void decode_launch_batch(int code, bool second, const DevView &V, const int32_t *pfx, int tiles, int worker, float *out,
+__global__ void __launch_bounds__(kDecThreads) k_decode_mx4(const __grid_constant__ DevView V, const int32_t *__restrict__ pfx, int worker,
+                                                            float *__restrict__ out)
+{
+    constexpr uint32_t PIECES = dec_tile(BATCH) / 8, U = 2;
+    grid_release();
+    const int li = find_layer(pfx, V.n_layers, blockIdx.x);
+    const LayerDesc &L = V.layers[li];
+    const uint8_t *__restrict__ st = V.state + worker * V.state_stride;
+    const uint32_t *__restrict__ words = (const uint32_t *)(st + L.a_off);
+    const uint8_t *__restrict__ scales = st + L.b_off;
+    const int64_t d = L.d, tile = blockIdx.x - pfx[li];
+    float *__restrict__ o = out + L.e_off;
+    const int64_t shift = ((uintptr_t)o >> 2) & 7;
+    const int64_t c0 = tile * PIECES + threadIdx.x, end = (tile + 1) * (int64_t)(8 * PIECES) >= d ? (d + shift + 7) / 8 : (tile + 1) * PIECES;
+    grid_wait();
+    for (int64_t c = c0; c < end; c += kDecThreads * U) {
+        uint32_t w[U], a[U], b[U];
+#pragma unroll
+        for (uint32_t u = 0; u < U; ++u) {
+            const int64_t e = (c + u * kDecThreads) * 8 - shift;
+            if (c + u * kDecThreads < end && e >= 0 && e + 8 <= d) {
+                w[u] = mx4_codes8(words, (uint32_t)e);
+                a[u] = scales[(uint32_t)e >> 5];
+                b[u] = scales[((uint32_t)e + 7u) >> 5];
+            }
+        }
+#pragma unroll
+        for (uint32_t u = 0; u < U; ++u) {
+            const int64_t e = (c + u * kDecThreads) * 8 - shift;
+            if (c + u * kDecThreads >= end)
+                break;
+            if (e >= 0 && e + 8 <= d) {
+                float v[8];
+                mx4_scaled8(w[u], (uint32_t)e, a[u], b[u], v);
+                store32(o + e, *(const uint32_t(*)[8])v);
+            } else {
+                for (int64_t j = e < 0 ? 0 : e; j < e + 8 && j < d; ++j)
+                    o[j] = __fmul_rn(mx4_value(words[j >> 3] >> (4 * (j & 7)) & 0xFu), mx4_pow(scales[j >> 5]));
+            }
+        }
+    }
+}
+
+template <int BATCH>
+inline void decode_launch_batch(bool int4, bool second, const DevView &V, const int32_t *pfx, int tiles, int worker, float *out,
                                 cudaStream_t s)
 {
-    auto *k = code == DEC_MX4    ? k_decode<DEC_MX4, false, BATCH>
-              : code == DEC_INT4 ? (second ? k_decode<DEC_INT4, true, BATCH> : k_decode<DEC_INT4, false, BATCH>)
-                                 : (second ? k_decode<DEC_INT8, true, BATCH> : k_decode<DEC_INT8, false, BATCH>);
+    auto *k = int4 ? (second ? k_decode<true, true, BATCH> : k_decode<true, false, BATCH>)
+                   : (second ? k_decode<false, true, BATCH> : k_decode<false, false, BATCH>);
     launch(k, dim3(tiles), kDecThreads, 0, s, V, pfx, worker, out);
 }
-inline void decode_launch(int batch, int code, bool second, const DevView &V, const int32_t *pfx, int tiles, int worker, float *out,
+inline void decode_launch(int batch, bool int4, bool second, const DevView &V, const int32_t *pfx, int tiles, int worker, float *out,
                           cudaStream_t s)
 {
     if (batch == 1)
-        decode_launch_batch<1>(code, second, V, pfx, tiles, worker, out, s);
+        decode_launch_batch<1>(int4, second, V, pfx, tiles, worker, out, s);
     else
-        decode_launch_batch<kDecBatch>(code, second, V, pfx, tiles, worker, out, s);
+        decode_launch_batch<kDecBatch>(int4, second, V, pfx, tiles, worker, out, s);
+}
+
+inline void decode_mx4_launch(int batch, const DevView &V, const int32_t *pfx, int tiles, int worker, float *out, cudaStream_t s)
+{
+    launch(batch == 1 ? k_decode_mx4<1> : k_decode_mx4<kDecBatch>, dim3(tiles), kDecThreads, 0, s, V, pfx, worker, out);
 }
 
 }  // namespace conef

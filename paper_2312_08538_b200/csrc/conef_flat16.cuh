@@ -269,11 +269,10 @@ __global__ void __launch_bounds__(kF16Threads, f16_ctas(ICO)) k_flat16(const __g
             const uint32_t b1 = blk_start + kept;
             if (left && base < b1 && base + left > blk_start) {
                 const uint32_t a = max(base, blk_start) - base, e = min(base + left, b1) - base;
-                members = ((1u << e) - 1u) & ~((1u << a) - 1u);
-                slot = base + a - blk_start;
+                sent = ((1u << e) - 1u) & ~((1u << a) - 1u);
             }
         }
-        if (QK != CONEF_Q_IDENTITY) {
+        if (QK == CONEF_Q_RANDK) {
             sent = members;
             float *gf = (float *)S.g;
             while (members) {
@@ -385,10 +384,34 @@ __global__ void __launch_bounds__(kF16Threads, f16_ctas(ICO)) k_flat16(const __g
 #pragma unroll
         for (int i = 0; i < 8; ++i)
             upk2(p2[i], r[2 * i], r[2 * i + 1]);
-        if (MX4 && QK != CONEF_Q_IDENTITY && sent && s1 != s1) {   // (a block of NaN: what was sent is zero all the same)
+        if (MX4 && QK == CONEF_Q_RANDK && sent && s1 != s1) {   // (a block of NaN: what was sent is zero all the same)
 #pragma unroll
             for (int q = 0; q < 16; ++q)
                 r[q] = (sent >> q) & 1u ? 0.f : r[q];
+        }
+        if (QK == CONEF_Q_RANDBLOCK && __any_sync(0xffffffffu, sent != 0u)) {
+            // the chunk's part of the block is a run of the message: p goes back to the stage, and the warp writes 32 values at a time.  (Lane by lane
+            // and element by element, 16384 x 1600 on two workers, a tenth sent, took 82 us with int4, this takes 60; microscaled 79 and 54.)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                S.g[f16_slot(lane * 4 + i)] = make_float4(r[4 * i], r[4 * i + 1], r[4 * i + 2], r[4 * i + 3]);
+            __syncwarp();
+            const float *gf = (const float *)S.g;
+            for (uint32_t e = lane; e < (uint32_t)kF16Chunk; e += 32u) {
+                const uint32_t j = c * (uint32_t)kF16Chunk + e, at = j - blk_start;   // (wraps to a large value below the block)
+                if (at < kept) {   // (the block lies within the tensor)
+                    msg[at] = gf[f16_slot(e >> 2) * 4u + (e & 3u)];
+                    if (worker == 0)
+                        idx[at] = j;
+                }
+            }
+#pragma unroll
+            for (int q = 0; q < 16; ++q)
+                r[q] = (sent >> q) & 1u ? 0.f : r[q];
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                p2[i] = pk2(r[2 * i], r[2 * i + 1]);
+            __syncwarp();
         }
         if (QK == CONEF_Q_IDENTITY) {   // everything is sent, nothing is left
             if (left == 16u && ((uintptr_t)(msg + base) & 15) == 0) {
@@ -411,12 +434,13 @@ __global__ void __launch_bounds__(kF16Threads, f16_ctas(ICO)) k_flat16(const __g
 #pragma unroll
         for (int x = 0; x < NS; ++x) {
             float amax = 0.f;
-#pragma unroll
-            for (int q = 0; q < 16; ++q)
-                amax = MX4 ? absmax_nan(amax, r[q]) : fmaxf(amax, fabsf(r[q]));
-            if (MX4) {
-                amax = absmax_nan(amax, __shfl_xor_sync(0xffffffffu, amax, 1));
+            if constexpr (MX4) {
+                amax = mx4_absmax<16>(r);
+                amax = mx4_absmax2(amax, __shfl_xor_sync(0xffffffffu, amax, 1));
             } else {
+#pragma unroll
+                for (int q = 0; q < 16; ++q)
+                    amax = fmaxf(amax, fabsf(r[q]));
 #pragma unroll
                 for (int o = 8; o >= 1; o >>= 1)
                     if (lpb > o)

@@ -252,7 +252,7 @@ __global__ void __launch_bounds__(kFlatThreads) k_flat(const __grid_constant__ D
             uint32_t code;
             if (V.ckind == CONEF_C_MX4_STOCHASTIC) {
                 const uint64_t stc = draw_stream(V.seed_c, worker, li, V.step);
-                code = mx4_stochastic(v, draw_of(draw_word(stc, base >> 2, kDrawRounding), base) * 64u + 32u);
+                code = mx4_stochastic(v, draw_of(draw_word(stc, base >> 2, kDrawRounding), base) * 256u + 128u);
             } else
                 code = mx4_nearest2(v, 0.f) & 0xFu;
             code = byte == kMx4Nan ? 0u : code;

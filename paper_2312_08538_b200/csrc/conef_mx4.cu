@@ -10,40 +10,28 @@ namespace conef {
 
 constexpr int kQThreads = 256;
 
-// eight elements from p on, of which `have` exist (the rest zero); VEC: p is aligned to their size
-template <class T, bool VEC>
-__device__ __forceinline__ void load8(const T *p, int have, float (&v)[8])
+// eight elements from p on, which is aligned to their size
+template <class T>
+__device__ __forceinline__ void load8(const T *p, float (&v)[8])
 {
-    if (VEC && have >= 8) {
-        if constexpr (sizeof(T) == 4) {
-            uint32_t w[8];
-            load32(p, w);
-#pragma unroll
-            for (int q = 0; q < 8; ++q)
-                v[q] = __uint_as_float(w[q]);
-        } else {
-            Vec16<T>::unpack(__ldcs((const uint4 *)p), v);
-        }
-    } else {
+    if constexpr (sizeof(T) == 4) {
+        uint32_t w[8];
+        load32(p, w);
 #pragma unroll
         for (int q = 0; q < 8; ++q)
-            v[q] = q < have ? to_f32(p[q]) : 0.f;
+            v[q] = __uint_as_float(w[q]);
+    } else {
+        Vec16<T>::unpack(__ldcs((const uint4 *)p), v);
     }
 }
 // x behind the dropout, rounded to fp32, of four columns
 __device__ __forceinline__ void drop4(float *v, uint64_t word, const Dropout &d)
 {
-    const uint32_t kept = dropout_kept(word, d);
-#pragma unroll
-    for (int q = 0; q < 4; ++q)
-        v[q] = (kept >> q) & 1u ? __fmul_rn(v[q], d.scale) : 0.f;
-}
-// max(a, |x|), or NaN where either is one
-__device__ __forceinline__ float mx4_absmax(float a, float x)
-{
-    float r;
-    asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(fabsf(x)));
-    return r;
+    const uint32_t lo = (uint32_t)word, hi = (uint32_t)(word >> 32);
+    v[0] = (lo << 16) > d.limit ? __fmul_rn(v[0], d.scale) : 0.f;
+    v[1] = lo > d.limit ? __fmul_rn(v[1], d.scale) : 0.f;
+    v[2] = (hi << 16) > d.limit ? __fmul_rn(v[2], d.scale) : 0.f;
+    v[3] = hi > d.limit ? __fmul_rn(v[3], d.scale) : 0.f;
 }
 
 struct QArgs {
@@ -54,53 +42,67 @@ struct QArgs {
 };
 
 // ------------------------------------------------------------------ rows
-// Four lanes per block, eight elements each, U blocks one after the other.  Blocks are counted over the padded tiles of scales, so that the bytes
-// of those that do not exist get their zero.
-template <class T, bool VEC, bool STOCH, bool DROP, int U>
-__global__ void __launch_bounds__(kQThreads) k_mx4_rows(const T *x, const __grid_constant__ QArgs A, const Divider padded, uint32_t units)
+// LANES lanes per block.  Blocks are counted over the padded tiles of scales, so that the bytes of those that do not exist get their zero.  Four lanes
+// load side by side, but what does not depend on the number of elements is then done for eight of them: 8192 x 6400 in bf16 took 34 us, with a lane per
+// block 18 (7.2 TB/s), with two 22; with stochastic rounding 52, 34, 41.  In fp32 a lane's 128 bytes are four requests to 32 lines each, and rounding to
+// nearest does less for them: 50257 x 1600 with four, two and one lane 58, 52, 62 us, stochastic 84, 70, 63.  So one, or two in fp32 without draws;
+// four where rows are not aligned, and where there are too few blocks for all SMs.
+template <class T, bool VEC, bool STOCH, bool DROP, int LANES>
+__global__ void __launch_bounds__(kQThreads) k_mx4_rows(const T *x, const __grid_constant__ QArgs A, const Divider padded, uint32_t row0, uint32_t units)
 {
+    constexpr int E = 32 / LANES, W = E / 8;   // elements and words of codes per lane
     grid_release();
-    const uint32_t blocks = (uint32_t)mx4_blocks(A.cols), tiles = padded.by / 4, part = threadIdx.x & 3;
-    const uint32_t u0 = blockIdx.x * (uint32_t)(kQThreads / 4 * U) + threadIdx.x / 4;
-    const uint64_t groups = (uint64_t)(A.cols + 3) / 4;
+    const uint32_t blocks = (uint32_t)mx4_blocks(A.cols), tiles = padded.by / 4, part = threadIdx.x % LANES;
+    const uint32_t u = blockIdx.x * (uint32_t)(kQThreads / LANES) + threadIdx.x / LANES;
+    const uint32_t groups = (uint32_t)(A.cols + 3) / 4, at = divide(u, padded), row = row0 + at, block = u - at * padded.by, c = block * 32u + part * E;
+    const T *p = x + (int64_t)row * A.ld + c;
+    const uint32_t have = u < units && row < A.rows && c < A.cols ? (uint32_t)A.cols - c : 0u;
     grid_wait();
-    float v[U][8];
-    uint32_t row[U], block[U];
+    float v[E];
+    if (VEC && have >= (uint32_t)E) {
 #pragma unroll
-    for (int i = 0; i < U; ++i) {
-        const uint32_t u = u0 + i * (kQThreads / 4);
-        row[i] = divide(u, padded);
-        block[i] = u - row[i] * padded.by;
-        const int64_t c = (int64_t)block[i] * 32 + part * 8;
-        const int64_t have = u < units && row[i] < A.rows && c < A.cols ? A.cols - c : 0;
-        load8<T, VEC>(x + (int64_t)row[i] * A.ld + c, (int)min(have, (int64_t)8), v[i]);
+        for (int w = 0; w < W; ++w)
+            load8<T>(p + 8 * w, *(float(*)[8])(v + 8 * w));
+    } else {
+#pragma unroll
+        for (int q = 0; q < E; ++q)
+            v[q] = (uint32_t)q < have ? to_f32(p[q]) : 0.f;
     }
+    const uint64_t group = (uint64_t)row * groups + block * 8u + part * (E / 4);
+    if (DROP) {
+        const uint64_t z = A.dropout + kDrawStep * group;
 #pragma unroll
-    for (int i = 0; i < U; ++i) {
-        const uint64_t group = (uint64_t)row[i] * groups + block[i] * 8u + part * 2u;
-        if (DROP) {
-            drop4(v[i], mix64(A.dropout + kDrawStep * group), A.drop);
-            drop4(v[i] + 4, mix64(A.dropout + kDrawStep * (group + 1)), A.drop);
-        }
-        float most = 0.f;
+        for (int g = 0; g < E / 4; ++g)
+            drop4(v + 4 * g, mix64(z + kDrawStep * g), A.drop);
+    }
+    float most = mx4_absmax<E>(v);
 #pragma unroll
-        for (int q = 0; q < 8; ++q)
-            most = mx4_absmax(most, v[i][q]);
-        most = mx4_absmax(most, __shfl_xor_sync(0xffffffffu, most, 1));
-        most = mx4_absmax(most, __shfl_xor_sync(0xffffffffu, most, 2));
-        const uint32_t byte = mx4_scale(__float_as_uint(most));
-        const float inv = mx4_inv(byte);
+    for (int o = 1; o < LANES; o *= 2)
+        most = mx4_absmax2(most, __shfl_xor_sync(0xffffffffu, most, o));
+    const uint32_t byte = mx4_scale(__float_as_uint(most));
+    const float inv = mx4_inv(byte);
 #pragma unroll
-        for (int q = 0; q < 8; ++q)
-            v[i][q] = __fmul_rn(v[i][q], inv);
-        uint32_t code = STOCH ? mx4_stochastic8(v[i], mix64(A.rounding + kDrawStep * group), mix64(A.rounding + kDrawStep * (group + 1))) : mx4_nearest8(v[i]);
-        code = byte == kMx4Nan ? 0u : code;   // (elements that do not exist are zero, which no number rounds up)
-        if (u0 + i * (kQThreads / 4) < units) {
-            const bool there = row[i] < A.rows && block[i] < blocks;
-            if (part == 0)
-                A.scales[mx4_scale_at(row[i], block[i], tiles)] = (uint8_t)(there ? byte : 0u);
-            if (there)
-                *(uint32_t *)(A.codes + ((uint64_t)row[i] * blocks + block[i]) * 16 + part * 4) = code;
+    for (int q = 0; q < E; ++q)
+        v[q] = __fmul_rn(v[q], inv);
+    uint32_t code[W];
+    const uint64_t z = A.rounding + kDrawStep * group;
+#pragma unroll
+    for (int w = 0; w < W; ++w) {
+        code[w] = STOCH ? mx4_stochastic8(v + 8 * w, mix64(z + kDrawStep * (2 * w)), mix64(z + kDrawStep * (2 * w + 1))) : mx4_nearest8(v + 8 * w);
+        code[w] = byte == kMx4Nan ? 0u : code[w];   // (elements that do not exist are zero, which no number rounds up)
+    }
+    if (u < units) {
+        const bool there = row < A.rows && block < blocks;
+        if (part == 0)
+            A.scales[mx4_scale_at(row, block, tiles)] = (uint8_t)(there ? byte : 0u);
+        if (there) {
+            uint8_t *o = A.codes + ((uint64_t)row * blocks + block) * 16 + part * (E / 2);
+            if constexpr (W == 4)
+                *(uint4 *)o = make_uint4(code[0], code[1], code[2], code[3]);
+            else if constexpr (W == 2)
+                *(uint2 *)o = make_uint2(code[0], code[1]);
+            else
+                *(uint32_t *)o = code[0];
         }
     }
 }
@@ -139,122 +141,135 @@ __global__ void __launch_bounds__(kBothWarps * 32) k_mx4_both(const T *x, const 
                 A.scales_t[mx4_scale_at(ct, r0 >> 5, scale_tiles_t)] = 0;
                 continue;
             }
-            // elements, in fp32 (16 bits: as they are, in M)
-            const bool whole = VEC && c0 + 32 <= A.cols;
-            float v[32];
-            if (whole) {
+            // a lane's row: 16 bits as they are, two to a word, or fp32
+            constexpr int RAW = SHORT ? 16 : 32;
+            uint32_t raw[RAW];
+            if (VEC && c0 + 32 <= A.cols) {
                 const T *p = x + r * A.ld + c0;
-                if (r < A.rows) {
 #pragma unroll
-                    for (int i = 0; i < 4; ++i)
-                        load8<T, true>(p + 8 * i, 8, *(float(*)[8])(v + 8 * i));
-                } else {
+                for (int i = 0; i < RAW; i += 8) {
+                    if (r < A.rows) {
+                        if constexpr (SHORT) {
+                            const uint4 a = __ldcs((const uint4 *)((const uint32_t *)p + i)), b = __ldcs((const uint4 *)((const uint32_t *)p + i + 4));
+                            raw[i] = a.x, raw[i + 1] = a.y, raw[i + 2] = a.z, raw[i + 3] = a.w, raw[i + 4] = b.x, raw[i + 5] = b.y, raw[i + 6] = b.z, raw[i + 7] = b.w;
+                        } else {
+                            load32(p + i, *(uint32_t(*)[8])(raw + i));
+                        }
+                    } else {
 #pragma unroll
-                    for (int i = 0; i < 32; ++i)
-                        v[i] = 0.f;
+                        for (int q = 0; q < 8; ++q)
+                            raw[i + q] = 0u;
+                    }
                 }
             } else {   // a row at a time, and turned
                 const T *p = x + r0 * A.ld + ct;
                 const int rows = (int)min((int64_t)32, A.rows - r0);
-                float t[32];
+                using Bits = std::conditional_t<SHORT, uint16_t, uint32_t>;
+                uint32_t t[32];
 #pragma unroll
                 for (int i = 0; i < 32; ++i)
-                    t[i] = i < rows && ct < A.cols ? to_f32(p[i * A.ld]) : 0.f;
+                    t[i] = i < rows && ct < A.cols ? (uint32_t)((const Bits *)p)[i * A.ld] : 0u;
 #pragma unroll
                 for (int i = 0; i < 32; ++i)
-                    M.v[i][lane] = __float_as_uint(t[i]);
+                    M.v[i][lane] = t[i];
                 __syncwarp();
 #pragma unroll
-                for (int i = 0; i < 32; ++i)
-                    v[i] = __uint_as_float(M.v[lane][i]);
+                for (int i = 0; i < RAW; ++i)
+                    raw[i] = SHORT ? M.v[lane][2 * i % 32] | M.v[lane][(2 * i + 1) % 32] << 16 : M.v[lane][i];
                 __syncwarp();
             }
             const uint64_t group = (uint64_t)r * groups + (uint64_t)(c0 >> 2);
             uint64_t word[STOCH ? 8 : 1];
+            if (STOCH) {
+                const uint64_t z = A.rounding + kDrawStep * group;
 #pragma unroll
-            for (int g = 0; g < 8; ++g) {
-                if (STOCH)
-                    word[g] = mix64(A.rounding + kDrawStep * (group + g));
-                uint32_t kept = 0xFu;
-                if (DROP)
-                    kept = dropout_kept(mix64(A.dropout + kDrawStep * (group + g)), A.drop);
+                for (int g = 0; g < 8; ++g)
+                    word[STOCH ? g : 0] = mix64(z + kDrawStep * g);
+            }
+            if (DROP) {
+                const uint64_t z = A.dropout + kDrawStep * group;
 #pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    const int i = 4 * g + q;
-                    if (DROP)
-                        v[i] = (kept >> q) & 1u ? v[i] : 0.f;
-                    if (SHORT) {   // (fp32 from 16 bits and back is exact, a NaN stays one)
-                        const T s = from_f32<T>(v[i]);
-                        M.v[lane][i] = (uint32_t) * (const uint16_t *)&s | (STOCH ? draw_of(word[g], q) << 16 : 0u);
-                    }
-                    if (DROP)
-                        v[i] = __fmul_rn(v[i], A.drop.scale);
-                    if (!SHORT) {
-                        M.v[lane][i] = __float_as_uint(v[i]);
-                        if (STOCH)
-                            M.u[lane][i] = (uint16_t)draw_of(word[g], q);
+                for (int g = 0; g < 8; ++g) {
+                    const uint64_t d = mix64(z + kDrawStep * g);
+                    const uint32_t lo = (uint32_t)d, hi = (uint32_t)(d >> 32), limit = A.drop.limit;
+                    if constexpr (SHORT) {
+                        raw[2 * g] &= ((lo << 16) > limit ? 0xFFFFu : 0u) | (lo > limit ? 0xFFFF0000u : 0u);
+                        raw[2 * g + 1] &= ((hi << 16) > limit ? 0xFFFFu : 0u) | (hi > limit ? 0xFFFF0000u : 0u);
+                    } else {
+                        drop4((float *)raw + 4 * g, d, A.drop);
                     }
                 }
             }
-            if (ROWS) {
-                float most = 0.f;
+            // for the columns: an element (16 bits: with its number above)
 #pragma unroll
-                for (int i = 0; i < 32; ++i)
-                    most = mx4_absmax(most, v[i]);
-                const uint32_t byte = mx4_scale(__float_as_uint(most));
+            for (int i = 0; i < 32; ++i) {
+                const uint32_t w = STOCH ? (uint32_t)(word[STOCH ? i / 4 : 0] >> (i & 2 ? 32 : 0)) : 0u;   // its number is one half of this
+                if (SHORT) {
+                    M.v[lane][i] = STOCH ? __byte_perm(raw[i / 2 % RAW], w, i & 1 ? 0x7632 : 0x5410) : i & 1 ? raw[i / 2 % RAW] >> 16 : raw[i / 2 % RAW];
+                } else {
+                    M.v[lane][i] = raw[i % RAW];
+                    if (STOCH)
+                        M.u[lane][i] = (uint16_t)(i & 1 ? w >> 16 : w);
+                }
+            }
+            float v[32];
+            // 32 scaled elements' codes; their scale
+            auto encode = [&](auto &&codes_of, uint32_t (&code)[4]) {
+                const uint32_t byte = mx4_scale(__float_as_uint(mx4_absmax<32>(v)));
                 const float inv = mx4_inv(byte);
-                uint32_t code[4];
 #pragma unroll
                 for (int i = 0; i < 32; ++i)
                     v[i] = __fmul_rn(v[i], inv);
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    code[i] = STOCH ? mx4_stochastic8(v + 8 * i, word[STOCH ? 2 * i : 0], word[STOCH ? 2 * i + 1 : 0]) : mx4_nearest8(v + 8 * i);
-                    code[i] = byte == kMx4Nan ? 0u : code[i];
+                    code[i] = codes_of(i);
+                    code[i] = byte == kMx4Nan ? 0u : code[i];   // (elements that do not exist are zero, which no number rounds up)
                 }
+                return byte;
+            };
+            uint32_t code[4];
+            if (ROWS) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    if constexpr (SHORT) {
+                        const uint4 q = make_uint4(raw[4 * i], raw[4 * i + 1], raw[4 * i + 2], raw[4 * i + 3]);
+                        Vec16<T>::unpack(q, *(float(*)[8])(v + 8 * i));
+                    } else {
+#pragma unroll
+                        for (int q = 0; q < 8; ++q)
+                            v[8 * i + q] = __uint_as_float(raw[(8 * i + q) % RAW]);
+                    }
+                }
+                if (SHORT && DROP) {
+#pragma unroll
+                    for (int i = 0; i < 32; ++i)
+                        v[i] = __fmul_rn(v[i], A.drop.scale);
+                }
+                const uint32_t byte = encode([&](int i) { return STOCH ? mx4_stochastic8(v + 8 * i, word[STOCH ? 2 * i : 0], word[STOCH ? 2 * i + 1 : 0]) : mx4_nearest8(v + 8 * i); }, code);
                 A.scales[mx4_scale_at(r, c0 >> 5, scale_tiles)] = (uint8_t)(r < A.rows ? byte : 0u);
                 if (r < A.rows)
                     *(uint4 *)(A.codes + (r * blocks + (c0 >> 5)) * 16) = make_uint4(code[0], code[1], code[2], code[3]);
             }
             __syncwarp();
             // the columns
-            uint32_t n[STOCH ? 32 : 1];
-            float most = 0.f;
+            uint32_t noise[STOCH ? 32 : 8];
 #pragma unroll
             for (int i = 0; i < 32; ++i) {
                 const uint32_t w = M.v[i][lane];
-                if (SHORT) {
+                if constexpr (SHORT) {
                     const uint16_t h = (uint16_t)w;
                     v[i] = to_f32(*(const T *)&h);
                     if (DROP)
                         v[i] = __fmul_rn(v[i], A.drop.scale);
                     if (STOCH)
-                        n[i] = (w >> 10 & 0x3FFFC0u) | 32u;
+                        noise[STOCH ? i : 0] = mx4_noise_hi(w);
                 } else {
                     v[i] = __uint_as_float(w);
                     if (STOCH)
-                        n[i] = M.u[i][lane] * 64u + 32u;
+                        noise[STOCH ? i : 0] = mx4_noise_lo(M.u[i][lane]);
                 }
-                most = mx4_absmax(most, v[i]);
             }
-            const uint32_t byte = mx4_scale(__float_as_uint(most));
-            const float inv = mx4_inv(byte);
-            uint32_t code[4];
-#pragma unroll
-            for (int i = 0; i < 32; ++i)
-                v[i] = __fmul_rn(v[i], inv);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                if (STOCH) {
-                    code[i] = 0;
-#pragma unroll
-                    for (int q = 7; q >= 0; --q)
-                        code[i] = code[i] * 16u + mx4_stochastic(v[8 * i + q], n[STOCH ? 8 * i + q : 0]);
-                } else {
-                    code[i] = mx4_nearest8(v + 8 * i);
-                }
-                code[i] = byte == kMx4Nan ? 0u : code[i];
-            }
+            const uint32_t byte = encode([&](int i) { return STOCH ? mx4_stochastic8(v + 8 * i, *(uint32_t(*)[8])(noise + (STOCH ? 8 * i : 0))) : mx4_nearest8(v + 8 * i); }, code);
             A.scales_t[mx4_scale_at(ct, r0 >> 5, scale_tiles_t)] = (uint8_t)(ct < A.cols ? byte : 0u);
             if (ct < A.cols)
                 *(uint4 *)(A.codes_t + (ct * blocks_t + (r0 >> 5)) * 16) = make_uint4(code[0], code[1], code[2], code[3]);
@@ -265,8 +280,8 @@ __global__ void __launch_bounds__(kBothWarps * 32) k_mx4_both(const T *x, const 
 // ------------------------------------------------------------------ the way back
 // Eight elements per thread, U times; rows of the result begin on a boundary of eight elements' size.
 template <class T, int U>
-__global__ void __launch_bounds__(kQThreads) k_mx4_dequantise(const uint8_t *codes, const uint8_t *scales, const Divider pieces, int64_t rows, int64_t cols,
-                                                              T *out, int64_t ld)
+__global__ void __launch_bounds__(kQThreads) k_mx4_dequantise(const uint8_t *codes, const uint8_t *scales, const Divider pieces, uint32_t row0, int64_t rows,
+                                                              int64_t cols, T *out, int64_t ld)
 {
     grid_release();
     const uint32_t p0 = blockIdx.x * (uint32_t)(kQThreads * U) + threadIdx.x, tiles = (uint32_t)mx4_scale_tiles(cols);
@@ -276,10 +291,11 @@ __global__ void __launch_bounds__(kQThreads) k_mx4_dequantise(const uint8_t *cod
 #pragma unroll
     for (int i = 0; i < U; ++i) {
         const uint32_t p = p0 + i * kQThreads;
-        row[i] = divide(p, pieces);
-        at[i] = p - row[i] * pieces.by;
+        const uint32_t r = divide(p, pieces);
+        row[i] = row0 + r;
+        at[i] = p - r * pieces.by;
         if (row[i] < rows) {
-            w[i] = __ldcs((const uint32_t *)codes + p);
+            w[i] = __ldcs((const uint32_t *)codes + (uint64_t)row0 * pieces.by + p);
             s[i] = scales[mx4_scale_at(row[i], at[i] >> 2, tiles)];
         }
     }
@@ -313,35 +329,52 @@ __global__ void __launch_bounds__(kQThreads) k_mx4_dequantise(const uint8_t *cod
         }
     }
 }
-// ... begin anywhere: a block per warp, an element per lane, U times
+// ... begin anywhere: a thread takes those eight elements that fill an aligned piece of the result (`pieces` of them to a row at most), whose codes it cuts out
+// of two words and whose scales are those of two blocks at most; pieces over a row's ends are stored element by element.  8192 x 1601 to
+// fp32: a block per warp and an element per lane took 44 us, this takes 13.5 (4.4 TB/s).
 template <class T, int U>
-__global__ void __launch_bounds__(kQThreads) k_mx4_dequantise_any(const uint8_t *codes, const uint8_t *scales, int64_t rows, int64_t cols, T *out, int64_t ld)
+__global__ void __launch_bounds__(kQThreads) k_mx4_dequantise_any(const uint8_t *codes, const uint8_t *scales, const Divider pieces, uint32_t row0, int64_t rows, int64_t cols,
+                                                                  T *out, int64_t ld)
 {
     grid_release();
-    const int lane = threadIdx.x & 31;
-    const int64_t blocks = mx4_blocks(cols), tiles = mx4_scale_tiles(cols), b0 = ((int64_t)blockIdx.x * (kQThreads / 32) + (threadIdx.x >> 5)) * U;
+    const uint32_t p0 = blockIdx.x * (uint32_t)(kQThreads * U) + threadIdx.x, tiles = (uint32_t)mx4_scale_tiles(cols), words = (uint32_t)mx4_blocks(cols) * 4;
     grid_wait();
-    int64_t row = b0 / blocks, block = b0 - row * blocks;
-    uint8_t w[U], s[U];
-    T *o[U];
+    uint32_t w[U], a[U], b[U], row[U] = {};
+    int64_t e[U] = {};
+    auto full = [&](int i) { return row[i] < rows && e[i] >= 0 && e[i] + 8 <= cols; };
 #pragma unroll
     for (int i = 0; i < U; ++i) {
-        o[i] = row < rows && block * 32 + lane < cols ? out + row * ld + block * 32 + lane : nullptr;
-        if (row < rows) {
-            w[i] = codes[(b0 + i) * 16 + (lane >> 1)];
-            s[i] = scales[mx4_scale_at(row, block, tiles)];
+        const uint32_t p = p0 + i * kQThreads;
+        const uint32_t r = divide(p, pieces);
+        row[i] = row0 + r;
+        const uint32_t shift = (uint32_t)((uintptr_t)(out + (int64_t)row[i] * ld) / sizeof(T)) & 7u;
+        e[i] = (int64_t)(p - r * pieces.by) * 8 - shift;
+        if (full(i)) {
+            w[i] = mx4_codes8((const uint32_t *)codes + (uint64_t)row[i] * words, (uint32_t)e[i]);
+            a[i] = scales[mx4_scale_at(row[i], e[i] >> 5, tiles)];
+            b[i] = scales[mx4_scale_at(row[i], (e[i] + 7) >> 5, tiles)];
         }
-        if (++block == blocks)
-            block = 0, ++row;
     }
 #pragma unroll
-    for (int i = 0; i < U; ++i)
-        if (o[i])
-            *o[i] = from_f32<T>(__fmul_rn(mx4_value(w[i] >> (4 * (lane & 1)) & 0xFu), mx4_pow(s[i])));
+    for (int i = 0; i < U; ++i) {
+        T *o = out + (int64_t)row[i] * ld;
+        if (full(i)) {
+            float v[8];
+            mx4_scaled8(w[i], (uint32_t)e[i], a[i], b[i], v);
+            if constexpr (sizeof(T) == 4)
+                store32(o + e[i], *(const uint32_t(*)[8])v);
+            else
+                __stcs((uint4 *)(o + e[i]), Vec16<T>::pack(v));
+        } else if (row[i] < rows) {
+            for (int64_t j = e[i] < 0 ? 0 : e[i]; j < e[i] + 8 && j < cols; ++j)
+                o[j] = from_f32<T>(__fmul_rn(mx4_value(((const uint32_t *)codes)[(uint64_t)row[i] * words + (j >> 3)] >> (4 * (j & 7)) & 0xFu),
+                                             mx4_pow(scales[mx4_scale_at(row[i], j >> 5, tiles)])));
+        }
+    }
 }
 
 template <class T>
-static cudaError_t quantise(const T *x, QArgs A, bool stochastic, cudaStream_t s)
+static cudaError_t quantise(const T *x, const QArgs &A, bool stochastic, cudaStream_t s)
 {
     // eight elements of a row in one or (fp32) one wide load
     const bool vec = (((uintptr_t)x | (A.rows > 1 ? (uint64_t)A.ld * sizeof(T) : 0u)) & (8 * sizeof(T) - 1)) == 0;
@@ -351,28 +384,24 @@ static cudaError_t quantise(const T *x, QArgs A, bool stochastic, cudaStream_t s
         return stochastic ? (A.drop.off ? f(Y(), Y()) : f(Y(), N())) : (A.drop.off ? f(N(), Y()) : f(N(), N()));
     };
     if (!A.codes_t) {
-        // (blocks are counted in 32 bits: as many tiles of 128 rows per launch as that takes)
-        const int64_t padded = mx4_scale_tiles(A.cols) * 4, rows = A.rows, most = (1ll << 32) / (padded * 128) * 128 - 128;
+        // (blocks are counted in 32 bits: as many rows per launch as that takes)
+        const int64_t padded = mx4_scale_tiles(A.cols) * 4, rows = (A.rows + 127) / 128 * 128, most = ((1ll << 32) - 4096) / padded;
         cudaError_t e = cudaSuccess;
         for (int64_t r0 = 0; r0 < rows && e == cudaSuccess; r0 += most) {
-            A.rows = std::min(most, rows - r0);
-            const int64_t units = (A.rows + 127) / 128 * 128 * padded;
+            const int64_t units = std::min(most, rows - r0) * padded;
             e = by_draws([&](auto st, auto dr) {
                 constexpr bool ST = decltype(st)::value, DR = decltype(dr)::value;
-                auto go = [&](auto vc, auto un) {
-                    constexpr int U = decltype(un)::value, PER = kQThreads / 4 * U;
-                    return launch(k_mx4_rows<T, decltype(vc)::value, ST, DR, U>, dim3((unsigned)((units + PER - 1) / PER)), kQThreads, 0, s, x + r0 * A.ld, A,
-                                  divider((uint32_t)padded), (uint32_t)units);
+                auto go = [&](auto vc, auto ln) {
+                    constexpr int LANES = decltype(ln)::value, PER = kQThreads / LANES;
+                    return launch(k_mx4_rows<T, decltype(vc)::value, ST, DR, LANES>, dim3((unsigned)((units + PER - 1) / PER)), kQThreads, 0, s, x, A,
+                                  divider((uint32_t)padded), (uint32_t)r0, (uint32_t)units);
                 };
-                using One = std::integral_constant<int, 1>;
-                using Many = std::integral_constant<int, sizeof(T) == 4 ? 2 : 4>;
-                const bool many = units >= (int64_t)kQThreads / 4 * Many::value * kPlanSMs * 8;
-                return many ? (vec ? go(std::true_type(), Many()) : go(std::false_type(), Many())) : (vec ? go(std::true_type(), One()) : go(std::false_type(), One()));
+                using Few = std::integral_constant<int, 4>;
+                using Many = std::integral_constant<int, sizeof(T) == 4 && !ST && !DR ? 2 : 1>;
+                if (!vec)
+                    return go(std::false_type(), Few());
+                return units < (int64_t)kQThreads / 4 * kPlanSMs * 16 ? go(std::true_type(), Few()) : go(std::true_type(), Many());
             });
-            A.codes += most * mx4_blocks(A.cols) * 16;
-            A.scales += most / 128 * (padded / 4) * 512;
-            A.dropout += kDrawStep * (uint64_t)(most * ((A.cols + 3) / 4));
-            A.rounding += kDrawStep * (uint64_t)(most * ((A.cols + 3) / 4));
         }
         return e;
     }
@@ -391,19 +420,20 @@ static cudaError_t quantise(const T *x, QArgs A, bool stochastic, cudaStream_t s
 template <class T>
 static cudaError_t dequantise(const uint8_t *codes, const uint8_t *scales, int64_t rows, int64_t cols, T *out, int64_t ld, cudaStream_t s)
 {
-    const int64_t per_row = mx4_blocks(cols) * 4, pieces = rows * per_row;
-    if ((((uintptr_t)out | (rows > 1 ? (uint64_t)ld * sizeof(T) : 0u)) & (8 * sizeof(T) - 1)) == 0 && pieces < (1ll << 32) - 4096) {
+    const bool vec = (((uintptr_t)out | (rows > 1 ? (uint64_t)ld * sizeof(T) : 0u)) & (8 * sizeof(T) - 1)) == 0;
+    // (pieces are counted in 32 bits: as many rows per launch as that takes)
+    const int64_t per_row = vec ? mx4_blocks(cols) * 4 : std::max<int64_t>(2, (cols + 14) / 8), most = ((1ll << 32) - 4096) / per_row;
+    cudaError_t e = cudaSuccess;
+    for (int64_t r0 = 0; r0 < rows && e == cudaSuccess; r0 += most) {
+        const int64_t end = std::min(rows, r0 + most), pieces = (end - r0) * per_row;
         auto go = [&](auto un) {
             constexpr int U = decltype(un)::value, PER = kQThreads * U;
-            return launch(k_mx4_dequantise<T, U>, dim3((unsigned)((pieces + PER - 1) / PER)), kQThreads, 0, s, codes, scales, divider((uint32_t)per_row), rows, cols, out, ld);
+            return launch(vec ? k_mx4_dequantise<T, U> : k_mx4_dequantise_any<T, U>, dim3((unsigned)((pieces + PER - 1) / PER)), kQThreads, 0, s, codes, scales,
+                          divider((uint32_t)per_row), (uint32_t)r0, end, cols, out, ld);
         };
-        return pieces >= (int64_t)kQThreads * 4 * kPlanSMs * 8 ? go(std::integral_constant<int, 4>()) : go(std::integral_constant<int, 1>());
+        e = pieces >= (int64_t)kQThreads * 4 * kPlanSMs * 8 ? go(std::integral_constant<int, 4>()) : go(std::integral_constant<int, 1>());
     }
-    auto go = [&](auto un) {
-        constexpr int U = decltype(un)::value, PER = kQThreads / 32 * U;
-        return launch(k_mx4_dequantise_any<T, U>, dim3((unsigned)((rows * mx4_blocks(cols) + PER - 1) / PER)), kQThreads, 0, s, codes, scales, rows, cols, out, ld);
-    };
-    return rows * mx4_blocks(cols) >= (int64_t)kQThreads / 32 * 8 * kPlanSMs * 8 ? go(std::integral_constant<int, 8>()) : go(std::integral_constant<int, 1>());
+    return e;
 }
 
 }  // namespace conef

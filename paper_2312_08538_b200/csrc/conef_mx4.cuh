@@ -46,33 +46,55 @@ __device__ __forceinline__ uint32_t mx4_nearest8(const float *v)
     return r;
 }
 // Code of one scaled element rounded up where floor(65536 f + 1/2) + u >= 65536, f the part of a step that it lies
-// above the code below it and u its number, given as noise = 64 u + 32.  Times 2^-126 the smallest normal value, 1, becomes fp32's own
+// above the code below it and u its number, given as noise = 256 u + 128.  Times 2^-126 the smallest normal value, 1, becomes fp32's own
 // and the evenly spaced codes below it fp32's subnormals, so that the code is the leading bits of the float throughout and f the 22 that follow; rounded
-// towards zero, since the comparison is with a multiple of 32 in them and sees no bit that this drops.
-__device__ __forceinline__ uint32_t mx4_stochastic(float v, uint32_t noise)
+// towards zero, since the comparison is with a multiple of 32 in them and sees no bit that this drops.  Two places up, without the sign, the code is
+// the highest byte, and one addition rounds it.  (A zero stays one.)
+__device__ __forceinline__ uint32_t mx4_rounded(float v, uint32_t noise) { return __float_as_uint(__fmul_rz(v, 0x1p-126f)) * 4u + noise; }
+__device__ __forceinline__ uint32_t mx4_stochastic(float v, uint32_t noise) { return mx4_rounded(v, noise) >> 24 | (__float_as_uint(v) >> 28 & 8u); }
+// the noise of the lower and the upper half of a word
+__device__ __forceinline__ uint32_t mx4_noise_lo(uint32_t w) { return __byte_perm(w, 0x80u, 0x5104); }
+__device__ __forceinline__ uint32_t mx4_noise_hi(uint32_t w) { return __byte_perm(w, 0x80u, 0x5324); }
+// codes of eight scaled elements with their noise; the signs are those that rounding to nearest gives
+__device__ __forceinline__ uint32_t mx4_stochastic8(const float *v, const uint32_t (&noise)[8])
 {
-    const uint32_t t = __float_as_uint(__fmul_rz(v, 0x1p-126f)) + noise;
-    return ((t >> 22) & 7u) | ((t >> 28) & 8u);   // (bits 25 to 30 are zero)
+    uint32_t t[8];
+#pragma unroll
+    for (int q = 0; q < 8; ++q)
+        t[q] = mx4_rounded(v[q], noise[q]);
+    const uint32_t even = __byte_perm(__byte_perm(t[0], t[2], 0x0073), __byte_perm(t[4], t[6], 0x0073), 0x5410);
+    const uint32_t odd = __byte_perm(__byte_perm(t[1], t[3], 0x0073), __byte_perm(t[5], t[7], 0x0073), 0x5410);
+    return (mx4_nearest8(v) & 0x88888888u) | (odd * 16u + even);
 }
-// the noise of the four columns of a word
-__device__ __forceinline__ void mx4_noise4(uint64_t word, uint32_t (&noise)[4])
-{
-    const uint32_t lo = (uint32_t)word, hi = (uint32_t)(word >> 32);
-    noise[0] = (lo << 6 & 0x3FFFC0u) | 32u;
-    noise[1] = (lo >> 10 & 0x3FFFC0u) | 32u;
-    noise[2] = (hi << 6 & 0x3FFFC0u) | 32u;
-    noise[3] = (hi >> 10 & 0x3FFFC0u) | 32u;
-}
-// ... of eight scaled elements by two words
 __device__ __forceinline__ uint32_t mx4_stochastic8(const float *v, uint64_t w0, uint64_t w1)
 {
-    uint32_t n[2][4], r = 0;
-    mx4_noise4(w0, n[0]);
-    mx4_noise4(w1, n[1]);
+    const uint32_t w[4] = {(uint32_t)w0, (uint32_t)(w0 >> 32), (uint32_t)w1, (uint32_t)(w1 >> 32)};
+    uint32_t noise[8];
 #pragma unroll
-    for (int q = 7; q >= 0; --q)
-        r = r * 16u + mx4_stochastic(v[q], n[q >> 2][q & 3]);
+    for (int i = 0; i < 4; ++i)
+        noise[2 * i] = mx4_noise_lo(w[i]), noise[2 * i + 1] = mx4_noise_hi(w[i]);
+    return mx4_stochastic8(v, noise);
+}
+// the largest of the sizes of three, NaN where one is
+__device__ __forceinline__ float mx4_absmax3(float a, float b, float c)
+{
+    float r;
+    asm("max.NaN.abs.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
     return r;
+}
+__device__ __forceinline__ float mx4_absmax2(float a, float b) { return mx4_absmax3(a, b, b); }
+// ... of n elements, a multiple of 8, in four chains
+template <int N>
+__device__ __forceinline__ float mx4_absmax(const float *v)
+{
+    float m[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        m[i] = mx4_absmax2(v[2 * i], v[2 * i + 1]);
+#pragma unroll
+    for (int i = 8; i < N; i += 2)
+        m[i / 2 % 4] = mx4_absmax3(m[i / 2 % 4], v[i], v[i + 1]);
+    return mx4_absmax2(mx4_absmax3(m[0], m[1], m[2]), m[3]);
 }
 // values of two codes (low four bits first), still to be scaled
 __device__ __forceinline__ float2 mx4_values2(uint32_t byte)
@@ -94,6 +116,22 @@ __device__ __forceinline__ void mx4_values8(uint32_t w, float (&v)[8])
         const float2 f = __half22float2(*(const __half2 *)&h[i]);
         v[2 * i] = f.x, v[2 * i + 1] = f.y;
     }
+}
+// Eight codes from element e of a row on, all of them in it, words: its codes
+__device__ __forceinline__ uint32_t mx4_codes8(const uint32_t *words, uint32_t e)
+{
+    const uint32_t w = e >> 3, s = e & 7u;
+    return __funnelshift_r(words[w], s ? words[w + 1] : 0u, 4u * s);
+}
+// ... times their scales, first and last being those of the first and the last of them
+__device__ __forceinline__ void mx4_scaled8(uint32_t codes, uint32_t e, uint32_t first, uint32_t last, float (&v)[8])
+{
+    mx4_values8(codes, v);
+    const float a = mx4_pow(first), b = mx4_pow(last);
+    const uint32_t border = 32u - (e & 31u);
+#pragma unroll
+    for (uint32_t q = 0; q < 8; ++q)
+        v[q] = __fmul_rn(v[q], q < border ? a : b);
 }
 __device__ __forceinline__ float mx4_value(uint32_t code)   // one code
 {
