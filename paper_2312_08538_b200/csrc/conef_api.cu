@@ -303,7 +303,7 @@ int make_plan(const conef_tensor *tensors, int n_tensors, int n_workers, const c
             }
             tiles[T_FLAT] = (int)ceil_div(L.nunits, kFlatUnitsPerCta);
             tiles[T_GS] = 1;
-            tiles[T_DECODE] = tiles[T_DENSE] = (int)ceil_div(L.d, c->kind == CONEF_C_IDENTITY ? kDecTile : dec_tile(P.dec_batch));
+            tiles[T_DECODE] = tiles[T_DENSE] = (int)ceil_div(L.d, c->kind == CONEF_C_IDENTITY ? kDecTile : mx4 ? dec_mx4_tile(P.dec_batch) : dec_tile(P.dec_batch));
             if (q->kind == CONEF_Q_IDENTITY) {
                 L.k = L.d;
             } else if (q->kind == CONEF_Q_RANDBLOCK) {

@@ -110,14 +110,17 @@ __global__ void __launch_bounds__(kDecThreads) k_decode(const __grid_constant__ 
 }
 
 // Microscaled 4-bit floats.  A thread takes eight elements at a time, those that fill 32 aligned bytes of the output wherever that begins: its codes are cut
-// out of two words, its scales are those of two blocks at most.  A tile has as many such pieces as the one above has elements of eight, the last one
-// may have one more; pieces over a tensor's ends are stored element by element.  Layers of a transformer, an odd one among them, 13.6 M elements:
-// where the output begins off a boundary, element by element took 33 us per worker, this takes 14.4 (4.3 TB/s).
+// out of two words, its scales are those of two blocks at most.  The last tile
+// may have one piece more than the others; pieces over a tensor's ends are stored element by element.  Layers of a transformer, an odd one among them, 13.6 M elements:
+// where the output begins off a boundary, element by element took 33 us per worker, this takes 10.8 (5.7 TB/s).
+// Elements per CTA, two pieces per thread at a time: 50257 x 1600 and 13.6 M elements of four layers 58.5 and 10.8 us; half a tile 60 and 11.3, all
+// four pieces at once 80 and 12.1, one piece per CTA and thread 65 and 12.7.
+__host__ __device__ constexpr int dec_mx4_tile(int batch) { return kDecThreads * 8 * batch; }
 template <int BATCH>
 __global__ void __launch_bounds__(kDecThreads) k_decode_mx4(const __grid_constant__ DevView V, const int32_t *__restrict__ pfx, int worker,
                                                             float *__restrict__ out)
 {
-    constexpr uint32_t PIECES = dec_tile(BATCH) / 8, U = 2;
+    constexpr uint32_t PIECES = dec_mx4_tile(BATCH) / 8, U = BATCH == 1 ? 1 : 2;
     grid_release();
     const int li = find_layer(pfx, V.n_layers, blockIdx.x);
     const LayerDesc &L = V.layers[li];

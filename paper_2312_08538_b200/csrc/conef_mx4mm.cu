@@ -1,9 +1,14 @@
 // Product of two matrices held in microscaled 4-bit floats, out[i][j] = sum over k of A[i][k] B[j][k], in fp32 on the tensor
 // cores' block-scaled path and rounded once to the output's type.
 //
-// A CTA per SM walks over tiles of 128 x BN outputs (BN 64 to 256), ten warps with a part each: one brings 256 elements of k at a time
-// into a ring of stages (codes by tiled copies, scales, which lie in memory as the tensor cores take them, by plain bulk ones), one
-// issues the products, and eight move the sums from tensor memory to registers, let the next tile begin, and store.
+// A CTA per SM, or a pair of CTAs on two SMs that share the rows of B, walks over tiles of 128 (256) x BN outputs, BN 64 to 256.  18 warps with a
+// part each: one brings 256 elements of k at a time into a ring of stages (codes by tiled copies; scales, which lie in memory as the
+// tensor cores take them, by plain bulk ones), one issues the products, and sixteen move the sums of a tile from tensor memory through registers and shared
+// memory to the output while the next tile's are formed in a second set.
+//
+// 8192 x 6400 x 1600 in bf16 takes 45 us (3.7 PFLOP/s).  The products alone would take 20 at full rate, the output's 105 MB 16 at the memory's.
+// What bounds it is the way into an SM: a pair's tile of 192 columns takes 217 KB per SM, 1.8 us at the 64 bytes per cycle that were measured,
+// its products 1.3 us.  Without the loads the kernel takes 33 us, without the stores 33, without either 30.
 #include <cuda.h>
 
 #include <algorithm>
@@ -28,7 +33,9 @@ struct MmArgs {
     uint32_t k64, stages_k;      // steps of 64 and of kMmK elements along k
     uint32_t tiles;              // tiles of scales along k
     uint32_t b_rows;             // ... of 128 rows of B
-    uint32_t bn, tiles_m, tiles_n;
+    uint32_t bn;
+    Divider band, low;           // tiles of a whole band, rows of tiles in the last one (2 at least)
+    uint32_t last_band, last_rows;
     uint32_t n_tiles, stages;
     uint32_t tiled;              // outputs go by tiled copies
     uint32_t sums, scale_column; // sets of sums in tensor memory, and the first column of scales
@@ -44,15 +51,21 @@ __host__ __device__ inline uint32_t mm_stage_bytes(uint32_t bn, bool pair) { ret
 inline uint32_t mm_staging(uint32_t bn) { return bn / 16 * 4096; }   // per storing warp 32 rows of 128 bytes, where outputs are turned from a row per lane
 
 // Tiles are taken in bands of kMmBand along m, so that what runs at a time is about as high as wide (8192 x 6400 x 1600, pairs of 256 columns: in bands
-// of 8 and of 4 53 us, of one 59, in one band of all 55.6; with 192 columns 47.6 to 48.8)
+// of 8 and of 4 53 us, of one 59, in one band of all 55.6; with 192 columns 47.6 to 48.8).  No division: a tile's place is
+// on the way of the products from one tile to the next.
 constexpr uint32_t kMmBand = 8;
 struct MmTile {
     uint32_t m, n;
 };
 __device__ __forceinline__ MmTile mm_tile(const MmArgs &P, uint32_t tile)
 {
-    const uint32_t band = tile / (kMmBand * P.tiles_n), in = tile - band * kMmBand * P.tiles_n, high = min(kMmBand, P.tiles_m - band * kMmBand);
-    return {band * kMmBand + in % high, in / high};
+    const uint32_t band = divide(tile, P.band), in = tile - band * P.band.by;
+    uint32_t n = in / kMmBand, rows = kMmBand;
+    if (band == P.last_band) {
+        rows = P.last_rows;
+        n = rows == 1 ? in : divide(in, P.low);
+    }
+    return {band * kMmBand + in - n * rows, n};
 }
 
 struct MmShared {
@@ -327,24 +340,27 @@ static bool encode(CUtensorMap *map, CUtensorMapDataType type, int elem, const v
                                             CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-// Columns per tile, and whether pairs of CTAs take tiles of 256 rows: the choice whose waves of tiles over the SMs take least.  Nanoseconds per wave from
-// 8192 x 6400 by 1600 and by 4096: what a step of 64 along k takes (128, 192, 256 columns: single CTAs 53, 69, 91, pairs 52, 62, 76; full rate
-// would be 35, 52, 70), and what does not depend on k (pairs 950, 1300, and 2460 where tensor memory has room for one set of sums only).
-// Single CTAs and pairs there: 64.4, 54.1, 52.3 us and 54.6, 47.8, 52.9 us.
+// Columns per tile, and whether pairs of CTAs take tiles of 256 rows: the choice whose waves of tiles over the SMs take least.  Nanoseconds per wave, from
+// 8192 x 6400 by 1600 and by 4096: what a step of 64 along k takes (64, 128, 192, 256 columns: single CTAs 45, 52, 67, 88, pairs 45, 48, 60, 73; full rate
+// would be 17, 35, 52, 70), what does not depend on k (pairs 970, 1240, and 2450 where tensor memory has room for one set of sums only), and a
+// microsecond more per launch of pairs.  Microseconds, single CTAs and pairs of these widths, the choice marked:
+//   8192 x 6400 x 1600   79.3  57.6  51.8  50.8   78.8  51.7  45.4* 51.8        1111 x 2601 x 651   8.7  8.2  7.1* 8.5   11.6  9.6  8.0  8.7
+//   8192 x 1600 x 1600   21.9  17.7  16.1  18.0   22.9  16.7  14.8* 18.7        4000 x 4000 x 300   15.0  12.1  11.9*  11.3   21.7  15.2  13.3  13.5
+//   2048 x 6400 x 1600   22.2  17.8  16.1  15.4   23.0  16.5  14.8* 16.1        300 x 300 x 1600    5.2*  5.9  6.7  8.0   6.0  6.6  7.1  8.2
 struct MmChoice {
     uint32_t bn;
     bool pair;
 };
 static MmChoice mm_choice(int64_t m, int64_t n, int64_t k)
 {
-    static const int per_step[2][4] = {{45, 53, 69, 91}, {45, 52, 62, 76}}, per_tile[4] = {700, 1000, 1350, 2400};
+    static const int per_step[2][4] = {{45, 52, 67, 88}, {45, 48, 60, 73}}, per_tile[4] = {700, 970, 1240, 2450};
     MmChoice best = {0, false};
     int64_t least = 0;
     for (int pair = 0; pair < 2; ++pair)
         for (uint32_t bn = 64; bn <= 256; bn += 64) {
             const int64_t rows = pair ? 2 * kMmM : kMmM, sets = pair ? kPlanSMs / 2 : kPlanSMs;
             const int64_t waves = ((m + rows - 1) / rows * ((n + bn - 1) / bn) + sets - 1) / sets;
-            const int64_t cost = waves * ((k + 63) / 64 * per_step[pair][bn / 64 - 1] + per_tile[bn / 64 - 1]);
+            const int64_t cost = waves * ((k + 63) / 64 * per_step[pair][bn / 64 - 1] + per_tile[bn / 64 - 1]) + pair * 1000;
             if (!best.bn || cost < least)
                 best = {bn, pair != 0}, least = cost;
         }
@@ -367,12 +383,14 @@ static int matmul(const uint8_t *a, const uint8_t *as, int64_t m, const uint8_t 
     P.tiles = (uint32_t)mx4_scale_tiles(k);
     P.b_rows = (uint32_t)((n + 127) / 128);
     P.bn = bn;
-    P.tiles_m = (uint32_t)((m + kRows - 1) / kRows);
-    const int64_t tiles = (int64_t)P.tiles_m * ((n + bn - 1) / bn);
-    if (tiles >= (1ll << 32) - kPlanSMs)
+    const int64_t tiles_m = (m + kRows - 1) / kRows, tiles_n = (n + bn - 1) / bn, tiles = tiles_m * tiles_n;
+    if (tiles >= (1ll << 32) - kPlanSMs || tiles_n >= (1ll << 28))
         return CONEF_ERR_UNSUPPORTED;
-    P.tiles_n = (uint32_t)((n + bn - 1) / bn);
     P.n_tiles = (uint32_t)tiles;
+    P.band = divider((uint32_t)(tiles_n * kMmBand));
+    P.last_band = (uint32_t)((tiles_m - 1) / kMmBand);
+    P.last_rows = (uint32_t)(tiles_m - (int64_t)P.last_band * kMmBand);
+    P.low = divider(std::max(2u, P.last_rows));
     // tensor memory: two sets of sums where that leaves room for the scales
     P.sums = bn <= 192 ? 2 : 1;
     P.scale_column = P.sums * bn > 256 ? 384 : 256;
