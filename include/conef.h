@@ -242,9 +242,9 @@ int64_t conef_state_bytes_per_worker(const conef_ctx *ctx);   /* compressed erro
 
 /* DEVICE pointer to worker's message buffer of the given kind. */
 int conef_get_message(const conef_ctx *ctx, int which, int worker, float **ptr /* HOST out */);
-/* DEVICE pointers to the stored error of (worker, tensor): a = codes (int8 or
- * packed int4), dense e (identity) or the sketch; b = scales (fp32 or fp16) or
- * NULL.  Sizes in bytes. */
+/* DEVICE pointers to the stored error of (worker, tensor): a = codes (int8,
+ * packed int4 or packed mx4), dense e (identity) or the sketch; b = scales (fp32,
+ * fp16, or mx4's bytes in order) or NULL.  Sizes in bytes. */
 int conef_get_state(const conef_ctx *ctx, int worker, int tensor, void **a, size_t *a_bytes,
                     void **b, size_t *b_bytes);
 /* The same for the second state q of iConEF-v1, or for e~ of iConEF-v2 (a = k fp32 values, b =
@@ -366,7 +366,8 @@ int conef_randk_indices_noalloc_select(uint64_t seed, int64_t tensor, int64_t st
  * worker + 1), tensor and step; element (r, c) of a matrix of C columns has, in the stream's hash of 2 (r ceil(C/4) +
  * floor(c/4)) (dropout) or of that + 1 (rounding), the 16 bits from 16 (c mod 4) on as its number u in 0..65535.
  * So the numbers depend on the draw, the number of columns and the element's place alone, and a
- * backward pass that names the draw of the forward pass has its numbers again. */
+ * backward pass that names the draw of the forward pass has its numbers again.  A call captured into a graph draws the
+ * numbers of the draw it was captured with in every replay. */
 typedef struct {
     uint64_t seed;
     int64_t worker, tensor, step; /* >= 0 */

@@ -248,8 +248,11 @@ def _same_device(where: str, device: torch.device, stream: Optional[torch.cuda.S
     for t in tensors:
         if t.device != device:
             _refuse(where, "the tensors are on different devices")
-    if stream is not None and stream.device != device:
-        _refuse(where, "the stream belongs to another device than the tensors")
+    if stream is not None:
+        if stream.device != device:
+            _refuse(where, "the stream belongs to another device than the tensors")
+        for t in tensors:   # (a tensor given up by its owner stays until the call is done with it)
+            t.record_stream(stream)
 
 
 def dropout(x: torch.Tensor, p: float, draw: Draw, add: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None,
@@ -274,7 +277,7 @@ def dropout(x: torch.Tensor, p: float, draw: Draw, add: Optional[torch.Tensor] =
     if out is not None:
         out_ld = _matrix(out, "dropout", "out")[2]
     device = x.device
-    _same_device("dropout", device, stream, *(t for t in (add, out) if t is not None))
+    _same_device("dropout", device, stream, *(t for t in (x, add, out) if t is not None))
     with _on(device, stream):
         if out is None:
             out = torch.empty_like(x, memory_format=torch.contiguous_format)
@@ -319,7 +322,7 @@ def mx4_quantise(x: torch.Tensor, forms: str = "rows", stochastic: bool = False,
         _refuse("mx4_quantise", "forms has to be rows, cols or both")
     device = x.device
     if stream is not None:
-        _same_device("mx4_quantise", device, stream)
+        _same_device("mx4_quantise", device, stream, x)
     with _on(device, stream):
         a = _form(rows, cols, device) if forms != "cols" else None
         t = _form(cols, rows, device) if forms != "rows" else None
@@ -338,7 +341,7 @@ def mx4_dequantise(a: MX4, dtype: torch.dtype = torch.float32, stream: Optional[
     if dtype not in _ELEM:
         _refuse("mx4_dequantise", "dtype has to be float32, bfloat16 or float16")
     device = a.codes.device
-    _same_device("mx4_dequantise", device, stream, a.scales)
+    _same_device("mx4_dequantise", device, stream, a.codes, a.scales)
     with _on(device, stream):
         out = torch.empty(a.rows, a.cols, dtype=dtype, device=device)
         _check(lib.conef_mx4_dequantise(a.codes.data_ptr(), a.scales.data_ptr(), a.rows, a.cols, out.data_ptr(), _ELEM[dtype], a.cols,
@@ -356,7 +359,7 @@ def mx4_matmul(a: MX4, b: MX4, dtype: torch.dtype = torch.bfloat16, stream: Opti
     if dtype not in _ELEM:
         _refuse("mx4_matmul", "dtype has to be float32, bfloat16 or float16")
     device = a.codes.device
-    _same_device("mx4_matmul", device, stream, a.scales, b.codes, b.scales)
+    _same_device("mx4_matmul", device, stream, a.codes, a.scales, b.codes, b.scales)
     with _on(device, stream):
         out = torch.empty(a.rows, b.rows, dtype=dtype, device=device)
         _check(lib.conef_mx4_matmul(a.codes.data_ptr(), a.scales.data_ptr(), a.rows, b.codes.data_ptr(), b.scales.data_ptr(), b.rows, a.cols,

@@ -118,17 +118,17 @@ __global__ void __launch_bounds__(kDecThreads) k_decode(const __grid_constant__ 
 __host__ __device__ constexpr int dec_mx4_tile(int batch) { return kDecThreads * 8 * batch; }
 template <int BATCH>
 __global__ void __launch_bounds__(kDecThreads) k_decode_mx4(const __grid_constant__ DevView V, const int32_t *__restrict__ pfx, int worker,
-                                                            float *__restrict__ out)
+                                                            float *out)
 {
     constexpr uint32_t PIECES = dec_mx4_tile(BATCH) / 8, U = BATCH == 1 ? 1 : 2;
     grid_release();
     const int li = find_layer(pfx, V.n_layers, blockIdx.x);
     const LayerDesc &L = V.layers[li];
-    const uint8_t *__restrict__ st = V.state + worker * V.state_stride;
-    const uint32_t *__restrict__ words = (const uint32_t *)(st + L.a_off);
+    const uint8_t *st = V.state + worker * V.state_stride;
+    const uint32_t *words = (const uint32_t *)(st + L.a_off);
     const uint8_t *__restrict__ scales = st + L.b_off;
     const int64_t d = L.d, tile = blockIdx.x - pfx[li];
-    float *__restrict__ o = out + L.e_off;
+    float *o = out + L.e_off;
     const int64_t shift = ((uintptr_t)o >> 2) & 7;
     const int64_t c0 = tile * PIECES + threadIdx.x, end = (tile + 1) * (int64_t)(8 * PIECES) >= d ? (d + shift + 7) / 8 : (tile + 1) * PIECES;
     grid_wait();

@@ -24,6 +24,7 @@ constexpr int kMmM = 128, kMmK = 256;                    // rows of A per tile, 
 constexpr int kMmEpilogue = 16, kMmThreads = (kMmEpilogue + 2) * 32;   // (four warps per 64 columns)
 constexpr int kMmMaxStages = 6;
 constexpr uint32_t kMmSmem = 226 * 1024;                 // of a CTA's 227 KB, beside the barriers
+constexpr uint32_t kMmAlone = 116 * 1024;                // more than half of an SM's 228 KB
 // tensor memory, all of it, so from column 0 on: the sums, then the scales of each stage, two tiles along k of 4 (A) and 8 columns (B)
 constexpr uint32_t kMmColumns = 512, kMmScaleColumns = 24;
 
@@ -397,20 +398,23 @@ static int matmul(const uint8_t *a, const uint8_t *as, int64_t m, const uint8_t 
     const uint32_t stage_bytes = mm_stage_bytes(bn, PAIR);
     const uint32_t room = kMmSmem - 1024 - mm_staging(bn);
     P.stages = std::min<uint32_t>({(uint32_t)kMmMaxStages, (kMmColumns - P.scale_column) / kMmScaleColumns, room / stage_bytes, std::max(2u, P.stages_k)});
-    P.tiled = (((uint64_t)ld * sizeof(T)) | (uintptr_t)out) % 16 == 0;
+    // (a tiled copy writes a row's last 16 bytes whole, whatever the map says of its end)
+    P.tiled = (((uint64_t)ld * sizeof(T)) | ((uint64_t)n * sizeof(T)) | (uintptr_t)out) % 16 == 0;
     MmMaps maps;
     const int64_t row_bytes = mx4_blocks(k) * 16, scale_bytes = (int64_t)P.tiles * 512;
     bool ok = encode(&maps.a, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, a, m, row_bytes, row_bytes, 128, kMmM) &&
               encode(&maps.b, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, b, n, row_bytes, row_bytes, 128, PAIR ? bn / 2 : bn);
     if (P.tiled)
         ok = ok && encode(&maps.out, sizeof(T) == 4 ? CU_TENSOR_MAP_DATA_TYPE_UINT32 : CU_TENSOR_MAP_DATA_TYPE_UINT16, sizeof(T), out, m, n * (int64_t)sizeof(T),
-                          (m > 1 ? ld : (n + 7) / 8 * 8) * (int64_t)sizeof(T), 128 / sizeof(T), 32);
+                          (m > 1 ? ld : n) * (int64_t)sizeof(T), 128 / sizeof(T), 32);
     if (PAIR)
         ok = ok && encode(&maps.as, CU_TENSOR_MAP_DATA_TYPE_UINT32, 4, as, (m + 127) / 128, scale_bytes, scale_bytes, 256, 1) &&
              encode(&maps.bs, CU_TENSOR_MAP_DATA_TYPE_UINT32, 4, bs, P.b_rows, scale_bytes, scale_bytes, 256, mm_scale_rows(bn));
     if (!ok)
         return launched(cudaErrorInvalidValue, "conef_mx4_matmul: tensor map");
-    const size_t smem = 1024 + (size_t)P.stages * stage_bytes + mm_staging(bn);
+    // Never two CTAs on an SM, of two products at once either: each takes all of tensor memory, and of two pairs on the same SMs
+    // each could hold one half.
+    const size_t smem = std::max<size_t>(1024 + (size_t)P.stages * stage_bytes + mm_staging(bn), kMmAlone);
     static int done[64];
     cudaError_t e = opt_in_smem(k_mx4_matmul<T, PAIR>, kMmSmem, done);
     if (e == cudaSuccess) {

@@ -417,3 +417,94 @@ def test_behind_a_kernel_that_writes_the_input_late(b):
         got = [b.dropout(x, 0.5, draw(b)), b.mx4_dequantise(b.mx4_quantise(x)), b.mx4_matmul(b.mx4_quantise(x), b.mx4_quantise(x))]
         torch.cuda.synchronize()
         assert all(torch.equal(p, q) for p, q in zip(want, got))
+
+
+def test_two_chains_at_once(b):
+    """Calls on two streams without an order between them: none keeps anything that the other could find."""
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    jobs = []
+    for i, (m, n, k) in enumerate([(1000, 700, 1600), (300, 64, 320)]):
+        jobs.append((matrix(m, k, torch.bfloat16, i), b.mx4_quantise(matrix(n, k, torch.bfloat16, 7 + i)), b.Draw(1, 0, i, 0)))
+
+    def chain(x, w, d, stream=None):
+        y = b.dropout(x, 0.1, d, stream=stream)
+        r, t = b.mx4_quantise(y, forms="both", stochastic=True, p=0.2, draw=d, stream=stream)
+        return b.mx4_matmul(r, w, dtype=torch.float32, stream=stream), b.mx4_dequantise(t, stream=stream)
+
+    want = [chain(*j) for j in jobs]
+    torch.cuda.synchronize()
+    got = [[chain(*j, stream=s) for _ in range(20)] for j, s in zip(jobs, streams)]
+    both = []
+    for _ in range(20):
+        for j, s in zip(jobs, streams):
+            both.append((j, chain(*j, stream=s)))
+    torch.cuda.synchronize()
+    for w, runs in zip(want, got):
+        for r in runs:
+            assert all(torch.equal(p, q) for p, q in zip(w, r))
+    for i, (_, r) in enumerate(both):
+        assert all(torch.equal(p, q) for p, q in zip(want[i % 2], r))
+
+
+def test_a_tensor_given_up_while_another_stream_works_on_it(b):
+    s = torch.cuda.Stream()
+    a = torch.randn(4096, 4096, device="cuda")
+    x = matrix(512, 1600, torch.float32)
+    want = b.dropout(x, 0.5, draw(b))
+    torch.cuda.synchronize()
+    for _ in range(4):
+        y = x.clone()
+        torch.cuda.synchronize()
+        with torch.cuda.stream(s):
+            for _ in range(3):
+                a = a @ a * 1e-4
+        got = b.dropout(y, 0.5, draw(b), stream=s)
+        del y
+        z = torch.full((512, 1600), 9.0, device="cuda")       # would take y's memory
+        torch.cuda.synchronize()
+        assert torch.equal(got, want)
+        del z
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("extra,front", [(0, 0), (1, 0), (3, 1), (8, 0), (16, 8), (13, 5)])
+@pytest.mark.parametrize("m,n,k", [(5, 70, 64), (140, 131, 96), (300, 256, 300)])
+def test_results_with_rows_further_apart(b, dtype, extra, front, m, n, k):
+    """Products and values into the columns of a wider matrix, through the C interface: what lies between the rows stays."""
+    a, c = b.mx4_quantise(matrix(m, k, torch.float32)), b.mx4_quantise(matrix(n, k, torch.float32, 1))
+    ld, code = n + front + extra, {torch.float32: b.F32, torch.bfloat16: b.BF16, torch.float16: b.F16}[dtype]
+    wide = torch.full((m + 2, ld), 7.0, dtype=dtype, device="cuda")
+    at = wide.data_ptr() + (ld + front) * wide.element_size()
+    assert b.lib.conef_mx4_matmul(a.codes.data_ptr(), a.scales.data_ptr(), m, c.codes.data_ptr(), c.scales.data_ptr(), n, k, at, code, ld, b._stream_handle(None)) == b.OK
+    inner = wide[1:-1, front:front + n]
+    assert torch.equal(inner, b.mx4_matmul(a, c, dtype=dtype))
+    inner.fill_(7.0)
+    assert (wide == 7).all()
+    q = b.mx4_quantise(matrix(m, n, torch.float32, 2))
+    assert b.lib.conef_mx4_dequantise(q.codes.data_ptr(), q.scales.data_ptr(), m, n, at, code, ld, b._stream_handle(None)) == b.OK
+    assert torch.equal(inner, b.mx4_dequantise(q, dtype=dtype))
+    inner.fill_(7.0)
+    assert (wide == 7).all()
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("rows,cols", [(5000, 1), (3000, 2), (1, 70000), (2, 33333), (129, 8192)])
+def test_narrow_and_long_matrices(b, dtype, rows, cols):
+    x = matrix(rows, cols, dtype)
+    check_dropout(b.dropout(x, 0.3, draw(b)), x, 0.3)
+    codes, scales = unpacked(b.mx4_quantise(x, stochastic=True, p=0.3, draw=draw(b)))
+    want = reference(x, True, 0.3, False)
+    assert np.array_equal(codes, want[0]) and np.array_equal(scales, want[1])
+    a, t = b.mx4_quantise(x, forms="both")
+    for form, transposed in ((a, False), (t, True)):
+        got, want = unpacked(form), reference(x, False, 0.0, transposed)
+        assert np.array_equal(got[0], want[0]) and np.array_equal(got[1], want[1])
+        assert np.array_equal(f64(b.mx4_dequantise(form)), mo.decode(*want))
+
+
+def test_a_row_of_a_larger_tensor_and_an_array_off_a_boundary(b):
+    whole = matrix(1, 40 * 999 + 5, torch.bfloat16)[0]
+    x = whole[5:].view(40, 999)
+    how = dict(stochastic=True, p=0.25, draw=draw(b))
+    for form, other in zip(b.mx4_quantise(x, forms="both", **how), b.mx4_quantise(x.clone(), forms="both", **how)):
+        assert torch.equal(form.codes, other.codes) and torch.equal(form.scales, other.scales)
