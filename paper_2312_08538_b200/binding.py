@@ -239,9 +239,15 @@ def _on(device: torch.device, stream: Optional[torch.cuda.Stream]):
     return _NOTHING if device.index == torch._C._cuda_getDevice() else torch.cuda.device(device)
 
 
-def _plain(x: torch.Tensor, stream: Optional[torch.cuda.Stream]) -> bool:
-    """Whether a call is for the current device and stream, and on whole rows one behind the other."""
-    return stream is None and x.is_cuda and x.is_contiguous() and x.dtype in _ELEM and x.dim() > 0 and x.get_device() == torch._C._cuda_getDevice()
+def _at_hand(stream: Optional[torch.cuda.Stream], *tensors: torch.Tensor) -> bool:
+    """Whether a call is for the current device, which holds the tensors, and its current stream: nothing to switch then."""
+    if stream is not None:
+        return False
+    here = torch._C._cuda_getDevice()
+    for t in tensors:
+        if t.get_device() != here:
+            return False
+    return True
 
 
 def _same_device(where: str, device: torch.device, stream: Optional[torch.cuda.Stream], *tensors: torch.Tensor) -> None:
@@ -259,11 +265,13 @@ def dropout(x: torch.Tensor, p: float, draw: Draw, add: Optional[torch.Tensor] =
             stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
     """x behind a dropout with probability p (a multiple of 2^-16), plus `add`.  The mask comes from `draw` and is not stored:
     the gradient of x is this call on the gradient of the result, with the same draw and without `add`."""
-    if add is None and out is None and _plain(x, stream):   # (what follows, without what it need not ask: a third of a small call's host time)
+    code = _ELEM.get(x.dtype)
+    if add is None and out is None and code is not None and x.is_contiguous() and x.is_cuda and _at_hand(stream, x) and x.dim():
+        # (what follows, without what it need not ask: a third of a small call's host time)
         cols = x.shape[-1]
         out = torch.empty_like(x)
-        rc = lib.conef_dropout(x.data_ptr(), None, out.data_ptr(), _ELEM[x.dtype], x.numel() // cols if cols else 0, cols, cols, cols, cols, p, draw,
-                               _stream_handle(None))
+        rc = lib.conef_dropout(x.data_ptr(), None, out.data_ptr(), code, x.numel() // cols if cols else 0, cols, cols, cols, cols, p, draw,
+                               torch._C._cuda_getCurrentRawStream(x.get_device()))
         if rc:
             _check(rc, "conef_dropout")
         return out
@@ -320,32 +328,36 @@ def mx4_quantise(x: torch.Tensor, forms: str = "rows", stochastic: bool = False,
     rows, cols, ld = _matrix(x, "mx4_quantise")
     if forms not in ("rows", "cols", "both"):
         _refuse("mx4_quantise", "forms has to be rows, cols or both")
-    device = x.device
-    if stream is not None:
-        _same_device("mx4_quantise", device, stream, x)
-    with _on(device, stream):
-        a = _form(rows, cols, device) if forms != "cols" else None
-        t = _form(cols, rows, device) if forms != "rows" else None
-        if rows and cols:
-            rc = lib.conef_mx4_quantise(x.data_ptr(), _ELEM[x.dtype], rows, cols, ld, p, 1 if stochastic else 0, draw, a.codes.data_ptr() if a else None,
-                                        a.scales.data_ptr() if a else None, t.codes.data_ptr() if t else None, t.scales.data_ptr() if t else None,
-                                        _stream_handle(None))
-            if rc:
-                _check(rc, "conef_mx4_quantise")
+    if not _at_hand(stream, x):
+        _same_device("mx4_quantise", x.device, stream, x)
+        with _on(x.device, stream):
+            return mx4_quantise(x, forms, stochastic, p, draw)
+    a = _form(rows, cols, x.device) if forms != "cols" else None
+    t = _form(cols, rows, x.device) if forms != "rows" else None
+    if rows and cols:
+        rc = lib.conef_mx4_quantise(x.data_ptr(), _ELEM[x.dtype], rows, cols, ld, p, 1 if stochastic else 0, draw, a.codes.data_ptr() if a else None,
+                                    a.scales.data_ptr() if a else None, t.codes.data_ptr() if t else None, t.scales.data_ptr() if t else None,
+                                    torch._C._cuda_getCurrentRawStream(x.get_device()))
+        if rc:
+            _check(rc, "conef_mx4_quantise")
     return (a, t) if forms == "both" else a if t is None else t
 
 
 def mx4_dequantise(a: MX4, dtype: torch.dtype = torch.float32, stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
     """The values of a form, rows x cols."""
     _mx4_check(a, "mx4_dequantise")
-    if dtype not in _ELEM:
+    code = _ELEM.get(dtype)
+    if code is None:
         _refuse("mx4_dequantise", "dtype has to be float32, bfloat16 or float16")
-    device = a.codes.device
-    _same_device("mx4_dequantise", device, stream, a.codes, a.scales)
-    with _on(device, stream):
-        out = torch.empty(a.rows, a.cols, dtype=dtype, device=device)
-        _check(lib.conef_mx4_dequantise(a.codes.data_ptr(), a.scales.data_ptr(), a.rows, a.cols, out.data_ptr(), _ELEM[dtype], a.cols,
-                                        _stream_handle(None)), "conef_mx4_dequantise")
+    rows, cols, codes, scales = a
+    if not _at_hand(stream, codes, scales):
+        _same_device("mx4_dequantise", codes.device, stream, codes, scales)
+        with _on(codes.device, stream):
+            return mx4_dequantise(a, dtype)
+    out = torch.empty(rows, cols, dtype=dtype, device=codes.device)
+    rc = lib.conef_mx4_dequantise(codes.data_ptr(), scales.data_ptr(), rows, cols, out.data_ptr(), code, cols, torch._C._cuda_getCurrentRawStream(codes.get_device()))
+    if rc:
+        _check(rc, "conef_mx4_dequantise")
     return out
 
 
@@ -356,14 +368,20 @@ def mx4_matmul(a: MX4, b: MX4, dtype: torch.dtype = torch.bfloat16, stream: Opti
     _mx4_check(b, "mx4_matmul")
     if a.cols != b.cols:
         _refuse("mx4_matmul", f"rows of {a.cols} against rows of {b.cols}")
-    if dtype not in _ELEM:
+    code = _ELEM.get(dtype)
+    if code is None:
         _refuse("mx4_matmul", "dtype has to be float32, bfloat16 or float16")
-    device = a.codes.device
-    _same_device("mx4_matmul", device, stream, a.codes, a.scales, b.codes, b.scales)
-    with _on(device, stream):
-        out = torch.empty(a.rows, b.rows, dtype=dtype, device=device)
-        _check(lib.conef_mx4_matmul(a.codes.data_ptr(), a.scales.data_ptr(), a.rows, b.codes.data_ptr(), b.scales.data_ptr(), b.rows, a.cols,
-                                    out.data_ptr(), _ELEM[dtype], b.rows, _stream_handle(None)), "conef_mx4_matmul")
+    m, k, codes, scales = a
+    n, _, b_codes, b_scales = b
+    if not _at_hand(stream, codes, scales, b_codes, b_scales):
+        _same_device("mx4_matmul", codes.device, stream, codes, scales, b_codes, b_scales)
+        with _on(codes.device, stream):
+            return mx4_matmul(a, b, dtype)
+    out = torch.empty(m, n, dtype=dtype, device=codes.device)
+    rc = lib.conef_mx4_matmul(codes.data_ptr(), scales.data_ptr(), m, b_codes.data_ptr(), b_scales.data_ptr(), n, k, out.data_ptr(), code, n,
+                              torch._C._cuda_getCurrentRawStream(codes.get_device()))
+    if rc:
+        _check(rc, "conef_mx4_matmul")
     return out
 
 
@@ -392,7 +410,8 @@ class ConEF:
                               C.byref(cc), float(lr), self._ws_ptr, nbytes, _stream_handle(stream)),
                "conef_init")
         self.h = h
-        self._dense1d = self.message_elems(MSG_DENSE1D)
+        self._msg_elems = [lib.conef_message_elems(h, which) for which in range(4)]
+        self._dense1d = self._msg_elems[MSG_DENSE1D]
 
     def close(self):
         if getattr(self, "h", None) and lib is not None:
@@ -410,7 +429,9 @@ class ConEF:
     def reduce_messages(self, which: int, out: Optional[torch.Tensor] = None, stream=None,
                         want_output: bool = True) -> Optional[torch.Tensor]:
         if out is None and want_output:
-            out = torch.empty(self.message_elems(which), dtype=torch.float32, device=self.device)
+            if not 0 <= which < len(self._msg_elems):
+                _check(ERR_INVALID_ARG, "conef_reduce_messages")
+            out = torch.empty(self._msg_elems[which], dtype=torch.float32, device=self.device)
         _check(lib.conef_reduce_messages(self.h, which, out.data_ptr() if out is not None else None,
                                          _stream_handle(stream)), "conef_reduce_messages")
         return out
