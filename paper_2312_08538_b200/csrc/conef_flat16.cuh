@@ -392,6 +392,7 @@ __global__ void __launch_bounds__(kF16Threads, f16_ctas(ICO)) k_flat16(const __g
         if (QK == CONEF_Q_RANDBLOCK && __any_sync(0xffffffffu, sent != 0u)) {
             // the chunk's part of the block is a run of the message: p goes back to the stage, and the warp writes 32 values at a time.  (Lane by lane
             // and element by element, 16384 x 1600 on two workers, a tenth sent, took 82 us with int4, this takes 60; microscaled 79 and 54.)
+            __syncwarp();   // (where the gradients are off a boundary, a lane reads the first of the next one's pieces)
 #pragma unroll
             for (int i = 0; i < 4; ++i)
                 S.g[f16_slot(lane * 4 + i)] = make_float4(r[4 * i], r[4 * i + 1], r[4 * i + 2], r[4 * i + 3]);
