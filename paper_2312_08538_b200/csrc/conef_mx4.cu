@@ -117,7 +117,7 @@ constexpr int kBothWarps = 4;
 // Both forms of 8192 x 6400 in bf16: rounded to nearest 60 us, where shared memory's and the cache's cycles are 75 % taken; stochastic behind a
 // dropout 74, bound by instructions (two hashes per four elements, two roundings each).
 template <class T, bool STOCH>
-struct alignas(1024) BothTile {
+struct alignas(128) BothTile {
     uint32_t v[32 * 32];
     uint16_t u[sizeof(T) == 4 && STOCH ? 32 : 1][34];
 };
