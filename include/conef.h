@@ -404,7 +404,8 @@ int conef_mx4_dequantise(const void *codes, const void *scales, int64_t rows, in
                          conef_stream stream);
 /* out[i][j] = sum over c < k of A[i][c] B[j][c] for forms A (m x k) and B (n x k), accumulated in fp32 and rounded once to the
  * type.  The bytes past a row's end and the scales of rows and blocks that do not exist have to be zero, as conef_mx4_quantise
- * leaves them.  k = 0 gives zeros. */
+ * leaves them.  k = 0 gives zeros.  The kernel's parts wait for one another, for two seconds at most; should a wait run out (not
+ * observed), the outputs that were not computed are NaN. */
 int conef_mx4_matmul(const void *a_codes, const void *a_scales, int64_t m, const void *b_codes, const void *b_scales, int64_t n,
                      int64_t k, void *out, int dtype, int64_t ld, conef_stream stream);
 

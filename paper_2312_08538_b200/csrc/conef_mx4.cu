@@ -114,19 +114,22 @@ __global__ void __launch_bounds__(kQThreads) k_mx4_rows(const T *x, const __grid
 constexpr int kBothWarps = 4;
 //
 // Words of a tile are exchanged within a row, 16 bytes at a time, so that a lane stores four at once and a column's are read without bank conflicts.
-// Both forms of 8192 x 6400 in bf16: rounded to nearest 60 us, where shared memory's and the cache's cycles are 75 % taken; stochastic behind a
-// dropout 74, bound by instructions (two hashes per four elements, two roundings each).
+// Rows come in lines of 128 bytes by eight lanes each, and are turned to a row per lane in shared memory, or (LINES false) straight to
+// the lane that has the row, 32 bytes per request.  8192 x 6400, lines and lanes: bf16 to nearest both forms 48 and 58 us, the columns alone 38 and 44; fp32 to
+// nearest 55 and 75, stochastic behind a dropout 86 and 87.  In bf16 with stochastic rounding, which is bound by instructions (two hashes per four elements, two
+// roundings each, ALU pipe 78 %), the turning costs more than it saves: 81 and 74 behind a dropout, 62 and 64 without.
 template <class T, bool STOCH>
 struct alignas(128) BothTile {
     uint32_t v[32 * 32];
+    uint32_t rows[sizeof(T) == 2 && !STOCH ? 32 * 32 : 4];   // 16 bits: 32 rows of 64 elements as they are
     uint16_t u[sizeof(T) == 4 && STOCH ? 32 : 1][34];
 };
 __device__ __forceinline__ uint32_t both_piece(uint32_t row, uint32_t piece) { return row * 32u + ((piece ^ (row & 7u)) << 2); }   // words
 __device__ __forceinline__ uint32_t both_word(uint32_t row, uint32_t col) { return both_piece(row, col >> 2) + (col & 3u); }
 template <class T, bool VEC, bool ROWS, bool STOCH, bool DROP>
-__global__ void __launch_bounds__(kBothWarps * 32) k_mx4_both(const T *x, const __grid_constant__ QArgs A, uint32_t tiles_c, int64_t n_tiles)
+__global__ void __launch_bounds__(kBothWarps * 32, STOCH ? 4 : 5) k_mx4_both(const T *x, const __grid_constant__ QArgs A, uint32_t tiles_c, int64_t n_tiles)
 {
-    constexpr bool SHORT = sizeof(T) == 2;
+    constexpr bool SHORT = sizeof(T) == 2, LINES = VEC && (!SHORT || !STOCH);
     __shared__ BothTile<T, STOCH> S[kBothWarps];
     grid_release();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -139,8 +142,9 @@ __global__ void __launch_bounds__(kBothWarps * 32) k_mx4_both(const T *x, const 
     grid_wait();
     if (tile >= n_tiles)
         return;
-    for (int sc = 0; sc < 2; ++sc)
-        for (int sr = 0; sr < 2; ++sr) {
+    const bool wide = cbase + 64 <= A.cols;
+    for (int sr = 0; sr < 2; ++sr)
+        for (int sc = 0; sc < 2; ++sc) {
             const int64_t r0 = rbase + sr * 32, c0 = cbase + sc * 32, r = r0 + lane, ct = c0 + lane;
             if (r0 >= A.rows || c0 >= A.cols) {   // scales of blocks that do not exist
                 if (ROWS)
@@ -151,7 +155,28 @@ __global__ void __launch_bounds__(kBothWarps * 32) k_mx4_both(const T *x, const 
             // a lane's row: 16 bits as they are, two to a word, or fp32
             constexpr int RAW = SHORT ? 16 : 32;
             uint32_t raw[RAW];
-            if (VEC && c0 + 32 <= A.cols) {
+            const bool lines = LINES && (SHORT ? wide : c0 + 32 <= A.cols);
+            if (lines) {
+                // eight lanes per 128-byte line, four lines at a time, turned to a row per lane in shared memory
+                uint32_t *const to = SHORT ? M.rows : M.v;
+                if (!SHORT || sc == 0) {
+                    uint4 w[8];
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) {
+                        const int64_t row = r0 + 4 * k + (lane >> 3);
+                        w[k] = row < A.rows ? __ldcs((const uint4 *)(x + row * A.ld + (SHORT ? cbase : c0)) + (lane & 7)) : make_uint4(0u, 0u, 0u, 0u);
+                    }
+#pragma unroll
+                    for (int k = 0; k < 8; ++k)
+                        *(uint4 *)&to[both_piece(4 * k + (lane >> 3), lane & 7)] = w[k];
+                    __syncwarp();
+                }
+#pragma unroll
+                for (int i = 0; i < RAW; i += 4) {
+                    const uint4 q = *(const uint4 *)&to[both_piece(lane, (SHORT ? sc * 4 : 0) + i / 4)];
+                    raw[i] = q.x, raw[i + 1] = q.y, raw[i + 2] = q.z, raw[i + 3] = q.w;
+                }
+            } else if (VEC && c0 + 32 <= A.cols) {
                 const T *p = x + r * A.ld + c0;
 #pragma unroll
                 for (int i = 0; i < RAW; i += 8) {
@@ -228,7 +253,8 @@ __global__ void __launch_bounds__(kBothWarps * 32) k_mx4_both(const T *x, const 
                             M.u[lane][4 * g + q] = (uint16_t)(q & 1 ? n >> 16 : n);
                     }
                 }
-                *(uint4 *)&M.v[both_piece(lane, g)] = make_uint4(w[0], w[1], w[2], w[3]);
+                if (SHORT || DROP || !lines)   // (else they are there)
+                    *(uint4 *)&M.v[both_piece(lane, g)] = make_uint4(w[0], w[1], w[2], w[3]);
             }
             float v[32];
             // 32 scaled elements' codes; their scale
