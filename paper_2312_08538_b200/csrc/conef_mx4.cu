@@ -114,22 +114,30 @@ __global__ void __launch_bounds__(kQThreads) k_mx4_rows(const T *x, const __grid
 constexpr int kBothWarps = 4;
 //
 // Words of a tile are exchanged within a row, 16 bytes at a time, so that a lane stores four at once and a column's are read without bank conflicts.
-// Rows come in lines of 128 bytes by eight lanes each, and are turned to a row per lane in shared memory, or (LINES false) straight to
-// the lane that has the row, 32 bytes per request.  8192 x 6400, lines and lanes: bf16 to nearest both forms 48 and 58 us, the columns alone 38 and 44; fp32 to
-// nearest 55 and 75, stochastic behind a dropout 86 and 87.  In bf16 with stochastic rounding, which is bound by instructions (two hashes per four elements, two
+// Rows come in lines of 128 bytes by eight lanes each, and are turned to a row per lane in shared memory, or (LINES and PAIRS false) straight to
+// the lane that has the row, 32 bytes per request.  8192 x 6400 in fp32, lines and lanes: to nearest 55 and 75 us, stochastic behind a dropout 86 and 87.
+// Elements of 16 bits to nearest (PAIRS) stay in shared memory as they came, 32 rows of 64, and a lane reads two columns at a time: it wrote and
+// read half as much there, which was what it spent its time on.  bf16 both forms 38 us, the columns alone 27; a word per element in lines 48 and 38, by lanes 58 and 44.
+// In bf16 with stochastic rounding, which is bound by instructions (two hashes per four elements, two
 // roundings each, ALU pipe 78 %), the turning costs more than it saves: 81 and 74 behind a dropout, 62 and 64 without.
 template <class T, bool STOCH>
 struct alignas(128) BothTile {
-    uint32_t v[32 * 32];
-    uint32_t rows[sizeof(T) == 2 && !STOCH ? 32 * 32 : 4];   // 16 bits: 32 rows of 64 elements as they are
+    uint32_t v[32 * 32];   // 32 x 32 elements, a word each; 16 bits to nearest also: 32 x 64, two to a word
     uint16_t u[sizeof(T) == 4 && STOCH ? 32 : 1][34];
 };
 __device__ __forceinline__ uint32_t both_piece(uint32_t row, uint32_t piece) { return row * 32u + ((piece ^ (row & 7u)) << 2); }   // words
 __device__ __forceinline__ uint32_t both_word(uint32_t row, uint32_t col) { return both_piece(row, col >> 2) + (col & 3u); }
+// four elements of 16 bits, two to a word: what their numbers keep (their scale comes later)
+__device__ __forceinline__ void drop_pairs(uint32_t &a, uint32_t &b, uint64_t d, const Dropout &drop)
+{
+    const uint32_t lo = (uint32_t)d, hi = (uint32_t)(d >> 32);
+    a &= ((lo << 16) > drop.limit ? 0xFFFFu : 0u) | (lo > drop.limit ? 0xFFFF0000u : 0u);
+    b &= ((hi << 16) > drop.limit ? 0xFFFFu : 0u) | (hi > drop.limit ? 0xFFFF0000u : 0u);
+}
 template <class T, bool VEC, bool ROWS, bool STOCH, bool DROP>
 __global__ void __launch_bounds__(kBothWarps * 32, STOCH ? 4 : 5) k_mx4_both(const T *x, const __grid_constant__ QArgs A, uint32_t tiles_c, int64_t n_tiles)
 {
-    constexpr bool SHORT = sizeof(T) == 2, LINES = VEC && (!SHORT || !STOCH);
+    constexpr bool SHORT = sizeof(T) == 2, LINES = VEC && !SHORT, PAIRS = VEC && SHORT && !STOCH;
     __shared__ BothTile<T, STOCH> S[kBothWarps];
     grid_release();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -142,8 +150,94 @@ __global__ void __launch_bounds__(kBothWarps * 32, STOCH ? 4 : 5) k_mx4_both(con
     grid_wait();
     if (tile >= n_tiles)
         return;
-    const bool wide = cbase + 64 <= A.cols;
-    for (int sr = 0; sr < 2; ++sr)
+    float v[32];
+    // 32 scaled elements' codes; their scale
+    auto encode = [&](auto &&codes_of, uint32_t (&code)[4]) {
+        float most = mx4_absmax<32>(v);
+        if (SHORT && DROP)   // (the largest product is that of the largest element)
+            most = __fmul_rn(most, A.drop.scale);
+        const uint32_t byte = mx4_scale(__float_as_uint(most));
+        float inv = mx4_inv(byte);
+        if (SHORT && DROP) {
+            // Times the dropout's scale, rounded, and times a power of two: one product by both is the same where neither step leaves the
+            // normal range.  From 2^-95 on (the byte 32) a product below it is 0 either way.
+            if (byte >= 32u) {
+                inv = __fmul_rn(inv, A.drop.scale);
+            } else {
+#pragma unroll
+                for (int i = 0; i < 32; ++i)
+                    v[i] = __fmul_rn(v[i], A.drop.scale);
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < 32; ++i)
+            v[i] = __fmul_rn(v[i], inv);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            code[i] = codes_of(i);
+            code[i] = byte == kMx4Nan ? 0u : code[i];   // (elements that do not exist are zero, which no number rounds up)
+        }
+        return byte;
+    };
+    for (int sr = 0; sr < 2; ++sr) {
+        if constexpr (PAIRS) if (rbase + sr * 32 < A.rows && cbase + 64 <= A.cols) {
+            const int64_t r0 = rbase + sr * 32, r = r0 + lane;
+            auto nearest = [&](int i) { return mx4_nearest8(v + 8 * i); };
+            uint32_t code[4];
+            uint4 w[8];
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                const int64_t row = r0 + 4 * k + (lane >> 3);
+                w[k] = row < A.rows ? __ldcs((const uint4 *)(x + row * A.ld + cbase) + (lane & 7)) : make_uint4(0u, 0u, 0u, 0u);
+            }
+#pragma unroll
+            for (int k = 0; k < 8; ++k)
+                *(uint4 *)&M.v[both_piece(4 * k + (lane >> 3), lane & 7)] = w[k];
+            __syncwarp();
+            if (ROWS || DROP) {
+                uint32_t bytes = 0;
+#pragma unroll
+                for (int sc = 0; sc < 2; ++sc) {
+                    const uint64_t z = A.dropout + kDrawStep * ((uint64_t)r * groups + (uint64_t)((cbase >> 2) + sc * 8));
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        uint4 q = *(const uint4 *)&M.v[both_piece(lane, sc * 4 + i)];
+                        if (DROP) {
+                            drop_pairs(q.x, q.y, mix64(z + kDrawStep * (2 * i)), A.drop);
+                            drop_pairs(q.z, q.w, mix64(z + kDrawStep * (2 * i + 1)), A.drop);
+                            *(uint4 *)&M.v[both_piece(lane, sc * 4 + i)] = q;
+                        }
+                        Vec16<T>::unpack(q, *(float(*)[8])(v + 8 * i));
+                    }
+                    if (ROWS) {
+                        bytes |= encode(nearest, code) << (8 * sc);
+                        if (r < A.rows)
+                            *(uint4 *)(A.codes + (r * blocks + (cbase >> 5) + sc) * 16) = make_uint4(code[0], code[1], code[2], code[3]);
+                    }
+                }
+                if (ROWS)
+                    *(uint16_t *)&A.scales[mx4_scale_at(r, cbase >> 5, scale_tiles)] = (uint16_t)(r < A.rows ? bytes : 0u);
+                if (DROP)
+                    __syncwarp();
+            }
+            uint32_t pair[32];   // two columns to a lane
+#pragma unroll
+            for (int i = 0; i < 32; ++i)
+                pair[i] = M.v[both_word(i, lane)];
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const int64_t ct = cbase + 2 * lane + h;
+#pragma unroll
+                for (int i = 0; i < 32; ++i) {
+                    const uint16_t e = (uint16_t)(pair[i] >> (16 * h));
+                    v[i] = to_f32(*(const T *)&e);
+                }
+                A.scales_t[mx4_scale_at(ct, r0 >> 5, scale_tiles_t)] = (uint8_t)encode(nearest, code);
+                *(uint4 *)(A.codes_t + (ct * blocks_t + (r0 >> 5)) * 16) = make_uint4(code[0], code[1], code[2], code[3]);
+            }
+            __syncwarp();
+            continue;
+        }
         for (int sc = 0; sc < 2; ++sc) {
             const int64_t r0 = rbase + sr * 32, c0 = cbase + sc * 32, r = r0 + lane, ct = c0 + lane;
             if (r0 >= A.rows || c0 >= A.cols) {   // scales of blocks that do not exist
@@ -155,25 +249,22 @@ __global__ void __launch_bounds__(kBothWarps * 32, STOCH ? 4 : 5) k_mx4_both(con
             // a lane's row: 16 bits as they are, two to a word, or fp32
             constexpr int RAW = SHORT ? 16 : 32;
             uint32_t raw[RAW];
-            const bool lines = LINES && (SHORT ? wide : c0 + 32 <= A.cols);
+            const bool lines = LINES && c0 + 32 <= A.cols;
             if (lines) {
                 // eight lanes per 128-byte line, four lines at a time, turned to a row per lane in shared memory
-                uint32_t *const to = SHORT ? M.rows : M.v;
-                if (!SHORT || sc == 0) {
-                    uint4 w[8];
+                uint4 w[8];
 #pragma unroll
-                    for (int k = 0; k < 8; ++k) {
-                        const int64_t row = r0 + 4 * k + (lane >> 3);
-                        w[k] = row < A.rows ? __ldcs((const uint4 *)(x + row * A.ld + (SHORT ? cbase : c0)) + (lane & 7)) : make_uint4(0u, 0u, 0u, 0u);
-                    }
-#pragma unroll
-                    for (int k = 0; k < 8; ++k)
-                        *(uint4 *)&to[both_piece(4 * k + (lane >> 3), lane & 7)] = w[k];
-                    __syncwarp();
+                for (int k = 0; k < 8; ++k) {
+                    const int64_t row = r0 + 4 * k + (lane >> 3);
+                    w[k] = row < A.rows ? __ldcs((const uint4 *)(x + row * A.ld + c0) + (lane & 7)) : make_uint4(0u, 0u, 0u, 0u);
                 }
 #pragma unroll
+                for (int k = 0; k < 8; ++k)
+                    *(uint4 *)&M.v[both_piece(4 * k + (lane >> 3), lane & 7)] = w[k];
+                __syncwarp();
+#pragma unroll
                 for (int i = 0; i < RAW; i += 4) {
-                    const uint4 q = *(const uint4 *)&to[both_piece(lane, (SHORT ? sc * 4 : 0) + i / 4)];
+                    const uint4 q = *(const uint4 *)&M.v[both_piece(lane, i / 4)];
                     raw[i] = q.x, raw[i + 1] = q.y, raw[i + 2] = q.z, raw[i + 3] = q.w;
                 }
             } else if (VEC && c0 + 32 <= A.cols) {
@@ -228,13 +319,10 @@ __global__ void __launch_bounds__(kBothWarps * 32, STOCH ? 4 : 5) k_mx4_both(con
 #pragma unroll
                 for (int g = 0; g < 8; ++g) {
                     const uint64_t d = mix64(z + kDrawStep * g);
-                    const uint32_t lo = (uint32_t)d, hi = (uint32_t)(d >> 32), limit = A.drop.limit;
-                    if constexpr (SHORT) {
-                        raw[2 * g] &= ((lo << 16) > limit ? 0xFFFFu : 0u) | (lo > limit ? 0xFFFF0000u : 0u);
-                        raw[2 * g + 1] &= ((hi << 16) > limit ? 0xFFFFu : 0u) | (hi > limit ? 0xFFFF0000u : 0u);
-                    } else {
+                    if constexpr (SHORT)
+                        drop_pairs(raw[2 * g], raw[2 * g + 1], d, A.drop);
+                    else
                         drop4((float *)raw + 4 * g, d, A.drop);
-                    }
                 }
             }
             // for the columns: an element (16 bits: with its number above)
@@ -256,35 +344,6 @@ __global__ void __launch_bounds__(kBothWarps * 32, STOCH ? 4 : 5) k_mx4_both(con
                 if (SHORT || DROP || !lines)   // (else they are there)
                     *(uint4 *)&M.v[both_piece(lane, g)] = make_uint4(w[0], w[1], w[2], w[3]);
             }
-            float v[32];
-            // 32 scaled elements' codes; their scale
-            auto encode = [&](auto &&codes_of, uint32_t (&code)[4]) {
-                float most = mx4_absmax<32>(v);
-                if (SHORT && DROP)   // (the largest product is that of the largest element)
-                    most = __fmul_rn(most, A.drop.scale);
-                const uint32_t byte = mx4_scale(__float_as_uint(most));
-                float inv = mx4_inv(byte);
-                if (SHORT && DROP) {
-                    // Times the dropout's scale, rounded, and times a power of two: one product by both is the same where neither step leaves the
-                    // normal range.  From 2^-95 on (the byte 32) a product below it is 0 either way.
-                    if (byte >= 32u) {
-                        inv = __fmul_rn(inv, A.drop.scale);
-                    } else {
-#pragma unroll
-                        for (int i = 0; i < 32; ++i)
-                            v[i] = __fmul_rn(v[i], A.drop.scale);
-                    }
-                }
-#pragma unroll
-                for (int i = 0; i < 32; ++i)
-                    v[i] = __fmul_rn(v[i], inv);
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    code[i] = codes_of(i);
-                    code[i] = byte == kMx4Nan ? 0u : code[i];   // (elements that do not exist are zero, which no number rounds up)
-                }
-                return byte;
-            };
             uint32_t code[4];
             if (ROWS) {
 #pragma unroll
@@ -326,6 +385,7 @@ __global__ void __launch_bounds__(kBothWarps * 32, STOCH ? 4 : 5) k_mx4_both(con
                 *(uint4 *)(A.codes_t + (ct * blocks_t + (r0 >> 5)) * 16) = make_uint4(code[0], code[1], code[2], code[3]);
             __syncwarp();
         }
+    }
 }
 
 // ------------------------------------------------------------------ the way back
