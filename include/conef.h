@@ -55,9 +55,9 @@ enum { CONEF_Q_IDENTITY = 0, CONEF_Q_RANDK = 1, CONEF_Q_LOWRANK = 2, CONEF_Q_RAN
 enum { CONEF_C_IDENTITY = 0, CONEF_C_INT8 = 1, CONEF_C_INT4 = 2, CONEF_C_COUNTSKETCH = 3,
        CONEF_C_ROWSKETCH = 4, CONEF_C_STOCHQUANT = 5, CONEF_C_MX4 = 6, CONEF_C_MX4_STOCHASTIC = 7 };
 enum { CONEF_SCALE_FP32 = 0, CONEF_SCALE_FP16 = 1 };
-/* message kinds */
 /* element types of the matrix operators */
 enum { CONEF_F32 = 0, CONEF_BF16 = 1, CONEF_F16 = 2 };
+/* message kinds */
 enum { CONEF_MSG_VALUES = 0, CONEF_MSG_P = 1, CONEF_MSG_Q = 2, CONEF_MSG_DENSE1D = 3 };
 
 #define CONEF_MAX_WORKERS 64

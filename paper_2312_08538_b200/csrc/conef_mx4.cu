@@ -110,19 +110,21 @@ __global__ void __launch_bounds__(kQThreads) k_mx4_rows(const T *x, const __grid
 // ------------------------------------------------------------------ the transpose, and rows with it
 // A warp takes 64 x 64 elements, 32 x 32 at a time: a lane has 32 elements of a row, which is a block of the rows' form, and hands them and
 // their numbers through shared memory to the lanes of the columns, of which each has a block of the transpose.  One reading
-// of x and one hash per four elements serve both.  Elements of 16 bits lie beside their number in a word.
-constexpr int kBothWarps = 4;
+// of x and one hash per four elements serve both.
 //
 // Words of a tile are exchanged within a row, 16 bytes at a time, so that a lane stores four at once and a column's are read without bank conflicts.
 // Rows come in lines of 128 bytes by eight lanes each, and are turned to a row per lane in shared memory, or (LINES and PAIRS false) straight to
 // the lane that has the row, 32 bytes per request.  8192 x 6400 in fp32, lines and lanes: to nearest 55 and 75 us, stochastic behind a dropout 86 and 87.
-// Elements of 16 bits to nearest (PAIRS) stay in shared memory as they came, 32 rows of 64, and a lane reads two columns at a time: it wrote and
-// read half as much there, which was what it spent its time on.  bf16 both forms 38 us, the columns alone 27; a word per element in lines 48 and 38, by lanes 58 and 44.
-// In bf16 with stochastic rounding, which is bound by instructions (two hashes per four elements, two
-// roundings each, ALU pipe 78 %), the turning costs more than it saves: 81 and 74 behind a dropout, 62 and 64 without.
-template <class T, bool STOCH>
+// Elements of 16 bits (PAIRS) stay in shared memory as they came, 32 rows of 64, their numbers in as many words again, and a lane
+// reads two columns at a time: to nearest it writes and reads half as much there, which was what it spent its time on; stochastic it need not put
+// elements and numbers together.  bf16 to nearest both forms 38 us, the columns alone 27; a word per element in lines 48 and 38, by lanes 58 and 44;
+// stochastic 56, a word per element 63.  Behind a dropout, which has a second hash per four elements, it was no faster
+// (77; a word per element, by lanes, 75: ALU pipe 78 %).
+constexpr int kBothWarps = 4;
+template <class T, bool STOCH, bool DROP>
 struct alignas(128) BothTile {
-    uint32_t v[32 * 32];   // 32 x 32 elements, a word each; 16 bits to nearest also: 32 x 64, two to a word
+    uint32_t v[32 * 32];   // 32 x 32 elements, a word each (16 bits: with their numbers above), or 32 x 64 of 16 bits, two to a word
+    uint32_t n[sizeof(T) == 2 && STOCH && !DROP ? 32 * 32 : 4];   // ... their numbers
     uint16_t u[sizeof(T) == 4 && STOCH ? 32 : 1][34];
 };
 __device__ __forceinline__ uint32_t both_piece(uint32_t row, uint32_t piece) { return row * 32u + ((piece ^ (row & 7u)) << 2); }   // words
@@ -137,12 +139,12 @@ __device__ __forceinline__ void drop_pairs(uint32_t &a, uint32_t &b, uint64_t d,
 template <class T, bool VEC, bool ROWS, bool STOCH, bool DROP>
 __global__ void __launch_bounds__(kBothWarps * 32, STOCH ? 4 : 5) k_mx4_both(const T *x, const __grid_constant__ QArgs A, uint32_t tiles_c, int64_t n_tiles)
 {
-    constexpr bool SHORT = sizeof(T) == 2, LINES = VEC && !SHORT, PAIRS = VEC && SHORT && !STOCH;
-    __shared__ BothTile<T, STOCH> S[kBothWarps];
+    constexpr bool SHORT = sizeof(T) == 2, LINES = VEC && !SHORT, PAIRS = VEC && SHORT && !(STOCH && DROP);
+    __shared__ BothTile<T, STOCH, DROP> S[kBothWarps];
     grid_release();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int64_t tile = (int64_t)blockIdx.x * kBothWarps + warp;
-    BothTile<T, STOCH> &M = S[warp];
+    BothTile<T, STOCH, DROP> &M = S[warp];
     const int64_t tr = tile / tiles_c, rbase = tr * 64, cbase = (tile - tr * tiles_c) * 64;
     const int64_t blocks = mx4_blocks(A.cols), blocks_t = mx4_blocks(A.rows), scale_tiles = mx4_scale_tiles(A.cols), scale_tiles_t = mx4_scale_tiles(A.rows);
     const uint64_t groups = (uint64_t)(A.cols + 3) / 4;
@@ -151,8 +153,8 @@ __global__ void __launch_bounds__(kBothWarps * 32, STOCH ? 4 : 5) k_mx4_both(con
     if (tile >= n_tiles)
         return;
     float v[32];
-    // 32 scaled elements' codes; their scale
-    auto encode = [&](auto &&codes_of, uint32_t (&code)[4]) {
+    // scales 32 elements; the scale
+    auto scaled = [&](float (&v)[32]) {
         float most = mx4_absmax<32>(v);
         if (SHORT && DROP)   // (the largest product is that of the largest element)
             most = __fmul_rn(most, A.drop.scale);
@@ -172,6 +174,11 @@ __global__ void __launch_bounds__(kBothWarps * 32, STOCH ? 4 : 5) k_mx4_both(con
 #pragma unroll
         for (int i = 0; i < 32; ++i)
             v[i] = __fmul_rn(v[i], inv);
+        return byte;
+    };
+    // 32 elements' codes; their scale
+    auto encode = [&](auto &&codes_of, uint32_t (&code)[4]) {
+        const uint32_t byte = scaled(v);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             code[i] = codes_of(i);
@@ -182,7 +189,6 @@ __global__ void __launch_bounds__(kBothWarps * 32, STOCH ? 4 : 5) k_mx4_both(con
     for (int sr = 0; sr < 2; ++sr) {
         if constexpr (PAIRS) if (rbase + sr * 32 < A.rows && cbase + 64 <= A.cols) {
             const int64_t r0 = rbase + sr * 32, r = r0 + lane;
-            auto nearest = [&](int i) { return mx4_nearest8(v + 8 * i); };
             uint32_t code[4];
             uint4 w[8];
 #pragma unroll
@@ -194,47 +200,69 @@ __global__ void __launch_bounds__(kBothWarps * 32, STOCH ? 4 : 5) k_mx4_both(con
             for (int k = 0; k < 8; ++k)
                 *(uint4 *)&M.v[both_piece(4 * k + (lane >> 3), lane & 7)] = w[k];
             __syncwarp();
-            if (ROWS || DROP) {
+            if (ROWS || DROP || STOCH) {
                 uint32_t bytes = 0;
 #pragma unroll
                 for (int sc = 0; sc < 2; ++sc) {
-                    const uint64_t z = A.dropout + kDrawStep * ((uint64_t)r * groups + (uint64_t)((cbase >> 2) + sc * 8));
+                    const uint64_t group = (uint64_t)r * groups + (uint64_t)((cbase >> 2) + sc * 8), zd = A.dropout + kDrawStep * group,
+                                   zr = A.rounding + kDrawStep * group;
+                    uint64_t word[STOCH ? 8 : 1];
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
-                        uint4 q = *(const uint4 *)&M.v[both_piece(lane, sc * 4 + i)];
+                        const uint32_t at = both_piece(lane, sc * 4 + i);
+                        uint4 q = *(const uint4 *)&M.v[at];
                         if (DROP) {
-                            drop_pairs(q.x, q.y, mix64(z + kDrawStep * (2 * i)), A.drop);
-                            drop_pairs(q.z, q.w, mix64(z + kDrawStep * (2 * i + 1)), A.drop);
-                            *(uint4 *)&M.v[both_piece(lane, sc * 4 + i)] = q;
+                            drop_pairs(q.x, q.y, mix64(zd + kDrawStep * (2 * i)), A.drop);
+                            drop_pairs(q.z, q.w, mix64(zd + kDrawStep * (2 * i + 1)), A.drop);
+                            *(uint4 *)&M.v[at] = q;
+                        }
+                        if constexpr (STOCH) {
+                            const uint64_t a = mix64(zr + kDrawStep * (2 * i)), b = mix64(zr + kDrawStep * (2 * i + 1));
+                            *(uint4 *)&M.n[at] = make_uint4((uint32_t)a, (uint32_t)(a >> 32), (uint32_t)b, (uint32_t)(b >> 32));
+                            word[2 * i] = a, word[2 * i + 1] = b;
                         }
                         Vec16<T>::unpack(q, *(float(*)[8])(v + 8 * i));
                     }
                     if (ROWS) {
-                        bytes |= encode(nearest, code) << (8 * sc);
+                        bytes |= encode([&](int i) { return STOCH ? mx4_stochastic8(v + 8 * i, word[STOCH ? 2 * i : 0], word[STOCH ? 2 * i + 1 : 0]) : mx4_nearest8(v + 8 * i); }, code) << (8 * sc);
                         if (r < A.rows)
                             *(uint4 *)(A.codes + (r * blocks + (cbase >> 5) + sc) * 16) = make_uint4(code[0], code[1], code[2], code[3]);
                     }
                 }
                 if (ROWS)
                     *(uint16_t *)&A.scales[mx4_scale_at(r, cbase >> 5, scale_tiles)] = (uint16_t)(r < A.rows ? bytes : 0u);
-                if (DROP)
-                    __syncwarp();
+                if (DROP || STOCH)
+                    __syncwarp();   // (lanes wrote to their own rows)
             }
-            uint32_t pair[32];   // two columns to a lane
+            // two columns to a lane
+            const int64_t ct = cbase + 2 * lane;
+            float v1[32];
 #pragma unroll
-            for (int i = 0; i < 32; ++i)
-                pair[i] = M.v[both_word(i, lane)];
+            for (int i = 0; i < 32; ++i) {
+                const uint32_t w = M.v[both_word(i, lane)];
+                const uint16_t lo = (uint16_t)w, hi = (uint16_t)(w >> 16);
+                v[i] = to_f32(*(const T *)&lo), v1[i] = to_f32(*(const T *)&hi);
+            }
+            const uint32_t byte = scaled(v), byte1 = scaled(v1);
+            uint32_t code1[4];
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const int64_t ct = cbase + 2 * lane + h;
+            for (int i = 0; i < 4; ++i) {
+                if constexpr (STOCH) {
+                    uint32_t lo[8], hi[8];
 #pragma unroll
-                for (int i = 0; i < 32; ++i) {
-                    const uint16_t e = (uint16_t)(pair[i] >> (16 * h));
-                    v[i] = to_f32(*(const T *)&e);
+                    for (int q = 0; q < 8; ++q) {
+                        const uint32_t w = M.n[both_word(8 * i + q, lane)];
+                        lo[q] = mx4_noise_lo(w), hi[q] = mx4_noise_hi(w);
+                    }
+                    code[i] = mx4_stochastic8(v + 8 * i, lo), code1[i] = mx4_stochastic8(v1 + 8 * i, hi);
+                } else {
+                    code[i] = mx4_nearest8(v + 8 * i), code1[i] = mx4_nearest8(v1 + 8 * i);
                 }
-                A.scales_t[mx4_scale_at(ct, r0 >> 5, scale_tiles_t)] = (uint8_t)encode(nearest, code);
-                *(uint4 *)(A.codes_t + (ct * blocks_t + (r0 >> 5)) * 16) = make_uint4(code[0], code[1], code[2], code[3]);
+                code[i] = byte == kMx4Nan ? 0u : code[i], code1[i] = byte1 == kMx4Nan ? 0u : code1[i];
             }
+            A.scales_t[mx4_scale_at(ct, r0 >> 5, scale_tiles_t)] = (uint8_t)byte, A.scales_t[mx4_scale_at(ct + 1, r0 >> 5, scale_tiles_t)] = (uint8_t)byte1;
+            uint8_t *const to = A.codes_t + (ct * blocks_t + (r0 >> 5)) * 16;
+            *(uint4 *)to = make_uint4(code[0], code[1], code[2], code[3]), *(uint4 *)(to + blocks_t * 16) = make_uint4(code1[0], code1[1], code1[2], code1[3]);
             __syncwarp();
             continue;
         }
