@@ -274,6 +274,32 @@ def test_quantise_blocks_at_the_edges(b, stochastic):
 
 
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("stochastic,p", [(False, 0.0), (True, 0.0), (False, 0.5), (True, 0.5)])
+@pytest.mark.parametrize("pad", [0, 8, 1])
+def test_quantise_16_bit_blocks_at_the_edges(b, dtype, stochastic, p, pad):
+    tiny = {torch.bfloat16: 2.0 ** -133, torch.float16: 2.0 ** -24}[dtype]   # the least subnormal
+    x = matrix(70, 192, dtype)
+    x[0, :32] = 0.0
+    x[1, :64] = -0.0
+    x[2, 5] = float("nan")
+    x[3, 40] = float("inf")
+    x[4, 71] = -float("inf")
+    x[5] = torch.finfo(dtype).max
+    x[6] = torch.finfo(dtype).min
+    x[7] = tiny
+    x[8, ::3] = -3 * tiny
+    x[9] = (matrix(1, 192, torch.float32)[0] * 2.0 ** -110).to(dtype)
+    x[10, 0], x[10, 1] = torch.finfo(dtype).max, tiny
+    x[12] = 5.0
+    x[13, :32] = 0.25
+    x[13, 0] = 6.0
+    for row in range(14, 44):                        # ties everywhere
+        x[row] = (torch.tensor([0.25, 0.75, 1.25, 1.75, 2.5, 3.5, 5.0, 6.0], device="cuda").repeat(24) * 2.0 ** (row - 30)).to(dtype)
+    x[64:] *= 64 * tiny                              # columns whose last rows are subnormals
+    check_forms(b, x, stochastic, p, strided(x, 0, pad)[0] if pad else None)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
 def test_dequantise_to_shorter_types(b, dtype):
     x = matrix(37, 205, torch.float32)
     a = b.mx4_quantise(x)
