@@ -132,8 +132,12 @@ typedef struct {
  * conef_mx4_quantise draws for (seed, worker i, tensor, t).  State: two
  * elements to a byte, then a scale byte per block of 32; `block` and
  * scale_dtype are not read.  Unlike the other codes, a residual that is
- * infinite or NaN makes its whole block NaN, in this step's state and, where
- * its elements are not all sent, in those after it.  iconef has to be 0.
+ * infinite or NaN makes its whole block NaN (scale byte 255, codes 0), in this
+ * step's state and in those after it until a step sends all of the block's
+ * elements (what is sent leaves zero, also where p is not finite).  With beta > 0 or low-rank Q, which keep
+ * a part of what is sent, such a block stays NaN.  A job clears it by writing
+ * 0 over its scale byte (conef_get_state) between two steps.  iconef has to
+ * be 0.
  * cs_chunk (count sketch only; 0 = off): the sketch of Sec. 4.2.2 applied to
  * runs of a tensor, one level below the paper's layer-wise use.  A tensor of
  * d elements is cut into nc = max(1, floor(d / cs_chunk)) runs of cs_chunk
@@ -187,7 +191,7 @@ int conef_init(conef_ctx **out /* HOST */, const conef_tensor *tensors /* HOST *
  * Non-finite gradients or states are not trapped and set no status: they
  * propagate IEEE-wise into p, the messages and the factors; a block maximum
  * skips NaN entries, and the stored code of a non-finite residual is
- * unspecified. */
+ * unspecified (but for mx4: see above conef_c_cfg). */
 int conef_step(conef_ctx *ctx, int64_t step, const float *const *grads, int phase,
                conef_stream stream);
 

@@ -179,7 +179,7 @@ void orc_randk_apply(const float *p, int64_t d, const uint32_t *idx, int64_t k, 
         r[j] = p[j];
     for (int64_t q = 0; q < k; ++q) {
         msg[q] = p[idx[q]];
-        r[idx[q]] = p[idx[q]] - p[idx[q]]; /* p - Delta on a transmitted entry */
+        r[idx[q]] = 0.0f; /* p - Delta on a transmitted entry, also where p is infinite or NaN */
     }
 }
 

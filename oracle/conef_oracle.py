@@ -625,7 +625,7 @@ class ConEFOracle:
             # line 6: Delta = Q(p); line 9: r = p - Delta
             if self.q.kind == "identity":
                 ls.msg = ps
-                rs = [p - p for p in ps]
+                rs = [np.zeros_like(p) for p in ps]   # (zero also where p is infinite or NaN)
             elif self.q.kind in ("randk", "randblock"):
                 pick = randk_indices if self.q.kind == "randk" else randblock_indices
                 ls.idx = pick(self.q.seed, l, t, d, self.k_of(l))

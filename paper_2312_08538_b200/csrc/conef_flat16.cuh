@@ -384,10 +384,12 @@ __global__ void __launch_bounds__(kF16Threads, f16_ctas(ICO)) k_flat16(const __g
 #pragma unroll
         for (int i = 0; i < 8; ++i)
             upk2(p2[i], r[2 * i], r[2 * i + 1]);
-        if (MX4 && QK == CONEF_Q_RANDK && sent && s1 != s1) {   // (a block of NaN: what was sent is zero all the same)
+        // Elements of a block of NaN that leave nothing all the same: those that were sent, and those that do not exist, whose code of zero gives NaN there
+        const uint32_t gone = MX4 && s1 != s1 ? sent | 0xFFFFu << left : sent;
+        if (MX4 && QK == CONEF_Q_RANDK && s1 != s1) {
 #pragma unroll
             for (int q = 0; q < 16; ++q)
-                r[q] = (sent >> q) & 1u ? 0.f : r[q];
+                r[q] = (gone >> q) & 1u ? 0.f : r[q];
         }
         if (QK == CONEF_Q_RANDBLOCK && __any_sync(0xffffffffu, sent != 0u)) {
             // the chunk's part of the block is a run of the message: p goes back to the stage, and the warp writes 32 values at a time.  (Lane by lane
@@ -408,7 +410,7 @@ __global__ void __launch_bounds__(kF16Threads, f16_ctas(ICO)) k_flat16(const __g
             }
 #pragma unroll
             for (int q = 0; q < 16; ++q)
-                r[q] = (sent >> q) & 1u ? 0.f : r[q];
+                r[q] = (gone >> q) & 1u ? 0.f : r[q];
 #pragma unroll
             for (int i = 0; i < 8; ++i)
                 p2[i] = pk2(r[2 * i], r[2 * i + 1]);
