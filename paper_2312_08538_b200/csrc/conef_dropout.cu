@@ -31,8 +31,9 @@ __device__ __forceinline__ uint4 dropped(const uint4 &x, const uint4 &add, uint3
 template <class T, bool ADD>
 __device__ __forceinline__ void dropped_one(const T *x, const T *add, T *out, bool kept, float scale)
 {
-    const float base = ADD ? to_f32(*add) : 0.f;
-    *out = from_f32<T>(kept ? __fmaf_rn(to_f32(*x), scale, base) : base);
+    // (as in dropped(): without a residual a product, whose zero keeps its sign)
+    const float v = to_f32(*x), base = ADD ? to_f32(*add) : 0.f, y = ADD ? __fmaf_rn(v, scale, base) : __fmul_rn(v, scale);
+    *out = from_f32<T>(kept ? y : base);
 }
 
 // ------------------------------------------------------------------ rows that are one array
