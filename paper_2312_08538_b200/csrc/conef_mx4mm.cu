@@ -173,7 +173,7 @@ __global__ void __launch_bounds__(kMmThreads, 1) k_mx4_matmul(const __grid_const
                         tc::bar_expect(&S.full[s], kMmM * 128 + b_bytes + scale_bytes * (1 + scale_rows));
                         tc::tile_load(st, &maps.a, ks * 128, tm * kMmM, &S.full[s]);
                         tc::tile_load(st + kMmM * 128, &maps.b, ks * 128, n0, &S.full[s]);
-                        tc::bulk_load(sc, as + ks * 1024u, scale_bytes, &S.full[s]);
+                        tc::bulk_load(sc, as + (size_t)ks * 1024, scale_bytes, &S.full[s]);
                         for (uint32_t r = 0; r < scale_rows; ++r)   // (rows past the last tile, whose products nobody stores: the last one's)
                             tc::bulk_load(sc + 1024 * (1 + r), P.bs + ((size_t)min(n0 / 128 + r, P.b_rows - 1) * P.tiles + ks * 2) * 512, scale_bytes, &S.full[s]);
                     }
