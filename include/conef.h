@@ -408,10 +408,17 @@ int conef_mx4_dequantise(const void *codes, const void *scales, int64_t rows, in
                          conef_stream stream);
 /* out[i][j] = sum over c < k of A[i][c] B[j][c] for forms A (m x k) and B (n x k), accumulated in fp32 and rounded once to the
  * type.  The bytes past a row's end and the scales of rows and blocks that do not exist have to be zero, as conef_mx4_quantise
- * leaves them.  k = 0 gives zeros.  The kernel's parts wait for one another, for two seconds at most; should a wait run out (not
- * observed), the outputs that were not computed are NaN. */
+ * leaves them.  k = 0 gives zeros.  The kernel's parts wait for one another, at a time for two seconds at most (for the sums of a tile of outputs
+ * four microseconds more per 256 of k).  Should a wait run out (not observed), the kernel ends within two seconds more, conef_mx4_timeouts counts it, and the
+ * outputs that were not computed are NaN. */
 int conef_mx4_matmul(const void *a_codes, const void *a_scales, int64_t m, const void *b_codes, const void *b_scales, int64_t n,
                      int64_t k, void *out, int dtype, int64_t ld, conef_stream stream);
+/* How many thread blocks of conef_mx4_matmul have had a wait run out, on the current device since the library was loaded, in work
+ * ahead in `stream` and what else has run.  Synchronises `stream`. */
+int conef_mx4_timeouts(int64_t *count /* HOST out */, conef_stream stream);
+/* For tests: the longest wait of the products that are enqueued from here on (0: two seconds), and the number of stages of 256 elements of k that
+ * each thread block, or the first and the second one of a pair, brings before it stops, as one that hangs would (-1: all of them).  Nothing is launched. */
+int conef_mx4_set_waits(int64_t nanoseconds, int64_t loads, int64_t loads_second);
 
 #ifdef __cplusplus
 }

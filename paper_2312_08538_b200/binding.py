@@ -37,7 +37,8 @@ EXPORTS = ["conef_workspace_bytes", "conef_init", "conef_step", "conef_reduce_me
            "conef_randk_indices_noalloc_select",
            "conef_get_error_step", "conef_set_error_step", "conef_set_fused", "conef_fused_info",
            "conef_get_fused_q",
-           "conef_dropout", "conef_mx4_bytes", "conef_mx4_quantise", "conef_mx4_dequantise", "conef_mx4_matmul"]
+           "conef_dropout", "conef_mx4_bytes", "conef_mx4_quantise", "conef_mx4_dequantise", "conef_mx4_matmul",
+           "conef_mx4_timeouts", "conef_mx4_set_waits"]
 
 
 class conef_tensor(C.Structure):
@@ -106,6 +107,8 @@ def _load() -> C.CDLL:
     L.conef_mx4_quantise.argtypes = [vp, i32, i64, i64, i64, C.c_double, i32, C.POINTER(Draw), vp, vp, vp, vp, vp]
     L.conef_mx4_dequantise.argtypes = [vp, vp, i64, i64, vp, i32, i64, vp]
     L.conef_mx4_matmul.argtypes = [vp, vp, i64, vp, vp, i64, i64, vp, i32, i64, vp]
+    L.conef_mx4_timeouts.argtypes = [C.POINTER(i64), vp]
+    L.conef_mx4_set_waits.argtypes = [i64, i64, i64]
     L.conef_error_string.argtypes = [i32]
     L.conef_error_string.restype = C.c_char_p
     return L
@@ -383,6 +386,20 @@ def mx4_matmul(a: MX4, b: MX4, dtype: torch.dtype = torch.bfloat16, stream: Opti
     if rc:
         _check(rc, "conef_mx4_matmul")
     return out
+
+
+def mx4_timeouts(device=None, stream: Optional[torch.cuda.Stream] = None) -> int:
+    """How many thread blocks of mx4_matmul have had a wait run out on a device (default: the current one) since the library was loaded; their outputs are
+    NaN.  Waits for the stream (default: the device's current one)."""
+    n = C.c_int64()
+    with torch.cuda.device(device) if stream is None else torch.cuda.stream(stream):
+        _check(lib.conef_mx4_timeouts(C.byref(n), _stream_handle(None)), "conef_mx4_timeouts")
+    return n.value
+
+
+def mx4_set_waits(seconds: float = 0.0, loads: int = -1, loads_second: int = -1) -> None:
+    """For tests: how long a wait of the products from here on lasts (0: two seconds), and after how many stages their loads stop (-1: never)."""
+    _check(lib.conef_mx4_set_waits(int(seconds * 1e9), loads, loads_second), "conef_mx4_set_waits")
 
 
 class ConEF:

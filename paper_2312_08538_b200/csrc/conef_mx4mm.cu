@@ -13,6 +13,7 @@
 #include <cuda.h>
 
 #include <algorithm>
+#include <atomic>
 
 #include "conef_mx4.cuh"
 #include "conef_common.cuh"
@@ -41,7 +42,11 @@ struct MmArgs {
     uint32_t n_tiles, stages;
     uint32_t tiled;              // outputs go by tiled copies
     uint32_t sums, scale_column; // sets of sums in tensor memory, and the first column of scales
+    uint64_t limit, sums_limit;  // nanoseconds that a wait takes at most, and the one for a tile's sums, which lasts for all of k
+    uint32_t loads[2];           // stages that the CTA(s) of a pair bring at most (tests)
 };
+// CTAs in which a wait has run out, since the library was loaded
+__device__ unsigned long long g_mm_ran_out;
 struct MmMaps {
     CUtensorMap a, b, out;       // (out: where it is `tiled`)
     CUtensorMap as, bs;          // of scales, for pairs, whose copies have to tell the leader's barrier
@@ -72,7 +77,7 @@ __device__ __forceinline__ MmTile mm_tile(const MmArgs &P, uint32_t tile)
 
 struct MmShared {
     uint64_t full[kMmMaxStages], empty[kMmMaxStages], sums[2], taken[2], drain;
-    uint32_t tmem;
+    uint32_t tmem, armed;        // (armed: stages brought)
     int dead;
 };
 
@@ -120,7 +125,7 @@ __global__ void __launch_bounds__(kMmThreads, 1) k_mx4_matmul(const __grid_const
     const uint32_t stage_bytes = mm_stage_bytes(P.bn, PAIR), scale_rows = mm_scale_rows(P.bn), b_bytes = P.bn * (PAIR ? 64u : 128u);
     const uint32_t rank = PAIR ? blockIdx.x & 1u : 0u, first = PAIR ? blockIdx.x / 2 : blockIdx.x, step = PAIR ? gridDim.x / 2 : gridDim.x;
     uint8_t *const ring = mm_smem + ((1024u - (tc::saddr(mm_smem) & 1023u)) & 1023u);
-    volatile int *const dead = &S.dead;
+    const tc::Waits waits = {&S.dead, PAIR ? tc::address_in(&S.dead, rank ^ 1u) : 0u, &g_mm_ran_out};
     if (warp == 0) {
         tc::tmem_alloc<PAIR>(&S.tmem, kMmColumns);
         if (lane == 0) {
@@ -146,46 +151,47 @@ __global__ void __launch_bounds__(kMmThreads, 1) k_mx4_matmul(const __grid_const
     grid_release();
     grid_wait();
 
+    // step ks of a tile into stage s: row tm of scales of A (128 rows of codes), columns from n0 on
+    auto load = [&](uint32_t s, uint32_t ks, uint32_t tm, uint32_t n0) {
+        const uint32_t st = tc::saddr(ring) + s * stage_bytes, sc = st + kMmM * 128 + b_bytes;
+        if constexpr (PAIR) {
+            // (what does not exist of rows and tiles of scales is filled with zeros)
+            const uint32_t bar = tc::leaders(&S.full[s]);
+            if (rank == 0)
+                tc::bar_expect(&S.full[s], 2 * stage_bytes);
+            tc::tile_load_pair(st, &maps.a, ks * 128, tm * kMmM, bar);
+            tc::tile_load_pair(st + kMmM * 128, &maps.b, ks * 128, n0 + rank * (P.bn / 2), bar);
+            tc::tile_load_pair(sc, &maps.as, ks * 256, tm, bar);
+            tc::tile_load_pair(sc + 1024, &maps.bs, ks * 256, n0 / 128, bar);
+        } else {
+            const uint32_t scale_bytes = min(P.tiles - ks * 2u, 2u) * 512u;
+            tc::bar_expect(&S.full[s], kMmM * 128 + b_bytes + scale_bytes * (1 + scale_rows));
+            tc::tile_load(st, &maps.a, ks * 128, tm * kMmM, &S.full[s]);
+            tc::tile_load(st + kMmM * 128, &maps.b, ks * 128, n0, &S.full[s]);
+            tc::bulk_load(sc, P.as + ((size_t)tm * P.tiles + ks * 2) * 512, scale_bytes, &S.full[s]);
+            for (uint32_t r = 0; r < scale_rows; ++r)   // (rows past the last tile, whose products nobody stores: the last one's)
+                tc::bulk_load(sc + 1024 * (1 + r), P.bs + ((size_t)min(n0 / 128 + r, P.b_rows - 1) * P.tiles + ks * 2) * 512, scale_bytes, &S.full[s]);
+        }
+    };
+    uint32_t armed = 0;   // (the loading warp's)
     if (warp == kMmEpilogue) {
-        const uint32_t ring0 = tc::saddr(ring);
-        uint32_t s = 0, phase = 0, armed = 0;
+        uint32_t s = 0, phase = 0;
         bool ok = true;
         for (uint32_t tile = first; ok && tile < P.n_tiles; tile += step) {
             const MmTile at = mm_tile(P, tile);
             const uint32_t tm = at.m * (PAIR ? 2 : 1) + rank, n0 = at.n * P.bn;   // (tm in 128 rows)
-            const uint8_t *as = P.as + (size_t)tm * P.tiles * 512;
             for (uint32_t ks = 0; ks < P.stages_k; ++ks) {
-                if (!(ok = tc::bar_wait(&S.empty[s], phase ^ 1u, dead)))
+                if (!(ok = armed < P.loads[rank] && tc::bar_wait(&S.empty[s], phase ^ 1u, waits, P.limit)))
                     break;
-                if (tc::elect()) {
-                    const uint32_t st = ring0 + s * stage_bytes, sc = st + kMmM * 128 + b_bytes;
-                    if constexpr (PAIR) {
-                        // (what does not exist of rows and tiles of scales is filled with zeros)
-                        const uint32_t bar = tc::leaders(&S.full[s]);
-                        if (rank == 0)
-                            tc::bar_expect(&S.full[s], 2 * stage_bytes);
-                        tc::tile_load_pair(st, &maps.a, ks * 128, tm * kMmM, bar);
-                        tc::tile_load_pair(st + kMmM * 128, &maps.b, ks * 128, n0 + rank * (P.bn / 2), bar);
-                        tc::tile_load_pair(sc, &maps.as, ks * 256, tm, bar);
-                        tc::tile_load_pair(sc + 1024, &maps.bs, ks * 256, n0 / 128, bar);
-                    } else {
-                        const uint32_t scale_bytes = min(P.tiles - ks * 2u, 2u) * 512u;
-                        tc::bar_expect(&S.full[s], kMmM * 128 + b_bytes + scale_bytes * (1 + scale_rows));
-                        tc::tile_load(st, &maps.a, ks * 128, tm * kMmM, &S.full[s]);
-                        tc::tile_load(st + kMmM * 128, &maps.b, ks * 128, n0, &S.full[s]);
-                        tc::bulk_load(sc, as + (size_t)ks * 1024, scale_bytes, &S.full[s]);
-                        for (uint32_t r = 0; r < scale_rows; ++r)   // (rows past the last tile, whose products nobody stores: the last one's)
-                            tc::bulk_load(sc + 1024 * (1 + r), P.bs + ((size_t)min(n0 / 128 + r, P.b_rows - 1) * P.tiles + ks * 2) * 512, scale_bytes, &S.full[s]);
-                    }
-                }
+                if (tc::elect())
+                    load(s, ks, tm, n0);
                 ++armed;
                 if (++s == P.stages)
                     s = 0, phase ^= 1u;
             }
         }
-        if (!ok && rank == 0)   // copies in flight (of both CTAs, which end together) end before the CTA does
-            for (uint32_t i = 0; i < P.stages && i < armed; ++i)
-                tc::bar_drain(&S.full[(armed - 1 - i) % P.stages], ((armed - 1 - i) / P.stages) & 1u);
+        if (lane == 0)
+            S.armed = armed;
         __syncwarp();
     } else if (warp == kMmEpilogue + 1) {
         const uint32_t instruction = tc::mx4_instruction<PAIR>(P.bn);
@@ -195,11 +201,11 @@ __global__ void __launch_bounds__(kMmThreads, 1) k_mx4_matmul(const __grid_const
         for (uint32_t tile = rank ? P.n_tiles : first; ok && tile < P.n_tiles; tile += step) {
             const uint32_t n0 = mm_tile(P, tile).n * P.bn, d = set * P.bn;
             const uint32_t shift = (n0 & 127u) >> 5;   // columns of the first tile of scales ahead of row n0
-            if (!(ok = tc::bar_wait(&S.taken[set], turn ^ 1u, dead)))
+            if (!(ok = tc::bar_wait(&S.taken[set], turn ^ 1u, waits, P.limit)))
                 break;
             tc::fence_after();
             for (uint32_t ks = 0; ks < P.stages_k; ++ks) {
-                if (!(ok = tc::bar_wait(&S.full[s], phase, dead)))
+                if (!(ok = tc::bar_wait(&S.full[s], phase, waits, P.limit)))
                     break;
                 tc::fence_after();
                 if (tc::elect()) {
@@ -230,12 +236,6 @@ __global__ void __launch_bounds__(kMmThreads, 1) k_mx4_matmul(const __grid_const
             if (++set == P.sums)
                 set = 0, turn ^= 1u;
         }
-        if (!ok) {   // products in flight end before tensor memory is given back
-            if (tc::elect())
-                tc::commit<PAIR>(&S.drain);
-            __syncwarp();
-            tc::bar_drain(&S.drain, 0);
-        }
         __syncwarp();
     } else {
         // sums of 32 rows (a lane each) and 64 columns
@@ -248,7 +248,7 @@ __global__ void __launch_bounds__(kMmThreads, 1) k_mx4_matmul(const __grid_const
         for (uint32_t tile = c0 < P.bn ? first : P.n_tiles; tile < P.n_tiles; tile += step) {
             const MmTile at = mm_tile(P, tile);
             const int64_t row0 = ((int64_t)at.m * (PAIR ? 2 : 1) + rank) * kMmM + (warp & 3) * 32, col0 = (int64_t)at.n * P.bn + c0;
-            ok = ok && tc::bar_wait(&S.sums[set], turn, dead);
+            ok = ok && tc::bar_wait(&S.sums[set], turn, waits, P.sums_limit);
             uint32_t v[64];
             if (ok) {
                 tc::fence_after();
@@ -312,6 +312,33 @@ __global__ void __launch_bounds__(kMmThreads, 1) k_mx4_matmul(const __grid_const
     if (PAIR)
         tc::cluster_sync();   // neither CTA tells a barrier of one that has ended
     tc::fence_after();
+    if (*waits.dead) {
+        // A wait has run out (in a pair both know by now).  What is in flight ends before shared and tensor memory are given back: the copies, for whose
+        // barriers to be told of all their bytes each CTA of a pair brings what the other has, and the products.
+        const uint64_t t0 = tc::nanoseconds();
+        if (warp == kMmEpilogue) {
+            const uint32_t all = PAIR ? max(armed, tc::load_at(tc::address_in(&S.armed, rank ^ 1u))) : armed;
+            for (; armed < all; ++armed) {
+                const uint32_t nth = armed / P.stages_k;
+                const MmTile at = mm_tile(P, first + nth * step);
+                if (tc::elect())
+                    load(armed % P.stages, armed - nth * P.stages_k, at.m * (PAIR ? 2 : 1) + rank, at.n * P.bn);
+                __syncwarp();
+            }
+            if (rank == 0)
+                for (uint32_t i = 0; i < P.stages && i < all; ++i)
+                    tc::bar_drain(&S.full[(all - 1 - i) % P.stages], ((all - 1 - i) / P.stages) & 1u, t0);
+        } else if (warp == kMmEpilogue + 1 && rank == 0) {
+            if (tc::elect())
+                tc::commit<PAIR>(&S.drain);
+            __syncwarp();
+            tc::bar_drain(&S.drain, 0, t0);
+        }
+        __syncthreads();
+        if (PAIR)
+            tc::cluster_sync();
+        tc::fence_after();
+    }
     if (warp == 0)
         tc::tmem_free<PAIR>(0, kMmColumns);
 }
@@ -369,6 +396,12 @@ static MmChoice mm_choice(int64_t m, int64_t n, int64_t k)
     return best;
 }
 
+struct MmLimit {
+    std::atomic<int64_t> nanoseconds{2000000000};
+    std::atomic<uint32_t> loads[2] = {{0xFFFFFFFFu}, {0xFFFFFFFFu}};
+};
+static MmLimit mm_limit;
+
 template <class T, bool PAIR>
 static int matmul(const uint8_t *a, const uint8_t *as, int64_t m, const uint8_t *b, const uint8_t *bs, int64_t n, int64_t k, T *out, int64_t ld, uint32_t bn,
                   cudaStream_t s)
@@ -382,6 +415,11 @@ static int matmul(const uint8_t *a, const uint8_t *as, int64_t m, const uint8_t 
     P.ld = ld;
     P.k64 = (uint32_t)((k + 63) / 64);
     P.stages_k = (uint32_t)((k + kMmK - 1) / kMmK);
+    P.limit = (uint64_t)mm_limit.nanoseconds.load();
+    // (a stage takes 0.4 us at most where nothing else runs)
+    P.sums_limit = P.limit + 4096ull * P.stages_k;
+    P.loads[0] = mm_limit.loads[0].load();
+    P.loads[1] = mm_limit.loads[1].load();
     P.tiles = (uint32_t)mx4_scale_tiles(k);
     P.b_rows = (uint32_t)((n + 127) / 128);
     P.bn = bn;
@@ -431,7 +469,9 @@ static int matmul(const uint8_t *a, const uint8_t *as, int64_t m, const uint8_t 
 
 using namespace conef;
 
-extern "C" int conef_mx4_matmul(const void *a_codes, const void *a_scales, int64_t m, const void *b_codes, const void *b_scales, int64_t n, int64_t k,
+extern "C" {
+
+int conef_mx4_matmul(const void *a_codes, const void *a_scales, int64_t m, const void *b_codes, const void *b_scales, int64_t n, int64_t k,
                                 void *out, int dtype, int64_t ld, conef_stream stream)
 {
     int rc = check_matrix(out, dtype, m, n, ld);
@@ -457,3 +497,27 @@ extern "C" int conef_mx4_matmul(const void *a_codes, const void *a_scales, int64
                                                              (const uint8_t *)b_scales, n, k, (T *)out, ld, c.bn, (cudaStream_t)stream);
     });
 }
+
+int conef_mx4_timeouts(int64_t *count, conef_stream stream)
+{
+    if (!count)
+        return CONEF_ERR_INVALID_ARG;
+    unsigned long long n = 0;
+    cudaError_t e = cudaMemcpyFromSymbolAsync(&n, g_mm_ran_out, sizeof n, 0, cudaMemcpyDeviceToHost, (cudaStream_t)stream);
+    if (e == cudaSuccess)
+        e = cudaStreamSynchronize((cudaStream_t)stream);
+    *count = (int64_t)n;
+    return launched(e, "conef_mx4_timeouts");
+}
+
+int conef_mx4_set_waits(int64_t nanoseconds, int64_t loads, int64_t loads_second)
+{
+    if (nanoseconds < 0 || loads < -1 || loads_second < -1 || loads >= 0xFFFFFFFFll || loads_second >= 0xFFFFFFFFll)
+        return CONEF_ERR_INVALID_ARG;
+    mm_limit.nanoseconds = nanoseconds ? nanoseconds : 2000000000;
+    mm_limit.loads[0] = (uint32_t)loads;           // (-1: 2^32 - 1, more than there are)
+    mm_limit.loads[1] = (uint32_t)loads_second;
+    return CONEF_OK;
+}
+
+}  // extern "C"

@@ -38,27 +38,37 @@ __device__ __forceinline__ uint64_t nanoseconds()
     asm volatile("mov.u64 %0, %globaltimer;" : "=l"(t));
     return t;
 }
-// A warp waits for a phase, for two seconds at most (a product takes milliseconds): past that, or once another warp's wait has
-// run out, *dead is set and the answer is no.
-constexpr uint64_t kLimit = 2000000000ull;
-__device__ __forceinline__ bool bar_wait(uint64_t *bar, uint32_t parity, volatile int *dead)
+// Waits are bounded.  `dead` says that one of a CTA's has run out, or one of the other CTA's of a pair: all that are not over then end.
+struct Waits {
+    volatile int *dead;
+    uint32_t others;                // the other CTA's `dead` (a cluster address), or 0
+    unsigned long long *ran_out;    // counts the CTAs in which a wait has run out
+};
+__device__ __forceinline__ void give_up(const Waits &w)
+{
+    if (atomicExch((int *)w.dead, 1) == 0)
+        atomicAdd(w.ran_out, 1ull);
+    if (w.others)
+        asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(w.others), "r"(1) : "memory");
+}
+// A warp waits for a phase, for `limit` nanoseconds or a little more; the answer is no where that runs out, or once another wait has.
+__device__ __forceinline__ bool bar_wait(uint64_t *bar, uint32_t parity, const Waits &w, uint64_t limit)
 {
     bool there = bar_try(bar, parity);
     if (!there) {
         const uint64_t t0 = nanoseconds();
-        for (int i = 1; !there && !*dead; ++i) {
+        for (int i = 1; !there && !*w.dead; ++i) {
             there = bar_try(bar, parity);
-            if (!there && i % 64 == 0 && nanoseconds() - t0 > kLimit)
-                *dead = 1;
+            if (!there && i % 64 == 0 && nanoseconds() - t0 > limit)
+                give_up(w);
         }
     }
     return __all_sync(0xffffffffu, there);
 }
-// ... of copies or products in flight that nobody will use: the same limit, whatever *dead says
-__device__ __forceinline__ void bar_drain(uint64_t *bar, uint32_t parity)
+// ... for copies or products in flight that nobody will use, two seconds at most after t0, whatever *dead says
+__device__ __forceinline__ void bar_drain(uint64_t *bar, uint32_t parity, uint64_t t0)
 {
-    const uint64_t t0 = nanoseconds();
-    while (!bar_try(bar, parity) && nanoseconds() - t0 <= kLimit) {
+    while (!bar_try(bar, parity) && nanoseconds() - t0 <= 2000000000ull) {
     }
 }
 
@@ -68,11 +78,19 @@ __device__ __forceinline__ void cluster_sync()
     asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
     asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
-__device__ __forceinline__ uint32_t leaders(const void *p)   // the leader's copy of a variable in shared memory
+// a variable in shared memory of either CTA, and that of the leader
+__device__ __forceinline__ uint32_t address_in(const void *p, uint32_t rank)
 {
     uint32_t r;
-    asm volatile("mapa.shared::cluster.u32 %0, %1, 0;" : "=r"(r) : "r"(saddr(p)));
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(saddr(p)), "r"(rank));
     return r;
+}
+__device__ __forceinline__ uint32_t leaders(const void *p) { return address_in(p, 0); }
+__device__ __forceinline__ uint32_t load_at(uint32_t at)
+{
+    uint32_t v;
+    asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(at) : "memory");
+    return v;
 }
 __device__ __forceinline__ void bar_arrive_at(uint32_t bar) { asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory"); }
 
