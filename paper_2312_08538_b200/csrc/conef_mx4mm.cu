@@ -370,23 +370,24 @@ static bool encode(CUtensorMap *map, CUtensorMapDataType type, int elem, const v
 }
 
 // Columns per tile, and whether pairs of CTAs take tiles of 256 rows: the choice whose waves of tiles over the SMs take least.  Nanoseconds per wave, from
-// 8192 x 6400 by 1600 and by 4096: what a step of 64 along k takes (64, 128, 192, 256 columns: single CTAs 45, 52, 67, 88, pairs 45, 48, 60, 73; full rate
+// 8192 x 6400 by 1600 and by 4096: what a step of 64 along k takes (64, 128, 192, 256 columns: single CTAs 45, 52, 67, 88, pairs from 128 on 48, 60, 73; full rate
 // would be 17, 35, 52, 70), what does not depend on k (pairs 970, 1240, and 2450 where tensor memory has room for one set of sums only), and a
-// microsecond more per launch of pairs.  Microseconds, single CTAs and pairs of these widths, the choice marked:
+// microsecond more per launch of pairs.  Pairs of 64 columns are left out: they take as many waves as single CTAs at least, none of them shorter.
+// Microseconds, single CTAs and pairs of these widths, the choice marked (for two of them it misses the fastest by a tenth):
 //   8192 x 6400 x 1600   79.3  57.6  51.8  50.8   78.8  51.7  45.4* 51.8        1111 x 2601 x 651   8.7  8.2  7.1* 8.5   11.6  9.6  8.0  8.7
-//   8192 x 1600 x 1600   21.9  17.7  16.1  18.0   22.9  16.7  14.8* 18.7        4000 x 4000 x 300   15.0  12.1  11.9*  11.3   21.7  15.2  13.3  13.5
-//   2048 x 6400 x 1600   22.2  17.8  16.1  15.4   23.0  16.5  14.8* 16.1        300 x 300 x 1600    5.2*  5.9  6.7  8.0   6.0  6.6  7.1  8.2
+//   8192 x 1600 x 1600   21.9  17.7  16.1* 18.0   22.9  16.7  14.8  18.7        4000 x 4000 x 300   15.0  12.1  11.9*  11.3   21.7  15.2  13.3  13.5
+//   2048 x 6400 x 1600   22.2  17.8  16.1* 15.4   23.0  16.5  14.8  16.1        300 x 300 x 1600    5.2*  5.9  6.7  8.0   6.0  6.6  7.1  8.2
 struct MmChoice {
     uint32_t bn;
     bool pair;
 };
 static MmChoice mm_choice(int64_t m, int64_t n, int64_t k)
 {
-    static const int per_step[2][4] = {{45, 52, 67, 88}, {45, 48, 60, 73}}, per_tile[4] = {700, 970, 1240, 2450};
+    static const int per_step[2][4] = {{45, 52, 67, 88}, {0, 48, 60, 73}}, per_tile[4] = {700, 970, 1240, 2450};
     MmChoice best = {0, false};
     int64_t least = 0;
     for (int pair = 0; pair < 2; ++pair)
-        for (uint32_t bn = 64; bn <= 256; bn += 64) {
+        for (uint32_t bn = pair ? 128 : 64; bn <= 256; bn += 64) {
             const int64_t rows = pair ? 2 * kMmM : kMmM, sets = pair ? kPlanSMs / 2 : kPlanSMs;
             const int64_t waves = ((m + rows - 1) / rows * ((n + bn - 1) / bn) + sets - 1) / sets;
             const int64_t cost = waves * ((k + 63) / 64 * per_step[pair][bn / 64 - 1] + per_tile[bn / 64 - 1]) + pair * 1000;
