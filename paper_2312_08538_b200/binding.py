@@ -193,7 +193,8 @@ def conef_randk_indices_noalloc_select(seed: int, tensor: int, step: int, d: int
 #
 # The last dimension of a tensor is a matrix' columns, those before it are its rows; a row's elements are adjacent, and rows
 # are evenly spaced (a slice of columns is taken as it is, other strides are refused).  Work is enqueued on `stream` (default:
-# the current stream of the tensors' device), on which outputs are allocated too.
+# the current stream of the tensors' device), on which outputs are allocated too.  Nothing is recorded for autograd: a tensor that
+# requires a gradient is refused where gradients are recorded (not under torch.no_grad(), nor in a torch.autograd.Function).
 
 _ELEM = {torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16}
 
@@ -204,6 +205,8 @@ def _refuse(where: str, why: str) -> None:
 
 def _matrix(x: torch.Tensor, where: str, name: str = "x") -> Tuple[int, int, int]:
     """(rows, cols, elements from row to row) of a tensor."""
+    if x.requires_grad and torch.is_grad_enabled():
+        _refuse(where, f"{name} requires a gradient, which nothing here records: call it under torch.no_grad() or in an autograd function")
     if not x.is_cuda:
         _refuse(where, f"{name} has to be on a GPU")
     if x.dtype not in _ELEM:
@@ -269,7 +272,7 @@ def dropout(x: torch.Tensor, p: float, draw: Draw, add: Optional[torch.Tensor] =
     """x behind a dropout with probability p (a multiple of 2^-16), plus `add`.  The mask comes from `draw` and is not stored:
     the gradient of x is this call on the gradient of the result, with the same draw and without `add`."""
     code = _ELEM.get(x.dtype)
-    if add is None and out is None and code is not None and x.is_contiguous() and x.is_cuda and _at_hand(stream, x) and x.dim():
+    if add is None and out is None and code is not None and x.is_contiguous() and not x.requires_grad and x.is_cuda and _at_hand(stream, x) and x.dim():
         # (what follows, without what it need not ask: a third of a small call's host time)
         cols = x.shape[-1]
         out = torch.empty_like(x)

@@ -18,3 +18,16 @@ def test_waits_refusals(b):
     b.mx4_set_waits(1.0, 3, 4)
     b.mx4_set_waits()
     assert b.lib.conef_mx4_timeouts(None, None) == b.ERR_INVALID_ARG
+
+
+def test_tensors_that_require_a_gradient_are_refused(b):
+    """... where gradients are recorded: the result would silently have none.  (Ahead of the other checks, which CPU tensors do not pass.)"""
+    import torch
+    x, leaf, d = torch.zeros(4, 8), torch.zeros(4, 8, requires_grad=True), b.Draw(1, 0, 0, 0)
+    calls = [lambda: b.dropout(leaf, 0.5, d), lambda: b.dropout(leaf * 2, 0.5, d), lambda: b.mx4_quantise(leaf), lambda: b.mx4_quantise(leaf, forms="both")]
+    for call in calls:
+        with pytest.raises(b.ConEFError, match="gradient") as e:
+            call()
+        assert e.value.code == b.ERR_INVALID_ARG
+        with torch.no_grad(), pytest.raises(b.ConEFError, match="on a GPU"):
+            call()
