@@ -453,8 +453,8 @@ static int matmul(const uint8_t *a, const uint8_t *as, int64_t m, const uint8_t 
     if (!ok)
         return launched(cudaErrorInvalidValue, "conef_mx4_matmul: tensor map");
     // Never two CTAs on an SM, of two products at once either: each takes all of tensor memory, and of two pairs on the same SMs
-    // each could hold one half.
-    const size_t smem = std::max<size_t>(1024 + (size_t)P.stages * stage_bytes + mm_staging(bn), kMmAlone);
+    // each could hold one half.  A pair leaves no shared memory at all, since the other one could be any kernel's.
+    const size_t smem = PAIR ? kMmSmem : std::max<size_t>(1024 + (size_t)P.stages * stage_bytes + mm_staging(bn), kMmAlone);
     static int done[64];
     cudaError_t e = opt_in_smem(k_mx4_matmul<T, PAIR>, kMmSmem, done);
     if (e == cudaSuccess) {
