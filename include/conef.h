@@ -129,15 +129,16 @@ typedef struct {
  * mx4, mx4-stochastic (a 4-bit float per element, see conef_mx4_quantise): the
  * row-major flattening of a tensor is quantised like one row of that many
  * elements, rounded to nearest even, or stochastically by the numbers that
- * conef_mx4_quantise draws for (seed, worker i, tensor, t).  State: two
- * elements to a byte, then a scale byte per block of 32; `block` and
- * scale_dtype are not read.  Unlike the other codes, a residual that is
- * infinite or NaN makes its whole block NaN (scale byte 255, codes 0), in this
- * step's state and in those after it until a step sends all of the block's
- * elements (what is sent leaves zero, also where p is not finite).  With beta > 0 or low-rank Q, which keep
- * a part of what is sent, such a block stays NaN.  A job clears it by writing
- * 0 over its scale byte (conef_get_state) between two steps.  iconef has to
- * be 0.
+ * conef_mx4_quantise draws for (seed, worker i, tensor, t).  (A context of one
+ * rank's worker has worker 0 alone: seed + rank gives it, and the stochastic
+ * quantiser's, the numbers of worker `rank`.)  State: two elements to a byte, then a
+ * scale byte per block of 32; `block` and scale_dtype are not read.  Unlike the
+ * other codes, a residual that is infinite or NaN makes its whole block NaN
+ * (scale byte 255, codes 0), in this step's state and in those after it until a
+ * step sends all of the block's elements (what is sent leaves zero, also where
+ * p is not finite).  With beta > 0 or low-rank Q, which keep a part of what is
+ * sent, such a block stays NaN.  A job clears it by writing 0 over its scale
+ * byte (conef_get_state) between two steps.  iconef has to be 0.
  * cs_chunk (count sketch only; 0 = off): the sketch of Sec. 4.2.2 applied to
  * runs of a tensor, one level below the paper's layer-wise use.  A tensor of
  * d elements is cut into nc = max(1, floor(d / cs_chunk)) runs of cs_chunk
@@ -413,8 +414,8 @@ int conef_mx4_dequantise(const void *codes, const void *scales, int64_t rows, in
  * outputs that were not computed are NaN. */
 int conef_mx4_matmul(const void *a_codes, const void *a_scales, int64_t m, const void *b_codes, const void *b_scales, int64_t n,
                      int64_t k, void *out, int dtype, int64_t ld, conef_stream stream);
-/* How many thread blocks of conef_mx4_matmul have had a wait run out, on the current device since the library was loaded, in work
- * ahead in `stream` and what else has run.  Synchronises `stream`. */
+/* How many thread blocks of conef_mx4_matmul have had a wait run out on the current device since the library was loaded, the work
+ * ahead in `stream` included.  Synchronises `stream`. */
 int conef_mx4_timeouts(int64_t *count /* HOST out */, conef_stream stream);
 /* For tests: the longest wait of the products that are enqueued from here on (0: two seconds), and the number of stages of 256 elements of k that
  * each thread block, or the first and the second one of a pair, brings before it stops, as one that hangs would (-1: all of them).  Nothing is launched. */

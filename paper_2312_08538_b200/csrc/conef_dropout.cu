@@ -1,7 +1,7 @@
 // Dropout whose mask is drawn from the counter-based stream in every pass and never stored: y = x 65536 / (65536 - off)
 // where the element's number is at least off, else 0; and a residual added in the same pass.
 //
-// HBM-bound: 2 or 3 values per element (8192 x 6400 in bf16 34.5 us, 6.1 TB/s).  A hash (two 64-bit multiplies, about 22 instructions) serves four elements, so a thread works on 16
+// HBM-bound: 2 or 3 values per element (8192 x 6400 in bf16 35 us, 6.0 TB/s, launches on one output; as a call whose output is allocated 5.5).  A hash (two 64-bit multiplies, about 22 instructions) serves four elements, so a thread works on 16
 // bytes at a time and hashes once for four or twice for eight of them.
 #include <algorithm>
 
@@ -213,6 +213,7 @@ __global__ void __launch_bounds__(kDropThreads) k_dropout_rows(const T *x, const
 }
 
 // ------------------------------------------------------------------ rows that begin differently: a group of four columns per thread
+// Element by element, since no 16 bytes of one lie on 16 of the other: 8192 x 6400 in bf16 83 us (2.5 TB/s; rows that begin alike 35).
 template <class T, bool ADD>
 __global__ void __launch_bounds__(kDropThreads) k_dropout(const T *x, const T *add, T *out, int64_t rows, uint32_t cols, int64_t x_ld, int64_t add_ld,
                                                           int64_t out_ld, uint64_t stream, const Dropout drop)

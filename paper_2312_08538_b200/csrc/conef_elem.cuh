@@ -71,7 +71,9 @@ struct Vec16<__half> {
     static __device__ __forceinline__ uint4 pack(const float (&f)[8]) { return make_uint4(pack2(f[0], f[1]), pack2(f[2], f[3]), pack2(f[4], f[5]), pack2(f[6], f[7])); }
 };
 
-struct Divider {   // division of 32-bit numbers by `by`, above 1, rounding down: high word of x m, corrected for m's 33rd bit
+// Division of 32-bit numbers by `by`, above 1, rounding down: high word of x m, corrected for m's 33rd bit (Granlund and Montgomery, "Division by invariant
+// integers using multiplication", 1994, the multiplier rounded up)
+struct Divider {
     uint32_t by, m, shift;
 };
 inline Divider divider(uint32_t by)

@@ -470,7 +470,7 @@ __global__ void __launch_bounds__(kQThreads) k_mx4_dequantise(const uint8_t *cod
 }
 // ... begin anywhere: a thread takes those eight elements that fill an aligned piece of the result (`pieces` of them to a row at most), whose codes it cuts out
 // of two words and whose scales are those of two blocks at most; pieces over a row's ends are stored element by element.  8192 x 1601 to
-// fp32: a block per warp and an element per lane took 44 us, this takes 13.5 (4.4 TB/s).
+// fp32: a block per warp and an element per lane took 44 us, this takes 13.5 (4.4 TB/s); 8192 x 6400 to fp32 and bf16 58 and 41 (on aligned rows 38 and 22).
 template <class T, int U>
 __global__ void __launch_bounds__(kQThreads) k_mx4_dequantise_any(const uint8_t *codes, const uint8_t *scales, const Divider pieces, uint32_t row0, int64_t rows, int64_t cols,
                                                                   T *out, int64_t ld)

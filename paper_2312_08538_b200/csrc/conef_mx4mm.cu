@@ -6,10 +6,12 @@
 // tensor cores take them, by plain bulk ones), one issues the products, and sixteen move the sums of a tile from tensor memory through registers and shared
 // memory to the output while the next tile's are formed in a second set.
 //
-// 8192 x 6400 x 1600 in bf16 takes 45 us (3.7 PFLOP/s).  The products alone would take 20 at full rate, the output's 105 MB 16 at the memory's.
-// What bounds it is the traffic with L2: tiles of 256 x 192 move 577 MB in and out, at 14 TB/s.  Without the loads the kernel takes 33 us, without
-// the stores 33, without either 30; with half of the stores 40; with stores that hit the same lines of L2 over and over, by plain coalesced stores
-// instead of tiled copies, or with a ring of four instead of five stages 46 to 48.
+// 8192 x 6400 x 1600 in bf16 takes 45.7 us on operands that the launch before left in L2, 50.3 on others (3.7 and 3.3 PFLOP/s).  The products alone would
+// take 20 at full rate, the output's 105 MB 16 at the memory's.  Without the loads the kernel takes 33 us, without the stores 33, without either 30, of which
+// only the products' 20 are accounted for; with half of the stores 40; with stores that hit the same lines of L2 over and over, by plain coalesced stores
+// instead of tiled copies, or with a ring of four instead of five stages 46 to 48.  It is not L2's rate that bounds it: tiles of 256 x 192 move 577 MB in
+// and out, 12.6 TB/s, L2's throughput counter reads 50 %, and at k = 4096 (83.5 us) it moves more per second.  A part is rows of codes that do not lie on lines
+// of 128 bytes, as those of 800 bytes at k = 1600: 9.0 M requests to L2 where k = 1536 has 6.2 M; k = 1536, 1600, 1664 and 1792 take 42.9, 50.3, 48.6 and 46.2 us.
 #include <cuda.h>
 
 #include <algorithm>
@@ -58,7 +60,7 @@ __host__ __device__ inline uint32_t mm_stage_bytes(uint32_t bn, bool pair) { ret
 inline uint32_t mm_staging(uint32_t bn) { return bn / 16 * 4096; }   // per storing warp 32 rows of 128 bytes, where outputs are turned from a row per lane
 
 // Tiles are taken in bands of kMmBand along m, so that what runs at a time is about as high as wide (8192 x 6400 x 1600, pairs of 256 columns: in bands
-// of 8 and of 4 53 us, of one 59, in one band of all 55.6; with 192 columns 47.6 to 48.8).  No division: a tile's place is
+// of 8 and of 4 53 us, of one 59, in one band of all 55.6; with 192 columns 47.6 to 48.8, by an earlier form).  No division: a tile's place is
 // on the way of the products from one tile to the next.
 constexpr uint32_t kMmBand = 8;
 struct MmTile {
