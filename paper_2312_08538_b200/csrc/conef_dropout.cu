@@ -31,9 +31,9 @@ __device__ __forceinline__ uint4 dropped(const uint4 &x, const uint4 &add, uint3
 template <class T, bool ADD>
 __device__ __forceinline__ void dropped_one(const T *x, const T *add, T *out, bool kept, float scale)
 {
-    // (as in dropped(): without a residual a product, whose zero keeps its sign)
-    const float v = to_f32(*x), base = ADD ? to_f32(*add) : 0.f, y = ADD ? __fmaf_rn(v, scale, base) : __fmul_rn(v, scale);
-    *out = from_f32<T>(kept ? y : base);
+    // (without a residual a product, as in dropped(): -0 is added, which leaves a zero its sign)
+    const float base = ADD ? to_f32(*add) : 0.f;
+    *out = from_f32<T>(kept ? __fmaf_rn(to_f32(*x), scale, ADD ? base : -0.f) : base);
 }
 
 // ------------------------------------------------------------------ rows that are one array
