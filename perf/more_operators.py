@@ -202,10 +202,10 @@ def _plain_norm(state):
     h = state["x"] if state["r"] is None else (state["x"].float() + state["r"].float()).to(dtype)
     wide = h.double()
     r = torch.rsqrt(wide.square().mean(1, keepdim=True) + _EPS)
-    out = dict(rstd=r.squeeze(1).float())
+    out = dict(rstd=r.squeeze(1).float())   # (y is formed with it as it is stored)
     if state["r"] is not None:
         out["h"] = h
-    y = wide * r * state["w"].double()
+    y = wide * out["rstd"].double().unsqueeze(1) * state["w"].double()
     if state["forms"] == "none":
         out["y"] = y.to(dtype)
     else:
@@ -353,7 +353,7 @@ def _exact_norm(case, state):
     out = dict(rstd=root)
     if state["r"] is not None:
         out["h"] = h.double()
-    y = torch.einsum("rc,r,c->rc", v, root, w)
+    y = torch.einsum("rc,r,c->rc", v, root.float().double(), w)   # (with the root as it is stored, by definition)
     if case["forms"] == "none":
         out["y"] = y
     else:
