@@ -57,6 +57,8 @@ enum { CONEF_C_IDENTITY = 0, CONEF_C_INT8 = 1, CONEF_C_INT4 = 2, CONEF_C_COUNTSK
 enum { CONEF_SCALE_FP32 = 0, CONEF_SCALE_FP16 = 1 };
 /* element types of the matrix operators */
 enum { CONEF_F32 = 0, CONEF_BF16 = 1, CONEF_F16 = 2 };
+/* elements of 8-bit forms: four exponent bits and three of mantissa (largest value 448), or five and two (57344) */
+enum { CONEF_E4M3 = 0, CONEF_E5M2 = 1 };
 /* message kinds */
 enum { CONEF_MSG_VALUES = 0, CONEF_MSG_P = 1, CONEF_MSG_Q = 2, CONEF_MSG_DENSE1D = 3 };
 
@@ -417,9 +419,64 @@ int conef_mx4_matmul(const void *a_codes, const void *a_scales, int64_t m, const
 /* How many thread blocks of conef_mx4_matmul have had a wait run out on the current device since the library was loaded, the work
  * ahead in `stream` included.  Synchronises `stream`. */
 int conef_mx4_timeouts(int64_t *count /* HOST out */, conef_stream stream);
-/* For tests: the longest wait of the products that are enqueued from here on (0: two seconds), and the number of stages of 256 elements of k that
- * each thread block, or the first and the second one of a pair, brings before it stops, as one that hangs would (-1: all of them).  Nothing is launched. */
+/* For tests: the longest wait of the products that are enqueued from here on (0: two seconds), and the number of stages of 256 elements of k (8-bit forms:
+ * 128, conef_orthogonalise: 64) that each thread block, or the first and the second one of a pair, brings before it stops, as one that hangs would
+ * (-1: all of them).  For the products of all formats.  Nothing is launched. */
 int conef_mx4_set_waits(int64_t nanoseconds, int64_t loads, int64_t loads_second);
+
+/* ---- 8-bit floats with a scale per block of 128, root-mean-square norms, orthogonalised updates ----
+ *
+ * (The paper has no counterpart to these either: a layer's way in, its products and its update, beside the exchange of gradients.)  The rules for
+ * matrix arguments above hold here too.
+ *
+ * A matrix in 8-bit floats with block scales: blocks of 128 consecutive elements of a row, the last of a row may be short; a code (CONEF_E4M3 or CONEF_E5M2) per
+ * element; a scale 2^E per block.  codes: ceil(cols/128) times 128 bytes per row, zero past the row's end.  scales: bytes E + 127 (255: NaN) in
+ * tiles of 128 rows by 4 blocks; row r, block b has byte 512 ((r/128) ceil(cols/512) + b/4) + 16 (r mod 32) + 4 (r mod 128 / 32) + b mod 4; those of rows
+ * and blocks that do not exist are zero.  Both are DEVICE memory, 16-byte aligned, of the sizes that conef_f8_bytes gives. */
+int conef_f8_bytes(int64_t rows, int64_t cols, size_t *code_bytes /* HOST out */, size_t *scale_bytes /* HOST out */);
+
+/* Quantise x: its rows into (codes, scales), and / or the rows of its transpose (cols x rows, blocks along x's columns) into (codes_t, scales_t); a form not asked
+ * for is NULL.  E is the least, not below -127, for which no element is above the type's largest value times 2^E; a block that holds an infinity or a NaN has
+ * scale 255 and codes 0.  Elements are rounded to nearest even.  With `square`, 128 rows by 128 columns are a block (and have their scale once per row): both
+ * forms then stand for the same values. */
+int conef_f8_quantise(const void *x, int dtype, int64_t rows, int64_t cols, int64_t ld, int kind, int square, void *codes, void *scales, void *codes_t, void *scales_t,
+                      conef_stream stream);
+/* The values of a form, code 2^E, rounded to the type (exact in fp32 and bf16 below 2^128, and infinite there). */
+int conef_f8_dequantise(const void *codes, const void *scales, int64_t rows, int64_t cols, int kind, void *out, int dtype, int64_t ld, conef_stream stream);
+/* out[i][j] = sum over c < k of A[i][c] B[j][c] for forms A (m x k) and B (n x k) of either kind, accumulated in fp32 and rounded once to the type.  What
+ * conef_mx4_matmul says of bytes past a row's end, of k = 0 and of waits holds here too; conef_f8_timeouts counts these. */
+int conef_f8_matmul(const void *a_codes, const void *a_scales, int a_kind, int64_t m, const void *b_codes, const void *b_scales, int b_kind, int64_t n, int64_t k, void *out,
+                    int dtype, int64_t ld, conef_stream stream);
+int conef_f8_timeouts(int64_t *count /* HOST out */, conef_stream stream);
+
+/* Root-mean-square norm of x's rows, behind the addition of a residual where `add` is not NULL: h = x + add, rounded to the type and written (without add, h is x
+ * and the argument NULL); rstd[r] = 1 / sqrt(mean over the row of h^2 + eps), computed in 64 bits and rounded to fp32 (DEVICE, one per row); and h rstd weight,
+ * either rounded to the type into y, or in 8-bit floats into (codes, scales) and / or (codes_t, scales_t) as conef_f8_quantise has them: the codes and scales are
+ * those of the exact products (where these are above 2^-100 in size).  y and the forms may all be NULL.  weight: `cols` elements of the matrices' type
+ * or of CONEF_F32.  A row that holds an infinity or a NaN has rstd 0 or NaN, and what follows by IEEE rules.  h may be x or add, y may be x, add or h
+ * (with the same ld); otherwise outputs do not overlap inputs. */
+int conef_rms_norm(const void *x, const void *add, const void *weight, int dtype, int weight_dtype, int64_t rows, int64_t cols, int64_t x_ld, int64_t add_ld, double eps,
+                   void *h, int64_t h_ld, float *rstd, void *y, int64_t y_ld, int kind, void *codes, void *scales, void *codes_t, void *scales_t, conef_stream stream);
+/* Its gradient: with n = h rstd and g = dy weight, dx = rstd (g - n mean(g n)) + add, the gradient of x and of the residual (add: the gradient that reaches h
+ * another way, or NULL), in fp32 and rounded once to the type; dweight[c] = sum over rows of dy n (fp32, DEVICE, or NULL), the same in every call.  dx may be
+ * dy or add (with the same ld).  `workspace`: DEVICE, 4-byte aligned, of the size that conef_rms_norm_grad_bytes gives; it is the call's until that has
+ * run on the stream. */
+int conef_rms_norm_grad_bytes(int64_t rows, int64_t cols, size_t *bytes /* HOST out */);
+int conef_rms_norm_grad(const void *dy, const void *h, const void *weight, const float *rstd, const void *add, int dtype, int weight_dtype, int64_t rows, int64_t cols,
+                        int64_t dy_ld, int64_t h_ld, int64_t add_ld, void *dx, int64_t dx_ld, float *dweight, void *workspace, size_t workspace_bytes,
+                        conef_stream stream);
+
+/* Newton-Schulz orthogonalisation (Muon) of `batch` matrices of rows x cols (elements of a row are consecutive, rows `ld` apart, matrices `stride`): X_0 = x / |x|, the
+ * Frobenius norm (a matrix of zeros stays one), `steps` (1..32) times X <- (c0 + c1 A + c2 A^2) X with A = X X^T, the shorter side in front, and
+ * out = scale X, rounded once to CONEF_BF16 or CONEF_F16.  Operands of the products are held to 22 bits under a power of two and summed in fp32, as exact as
+ * the same in fp32.  coefficients: HOST, three; the polynomial s (c0 + c1 s^2 + c2 s^4) has to keep singular values below 10^4 in size over the steps (else
+ * CONEF_ERR_INVALID_ARG).  A matrix that holds an infinity or a NaN becomes NaN.  out may be x (with the same distances).  `workspace`: DEVICE, 128-byte
+ * aligned, of the size that conef_orthogonalise_bytes gives; it is the call's until that has run on the stream.  Waits are bounded as conef_mx4_matmul's,
+ * conef_orthogonalise_timeouts counts these. */
+int conef_orthogonalise_bytes(int64_t batch, int64_t rows, int64_t cols, size_t *bytes /* HOST out */);
+int conef_orthogonalise(const void *x, int dtype, int64_t batch, int64_t rows, int64_t cols, int64_t ld, int64_t stride, int steps, const double *coefficients /* HOST */,
+                        double scale, void *out, int out_dtype, int64_t out_ld, int64_t out_stride, void *workspace, size_t workspace_bytes, conef_stream stream);
+int conef_orthogonalise_timeouts(int64_t *count /* HOST out */, conef_stream stream);
 
 #ifdef __cplusplus
 }

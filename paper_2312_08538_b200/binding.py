@@ -24,6 +24,7 @@ NOALLOC_MAX_ELEMS = 1 << 24
 Q_IDENTITY, Q_RANDK, Q_LOWRANK, Q_RANDBLOCK = 0, 1, 2, 3
 C_IDENTITY, C_INT8, C_INT4, C_COUNTSKETCH, C_ROWSKETCH, C_STOCHQUANT, C_MX4, C_MX4_STOCHASTIC = 0, 1, 2, 3, 4, 5, 6, 7
 F32, BF16, F16 = 0, 1, 2
+E4M3, E5M2 = 0, 1
 SCALE_FP32, SCALE_FP16 = 0, 1
 MSG_VALUES, MSG_P, MSG_Q, MSG_DENSE1D = 0, 1, 2, 3
 SELECT_NORMAL, SELECT_MISS, SELECT_FULL, SELECT_STALE, SELECT_HALF = 0, 1, 2, 3, 4
@@ -38,7 +39,10 @@ EXPORTS = ["conef_workspace_bytes", "conef_init", "conef_step", "conef_reduce_me
            "conef_get_error_step", "conef_set_error_step", "conef_set_fused", "conef_fused_info",
            "conef_get_fused_q",
            "conef_dropout", "conef_mx4_bytes", "conef_mx4_quantise", "conef_mx4_dequantise", "conef_mx4_matmul",
-           "conef_mx4_timeouts", "conef_mx4_set_waits"]
+           "conef_mx4_timeouts", "conef_mx4_set_waits",
+           "conef_f8_bytes", "conef_f8_quantise", "conef_f8_dequantise", "conef_f8_matmul", "conef_f8_timeouts",
+           "conef_rms_norm", "conef_rms_norm_grad_bytes", "conef_rms_norm_grad",
+           "conef_orthogonalise_bytes", "conef_orthogonalise", "conef_orthogonalise_timeouts"]
 
 
 class conef_tensor(C.Structure):
@@ -109,6 +113,18 @@ def _load() -> C.CDLL:
     L.conef_mx4_matmul.argtypes = [vp, vp, i64, vp, vp, i64, i64, vp, i32, i64, vp]
     L.conef_mx4_timeouts.argtypes = [C.POINTER(i64), vp]
     L.conef_mx4_set_waits.argtypes = [i64, i64, i64]
+    size_p = C.POINTER(C.c_size_t)
+    L.conef_f8_bytes.argtypes = [i64, i64, size_p, size_p]
+    L.conef_f8_quantise.argtypes = [vp, i32, i64, i64, i64, i32, i32, vp, vp, vp, vp, vp]
+    L.conef_f8_dequantise.argtypes = [vp, vp, i64, i64, i32, vp, i32, i64, vp]
+    L.conef_f8_matmul.argtypes = [vp, vp, i32, i64, vp, vp, i32, i64, i64, vp, i32, i64, vp]
+    L.conef_f8_timeouts.argtypes = [C.POINTER(i64), vp]
+    L.conef_rms_norm.argtypes = [vp, vp, vp, i32, i32, i64, i64, i64, i64, C.c_double, vp, i64, vp, vp, i64, i32, vp, vp, vp, vp, vp]
+    L.conef_rms_norm_grad_bytes.argtypes = [i64, i64, size_p]
+    L.conef_rms_norm_grad.argtypes = [vp, vp, vp, vp, vp, i32, i32, i64, i64, i64, i64, i64, vp, i64, vp, vp, C.c_size_t, vp]
+    L.conef_orthogonalise_bytes.argtypes = [i64, i64, i64, size_p]
+    L.conef_orthogonalise.argtypes = [vp, i32, i64, i64, i64, i64, i64, i32, C.POINTER(C.c_double), C.c_double, vp, i32, i64, i64, vp, C.c_size_t, vp]
+    L.conef_orthogonalise_timeouts.argtypes = [C.POINTER(i64), vp]
     L.conef_error_string.argtypes = [i32]
     L.conef_error_string.restype = C.c_char_p
     return L
@@ -403,6 +419,266 @@ def mx4_timeouts(device=None, stream: Optional[torch.cuda.Stream] = None) -> int
 def mx4_set_waits(seconds: float = 0.0, loads: int = -1, loads_second: int = -1) -> None:
     """For tests: how long a wait of the products from here on lasts (0: two seconds), and after how many stages their loads stop (-1: never)."""
     _check(lib.conef_mx4_set_waits(int(seconds * 1e9), loads, loads_second), "conef_mx4_set_waits")
+
+
+# ---- 8-bit floats with a scale per block of 128, root-mean-square norms, orthogonalised updates (tensors and streams as above)
+
+_F8KIND = {"e4m3": E4M3, "e5m2": E5M2}
+
+
+class F8(NamedTuple):
+    """A rows x cols matrix in 8-bit floats ("e4m3" or "e5m2") with block scales, as conef_f8_quantise leaves it: flat or shaped uint8 tensors."""
+    rows: int
+    cols: int
+    kind: str
+    codes: torch.Tensor
+    scales: torch.Tensor
+
+
+def _f8_sizes(rows: int, cols: int) -> Tuple[int, int]:
+    return rows * ((cols + 127) // 128) * 128, (rows + 127) // 128 * ((cols + 511) // 512) * 512
+
+
+def _f8_check(a: F8, where: str) -> None:
+    rows, cols, kind, codes, scales = a
+    if rows < 0 or cols < 0:
+        _refuse(where, "a size is negative")
+    if kind not in _F8KIND:
+        _refuse(where, "kind has to be e4m3 or e5m2")
+    for t, size, name in zip((codes, scales), _f8_sizes(rows, cols), ("codes", "scales")):
+        if t.numel() != size or t.dtype is not torch.uint8 or not t.is_cuda or not t.is_contiguous():
+            _refuse(where, f"the {name} of a {rows} x {cols} form are {size} contiguous uint8 on a GPU")
+
+
+def _f8_form(rows: int, cols: int, kind: str, device: torch.device) -> F8:
+    """A form to be written."""
+    code_bytes, scale_bytes = _f8_sizes(rows, cols)
+    return F8(rows, cols, kind, torch.empty(code_bytes, dtype=torch.uint8, device=device), torch.empty(scale_bytes, dtype=torch.uint8, device=device))
+
+
+def _f8_forms(rows: int, cols: int, forms: str, kind: str, device: torch.device, where: str) -> Tuple[Optional[F8], Optional[F8]]:
+    if forms not in ("rows", "cols", "both"):
+        _refuse(where, "forms has to be rows, cols or both")
+    if kind not in _F8KIND:
+        _refuse(where, "kind has to be e4m3 or e5m2")
+    return _f8_form(rows, cols, kind, device) if forms != "cols" else None, _f8_form(cols, rows, kind, device) if forms != "rows" else None
+
+
+def f8_quantise(x: torch.Tensor, forms: str = "rows", kind: str = "e4m3", square: bool = False, stream: Optional[torch.cuda.Stream] = None) -> Union[F8, Tuple[F8, F8]]:
+    """x in 8-bit floats with a scale per 128 elements: forms = "rows", "cols" (the form of x's transpose) or "both" (a pair, from one reading of x).
+    With square=True a block is 128 x 128 elements, and both forms stand for the same values, as a weight's do that two products read."""
+    rows, cols, ld = _matrix(x, "f8_quantise")
+    if not _at_hand(stream, x):
+        _same_device("f8_quantise", x.device, stream, x)
+        with _on(x.device, stream):
+            return f8_quantise(x, forms, kind, square)
+    a, t = _f8_forms(rows, cols, forms, kind, x.device, "f8_quantise")
+    if rows and cols:
+        rc = lib.conef_f8_quantise(x.data_ptr(), _ELEM[x.dtype], rows, cols, ld, _F8KIND[kind], 1 if square else 0, a.codes.data_ptr() if a else None,
+                                   a.scales.data_ptr() if a else None, t.codes.data_ptr() if t else None, t.scales.data_ptr() if t else None,
+                                   torch._C._cuda_getCurrentRawStream(x.get_device()))
+        if rc:
+            _check(rc, "conef_f8_quantise")
+    return (a, t) if forms == "both" else a if t is None else t
+
+
+def f8_dequantise(a: F8, dtype: torch.dtype = torch.float32, stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
+    """The values of a form, rows x cols (exact in float32 and bfloat16)."""
+    _f8_check(a, "f8_dequantise")
+    code = _ELEM.get(dtype)
+    if code is None:
+        _refuse("f8_dequantise", "dtype has to be float32, bfloat16 or float16")
+    rows, cols, kind, codes, scales = a
+    if not _at_hand(stream, codes, scales):
+        _same_device("f8_dequantise", codes.device, stream, codes, scales)
+        with _on(codes.device, stream):
+            return f8_dequantise(a, dtype)
+    out = torch.empty(rows, cols, dtype=dtype, device=codes.device)
+    rc = lib.conef_f8_dequantise(codes.data_ptr(), scales.data_ptr(), rows, cols, _F8KIND[kind], out.data_ptr(), code, cols,
+                                 torch._C._cuda_getCurrentRawStream(codes.get_device()))
+    if rc:
+        _check(rc, "conef_f8_dequantise")
+    return out
+
+
+def f8_matmul(a: F8, b: F8, dtype: torch.dtype = torch.bfloat16, stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
+    """a b^T (a.rows x b.rows): rows of both, of either kind, against each other.  A layer's products take forms as mx4_matmul's do."""
+    _f8_check(a, "f8_matmul")
+    _f8_check(b, "f8_matmul")
+    if a.cols != b.cols:
+        _refuse("f8_matmul", f"rows of {a.cols} against rows of {b.cols}")
+    code = _ELEM.get(dtype)
+    if code is None:
+        _refuse("f8_matmul", "dtype has to be float32, bfloat16 or float16")
+    m, k, a_kind, codes, scales = a
+    n, _, b_kind, b_codes, b_scales = b
+    if not _at_hand(stream, codes, scales, b_codes, b_scales):
+        _same_device("f8_matmul", codes.device, stream, codes, scales, b_codes, b_scales)
+        with _on(codes.device, stream):
+            return f8_matmul(a, b, dtype)
+    out = torch.empty(m, n, dtype=dtype, device=codes.device)
+    rc = lib.conef_f8_matmul(codes.data_ptr(), scales.data_ptr(), _F8KIND[a_kind], m, b_codes.data_ptr(), b_scales.data_ptr(), _F8KIND[b_kind], n, k, out.data_ptr(), code, n,
+                             torch._C._cuda_getCurrentRawStream(codes.get_device()))
+    if rc:
+        _check(rc, "conef_f8_matmul")
+    return out
+
+
+def _timeouts(name: str, device, stream: Optional[torch.cuda.Stream]) -> int:
+    n = C.c_int64()
+    with torch.cuda.device(device) if stream is None else torch.cuda.stream(stream):
+        _check(getattr(lib, name)(C.byref(n), _stream_handle(None)), name)
+    return n.value
+
+
+def f8_timeouts(device=None, stream: Optional[torch.cuda.Stream] = None) -> int:
+    """mx4_timeouts for f8_matmul."""
+    return _timeouts("conef_f8_timeouts", device, stream)
+
+
+def orthogonalise_timeouts(device=None, stream: Optional[torch.cuda.Stream] = None) -> int:
+    """mx4_timeouts for orthogonalise."""
+    return _timeouts("conef_orthogonalise_timeouts", device, stream)
+
+
+class Normed(NamedTuple):
+    """What rms_norm leaves: y (a tensor, a form, or a pair of them), h = x + add (x itself without add), and the rows' 1 / sqrt(mean h^2 + eps)."""
+    y: Union[torch.Tensor, F8, Tuple[F8, F8]]
+    h: torch.Tensor
+    rstd: torch.Tensor
+
+
+def _weight(weight: torch.Tensor, x: torch.Tensor, cols: int, where: str) -> None:
+    if weight.requires_grad and torch.is_grad_enabled():
+        _refuse(where, "weight requires a gradient, which nothing here records: call it under torch.no_grad() or in an autograd function")
+    if not weight.is_cuda or weight.numel() != cols or not weight.is_contiguous() or weight.dtype not in (x.dtype, torch.float32):
+        _refuse(where, f"weight has to be {cols} contiguous elements of the matrix' type or float32 on a GPU")
+
+
+def rms_norm(x: torch.Tensor, weight: torch.Tensor, eps: float = 1e-6, add: Optional[torch.Tensor] = None, forms: Optional[str] = None, kind: str = "e4m3",
+             stream: Optional[torch.cuda.Stream] = None) -> Normed:
+    """The root-mean-square norm of x's rows, behind the addition of `add` where there is one: h = x + add (rounded to the type), y = h rstd weight.  y has
+    x's type, or with forms = "rows", "cols" or "both" it is held in 8-bit floats, as f8_matmul reads them, and stands for the rounded exact products."""
+    rows, cols, ld = _matrix(x, "rms_norm")
+    _weight(weight, x, cols, "rms_norm")
+    add_ld = cols
+    if add is not None:
+        if add.shape != x.shape or add.dtype != x.dtype:
+            _refuse("rms_norm", "add differs from x in shape or type")
+        add_ld = _matrix(add, "rms_norm", "add")[2]
+    if not _at_hand(stream, x, weight) or (add is not None and not _at_hand(None, add)):
+        given = (x, weight) if add is None else (x, weight, add)
+        _same_device("rms_norm", x.device, stream, *given)
+        with _on(x.device, stream):
+            return rms_norm(x, weight, eps, add, forms, kind)
+    device = x.device
+    a = t = y = None
+    if forms is None:
+        y = torch.empty_like(x, memory_format=torch.contiguous_format)
+    else:
+        a, t = _f8_forms(rows, cols, forms, kind, device, "rms_norm")
+    h = x if add is None else torch.empty_like(x, memory_format=torch.contiguous_format)
+    rstd = torch.empty(x.shape[:-1], dtype=torch.float32, device=device)
+    rc = lib.conef_rms_norm(x.data_ptr(), None if add is None else add.data_ptr(), weight.data_ptr(), _ELEM[x.dtype], _ELEM[weight.dtype], rows, cols, ld, add_ld, eps,
+                            None if add is None else h.data_ptr(), cols, rstd.data_ptr(), None if y is None else y.data_ptr(), cols, _F8KIND.get(kind, -1),
+                            a.codes.data_ptr() if a else None, a.scales.data_ptr() if a else None, t.codes.data_ptr() if t else None,
+                            t.scales.data_ptr() if t else None, torch._C._cuda_getCurrentRawStream(x.get_device()))
+    if rc:
+        _check(rc, "conef_rms_norm")
+    if cols == 0:   # (the mean of nothing: nothing is launched)
+        rstd.fill_(float("nan"))
+    return Normed(y if forms is None else (a, t) if forms == "both" else a if t is None else t, h, rstd)
+
+
+def rms_norm_grad(dy: torch.Tensor, h: torch.Tensor, weight: torch.Tensor, rstd: torch.Tensor, add: Optional[torch.Tensor] = None,
+                  stream: Optional[torch.cuda.Stream] = None) -> Tuple[torch.Tensor, torch.Tensor]:
+    """(dx, dweight) of rms_norm from the gradient of y and what rms_norm left: dx, plus `add` (the gradient that reaches h another way), is the gradient of x and
+    of the residual; dweight is in float32."""
+    rows, cols, ld = _matrix(dy, "rms_norm_grad", "dy")
+    h_ld = _matrix(h, "rms_norm_grad", "h")[2]
+    _weight(weight, dy, cols, "rms_norm_grad")
+    add_ld = cols
+    for t, name in ((h, "h"), (add, "add")):
+        if t is not None and (t.shape != dy.shape or t.dtype != dy.dtype):
+            _refuse("rms_norm_grad", f"{name} differs from dy in shape or type")
+    if rstd.numel() != rows or rstd.dtype is not torch.float32 or not rstd.is_cuda or not rstd.is_contiguous():
+        _refuse("rms_norm_grad", f"rstd has to be {rows} contiguous float32 on a GPU")
+    if add is not None:
+        add_ld = _matrix(add, "rms_norm_grad", "add")[2]
+    given = (dy, h, weight, rstd) if add is None else (dy, h, weight, rstd, add)
+    if not _at_hand(stream, *given):
+        _same_device("rms_norm_grad", dy.device, stream, *given)
+        with _on(dy.device, stream):
+            return rms_norm_grad(dy, h, weight, rstd, add)
+    device = dy.device
+    size = C.c_size_t()
+    _check(lib.conef_rms_norm_grad_bytes(rows, cols, C.byref(size)), "conef_rms_norm_grad_bytes")
+    workspace = torch.empty(size.value, dtype=torch.uint8, device=device)
+    dx = torch.empty_like(dy, memory_format=torch.contiguous_format)
+    dweight = torch.empty(weight.shape, dtype=torch.float32, device=device)
+    rc = lib.conef_rms_norm_grad(dy.data_ptr(), h.data_ptr(), weight.data_ptr(), rstd.data_ptr(), None if add is None else add.data_ptr(), _ELEM[dy.dtype],
+                                 _ELEM[weight.dtype], rows, cols, ld, h_ld, add_ld, dx.data_ptr(), cols, dweight.data_ptr(), workspace.data_ptr(), size.value,
+                                 torch._C._cuda_getCurrentRawStream(dy.get_device()))
+    if rc:
+        _check(rc, "conef_rms_norm_grad")
+    return dx, dweight
+
+
+_QUINTIC = (3.4445, -4.7750, 2.0315)   # (singular values go to between 0.7 and 1.2 in five steps)
+
+
+def orthogonalise(x: torch.Tensor, steps: int = 5, scale: float = 1.0, coefficients: Sequence[float] = _QUINTIC, dtype: Optional[torch.dtype] = None,
+                  out: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
+    """x, a matrix or a stack of them (the dimensions before the last two), brought near the orthogonal matrix next to it by `steps` Newton-Schulz products of
+    its quotient by its Frobenius norm, X <- (c0 + c1 X X^T + c2 (X X^T)^2) X, times `scale`: an update as the Muon optimiser applies it.  The result is in
+    bfloat16 or float16 (default: x's type, bfloat16 for float32); out may be x."""
+    where = "orthogonalise"
+    if x.dim() < 2:
+        _refuse(where, "x has fewer than two dimensions")
+    dtype = out.dtype if out is not None and dtype is None else dtype or (x.dtype if x.dtype != torch.float32 else torch.bfloat16)
+    if dtype not in (torch.bfloat16, torch.float16):
+        _refuse(where, "the result's type has to be bfloat16 or float16")
+    if out is not None and (out.shape != x.shape or out.dtype != dtype):
+        _refuse(where, "out differs in shape or type")
+    if len(coefficients) != 3:
+        _refuse(where, "there are three coefficients")
+    rows, cols = x.shape[-2:]
+
+    def stack(t, name):
+        """(matrices, elements from row to row, elements from matrix to matrix)"""
+        _, _, ld = _matrix(t[(0,) * (t.dim() - 2)] if t.numel() else t, where, name)
+        if t.requires_grad and torch.is_grad_enabled():
+            _refuse(where, f"{name} requires a gradient, which nothing here records: call it under torch.no_grad() or in an autograd function")
+        batch, step, expect = 1, rows * ld, None
+        for size, gap in zip(reversed(t.shape[:-2]), reversed(t.stride()[:-2])):
+            if size != 1:
+                if expect is None:
+                    step = gap
+                elif gap != expect:
+                    _refuse(where, f"the matrices of {name} are not evenly spaced")
+                expect = gap * size
+            batch *= size
+        if batch > 1 and step < (rows - 1) * ld + cols and rows and cols:
+            _refuse(where, f"the matrices of {name} overlap")
+        return batch, ld, step
+
+    batch, ld, step = stack(x, "x")
+    given = (x,) if out is None else (x, out)
+    if not _at_hand(stream, *given):
+        _same_device(where, x.device, stream, *given)
+        with _on(x.device, stream):
+            return orthogonalise(x, steps, scale, coefficients, dtype, out)
+    if out is None:
+        out = torch.empty(x.shape, dtype=dtype, device=x.device)
+    _, out_ld, out_step = stack(out, "out")
+    size = C.c_size_t()
+    _check(lib.conef_orthogonalise_bytes(batch, rows, cols, C.byref(size)), "conef_orthogonalise_bytes")
+    workspace = torch.empty(size.value, dtype=torch.uint8, device=x.device)
+    rc = lib.conef_orthogonalise(x.data_ptr(), _ELEM[x.dtype], batch, rows, cols, ld, step, int(steps), (C.c_double * 3)(*coefficients), scale, out.data_ptr(), _ELEM[dtype],
+                                 out_ld, out_step, workspace.data_ptr(), size.value, torch._C._cuda_getCurrentRawStream(x.get_device()))
+    if rc:
+        _check(rc, "conef_orthogonalise")
+    return out
 
 
 class ConEF:

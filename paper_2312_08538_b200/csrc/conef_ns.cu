@@ -1,0 +1,648 @@
+// A matrix brought near the orthogonal one next to it by Newton-Schulz products (as the Muon optimiser does with its updates): X0 = G / |G|, the
+// Frobenius norm, then so many times X <- (a + b A + c A^2) X with A = X X^T, X having no more rows than columns (else it is G's transpose).
+// For X0 = U S V^T that is U f(f(..S)) V^T with f(s) = a s + b s^3 + c s^5.
+//
+// Each time f raises small singular values by a (3.4 times; five times over 480), and with them what a rounding put next to them.  With operands of 16
+// bits alone an update whose spectrum falls off by two decades is off by 1e-2 to 5e-2 (bf16) or 1e-3 to 6e-3 (fp16) of its size; rounded to bf16, which loses
+// 1.7e-3, it should not be.  So X, A and B = a + b A + c A^2 are kept as two fp16 each, hi + lo, under a power of two that keeps them
+// below fp16's largest (bounds of all three follow from the coefficients on the host), which is 22 bits, and a product is the sum of hi hi, hi lo and lo hi in one set of
+// fp32 sums on the tensor cores: as exact as 32-bit arithmetic at three times 16-bit's cost, not at the 20 times that 32-bit units take.
+//
+// Per step three launches: A (symmetric: tiles on and above the diagonal, stored twice), B (likewise, A added on the way out), B X.
+#include <cuda.h>
+#include <cuda_fp16.h>
+
+#include <algorithm>
+#include <atomic>
+#include <cmath>
+
+#include "conef_common.cuh"
+#include "conef_elem.cuh"
+#include "conef_mm.cuh"
+
+namespace conef {
+
+// A stack of n x m matrices kept as hi + lo, rows `pitch` elements apart
+struct Split {
+    __half *hi, *lo;
+    int64_t rows, cols, pitch;
+};
+__device__ __forceinline__ void split(float v, __half &hi, __half &lo)
+{
+    hi = __float2half_rn(v);
+    lo = __float2half_rn(v - __half2float(hi));
+}
+
+// ------------------------------------------------------------------ the norm and X0
+constexpr int kNsParts = 64;   // partial sums per matrix at most
+struct NsIn {
+    const void *x;
+    int64_t rows, cols, ld, stride;   // as the caller has it
+    double *parts;                    // kNsParts per matrix
+    uint32_t n_parts;
+};
+// sums of squares of a matrix's rows, part by part, in 64 bits
+template <class T>
+__global__ void __launch_bounds__(256) k_ns_squares(const __grid_constant__ NsIn A)
+{
+    __shared__ double part[8];
+    grid_release();
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const T *const x = (const T *)A.x + blockIdx.y * A.stride;
+    grid_wait();
+    double sum = 0;
+    for (int64_t row = (int64_t)blockIdx.x * 8 + warp; row < A.rows; row += (int64_t)A.n_parts * 8)
+#pragma unroll 8
+        for (int64_t c = lane; c < A.cols; c += 32) {
+            const double v = (double)to_f32(x[row * A.ld + c]);
+            sum = __fma_rn(v, v, sum);
+        }
+#pragma unroll
+    for (int o = 16; o; o /= 2)
+        sum += __shfl_xor_sync(0xffffffffu, sum, o);
+    if (lane == 0)
+        part[warp] = sum;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        for (int i = 1; i < 8; ++i)
+            sum += part[i];
+        A.parts[blockIdx.y * kNsParts + blockIdx.x] = sum;
+    }
+}
+// X0 times a power of two, in tiles of 64 x 64 (FLIP: X is the transpose)
+template <class T, bool FLIP>
+__global__ void __launch_bounds__(256) k_ns_start(const __grid_constant__ NsIn A, const Split X, uint32_t tiles_c, double scale)
+{
+    __shared__ float tile[FLIP ? 64 : 1][65];
+    grid_release();
+    const uint32_t tr = blockIdx.x / tiles_c, tc = blockIdx.x - tr * tiles_c;
+    const int64_t r0 = (int64_t)tr * 64, c0 = (int64_t)tc * 64, batch = blockIdx.y;
+    const T *const x = (const T *)A.x + batch * A.stride;
+    __half *const hi = X.hi + batch * X.rows * X.pitch, *const lo = X.lo + batch * X.rows * X.pitch;
+    grid_wait();
+    double sum = 0;
+    for (uint32_t i = 0; i < A.n_parts; ++i)
+        sum += A.parts[batch * kNsParts + i];
+    const double by = sum == 0 ? 0 : scale / sqrt(sum);   // (a matrix of zeros stays one)
+    const int c = threadIdx.x & 63;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+        const int r = i * 4 + (threadIdx.x >> 6);
+        if (r0 + r < A.rows && c0 + c < A.cols) {
+            const float v = (float)((double)to_f32(x[(r0 + r) * A.ld + c0 + c]) * by);
+            if constexpr (FLIP) {
+                tile[r][c] = v;
+            } else {
+                __half h, l;
+                split(v, h, l);
+                hi[(r0 + r) * X.pitch + c0 + c] = h;
+                lo[(r0 + r) * X.pitch + c0 + c] = l;
+            }
+        }
+    }
+    if constexpr (FLIP) {
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            const int r = i * 4 + (threadIdx.x >> 6);   // (a row of X)
+            if (c0 + r < A.cols && r0 + c < A.rows) {
+                __half h, l;
+                split(tile[c][r], h, l);
+                hi[(c0 + r) * X.pitch + r0 + c] = h;
+                lo[(c0 + r) * X.pitch + r0 + c] = l;
+            }
+        }
+    }
+}
+
+// ------------------------------------------------------------------ products
+// D = f_sum (L R) + f_add E + f_one 1 for stacks of matrices; R along k like L (A = X X^T, A A), or (CROSS) as it is multiplied, along D's columns (B X).
+// The kernel is that of conef_mm.cuh with another stage and another way out: 64 elements of k of L's and R's hi and lo; what leaves is split again, or rounded to the result.
+struct NsArgs {
+    Split out, add;              // (add.hi: NULL without E)
+    void *result;                // the last product's, instead of out
+    int64_t result_ld, result_stride;
+    float f_sum, f_add, f_one;
+    uint32_t n, m, k;            // of D = n x m
+    uint32_t k_steps, stages_k, per_matrix, tiles_m, n_tiles, stages;
+    uint32_t symmetric, flip, dtype, terms;
+    uint64_t limit, sums_limit;
+    uint32_t loads[2];
+};
+struct NsMaps {
+    CUtensorMap lh, ll, rh, rl;
+};
+constexpr uint32_t kNsPart = 128 * 128;   // bytes: 128 rows (CROSS: of k's 64, two columns of 64 elements) of hi or lo
+struct NsTile {
+    uint32_t batch, i, j;
+};
+template <class A>
+__device__ __forceinline__ NsTile ns_tile(const A &P, uint32_t tile)
+{
+    NsTile t;
+    t.batch = tile / P.per_matrix;
+    uint32_t in = tile - t.batch * P.per_matrix;
+    if (P.symmetric) {   // columns of a triangle
+        uint32_t j = (uint32_t)((sqrtf(8.f * (float)in + 1.f) - 1.f) * 0.5f);
+        while (j * (j + 1) / 2 > in)
+            --j;
+        while ((j + 1) * (j + 2) / 2 <= in)
+            ++j;
+        t.j = j, t.i = in - j * (j + 1) / 2;
+    } else {
+        t.j = in / P.tiles_m, t.i = in - t.j * P.tiles_m;
+    }
+    return t;
+}
+
+// A tile is 128 x 128, or of a pair of CTAs 256 x 256: with 128 x 128 a product reads as many bytes of shared memory per cycle as there are, so that the copies into it
+// have to wait; a pair's CTA has half of R for twice the outputs.
+template <bool PAIR, bool CROSS>
+__global__ void __launch_bounds__(kMmThreads, 1) k_ns_product(const __grid_constant__ NsMaps maps, const __grid_constant__ NsArgs P)
+{
+    constexpr uint32_t BN = PAIR ? 256 : 128, BM = PAIR ? 256 : 128;
+    constexpr uint32_t stage_bytes = 4 * kNsPart;
+    extern __shared__ __align__(1024) uint8_t mm_smem[];
+    __shared__ MmShared S;
+    const int warp = __shfl_sync(0xffffffffu, (int)(threadIdx.x >> 5), 0), lane = threadIdx.x & 31;
+    const uint32_t rank = PAIR ? blockIdx.x & 1u : 0u, first = PAIR ? blockIdx.x / 2 : blockIdx.x, step = PAIR ? gridDim.x / 2 : gridDim.x;
+    uint8_t *const ring = mm_smem + ((1024u - (tc::saddr(mm_smem) & 1023u)) & 1023u);
+    const tc::Waits waits = {&S.dead, PAIR ? tc::address_in(&S.dead, rank ^ 1u) : 0u, &g_mm_ran_out};
+    if (warp == 0) {
+        tc::tmem_alloc<PAIR>(&S.tmem, kMmColumns);
+        if (lane == 0) {
+            for (int i = 0; i < kMmMaxStages; ++i) {
+                tc::bar_init(&S.full[i], 1);
+                tc::bar_init(&S.empty[i], 1);
+            }
+            for (int i = 0; i < 2; ++i) {
+                tc::bar_init(&S.sums[i], 1);
+                tc::bar_init(&S.taken[i], BN / 16 * (PAIR ? 2 : 1));
+            }
+            tc::bar_init(&S.drain, 1);
+            S.dead = 0;
+            asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        }
+        tc::fence_before();
+    }
+    __syncthreads();
+    if (PAIR)
+        tc::cluster_sync();
+    tc::fence_after();
+    grid_release();
+    grid_wait();
+    asm volatile("fence.proxy.async;" ::: "memory");   // (what the launch before stored, ordinary stores, is read by copies)
+
+    auto load = [&](uint32_t s, uint32_t ks, const NsTile &t) {
+        const uint32_t st = tc::saddr(ring) + s * stage_bytes, k0 = ks * 64, i0 = t.i * BM + rank * 128, j0 = t.j * BN + rank * (BN / 2);
+        const uint32_t parts = P.terms == 1 ? 2 : 4;
+        if constexpr (PAIR) {
+            const uint32_t bar = tc::leaders(&S.full[s]);
+            if (rank == 0)
+                tc::bar_expect(&S.full[s], 2 * parts * kNsPart);
+            tc::tile_load3_pair(st, &maps.lh, k0, i0, t.batch, bar);
+            if (parts == 4)
+                tc::tile_load3_pair(st + kNsPart, &maps.ll, k0, i0, t.batch, bar);
+            if constexpr (CROSS) {
+                tc::tile_load3_pair(st + 2 * kNsPart, &maps.rh, j0, k0, t.batch, bar);
+                tc::tile_load3_pair(st + 2 * kNsPart + kNsPart / 2, &maps.rh, j0 + 64, k0, t.batch, bar);
+                if (parts == 4) {
+                    tc::tile_load3_pair(st + 3 * kNsPart, &maps.rl, j0, k0, t.batch, bar);
+                    tc::tile_load3_pair(st + 3 * kNsPart + kNsPart / 2, &maps.rl, j0 + 64, k0, t.batch, bar);
+                }
+            } else {
+                tc::tile_load3_pair(st + 2 * kNsPart, &maps.rh, k0, j0, t.batch, bar);
+                if (parts == 4)
+                    tc::tile_load3_pair(st + 3 * kNsPart, &maps.rl, k0, j0, t.batch, bar);
+            }
+        } else {
+            uint64_t *const bar = &S.full[s];
+            tc::bar_expect(bar, parts * kNsPart);
+            tc::tile_load3(st, &maps.lh, k0, i0, t.batch, bar);
+            if (parts == 4)
+                tc::tile_load3(st + kNsPart, &maps.ll, k0, i0, t.batch, bar);
+            if constexpr (CROSS) {
+                tc::tile_load3(st + 2 * kNsPart, &maps.rh, j0, k0, t.batch, bar);
+                tc::tile_load3(st + 2 * kNsPart + kNsPart / 2, &maps.rh, j0 + 64, k0, t.batch, bar);
+                if (parts == 4) {
+                    tc::tile_load3(st + 3 * kNsPart, &maps.rl, j0, k0, t.batch, bar);
+                    tc::tile_load3(st + 3 * kNsPart + kNsPart / 2, &maps.rl, j0 + 64, k0, t.batch, bar);
+                }
+            } else {
+                tc::tile_load3(st + 2 * kNsPart, &maps.rh, k0, j0, t.batch, bar);
+                if (parts == 4)
+                    tc::tile_load3(st + 3 * kNsPart, &maps.rl, k0, j0, t.batch, bar);
+            }
+        }
+    };
+    uint32_t armed = 0;
+    if (warp == kMmEpilogue) {
+        uint32_t s = 0, phase = 0;
+        bool ok = true;
+        for (uint32_t tile = first; ok && tile < P.n_tiles; tile += step) {
+            const NsTile t = ns_tile(P, tile);
+            for (uint32_t ks = 0; ks < P.stages_k; ++ks) {
+                if (!(ok = armed < P.loads[rank] && tc::bar_wait(&S.empty[s], phase ^ 1u, waits, P.limit)))
+                    break;
+                if (tc::elect())
+                    load(s, ks, t);
+                ++armed;
+                if (++s == P.stages)
+                    s = 0, phase ^= 1u;
+            }
+        }
+        if (lane == 0)
+            S.armed = armed;
+        __syncwarp();
+    } else if (warp == kMmEpilogue + 1) {
+        const uint32_t instruction = tc::f16_instruction<PAIR, CROSS>(BN);
+        constexpr uint32_t part16 = kNsPart / 16, k_step = CROSS ? 128 : 2;   // (16 of k: 32 bytes of a row, or two groups of eight rows)
+        const uint32_t a0 = tc::desc_low(ring), b0 = CROSS ? tc::desc_low_across(tc::saddr(ring) + 2 * kNsPart, kNsPart / 2) : a0 + 2 * part16;
+        uint32_t s = 0, phase = 0, set = 0, turn = 0;
+        bool ok = true;
+        for (uint32_t tile = rank ? P.n_tiles : first; ok && tile < P.n_tiles; tile += step) {
+            const uint32_t d = set * BN;
+            if (!(ok = tc::bar_wait(&S.taken[set], turn ^ 1u, waits, P.limit)))
+                break;
+            tc::fence_after();
+            for (uint32_t ks = 0; ks < P.stages_k; ++ks) {
+                if (!(ok = tc::bar_wait(&S.full[s], phase, waits, P.limit)))
+                    break;
+                tc::fence_after();
+                if (tc::elect()) {
+                    const uint32_t steps = P.k_steps - ks * 4u, a = a0 + s * (stage_bytes / 16), b = b0 + s * (stage_bytes / 16);
+#pragma unroll
+                    for (uint32_t t = 0; t < 4; ++t)
+                        if (t < steps) {
+                            tc::f16_product<PAIR>(d, a + 2 * t, b + k_step * t, instruction, ks + t);
+                            if (P.terms > 1) {
+                                tc::f16_product<PAIR>(d, a + 2 * t, b + part16 + k_step * t, instruction, 1);
+                                tc::f16_product<PAIR>(d, a + part16 + 2 * t, b + k_step * t, instruction, 1);
+                            }
+                        }
+                    tc::commit<PAIR>(&S.empty[s]);
+                }
+                if (++s == P.stages)
+                    s = 0, phase ^= 1u;
+            }
+            if (ok && tc::elect())
+                tc::commit<PAIR>(&S.sums[set]);
+            if (++set == 2)
+                set = 0, turn ^= 1u;
+        }
+        __syncwarp();
+    } else {
+        // sums of 32 rows (a lane each) and 64 columns, 32 at a time
+        uint32_t set = 0, turn = 0;
+        bool ok = true;
+        const uint32_t c0 = (uint32_t)(warp >> 2) * 64;
+        for (uint32_t tile = c0 < BN ? first : P.n_tiles; tile < P.n_tiles; tile += step) {
+            const NsTile t = ns_tile(P, tile);
+            const uint32_t row = t.i * BM + rank * 128 + (warp & 3) * 32 + lane, col0 = t.j * BN + c0;
+            const bool mirror = P.symmetric && t.i != t.j;
+            ok = ok && tc::bar_wait(&S.sums[set], turn, waits, P.sums_limit);
+            if (ok)
+                tc::fence_after();
+#pragma unroll
+            for (uint32_t half = 0; half < 2; ++half) {
+                uint32_t v[32];
+                const uint32_t col = col0 + half * 32;
+                __syncwarp();
+                if (ok) {
+                    tc::tmem_load32(((uint32_t)(warp & 3) << 21) + set * BN + c0 + half * 32, v);
+                    tc::tmem_load_wait();
+                    if (half == 1) {
+                        tc::fence_before();
+                        __syncwarp();
+                        if (lane == 0) {
+                            if (PAIR)
+                                tc::bar_arrive_at(tc::leaders(&S.taken[set]));
+                            else
+                                tc::bar_arrive(&S.taken[set]);
+                        }
+                    }
+                } else {   // a wait ran out: what was not computed is NaN
+#pragma unroll
+                    for (int i = 0; i < 32; ++i)
+                        v[i] = 0x7FFFFFFFu;
+                }
+                if (row >= P.n || col >= P.m)
+                    continue;
+                float f[32];
+#pragma unroll
+                for (int i = 0; i < 32; ++i)
+                    f[i] = __fmul_rn(__uint_as_float(v[i]), P.f_sum);
+                if (P.add.hi) {
+                    const int64_t at = ((int64_t)t.batch * P.add.rows + row) * P.add.pitch + col;
+#pragma unroll
+                    for (int i = 0; i < 32; i += 8) {   // (rows are padded to 64 elements)
+                        const uint4 h = *(const uint4 *)(P.add.hi + at + i), l = *(const uint4 *)(P.add.lo + at + i);
+                        float a[8], b[8];
+                        Vec16<__half>::unpack(h, a), Vec16<__half>::unpack(l, b);
+#pragma unroll
+                        for (int q = 0; q < 8; ++q)
+                            f[i + q] = __fmaf_rn(__fadd_rn(a[q], b[q]), P.f_add, f[i + q]);
+                    }
+                }
+#pragma unroll
+                for (int i = 0; i < 32; ++i)
+                    if (row == col + i)
+                        f[i] = __fadd_rn(f[i], P.f_one);
+                const uint32_t have = min(32u, P.m - col);
+                if (P.result) {
+                    const int64_t base = (int64_t)t.batch * P.result_stride;
+                    if (P.flip) {
+#pragma unroll
+                        for (int i = 0; i < 32; ++i)
+                            if ((uint32_t)i < have) {
+                                const int64_t at = base + (int64_t)(col + i) * P.result_ld + row;
+                                if (P.dtype == CONEF_BF16)
+                                    ((__nv_bfloat16 *)P.result)[at] = __float2bfloat16_rn(f[i]);
+                                else
+                                    ((__half *)P.result)[at] = __float2half_rn(f[i]);
+                            }
+                    } else {
+                        const int64_t at = base + (int64_t)row * P.result_ld + col;
+#pragma unroll
+                        for (int i = 0; i < 32; ++i)
+                            if ((uint32_t)i < have) {
+                                if (P.dtype == CONEF_BF16)
+                                    ((__nv_bfloat16 *)P.result)[at + i] = __float2bfloat16_rn(f[i]);
+                                else
+                                    ((__half *)P.result)[at + i] = __float2half_rn(f[i]);
+                            }
+                    }
+                } else {
+                    const int64_t base = (int64_t)t.batch * P.out.rows * P.out.pitch, at = base + (int64_t)row * P.out.pitch + col;
+#pragma unroll
+                    for (int i = 0; i < 32; i += 8) {
+                        __half h[8], l[8];
+#pragma unroll
+                        for (int q = 0; q < 8; ++q)
+                            split(f[i + q], h[q], l[q]);
+                        *(uint4 *)(P.out.hi + at + i) = *(const uint4 *)h;   // (what lies past a row's end is not read)
+                        *(uint4 *)(P.out.lo + at + i) = *(const uint4 *)l;
+                        if (mirror) {
+#pragma unroll
+                            for (int q = 0; q < 8; ++q)
+                                if ((uint32_t)(i + q) < have) {
+                                    P.out.hi[base + (int64_t)(col + i + q) * P.out.pitch + row] = h[q];
+                                    P.out.lo[base + (int64_t)(col + i + q) * P.out.pitch + row] = l[q];
+                                }
+                        }
+                    }
+                }
+            }
+            if (++set == 2)
+                set = 0, turn ^= 1u;
+        }
+        __syncwarp();
+    }
+    tc::fence_before();
+    __syncthreads();
+    if (PAIR)
+        tc::cluster_sync();   // neither CTA tells a barrier of one that has ended
+    tc::fence_after();
+    if (*waits.dead) {   // as in conef_mm.cuh: what is in flight ends before shared and tensor memory are given back
+        const uint64_t t0 = tc::nanoseconds();
+        if (warp == kMmEpilogue) {
+            const uint32_t all = PAIR ? max(armed, tc::load_at(tc::address_in(&S.armed, rank ^ 1u))) : armed;
+            for (; armed < all; ++armed) {
+                const uint32_t nth = armed / P.stages_k;
+                const NsTile t = ns_tile(P, first + nth * step);
+                if (tc::elect())
+                    load(armed % P.stages, armed - nth * P.stages_k, t);
+                __syncwarp();
+            }
+            if (rank == 0)
+                for (uint32_t i = 0; i < P.stages && i < all; ++i)
+                    tc::bar_drain(&S.full[(all - 1 - i) % P.stages], ((all - 1 - i) / P.stages) & 1u, t0);
+        } else if (warp == kMmEpilogue + 1 && rank == 0) {
+            if (tc::elect())
+                tc::commit<PAIR>(&S.drain);
+            __syncwarp();
+            tc::bar_drain(&S.drain, 0, t0);
+        }
+        __syncthreads();
+        if (PAIR)
+            tc::cluster_sync();
+        tc::fence_after();
+    }
+    if (warp == 0)
+        tc::tmem_free<PAIR>(0, kMmColumns);
+}
+
+// ------------------------------------------------------------------ host
+
+// tiles of `box` rows of 64 elements
+static bool encode_split(CUtensorMap *map, const __half *p, int64_t rows, int64_t cols, int64_t pitch, int64_t batch, uint32_t box)
+{
+    const cuuint64_t dims[3] = {(cuuint64_t)cols, (cuuint64_t)rows, (cuuint64_t)batch}, strides[2] = {(cuuint64_t)pitch * 2, (cuuint64_t)(pitch * rows) * 2};
+    const cuuint32_t tile[3] = {64, box, 1}, steps[3] = {1, 1, 1};
+    return encode_tiled() && encode_tiled()(map, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 3, (void *)p, dims, strides, tile, steps, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                                            CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+constexpr uint32_t kNsStages = 3;
+constexpr size_t kNsSmem = 1024 + kNsStages * 4 * kNsPart;
+
+template <bool CROSS>
+static cudaError_t ns_product(const Split &L, const Split &R, int64_t batch, NsArgs P, bool pair, cudaStream_t s)
+{
+    const uint32_t side = pair ? 256 : 128;
+    P.n = (uint32_t)L.rows;
+    P.m = (uint32_t)(CROSS ? R.cols : R.rows);
+    P.k = (uint32_t)L.cols;
+    P.k_steps = (P.k + 15) / 16;
+    P.stages_k = (P.k + 63) / 64;
+    P.tiles_m = (P.n + side - 1) / side;
+    const int64_t per = P.symmetric ? (int64_t)P.tiles_m * (P.tiles_m + 1) / 2 : (int64_t)P.tiles_m * ((P.m + side - 1) / side);
+    if (per * batch >= (1ll << 31))
+        return cudaErrorInvalidValue;
+    P.per_matrix = (uint32_t)per;
+    P.n_tiles = (uint32_t)(per * batch);
+    P.stages = kNsStages;
+    P.limit = (uint64_t)mm_limit.nanoseconds.load();
+    P.sums_limit = P.limit + 4096ull * P.stages_k;
+    P.loads[0] = mm_limit.loads[0].load();
+    P.loads[1] = mm_limit.loads[1].load();
+    NsMaps maps;
+    if (!encode_split(&maps.lh, L.hi, L.rows, L.cols, L.pitch, batch, 128) || !encode_split(&maps.ll, L.lo, L.rows, L.cols, L.pitch, batch, 128) ||
+        !encode_split(&maps.rh, R.hi, R.rows, R.cols, R.pitch, batch, CROSS ? 64 : 128) || !encode_split(&maps.rl, R.lo, R.rows, R.cols, R.pitch, batch, CROSS ? 64 : 128))
+        return cudaErrorInvalidValue;
+    static int done[2][64];
+    cudaError_t e = pair ? opt_in_smem(k_ns_product<true, CROSS>, kMmSmem, done[1]) : opt_in_smem(k_ns_product<false, CROSS>, kMmSmem, done[0]);
+    if (e != cudaSuccess)
+        return e;
+    // (a pair leaves no shared memory on its SMs: conef_mm.cuh)
+    return pair ? launch_cluster(k_ns_product<true, CROSS>, (int)std::min<uint32_t>(P.n_tiles, kPlanSMs / 2), 2, kMmThreads, s, (size_t)kMmSmem, maps, P)
+                : launch(k_ns_product<false, CROSS>, dim3(std::min<uint32_t>(P.n_tiles, kPlanSMs)), kMmThreads, kNsSmem, s, maps, P);
+}
+
+// the largest |a + b t + c t^2| for 0 <= t <= top, and the largest |s (a + b s^2 + c s^4)| for 0 <= s <= top
+static double largest_factor(double a, double b, double c, double top)
+{
+    double most = std::max(std::fabs(a), std::fabs(a + b * top + c * top * top));
+    const double t = c != 0 ? -b / (2 * c) : -1;
+    if (t > 0 && t < top)
+        most = std::max(most, std::fabs(a + b * t + c * t * t));
+    return most;
+}
+static double largest_value(double a, double b, double c, double top)
+{
+    auto f = [&](double s) { return std::fabs(s * (a + b * s * s + c * s * s * s * s)); };
+    double most = f(top);
+    const double root = 9 * b * b - 20 * a * c;   // f' = a + 3 b t + 5 c t^2, t = s^2
+    auto at = [&](double t) {
+        if (t > 0 && t < top * top)
+            most = std::max(most, f(std::sqrt(t)));
+    };
+    if (c != 0 && root >= 0) {
+        at((-3 * b + std::sqrt(root)) / (10 * c));
+        at((-3 * b - std::sqrt(root)) / (10 * c));
+    } else if (c == 0 && b != 0) {
+        at(-a / (3 * b));
+    }
+    return most;
+}
+// a power of two that brings `bound` below 2^15, half of fp16's range
+static double fp16_scale(double bound) { return std::ldexp(1.0, 14 - std::ilogb(std::max(bound, 1e-30))); }
+
+struct NsSizes {
+    int64_t n, m, pitch_x, pitch_a;   // rows <= columns
+    bool flip;
+};
+static NsSizes ns_sizes(int64_t rows, int64_t cols)
+{
+    NsSizes z;
+    z.flip = rows > cols;
+    z.n = std::min(rows, cols), z.m = std::max(rows, cols);
+    z.pitch_x = (z.m + 63) / 64 * 64, z.pitch_a = (z.n + 63) / 64 * 64;
+    return z;
+}
+
+}  // namespace conef
+
+using namespace conef;
+
+extern "C" {
+
+int conef_orthogonalise_bytes(int64_t batch, int64_t rows, int64_t cols, size_t *bytes)
+{
+    if (batch < 0 || rows < 0 || cols < 0 || !bytes)
+        return CONEF_ERR_INVALID_ARG;
+    if (rows >= (1ll << 31) || cols >= (1ll << 31) || batch >= (1ll << 16))
+        return CONEF_ERR_UNSUPPORTED;
+    const NsSizes z = ns_sizes(rows, cols);
+    // X twice, A and B, hi and lo each, and the norms' parts
+    *bytes = batch && rows && cols ? ((size_t)batch * z.n * (2 * z.pitch_x + 2 * z.pitch_a) * 2 * sizeof(__half) + (size_t)batch * kNsParts * sizeof(double)) : 0;
+    return CONEF_OK;
+}
+
+int conef_orthogonalise(const void *x, int dtype, int64_t batch, int64_t rows, int64_t cols, int64_t ld, int64_t stride, int steps, const double *coefficients, double scale,
+                        void *out, int out_dtype, int64_t out_ld, int64_t out_stride, void *workspace, size_t workspace_bytes, conef_stream stream)
+{
+    int rc = check_matrix(x, dtype, batch ? rows : 0, cols, ld);
+    if (rc == CONEF_OK)
+        rc = check_matrix(out, out_dtype, batch ? rows : 0, cols, out_ld);
+    if (rc != CONEF_OK)
+        return rc;
+    if (batch < 0 || out_dtype == CONEF_F32 || steps < 1 || steps > 32 || !coefficients || !std::isfinite(scale) || std::fabs(scale) > 1e30)
+        return CONEF_ERR_INVALID_ARG;
+    if (batch > 1 && rows && cols && (stride < (rows - 1) * ld + cols || out_stride < (rows - 1) * out_ld + cols))
+        return CONEF_ERR_INVALID_ARG;
+    // bounds of X, A and B before each step: a power of two each that keeps them within fp16
+    double top[33];
+    const double a = coefficients[0], b = coefficients[1], c = coefficients[2];
+    top[0] = 1.0;
+    for (int t = 0; t < steps; ++t) {
+        top[t + 1] = largest_value(a, b, c, top[t]);
+        if (!(top[t + 1] <= 1e4))
+            return CONEF_ERR_INVALID_ARG;   // (the polynomial does not keep singular values bounded)
+    }
+    size_t need = 0;
+    if ((rc = conef_orthogonalise_bytes(batch, rows, cols, &need)) != CONEF_OK)
+        return rc;
+    if (!need)
+        return CONEF_OK;
+    if (!workspace || workspace_bytes < need)
+        return CONEF_ERR_WORKSPACE_TOO_SMALL;
+    if ((uintptr_t)workspace & 127)
+        return CONEF_ERR_INVALID_ARG;
+    const NsSizes z = ns_sizes(rows, cols);
+    cudaStream_t s = (cudaStream_t)stream;
+    __half *at = (__half *)workspace;
+    auto take = [&](int64_t columns, int64_t pitch) {
+        Split m = {at, at + batch * z.n * pitch, z.n, columns, pitch};
+        at += 2 * batch * z.n * pitch;
+        return m;
+    };
+    Split X = take(z.m, z.pitch_x), Y = take(z.m, z.pitch_x), A = take(z.n, z.pitch_a), B = take(z.n, z.pitch_a);
+    NsIn in = {x, rows, cols, ld, stride, (double *)at, (uint32_t)std::min<int64_t>(kNsParts, (rows + 7) / 8)};
+    double sx = fp16_scale(top[0]);
+    cudaError_t e = cudaErrorInvalidValue;
+    const int64_t tiles_c = (cols + 63) / 64, tiles = (rows + 63) / 64 * tiles_c;
+    if (tiles >= (1ll << 31))
+        return CONEF_ERR_UNSUPPORTED;
+    with_elem(dtype, [&](auto t) {
+        using T = decltype(t);
+        e = launch(k_ns_squares<T>, dim3(in.n_parts, (unsigned)batch), 256, 0, s, in);
+        if (e == cudaSuccess)
+            e = launch(z.flip ? k_ns_start<T, true> : k_ns_start<T, false>, dim3((unsigned)tiles, (unsigned)batch), 256, 0, s, in, X, (uint32_t)tiles_c, sx);
+        return 0;
+    });
+    // tiles of pairs where there are enough of them
+    const int64_t sides = (z.n + 255) / 256;
+    const bool pair_a = sides * (sides + 1) / 2 * batch >= kPlanSMs / 4, pair_x = sides * ((z.m + 255) / 256) * batch >= kPlanSMs / 4;
+    for (int t = 0; t < steps && e == cudaSuccess; ++t) {
+        const double sa = fp16_scale(top[t] * top[t]), sb = fp16_scale(largest_factor(a, b, c, top[t] * top[t])), sy = fp16_scale(top[t + 1]);
+        NsArgs P = {};
+        P.terms = 3;
+        P.symmetric = 1;
+        P.out = A;
+        P.f_sum = (float)(sa / (sx * sx));
+        e = ns_product<false>(X, X, batch, P, pair_a, s);
+        if (e != cudaSuccess)
+            break;
+        P.out = B;
+        P.add = A;
+        P.f_sum = (float)(c * sb / (sa * sa));
+        P.f_add = (float)(b * sb / sa);
+        P.f_one = (float)(a * sb);
+        e = ns_product<false>(A, A, batch, P, pair_a, s);
+        if (e != cudaSuccess)
+            break;
+        NsArgs U = {};
+        U.terms = 3;
+        if (t + 1 == steps) {
+            U.result = out;
+            U.result_ld = rows > 1 ? out_ld : cols;
+            U.result_stride = batch > 1 ? out_stride : 0;
+            U.flip = z.flip;
+            U.dtype = (uint32_t)out_dtype;
+            U.f_sum = (float)(scale / (sb * sx));
+        } else {
+            U.out = Y;
+            U.f_sum = (float)(sy / (sb * sx));
+        }
+        e = ns_product<true>(B, X, batch, U, pair_x, s);
+        std::swap(X, Y);
+        sx = sy;
+    }
+    return launched(e, "conef_orthogonalise");
+}
+
+int conef_orthogonalise_timeouts(int64_t *count, conef_stream stream)
+{
+    if (!count)
+        return CONEF_ERR_INVALID_ARG;
+    unsigned long long n = 0;
+    cudaError_t e = cudaMemcpyFromSymbolAsync(&n, g_mm_ran_out, sizeof n, 0, cudaMemcpyDeviceToHost, (cudaStream_t)stream);
+    if (e == cudaSuccess)
+        e = cudaStreamSynchronize((cudaStream_t)stream);
+    *count = (int64_t)n;
+    return launched(e, "conef_orthogonalise_timeouts");
+}
+
+}  // extern "C"

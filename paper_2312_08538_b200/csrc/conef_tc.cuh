@@ -112,6 +112,19 @@ __device__ __forceinline__ void tile_load_pair(uint32_t dst, const void *map, ui
                  "r"(y), "r"(bar)
                  : "memory");
 }
+// ... of tiles of a stack of matrices
+__device__ __forceinline__ void tile_load3(uint32_t dst, const void *map, uint32_t x, uint32_t y, uint32_t z, uint64_t *bar)
+{
+    asm volatile("cp.async.bulk.tensor.3d.shared::cta.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(dst), "l"(map), "r"(x), "r"(y),
+                 "r"(z), "r"(saddr(bar))
+                 : "memory");
+}
+__device__ __forceinline__ void tile_load3_pair(uint32_t dst, const void *map, uint32_t x, uint32_t y, uint32_t z, uint32_t bar)
+{
+    asm volatile("cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(dst), "l"(map),
+                 "r"(x), "r"(y), "r"(z), "r"(bar)
+                 : "memory");
+}
 
 // ... and out of it: one thread stores a tile that the warp wrote (store_fence by each writer, then a barrier), and waits until the memory
 // may be written again, or until all its stores have ended
@@ -193,6 +206,43 @@ __device__ __forceinline__ void mx4_product(uint32_t d, uint32_t a, uint32_t b, 
     else
         asm volatile("{\n\t.reg .pred q;\n\tsetp.ne.u32 q, %6, 0;\n\ttcgen05.mma.cta_group::1.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%4], [%5], q;\n\t}" ::"r"(d),
                      "l"(da), "l"(db), "r"(instruction), "r"(sa), "r"(sb), "r"(add)
+                     : "memory");
+}
+// 8-bit floats (kinds: 0 e4m3, 1 e5m2), likewise; 32 elements along k, number n of the four scales in a column's word as n << 4 | n << 29 in `instruction`
+template <bool PAIR>
+__device__ __forceinline__ uint32_t f8_instruction(uint32_t n, uint32_t kind_a, uint32_t kind_b)
+{
+    return (kind_a << 7) | (kind_b << 10) | ((n >> 3) << 17) | (1u << 23) | ((PAIR ? 16u : 8u) << 24);
+}
+template <bool PAIR>
+__device__ __forceinline__ void f8_product(uint32_t d, uint32_t a, uint32_t b, uint32_t instruction, uint32_t sa, uint32_t sb, uint32_t add)
+{
+    const uint64_t da = (uint64_t)kDescRows128 << 32 | a, db = (uint64_t)kDescRows128 << 32 | b;
+    if constexpr (PAIR)
+        asm volatile("{\n\t.reg .pred q;\n\tsetp.ne.u32 q, %6, 0;\n\ttcgen05.mma.cta_group::2.kind::mxf8f6f4.block_scale.scale_vec::1X [%0], %1, %2, %3, [%4], [%5], q;\n\t}" ::"r"(d),
+                     "l"(da), "l"(db), "r"(instruction), "r"(sa), "r"(sb), "r"(add)
+                     : "memory");
+    else
+        asm volatile("{\n\t.reg .pred q;\n\tsetp.ne.u32 q, %6, 0;\n\ttcgen05.mma.cta_group::1.kind::mxf8f6f4.block_scale.scale_vec::1X [%0], %1, %2, %3, [%4], [%5], q;\n\t}" ::"r"(d),
+                     "l"(da), "l"(db), "r"(instruction), "r"(sa), "r"(sb), "r"(add)
+                     : "memory");
+}
+// 16-bit floats (fp16), 128 rows of A (PAIR: of each CTA), n of B; B along k like A, or (CROSS) along n: 64 of n to a row of 128 bytes, eight of k to a group
+// of 1024 bytes, `across` bytes from one 64 of n to the next.  16 elements along k.
+template <bool PAIR, bool CROSS>
+__device__ __forceinline__ uint32_t f16_instruction(uint32_t n) { return (1u << 4) | ((CROSS ? 1u : 0u) << 16) | ((n >> 3) << 17) | ((PAIR ? 16u : 8u) << 24); }
+__device__ __forceinline__ uint32_t desc_low_across(uint32_t address, uint32_t across) { return ((address & 0x3FFFFu) >> 4) | ((across >> 4) << 16); }
+template <bool PAIR>
+__device__ __forceinline__ void f16_product(uint32_t d, uint32_t a, uint32_t b, uint32_t instruction, uint32_t add)
+{
+    const uint64_t da = (uint64_t)kDescRows128 << 32 | a, db = (uint64_t)kDescRows128 << 32 | b;
+    if constexpr (PAIR)
+        asm volatile("{\n\t.reg .pred q;\n\tsetp.ne.u32 q, %4, 0;\n\ttcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, q;\n\t}" ::"r"(d), "l"(da), "l"(db),
+                     "r"(instruction), "r"(add)
+                     : "memory");
+    else
+        asm volatile("{\n\t.reg .pred q;\n\tsetp.ne.u32 q, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, q;\n\t}" ::"r"(d), "l"(da), "l"(db),
+                     "r"(instruction), "r"(add)
                      : "memory");
 }
 // the barrier (PAIR: that of each CTA) is told when all that this lane has issued is done
