@@ -123,10 +123,8 @@ __global__ void __launch_bounds__(kF8Threads) k_f8_tiles(const T *x, const __gri
             float v[16];
             p[i].unpack(v);
             if constexpr (NORM) {
-                const float r = row < A.rows ? A.rstd[row] : 0.f;
-#pragma unroll
-                for (int q = 0; q < 16; ++q)
-                    v[q] = norm_value(v[q], w[q], r);
+                if (row < A.rows)   // (else zeros stay ones without a sign)
+                    norm_values<16>(v, w, A.rstd[row]);
             }
             if (A.out.codes_t) {
                 if constexpr (WIDE) {
@@ -199,12 +197,13 @@ __global__ void __launch_bounds__(kF8Threads) k_f8_tiles(const T *x, const __gri
                 const int64_t row = r0 + at;
                 float v[4];
                 uint32_t most = 0;
-                const float r = NORM && row < A.rows ? A.rstd[row] : 0.f;
+#pragma unroll
+                for (int q = 0; q < 4; ++q)
+                    v[q] = to_f32(*(const T *)&b[i][q]);
+                if (NORM && row < A.rows)
+                    norm_values<4>(v, w, A.rstd[row]);
 #pragma unroll
                 for (int q = 0; q < 4; ++q) {
-                    v[q] = to_f32(*(const T *)&b[i][q]);
-                    if constexpr (NORM)
-                        v[q] = norm_value(v[q], w[q], r);
                     most = f8_larger(most, v[q]);
                     if constexpr (WIDE)
                         tile[at * 128 + place(q * 32 + lane)] = __float_as_uint(v[q]);

@@ -3,12 +3,16 @@
 // For X0 = U S V^T that is U f(f(..S)) V^T with f(s) = a s + b s^3 + c s^5.
 //
 // Each time f raises small singular values by a (3.4 times; five times over 480), and with them what a rounding put next to them.  With operands of 16
-// bits alone an update whose spectrum falls off by two decades is off by 1e-2 to 5e-2 (bf16) or 1e-3 to 6e-3 (fp16) of its size; rounded to bf16, which loses
-// 1.7e-3, it should not be.  So X, A and B = a + b A + c A^2 are kept as two fp16 each, hi + lo, under a power of two that keeps them
-// below fp16's largest (bounds of all three follow from the coefficients on the host), which is 22 bits, and a product is the sum of hi hi, hi lo and lo hi in one set of
-// fp32 sums on the tensor cores: as exact as 32-bit arithmetic at three times 16-bit's cost, not at the 20 times that 32-bit units take.
+// bits an update whose spectrum falls off by two decades is off by 1e-2 to 5e-2 (bf16) or 1e-3 to 6e-3 (fp16) of its size, where rounding the result
+// to bf16 loses 1.7e-3.  So:
+//  - X is kept as two fp16, hi + lo, under a power of two that keeps it below fp16's largest (bounds of X, A and C follow from the coefficients on the
+//    host), which is 22 bits; a X is added in fp32 and only C X, C = b A + c A^2, is a product: its share of a rounding's noise in the directions
+//    of small singular values is as small as A has them.
+//  - A and C are kept likewise, and a product is the sum of hi hi, hi lo and lo hi in one set of fp32 sums on the tensor cores: as exact as 32-bit
+//    arithmetic at three times 16-bit's cost, not at the 20 times that 32-bit units take.
+//  - The first steps' products are hi hi alone (single_steps()).
 //
-// Per step three launches: A (symmetric: tiles on and above the diagonal, stored twice), B (likewise, A added on the way out), B X.
+// Per step three launches: A (symmetric: tiles on and above the diagonal, stored twice), C (likewise, A added on the way out), C X (a X added).
 #include <cuda.h>
 #include <cuda_fp16.h>
 
@@ -17,7 +21,7 @@
 #include <cmath>
 
 #include "conef_common.cuh"
-#include "conef_elem.cuh"
+#include "conef_f8.cuh"
 #include "conef_mm.cuh"
 
 namespace conef {
@@ -34,17 +38,18 @@ __device__ __forceinline__ void split(float v, __half &hi, __half &lo)
 }
 
 // ------------------------------------------------------------------ the norm and X0
-constexpr int kNsParts = 64;   // partial sums per matrix at most
+constexpr int kNsParts = 512;   // partial sums per matrix at most
 struct NsIn {
     const void *x;
     int64_t rows, cols, ld, stride;   // as the caller has it
     double *parts;                    // kNsParts per matrix
     uint32_t n_parts;
 };
-// sums of squares of a matrix's rows, part by part, in 64 bits
-template <class T>
+// Sums of squares of a matrix's rows, part by part, in 64 bits (VEC: 16 bytes of a row at a time)
+template <class T, bool VEC>
 __global__ void __launch_bounds__(256) k_ns_squares(const __grid_constant__ NsIn A)
 {
+    constexpr int N = VEC ? Vec16<T>::N : 1;
     __shared__ double part[8];
     grid_release();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -52,10 +57,23 @@ __global__ void __launch_bounds__(256) k_ns_squares(const __grid_constant__ NsIn
     grid_wait();
     double sum = 0;
     for (int64_t row = (int64_t)blockIdx.x * 8 + warp; row < A.rows; row += (int64_t)A.n_parts * 8)
-#pragma unroll 8
-        for (int64_t c = lane; c < A.cols; c += 32) {
-            const double v = (double)to_f32(x[row * A.ld + c]);
-            sum = __fma_rn(v, v, sum);
+#pragma unroll 4
+        for (int64_t c = (int64_t)lane * N; c < A.cols; c += 32 * N) {
+            float v[N];
+            if constexpr (VEC) {
+                if (c + N <= A.cols) {
+                    Vec16<T>::unpack(*(const uint4 *)(x + row * A.ld + c), v);
+                } else {
+#pragma unroll
+                    for (int q = 0; q < N; ++q)
+                        v[q] = c + q < A.cols ? to_f32(x[row * A.ld + c + q]) : 0.f;
+                }
+            } else {
+                v[0] = to_f32(x[row * A.ld + c]);
+            }
+#pragma unroll
+            for (int q = 0; q < N; ++q)
+                sum = __fma_rn((double)v[q], (double)v[q], sum);
         }
 #pragma unroll
     for (int o = 16; o; o /= 2)
@@ -69,63 +87,89 @@ __global__ void __launch_bounds__(256) k_ns_squares(const __grid_constant__ NsIn
         A.parts[blockIdx.y * kNsParts + blockIdx.x] = sum;
     }
 }
-// X0 times a power of two, in tiles of 64 x 64 (FLIP: X is the transpose)
-template <class T, bool FLIP>
+// X0 times a power of two, in tiles of 64 x 64 (FLIP: X is the transpose).  VEC: a thread reads 16 bytes.
+template <class T, bool FLIP, bool VEC>
 __global__ void __launch_bounds__(256) k_ns_start(const __grid_constant__ NsIn A, const Split X, uint32_t tiles_c, double scale)
 {
     __shared__ float tile[FLIP ? 64 : 1][65];
+    __shared__ double part[8];
+    __shared__ float factor[2];
     grid_release();
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint32_t tr = blockIdx.x / tiles_c, tc = blockIdx.x - tr * tiles_c;
     const int64_t r0 = (int64_t)tr * 64, c0 = (int64_t)tc * 64, batch = blockIdx.y;
     const T *const x = (const T *)A.x + batch * A.stride;
     __half *const hi = X.hi + batch * X.rows * X.pitch, *const lo = X.lo + batch * X.rows * X.pitch;
     grid_wait();
-    double sum = 0;
-    for (uint32_t i = 0; i < A.n_parts; ++i)
-        sum += A.parts[batch * kNsParts + i];
-    const double by = sum == 0 ? 0 : scale / sqrt(sum);   // (a matrix of zeros stays one)
-    const int c = threadIdx.x & 63;
+    // a thread's elements: 16 of a row
+    const int r = threadIdx.x >> 2, c = (threadIdx.x & 3) * 16;
+    const bool there = r0 + r < A.rows;
+    const T *const from = x + (r0 + r) * A.ld + c0 + c;
+    float v[16];
+    if (VEC && there && c0 + c + 16 <= A.cols) {
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
-        const int r = i * 4 + (threadIdx.x >> 6);
-        if (r0 + r < A.rows && c0 + c < A.cols) {
-            const float v = (float)((double)to_f32(x[(r0 + r) * A.ld + c0 + c]) * by);
-            if constexpr (FLIP) {
-                tile[r][c] = v;
-            } else {
-                __half h, l;
-                split(v, h, l);
-                hi[(r0 + r) * X.pitch + c0 + c] = h;
-                lo[(r0 + r) * X.pitch + c0 + c] = l;
-            }
-        }
+        for (int q = 0; q < 16; q += Vec16<T>::N)
+            Vec16<T>::unpack(*(const uint4 *)(from + q), *(float(*)[Vec16<T>::N])(v + q));
+    } else {
+#pragma unroll
+        for (int q = 0; q < 16; ++q)
+            v[q] = there && c0 + c + q < A.cols ? to_f32(from[q]) : 0.f;
     }
+    double sum = 0;
+    for (uint32_t i = threadIdx.x; i < A.n_parts; i += 256)
+        sum += A.parts[batch * kNsParts + i];
+#pragma unroll
+    for (int o = 16; o; o /= 2)
+        sum += __shfl_xor_sync(0xffffffffu, sum, o);
+    if (lane == 0)
+        part[warp] = sum;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        for (int i = 1; i < 8; ++i)
+            sum += part[i];
+        const double by = sum == 0 ? 0 : scale / sqrt(sum);   // (a matrix of zeros stays one)
+        // (in two factors, the first a power of two: either alone, times elements of any size, stays in range)
+        const double first = sum == 0 || !(by > 0) ? 1.0 : ldexp(1.0, ilogb(by) / 2);
+        factor[0] = (float)first, factor[1] = (float)(by / first);
+    }
+    __syncthreads();
+    const float f0 = factor[0], f1 = factor[1];
+#pragma unroll
+    for (int q = 0; q < 16; ++q)
+        v[q] = __fmul_rn(__fmul_rn(v[q], f0), f1);
     if constexpr (FLIP) {
+#pragma unroll
+        for (int q = 0; q < 16; ++q)
+            tile[r][c + q] = v[q];
         __syncthreads();
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            const int r = i * 4 + (threadIdx.x >> 6);   // (a row of X)
-            if (c0 + r < A.cols && r0 + c < A.rows) {
-                __half h, l;
-                split(tile[c][r], h, l);
-                hi[(c0 + r) * X.pitch + r0 + c] = h;
-                lo[(c0 + r) * X.pitch + r0 + c] = l;
-            }
-        }
+        for (int q = 0; q < 16; ++q)
+            v[q] = tile[c + q][r];   // (a row of X)
+    }
+    const int64_t row = (FLIP ? c0 : r0) + r, col = (FLIP ? r0 : c0) + c;
+    if (row < X.rows && col < X.cols) {   // (rows are padded to 64 elements, which nothing reads)
+        __half h[16], l[16];
+#pragma unroll
+        for (int q = 0; q < 16; ++q)
+            split(v[q], h[q], l[q]);
+        store32_keep(hi + row * X.pitch + col, *(const uint32_t(*)[8])h);
+        store32_keep(lo + row * X.pitch + col, *(const uint32_t(*)[8])l);
     }
 }
 
 // ------------------------------------------------------------------ products
-// D = f_sum (L R) + f_add E + f_one 1 for stacks of matrices; R along k like L (A = X X^T, A A), or (CROSS) as it is multiplied, along D's columns (B X).
-// The kernel is that of conef_mm.cuh with another stage and another way out: 64 elements of k of L's and R's hi and lo; what leaves is split again, or rounded to the result.
+// D = f_sum (L R) + f_add E for stacks of matrices; R along k like L (A = X X^T, A A), or (CROSS) as it is multiplied, along D's columns (B X).
+// The kernel is that of conef_mm.cuh with another stage and another way out.  A stage has 64 elements of k of L's and R's hi and lo, or 128 of hi alone; what
+// leaves is split again, or rounded to the result.
 struct NsArgs {
-    Split out, add;              // (add.hi: NULL without E)
+    Split out, add;              // (add.hi: NULL without E; lo: NULL where hi alone is written or added)
     void *result;                // the last product's, instead of out
     int64_t result_ld, result_stride;
-    float f_sum, f_add, f_one;
+    float f_sum, f_add;
     uint32_t n, m, k;            // of D = n x m
     uint32_t k_steps, stages_k, per_matrix, tiles_m, n_tiles, stages;
-    uint32_t symmetric, flip, dtype, terms;
+    uint32_t symmetric, flip, dtype, single;
+    uint32_t wide;               // the result's rows (flip: columns in pairs) can be stored 16 (4) bytes at a time
     uint64_t limit, sums_limit;
     uint32_t loads[2];
 };
@@ -153,6 +197,47 @@ __device__ __forceinline__ NsTile ns_tile(const A &P, uint32_t tile)
         t.j = in / P.tiles_m, t.i = in - t.j * P.tiles_m;
     }
     return t;
+}
+
+// 32 columns of a lane's row, rounded to the result
+__device__ __forceinline__ void ns_result(const NsArgs &P, uint32_t batch, uint32_t row, uint32_t col, uint32_t have, int lane, bool there, const float (&f)[32])
+{
+    uint32_t w[16];   // two columns each
+#pragma unroll
+    for (int i = 0; i < 16; ++i)
+        w[i] = P.dtype == CONEF_BF16 ? Vec16<__nv_bfloat16>::pack2(f[2 * i], f[2 * i + 1]) : Vec16<__half>::pack2(f[2 * i], f[2 * i + 1]);
+    uint16_t *const out = (uint16_t *)P.result + (int64_t)batch * P.result_stride;
+    if (P.flip) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            // two rows of a column to a lane
+            const uint32_t other = __shfl_xor_sync(0xffffffffu, w[i], 1), c = 2 * i + (lane & 1);
+            const uint32_t both = lane & 1 ? __byte_perm(other, w[i], 0x7632) : __byte_perm(w[i], other, 0x5410);
+            const int64_t to = (int64_t)(col + c) * P.result_ld + (row & ~1u);
+            if (c < have) {
+                if (P.wide && (row | 1u) < P.n) {
+                    *(uint32_t *)(out + to) = both;
+                } else {
+                    if ((row & ~1u) < P.n)
+                        out[to] = (uint16_t)both;
+                    if ((row | 1u) < P.n)
+                        out[to + 1] = (uint16_t)(both >> 16);
+                }
+            }
+        }
+    } else if (there) {
+        uint16_t *const to = out + (int64_t)row * P.result_ld + col;
+        if (P.wide && have == 32) {
+#pragma unroll
+            for (int i = 0; i < 16; i += 4)
+                *(uint4 *)(to + 2 * i) = make_uint4(w[i], w[i + 1], w[i + 2], w[i + 3]);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 32; ++i)
+                if ((uint32_t)i < have)
+                    to[i] = (uint16_t)(w[i / 2] >> (16 * (i & 1)));
+        }
+    }
 }
 
 // A tile is 128 x 128, or of a pair of CTAs 256 x 256: with 128 x 128 a product reads as many bytes of shared memory per cycle as there are, so that the copies into it
@@ -195,45 +280,28 @@ __global__ void __launch_bounds__(kMmThreads, 1) k_ns_product(const __grid_const
     asm volatile("fence.proxy.async;" ::: "memory");   // (what the launch before stored, ordinary stores, is read by copies)
 
     auto load = [&](uint32_t s, uint32_t ks, const NsTile &t) {
-        const uint32_t st = tc::saddr(ring) + s * stage_bytes, k0 = ks * 64, i0 = t.i * BM + rank * 128, j0 = t.j * BN + rank * (BN / 2);
-        const uint32_t parts = P.terms == 1 ? 2 : 4;
-        if constexpr (PAIR) {
-            const uint32_t bar = tc::leaders(&S.full[s]);
-            if (rank == 0)
-                tc::bar_expect(&S.full[s], 2 * parts * kNsPart);
-            tc::tile_load3_pair(st, &maps.lh, k0, i0, t.batch, bar);
-            if (parts == 4)
-                tc::tile_load3_pair(st + kNsPart, &maps.ll, k0, i0, t.batch, bar);
-            if constexpr (CROSS) {
-                tc::tile_load3_pair(st + 2 * kNsPart, &maps.rh, j0, k0, t.batch, bar);
-                tc::tile_load3_pair(st + 2 * kNsPart + kNsPart / 2, &maps.rh, j0 + 64, k0, t.batch, bar);
-                if (parts == 4) {
-                    tc::tile_load3_pair(st + 3 * kNsPart, &maps.rl, j0, k0, t.batch, bar);
-                    tc::tile_load3_pair(st + 3 * kNsPart + kNsPart / 2, &maps.rl, j0 + 64, k0, t.batch, bar);
-                }
-            } else {
-                tc::tile_load3_pair(st + 2 * kNsPart, &maps.rh, k0, j0, t.batch, bar);
-                if (parts == 4)
-                    tc::tile_load3_pair(st + 3 * kNsPart, &maps.rl, k0, j0, t.batch, bar);
-            }
+        // parts of a stage: L's hi and lo, or hi and the next 64 of k; R's
+        const uint32_t st = tc::saddr(ring) + s * stage_bytes, k0 = ks * (P.single ? 128 : 64), k1 = P.single ? k0 + 64 : k0;
+        const uint32_t i0 = t.i * BM + rank * 128, j0 = t.j * BN + rank * (BN / 2);
+        const void *const l1 = P.single ? &maps.lh : &maps.ll, *const r1 = P.single ? &maps.rh : &maps.rl;
+        auto part = [&](uint32_t dst, const void *map, uint32_t x, uint32_t y) {
+            if constexpr (PAIR)
+                tc::tile_load3_pair(dst, map, x, y, t.batch, tc::leaders(&S.full[s]));
+            else
+                tc::tile_load3(dst, map, x, y, t.batch, &S.full[s]);
+        };
+        if (rank == 0)
+            tc::bar_expect(&S.full[s], (PAIR ? 2 : 1) * stage_bytes);
+        part(st, &maps.lh, k0, i0);
+        part(st + kNsPart, l1, k1, i0);
+        if constexpr (CROSS) {
+            part(st + 2 * kNsPart, &maps.rh, j0, k0);
+            part(st + 2 * kNsPart + kNsPart / 2, &maps.rh, j0 + 64, k0);
+            part(st + 3 * kNsPart, r1, j0, k1);
+            part(st + 3 * kNsPart + kNsPart / 2, r1, j0 + 64, k1);
         } else {
-            uint64_t *const bar = &S.full[s];
-            tc::bar_expect(bar, parts * kNsPart);
-            tc::tile_load3(st, &maps.lh, k0, i0, t.batch, bar);
-            if (parts == 4)
-                tc::tile_load3(st + kNsPart, &maps.ll, k0, i0, t.batch, bar);
-            if constexpr (CROSS) {
-                tc::tile_load3(st + 2 * kNsPart, &maps.rh, j0, k0, t.batch, bar);
-                tc::tile_load3(st + 2 * kNsPart + kNsPart / 2, &maps.rh, j0 + 64, k0, t.batch, bar);
-                if (parts == 4) {
-                    tc::tile_load3(st + 3 * kNsPart, &maps.rl, j0, k0, t.batch, bar);
-                    tc::tile_load3(st + 3 * kNsPart + kNsPart / 2, &maps.rl, j0 + 64, k0, t.batch, bar);
-                }
-            } else {
-                tc::tile_load3(st + 2 * kNsPart, &maps.rh, k0, j0, t.batch, bar);
-                if (parts == 4)
-                    tc::tile_load3(st + 3 * kNsPart, &maps.rl, k0, j0, t.batch, bar);
-            }
+            part(st + 2 * kNsPart, &maps.rh, k0, j0);
+            part(st + 3 * kNsPart, r1, k1, j0);
         }
     };
     uint32_t armed = 0;
@@ -271,16 +339,23 @@ __global__ void __launch_bounds__(kMmThreads, 1) k_ns_product(const __grid_const
                     break;
                 tc::fence_after();
                 if (tc::elect()) {
-                    const uint32_t steps = P.k_steps - ks * 4u, a = a0 + s * (stage_bytes / 16), b = b0 + s * (stage_bytes / 16);
+                    const uint32_t a = a0 + s * (stage_bytes / 16), b = b0 + s * (stage_bytes / 16);
+                    if (P.single) {
+                        const uint32_t steps = P.k_steps - ks * 8u;
 #pragma unroll
-                    for (uint32_t t = 0; t < 4; ++t)
-                        if (t < steps) {
-                            tc::f16_product<PAIR>(d, a + 2 * t, b + k_step * t, instruction, ks + t);
-                            if (P.terms > 1) {
+                        for (uint32_t t = 0; t < 8; ++t)
+                            if (t < steps)
+                                tc::f16_product<PAIR>(d, a + part16 * (t / 4) + 2 * (t % 4), b + part16 * (t / 4) + k_step * (t % 4), instruction, ks + t);
+                    } else {
+                        const uint32_t steps = P.k_steps - ks * 4u;
+#pragma unroll
+                        for (uint32_t t = 0; t < 4; ++t)
+                            if (t < steps) {
+                                tc::f16_product<PAIR>(d, a + 2 * t, b + k_step * t, instruction, ks + t);
                                 tc::f16_product<PAIR>(d, a + 2 * t, b + part16 + k_step * t, instruction, 1);
                                 tc::f16_product<PAIR>(d, a + part16 + 2 * t, b + k_step * t, instruction, 1);
                             }
-                        }
+                    }
                     tc::commit<PAIR>(&S.empty[s]);
                 }
                 if (++s == P.stages)
@@ -327,69 +402,65 @@ __global__ void __launch_bounds__(kMmThreads, 1) k_ns_product(const __grid_const
                     for (int i = 0; i < 32; ++i)
                         v[i] = 0x7FFFFFFFu;
                 }
-                if (row >= P.n || col >= P.m)
+                if (col >= P.m)   // (the same for all lanes)
                     continue;
+                const bool there = row < P.n;
+                const uint32_t have = min(32u, P.m - col);
                 float f[32];
 #pragma unroll
                 for (int i = 0; i < 32; ++i)
                     f[i] = __fmul_rn(__uint_as_float(v[i]), P.f_sum);
-                if (P.add.hi) {
-                    const int64_t at = ((int64_t)t.batch * P.add.rows + row) * P.add.pitch + col;
+                if (P.add.hi && there) {
+                    const int64_t at = ((int64_t)t.batch * P.add.rows + row) * P.add.pitch + col;   // (rows are padded to 64 elements)
 #pragma unroll
-                    for (int i = 0; i < 32; i += 8) {   // (rows are padded to 64 elements)
-                        const uint4 h = *(const uint4 *)(P.add.hi + at + i), l = *(const uint4 *)(P.add.lo + at + i);
-                        float a[8], b[8];
-                        Vec16<__half>::unpack(h, a), Vec16<__half>::unpack(l, b);
+                    for (int i = 0; i < 32; i += 16) {
+                        uint32_t h[8], l[8] = {};
+                        load32_keep(P.add.hi + at + i, h);
+                        if (P.add.lo)
+                            load32_keep(P.add.lo + at + i, l);
 #pragma unroll
-                        for (int q = 0; q < 8; ++q)
-                            f[i + q] = __fmaf_rn(__fadd_rn(a[q], b[q]), P.f_add, f[i + q]);
+                        for (int q = 0; q < 8; ++q) {
+                            const float2 a = __half22float2(*(const __half2 *)&h[q]), b = __half22float2(*(const __half2 *)&l[q]);
+                            f[i + 2 * q] = __fmaf_rn(__fadd_rn(a.x, b.x), P.f_add, f[i + 2 * q]);
+                            f[i + 2 * q + 1] = __fmaf_rn(__fadd_rn(a.y, b.y), P.f_add, f[i + 2 * q + 1]);
+                        }
                     }
                 }
-#pragma unroll
-                for (int i = 0; i < 32; ++i)
-                    if (row == col + i)
-                        f[i] = __fadd_rn(f[i], P.f_one);
-                const uint32_t have = min(32u, P.m - col);
                 if (P.result) {
-                    const int64_t base = (int64_t)t.batch * P.result_stride;
-                    if (P.flip) {
-#pragma unroll
-                        for (int i = 0; i < 32; ++i)
-                            if ((uint32_t)i < have) {
-                                const int64_t at = base + (int64_t)(col + i) * P.result_ld + row;
-                                if (P.dtype == CONEF_BF16)
-                                    ((__nv_bfloat16 *)P.result)[at] = __float2bfloat16_rn(f[i]);
-                                else
-                                    ((__half *)P.result)[at] = __float2half_rn(f[i]);
-                            }
-                    } else {
-                        const int64_t at = base + (int64_t)row * P.result_ld + col;
-#pragma unroll
-                        for (int i = 0; i < 32; ++i)
-                            if ((uint32_t)i < have) {
-                                if (P.dtype == CONEF_BF16)
-                                    ((__nv_bfloat16 *)P.result)[at + i] = __float2bfloat16_rn(f[i]);
-                                else
-                                    ((__half *)P.result)[at + i] = __float2half_rn(f[i]);
-                            }
-                    }
+                    ns_result(P, t.batch, row, col, have, lane, there, f);
                 } else {
                     const int64_t base = (int64_t)t.batch * P.out.rows * P.out.pitch, at = base + (int64_t)row * P.out.pitch + col;
+                    uint32_t w[32];   // hi, lo
 #pragma unroll
-                    for (int i = 0; i < 32; i += 8) {
-                        __half h[8], l[8];
+                    for (int i = 0; i < 32; ++i) {
+                        __half h, l;
+                        split(f[i], h, l);
+                        w[i] = (uint32_t)__half_as_ushort(h) | (uint32_t)__half_as_ushort(l) << 16;
+                    }
+                    if (there) {
 #pragma unroll
-                        for (int q = 0; q < 8; ++q)
-                            split(f[i + q], h[q], l[q]);
-                        *(uint4 *)(P.out.hi + at + i) = *(const uint4 *)h;   // (what lies past a row's end is not read)
-                        *(uint4 *)(P.out.lo + at + i) = *(const uint4 *)l;
-                        if (mirror) {
+                        for (int i = 0; i < 32; i += 16) {   // (what lies past a row's end is not read)
+                            uint32_t h[8], l[8];
 #pragma unroll
                             for (int q = 0; q < 8; ++q)
-                                if ((uint32_t)(i + q) < have) {
-                                    P.out.hi[base + (int64_t)(col + i + q) * P.out.pitch + row] = h[q];
-                                    P.out.lo[base + (int64_t)(col + i + q) * P.out.pitch + row] = l[q];
-                                }
+                                h[q] = __byte_perm(w[i + 2 * q], w[i + 2 * q + 1], 0x5410), l[q] = __byte_perm(w[i + 2 * q], w[i + 2 * q + 1], 0x7632);
+                            store32_keep(P.out.hi + at + i, h);
+                            if (P.out.lo)
+                                store32_keep(P.out.lo + at + i, l);
+                        }
+                    }
+                    if (mirror) {
+                        // two rows of a column to a lane: even lanes take even columns, odd ones odd columns, of both rows
+#pragma unroll
+                        for (int i = 0; i < 32; i += 2) {
+                            const uint32_t other = __shfl_xor_sync(0xffffffffu, lane & 1 ? w[i] : w[i + 1], 1);
+                            const uint32_t upper = lane & 1 ? other : w[i], lower = lane & 1 ? w[i + 1] : other, c = i + (lane & 1);
+                            if ((row & ~1u) < P.n && c < have) {
+                                const int64_t to = base + (int64_t)(col + c) * P.out.pitch + (row & ~1u);
+                                *(uint32_t *)(P.out.hi + to) = __byte_perm(upper, lower, 0x5410);
+                                if (P.out.lo)
+                                    *(uint32_t *)(P.out.lo + to) = __byte_perm(upper, lower, 0x7632);
+                            }
                         }
                     }
                 }
@@ -455,7 +526,7 @@ static cudaError_t ns_product(const Split &L, const Split &R, int64_t batch, NsA
     P.m = (uint32_t)(CROSS ? R.cols : R.rows);
     P.k = (uint32_t)L.cols;
     P.k_steps = (P.k + 15) / 16;
-    P.stages_k = (P.k + 63) / 64;
+    P.stages_k = P.single ? (P.k + 127) / 128 : (P.k + 63) / 64;
     P.tiles_m = (P.n + side - 1) / side;
     const int64_t per = P.symmetric ? (int64_t)P.tiles_m * (P.tiles_m + 1) / 2 : (int64_t)P.tiles_m * ((P.m + side - 1) / side);
     if (per * batch >= (1ll << 31))
@@ -480,13 +551,13 @@ static cudaError_t ns_product(const Split &L, const Split &R, int64_t batch, NsA
                 : launch(k_ns_product<false, CROSS>, dim3(std::min<uint32_t>(P.n_tiles, kPlanSMs)), kMmThreads, kNsSmem, s, maps, P);
 }
 
-// the largest |a + b t + c t^2| for 0 <= t <= top, and the largest |s (a + b s^2 + c s^4)| for 0 <= s <= top
-static double largest_factor(double a, double b, double c, double top)
+// the largest |b t + c t^2| for 0 <= t <= top, and the largest |s (a + b s^2 + c s^4)| for 0 <= s <= top
+static double largest_factor(double b, double c, double top)
 {
-    double most = std::max(std::fabs(a), std::fabs(a + b * top + c * top * top));
+    double most = std::fabs(b * top + c * top * top);
     const double t = c != 0 ? -b / (2 * c) : -1;
     if (t > 0 && t < top)
-        most = std::max(most, std::fabs(a + b * t + c * t * t));
+        most = std::max(most, std::fabs(b * t + c * t * t));
     return most;
 }
 static double largest_value(double a, double b, double c, double top)
@@ -508,6 +579,18 @@ static double largest_value(double a, double b, double c, double top)
 }
 // a power of two that brings `bound` below 2^15, half of fp16's range
 static double fp16_scale(double bound) { return std::ldexp(1.0, 14 - std::ilogb(std::max(bound, 1e-30))); }
+
+// Steps, from the first on, whose products are of fp16's 11 bits alone.  Singular values are small then (at most 1 in all, in squares), so C, and what a rounding adds to C X, is
+// small, and falls off with the singular value as A does; it counts less the more elements it is averaged over.  Errors of the result relative to its size, the largest of
+// spectra that are flat, fall off as 1/i or exponentially, and of 1 to 128 directions with and without noise, 128 to 512 rows and one to four times the columns: one
+// step 3.7e-4 (256 rows; 512: 0.9e-4), two 3.0e-4 (2.1e-4), three 6.2e-4 (4.7e-4 and, flat with more columns, 7.6e-4) where the third step's A A is not, four
+// 1.5e-3.  Rounding to bf16 loses 1.7e-3, to fp16 2.1e-4: three steps for bf16 from 256 rows on, one for fp16 from 512.  For coefficients beyond 5 none.
+static int single_steps(int64_t n, int out_dtype, double a, double b, double c)
+{
+    if (std::max({std::fabs(a), std::fabs(b), std::fabs(c)}) > 5)
+        return 0;
+    return out_dtype == CONEF_BF16 ? (n >= 256 ? 3 : 0) : (n >= 512 ? 1 : 0);
+}
 
 struct NsSizes {
     int64_t n, m, pitch_x, pitch_a;   // rows <= columns
@@ -535,7 +618,7 @@ int conef_orthogonalise_bytes(int64_t batch, int64_t rows, int64_t cols, size_t 
     if (rows >= (1ll << 31) || cols >= (1ll << 31) || batch >= (1ll << 16))
         return CONEF_ERR_UNSUPPORTED;
     const NsSizes z = ns_sizes(rows, cols);
-    // X twice, A and B, hi and lo each, and the norms' parts
+    // X twice, A and C, hi and lo each, and the norms' parts
     *bytes = batch && rows && cols ? ((size_t)batch * z.n * (2 * z.pitch_x + 2 * z.pitch_a) * 2 * sizeof(__half) + (size_t)batch * kNsParts * sizeof(double)) : 0;
     return CONEF_OK;
 }
@@ -552,7 +635,7 @@ int conef_orthogonalise(const void *x, int dtype, int64_t batch, int64_t rows, i
         return CONEF_ERR_INVALID_ARG;
     if (batch > 1 && rows && cols && (stride < (rows - 1) * ld + cols || out_stride < (rows - 1) * out_ld + cols))
         return CONEF_ERR_INVALID_ARG;
-    // bounds of X, A and B before each step: a power of two each that keeps them within fp16
+    // bounds of X before each step: a power of two each that keeps them within fp16
     double top[33];
     const double a = coefficients[0], b = coefficients[1], c = coefficients[2];
     top[0] = 1.0;
@@ -578,7 +661,7 @@ int conef_orthogonalise(const void *x, int dtype, int64_t batch, int64_t rows, i
         at += 2 * batch * z.n * pitch;
         return m;
     };
-    Split X = take(z.m, z.pitch_x), Y = take(z.m, z.pitch_x), A = take(z.n, z.pitch_a), B = take(z.n, z.pitch_a);
+    Split X = take(z.m, z.pitch_x), Y = take(z.m, z.pitch_x), A = take(z.n, z.pitch_a), C = take(z.n, z.pitch_a);
     NsIn in = {x, rows, cols, ld, stride, (double *)at, (uint32_t)std::min<int64_t>(kNsParts, (rows + 7) / 8)};
     double sx = fp16_scale(top[0]);
     cudaError_t e = cudaErrorInvalidValue;
@@ -587,46 +670,56 @@ int conef_orthogonalise(const void *x, int dtype, int64_t batch, int64_t rows, i
         return CONEF_ERR_UNSUPPORTED;
     with_elem(dtype, [&](auto t) {
         using T = decltype(t);
-        e = launch(k_ns_squares<T>, dim3(in.n_parts, (unsigned)batch), 256, 0, s, in);
+        const bool vec = rows_on<T>(x, rows, ld, 16) && (batch == 1 || stride * (int64_t)sizeof(T) % 16 == 0);
+        e = launch(vec ? k_ns_squares<T, true> : k_ns_squares<T, false>, dim3(in.n_parts, (unsigned)batch), 256, 0, s, in);
         if (e == cudaSuccess)
-            e = launch(z.flip ? k_ns_start<T, true> : k_ns_start<T, false>, dim3((unsigned)tiles, (unsigned)batch), 256, 0, s, in, X, (uint32_t)tiles_c, sx);
+            e = launch(z.flip ? (vec ? k_ns_start<T, true, true> : k_ns_start<T, true, false>) : (vec ? k_ns_start<T, false, true> : k_ns_start<T, false, false>),
+                       dim3((unsigned)tiles, (unsigned)batch), 256, 0, s, in, X, (uint32_t)tiles_c, sx);
         return 0;
     });
     // tiles of pairs where there are enough of them
     const int64_t sides = (z.n + 255) / 256;
     const bool pair_a = sides * (sides + 1) / 2 * batch >= kPlanSMs / 4, pair_x = sides * ((z.m + 255) / 256) * batch >= kPlanSMs / 4;
+    const int single = single_steps(z.n, out_dtype, a, b, c);
     for (int t = 0; t < steps && e == cudaSuccess; ++t) {
-        const double sa = fp16_scale(top[t] * top[t]), sb = fp16_scale(largest_factor(a, b, c, top[t] * top[t])), sy = fp16_scale(top[t + 1]);
+        const double sa = fp16_scale(top[t] * top[t]), sc = fp16_scale(largest_factor(b, c, top[t] * top[t])), sy = fp16_scale(top[t + 1]);
+        const bool one = t < single, one_c = one && t < 2;
         NsArgs P = {};
-        P.terms = 3;
         P.symmetric = 1;
+        P.single = one;
         P.out = A;
+        if (one_c)
+            P.out.lo = nullptr;
         P.f_sum = (float)(sa / (sx * sx));
         e = ns_product<false>(X, X, batch, P, pair_a, s);
         if (e != cudaSuccess)
             break;
-        P.out = B;
-        P.add = A;
-        P.f_sum = (float)(c * sb / (sa * sa));
-        P.f_add = (float)(b * sb / sa);
-        P.f_one = (float)(a * sb);
+        P.single = one_c;
+        P.add = P.out;
+        P.out = C;
+        if (one)
+            P.out.lo = nullptr;
+        P.f_sum = (float)(c * sc / (sa * sa));
+        P.f_add = (float)(b * sc / sa);
         e = ns_product<false>(A, A, batch, P, pair_a, s);
         if (e != cudaSuccess)
             break;
         NsArgs U = {};
-        U.terms = 3;
+        U.single = one;
+        U.add = X;
+        U.out = Y;
         if (t + 1 == steps) {
             U.result = out;
             U.result_ld = rows > 1 ? out_ld : cols;
             U.result_stride = batch > 1 ? out_stride : 0;
             U.flip = z.flip;
             U.dtype = (uint32_t)out_dtype;
-            U.f_sum = (float)(scale / (sb * sx));
-        } else {
-            U.out = Y;
-            U.f_sum = (float)(sy / (sb * sx));
+            U.wide = (((uintptr_t)out | (uint64_t)(U.result_ld | U.result_stride) * 2) & (z.flip ? 3 : 15)) == 0;
         }
-        e = ns_product<true>(B, X, batch, U, pair_x, s);
+        const double to = t + 1 == steps ? scale : sy;
+        U.f_sum = (float)(to / (sc * sx));
+        U.f_add = (float)(a * to / sx);
+        e = ns_product<true>(C, X, batch, U, pair_x, s);
         std::swap(X, Y);
         sx = sy;
     }
