@@ -129,6 +129,39 @@ __device__ __forceinline__ void store32(void *p, const uint32_t (&w)[8])
                  : "memory");
 }
 
+// the largest of the sizes of three, NaN where one is
+__device__ __forceinline__ float absmax3(float a, float b, float c)
+{
+    float r;
+    asm("max.NaN.abs.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+    return r;
+}
+__device__ __forceinline__ float absmax2(float a, float b) { return absmax3(a, b, b); }
+// ... of n elements, a multiple of 8, in four chains
+template <int N>
+__device__ __forceinline__ float absmax(const float *v)
+{
+    float m[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        m[i] = absmax2(v[2 * i], v[2 * i + 1]);
+#pragma unroll
+    for (int i = 8; i < N; i += 2)
+        m[i / 2 % 4] = absmax3(m[i / 2 % 4], v[i], v[i + 1]);
+    return absmax2(absmax3(m[0], m[1], m[2]), m[3]);
+}
+// products of pairs, two to an instruction
+__device__ __forceinline__ uint64_t pair_of(float a, float b)
+{
+    uint64_t p;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(p) : "f"(a), "f"(b));
+    return p;
+}
+__device__ __forceinline__ void mul2(float &a, float &b, uint64_t by)
+{
+    asm("{\n\t.reg .b64 p;\n\tmov.b64 p, {%0, %1};\n\tmul.rn.f32x2 p, p, %2;\n\tmov.b64 {%0, %1}, p;\n\t}" : "+f"(a), "+f"(b) : "l"(by));
+}
+
 // the code of a call's launches; what CUDA says is kept for conef_error_string (conef_api.cu)
 int launched(cudaError_t e, const char *what);
 

@@ -99,9 +99,7 @@ __global__ void __launch_bounds__(kF8Threads) k_f8_tiles(const T *x, const __gri
             for (int i = 0; i < 4; ++i) {
                 float v[16];
                 p[i].unpack(v);
-#pragma unroll
-                for (int q = 0; q < 16; ++q)
-                    all = f8_larger(all, v[q]);
+                all = max(all, __float_as_uint(absmax<16>(v)));
             }
             all = __reduce_max_sync(0xffffffffu, all);
             if (lane == 0)
@@ -140,9 +138,7 @@ __global__ void __launch_bounds__(kF8Threads) k_f8_tiles(const T *x, const __gri
             if (A.out.codes) {
                 uint32_t most = all;
                 if (!A.square) {
-#pragma unroll
-                    for (int q = 0; q < 16; ++q)
-                        most = f8_larger(most, v[q]);
+                    most = __float_as_uint(absmax<16>(v));
 #pragma unroll
                     for (int o = 1; o < 8; o *= 2)
                         most = max(most, __shfl_xor_sync(0xffffffffu, most, o));
@@ -196,7 +192,6 @@ __global__ void __launch_bounds__(kF8Threads) k_f8_tiles(const T *x, const __gri
                 const int at = half * 32 + i * 8 + warp;
                 const int64_t row = r0 + at;
                 float v[4];
-                uint32_t most = 0;
 #pragma unroll
                 for (int q = 0; q < 4; ++q)
                     v[q] = to_f32(*(const T *)&b[i][q]);
@@ -204,13 +199,12 @@ __global__ void __launch_bounds__(kF8Threads) k_f8_tiles(const T *x, const __gri
                     norm_values<4>(v, w, A.rstd[row]);
 #pragma unroll
                 for (int q = 0; q < 4; ++q) {
-                    most = f8_larger(most, v[q]);
                     if constexpr (WIDE)
                         tile[at * 128 + place(q * 32 + lane)] = __float_as_uint(v[q]);
                     else
                         ((uint16_t *)tile)[at * 128 + q * 32 + lane] = b[i][q];
                 }
-                most = __reduce_max_sync(0xffffffffu, most);
+                const uint32_t most = __reduce_max_sync(0xffffffffu, __float_as_uint(absmax4(v)));
                 if (A.square)
                     all = max(all, most);
                 else if (A.out.codes)
@@ -245,7 +239,6 @@ __global__ void __launch_bounds__(kF8Threads) k_f8_tiles(const T *x, const __gri
     const int pair = threadIdx.x & 63, quarter = threadIdx.x >> 6;
     const int64_t c = c0 + 2 * pair;
     float v[2][32];
-    uint32_t most[2] = {0, 0};
 #pragma unroll
     for (int i = 0; i < 32; ++i) {
         if constexpr (WIDE) {
@@ -256,8 +249,8 @@ __global__ void __launch_bounds__(kF8Threads) k_f8_tiles(const T *x, const __gri
             const uint16_t lo = (uint16_t)word, hi = (uint16_t)(word >> 16);
             v[0][i] = to_f32(*(const T *)&lo), v[1][i] = to_f32(*(const T *)&hi);
         }
-        most[0] = f8_larger(most[0], v[0][i]), most[1] = f8_larger(most[1], v[1][i]);
     }
+    uint32_t most[2] = {__float_as_uint(absmax<32>(v[0])), __float_as_uint(absmax<32>(v[1]))};
     if (!A.square) {
         *(uint2 *)&col_most[quarter][2 * pair] = make_uint2(most[0], most[1]);
         __syncthreads();

@@ -21,6 +21,7 @@ __host__ __device__ inline int64_t f8_scale_at(int64_t row, int64_t block, int64
     return ((row >> 7) * tiles + (block >> 2)) * 512 + (row & 31) * 16 + ((row >> 5) & 3) * 4 + (block & 3);
 }
 
+__device__ __forceinline__ float absmax4(const float *v) { return absmax3(absmax2(v[0], v[1]), v[2], v[3]); }
 // scale byte of a block from the largest |x| in it as bits (as integers NaN > infinity > every finite value)
 __device__ __forceinline__ uint32_t f8_scale(uint32_t abs_bits, int kind)
 {
@@ -52,12 +53,11 @@ template <int N>
 __device__ __forceinline__ void f8_encode(const float *v, uint32_t byte, int kind, uint32_t *code)
 {
     const float inv = f8_inv(byte);
+    const uint64_t both = pair_of(inv, inv);
 #pragma unroll
     for (int i = 0; i < N / 4; ++i) {
-        float s[4];
-#pragma unroll
-        for (int q = 0; q < 4; ++q)
-            s[q] = __fmul_rn(v[4 * i + q], inv);
+        float s[4] = {v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]};
+        mul2(s[0], s[1], both), mul2(s[2], s[3], both);
         const uint32_t c = f8_codes4(s, kind);
         code[i] = byte == kF8Nan ? 0u : c;
     }
@@ -73,14 +73,11 @@ __device__ __forceinline__ void f8_values4(uint32_t w, int kind, float *v)
     const float2 a = __half22float2(*(const __half2 *)&lo), b = __half22float2(*(const __half2 *)&hi);
     v[0] = a.x, v[1] = a.y, v[2] = b.x, v[3] = b.y;
 }
-// the larger size of two, as bits: NaN above all
-__device__ __forceinline__ uint32_t f8_larger(uint32_t most, float v) { return max(most, __float_as_uint(v) & 0x7FFFFFFFu); }
-
 // ------------------------------------------------------------------ rows by warps
-// A warp takes 512 elements of a row at a time, four blocks, 16 elements to a lane.  Where rows are aligned (VEC) they are consecutive, a block with eight
-// lanes; else a lane has every 32nd of a block, four of each of the four, so that single elements come by whole lines.
-template <class T, bool VEC>
-__device__ __forceinline__ uint32_t lane_col(uint32_t c0, int lane, int q) { return VEC ? c0 + lane * 16 + q : c0 + (q >> 2) * 128 + (q & 3) * 32 + lane; }
+// A warp takes 32 N elements of a row at a time, N (8 or 16) to a lane: two or four blocks.  Where rows are aligned (VEC) a lane's are consecutive; else it has every
+// 32nd of a block, four of each block, so that single elements come by whole lines.
+template <bool VEC, int N>
+__device__ __forceinline__ uint32_t lane_col(uint32_t c0, int lane, int q) { return VEC ? c0 + lane * N + q : c0 + (q >> 2) * 128 + (q & 3) * 32 + lane; }
 
 // 32 bytes that other kernels may read again
 __device__ __forceinline__ void load32_keep(const void *p, uint32_t (&w)[8])
@@ -96,20 +93,20 @@ __device__ __forceinline__ void store32_keep(void *p, const uint32_t (&w)[8])
                  "r"(w[7])
                  : "memory");
 }
-// 16 elements of a lane, as they lie in memory (VEC: in sizeof(T) * 4 words) or one to a word; zero behind the row's end
-template <class T, bool VEC>
+// N elements of a lane, as they lie in memory (VEC: in sizeof(T) N / 4 words) or one to a word; zero behind the row's end
+template <class T, bool VEC, int N = 16>
 struct Piece {
-    static constexpr int WORDS = VEC ? (int)sizeof(T) * 4 : 16;
+    static constexpr int WORDS = VEC ? (int)sizeof(T) * N / 4 : N;
     uint32_t w[WORDS];
 
     __device__ __forceinline__ void load(const T *row, uint32_t c0, uint32_t cols, int lane, bool aligned32)
     {
         if constexpr (VEC) {
-            const uint32_t c = c0 + lane * 16;
-            if (c + 16 <= cols) {
-                if (aligned32) {
+            const uint32_t c = c0 + lane * N;
+            if (c + N <= cols) {
+                if (WORDS >= 8 && aligned32) {
 #pragma unroll
-                    for (int i = 0; i < WORDS; i += 8)
+                    for (int i = 0; i + 8 <= WORDS; i += 8)
                         load32_keep((const uint32_t *)(row + c) + i, *(uint32_t(*)[8])(w + i));
                 } else {
 #pragma unroll
@@ -132,8 +129,8 @@ struct Piece {
         } else {
             using Bits = std::conditional_t<sizeof(T) == 2, uint16_t, uint32_t>;
 #pragma unroll
-            for (int q = 0; q < 16; ++q) {
-                const uint32_t c = lane_col<T, VEC>(c0, lane, q);
+            for (int q = 0; q < N; ++q) {
+                const uint32_t c = lane_col<VEC, N>(c0, lane, q);
                 w[q] = c < cols ? (uint32_t)((const Bits *)row)[c] : 0u;
             }
         }
@@ -146,7 +143,7 @@ struct Piece {
                 Vec16<T>::unpack(make_uint4(w[i], w[i + 1], w[i + 2], w[i + 3]), *(float(*)[Vec16<T>::N])(v + i / 4 * Vec16<T>::N));
         } else {
 #pragma unroll
-            for (int q = 0; q < 16; ++q) {
+            for (int q = 0; q < N; ++q) {
                 if constexpr (sizeof(T) == 2) {
                     const uint16_t h = (uint16_t)w[q];
                     v[q] = to_f32(*(const T *)&h);
@@ -166,7 +163,7 @@ struct Piece {
             }
         } else {
 #pragma unroll
-            for (int q = 0; q < 16; ++q) {
+            for (int q = 0; q < N; ++q) {
                 const T t = from_f32<T>(v[q]);
                 if constexpr (sizeof(T) == 2)
                     w[q] = *(const uint16_t *)&t;
@@ -179,11 +176,11 @@ struct Piece {
     {
         using Bits = std::conditional_t<sizeof(T) == 2, uint16_t, uint32_t>;
         if constexpr (VEC) {
-            const uint32_t c = c0 + lane * 16;
-            if (c + 16 <= cols) {
-                if (aligned32) {
+            const uint32_t c = c0 + lane * N;
+            if (c + N <= cols) {
+                if (WORDS >= 8 && aligned32) {
 #pragma unroll
-                    for (int i = 0; i < WORDS; i += 8)
+                    for (int i = 0; i + 8 <= WORDS; i += 8)
                         store32_keep((uint32_t *)(row + c) + i, *(const uint32_t(*)[8])(w + i));
                 } else {
 #pragma unroll
@@ -193,14 +190,14 @@ struct Piece {
             } else {
                 Bits *p = (Bits *)(row + c);
 #pragma unroll
-                for (int q = 0; q < 16; ++q)
+                for (int q = 0; q < N; ++q)
                     if (c + q < cols)
                         p[q] = sizeof(T) == 2 ? (Bits)(w[q / 2] >> (16 * (q & 1))) : (Bits)w[q % WORDS];
             }
         } else {
 #pragma unroll
-            for (int q = 0; q < 16; ++q) {
-                const uint32_t c = lane_col<T, VEC>(c0, lane, q);
+            for (int q = 0; q < N; ++q) {
+                const uint32_t c = lane_col<VEC, N>(c0, lane, q);
                 if (c < cols)
                     ((Bits *)row)[c] = (Bits)w[q];
             }
@@ -208,35 +205,33 @@ struct Piece {
     }
 };
 
-// The codes and scales of a warp's 512 elements from c0 (a multiple of 512) on.  scales_tile: where the row's four bytes of that tile lie.  Blocks that do not exist get the
+// The codes and scales of a warp's 32 N elements from c0 (a multiple of them) on; scales: where the row's byte of the first block lies.  Blocks that do not exist get the
 // byte zero; `there`: the row does.
-template <class T, bool VEC>
-__device__ __forceinline__ void f8_store_row(const float *v, uint32_t c0, uint32_t blocks, int lane, int kind, bool there, uint8_t *codes_row, uint8_t *scales_tile)
+template <class T, bool VEC, int N = 16>
+__device__ __forceinline__ void f8_store_row(const float *v, uint32_t c0, uint32_t blocks, int lane, int kind, bool there, uint8_t *codes_row, uint8_t *scales)
 {
     if constexpr (VEC) {
-        uint32_t most = 0;
+        constexpr int LANES = 128 / N;   // of a block
+        uint32_t most = __float_as_uint(absmax<N>(v));
 #pragma unroll
-        for (int q = 0; q < 16; ++q)
-            most = f8_larger(most, v[q]);
-#pragma unroll
-        for (int o = 1; o < 8; o *= 2)
+        for (int o = 1; o < LANES; o *= 2)
             most = max(most, __shfl_xor_sync(0xffffffffu, most, o));
-        const uint32_t byte = f8_scale(most, kind), block = c0 / 128 + (lane >> 3);
-        uint32_t code[4];
-        f8_encode<16>(v, byte, kind, code);
-        if (there && block < blocks)
-            *(uint4 *)(codes_row + c0 + lane * 16) = make_uint4(code[0], code[1], code[2], code[3]);
-        if ((lane & 7) == 0)
-            scales_tile[lane >> 3] = (uint8_t)(there && block < blocks ? byte : 0u);
+        const uint32_t byte = f8_scale(most, kind), block = c0 / 128 + lane / LANES;
+        uint32_t code[N / 4];
+        f8_encode<N>(v, byte, kind, code);
+        if (there && block < blocks) {
+            if constexpr (N == 16)
+                *(uint4 *)(codes_row + c0 + lane * N) = make_uint4(code[0], code[1], code[2], code[3]);
+            else
+                *(uint2 *)(codes_row + c0 + lane * N) = make_uint2(code[0], code[1]);
+        }
+        if (lane % LANES == 0)
+            scales[lane / LANES] = (uint8_t)(there && block < blocks ? byte : 0u);
     } else {
         uint32_t bytes = 0;
 #pragma unroll
-        for (int b = 0; b < 4; ++b) {
-            uint32_t most = 0;
-#pragma unroll
-            for (int q = 0; q < 4; ++q)
-                most = f8_larger(most, v[4 * b + q]);
-            most = __reduce_max_sync(0xffffffffu, most);
+        for (int b = 0; b < N / 4; ++b) {
+            const uint32_t most = __reduce_max_sync(0xffffffffu, __float_as_uint(absmax4(v + 4 * b)));
             const uint32_t byte = f8_scale(most, kind);
             uint32_t code;
             f8_encode<4>(v + 4 * b, byte, kind, &code);
@@ -247,8 +242,8 @@ __device__ __forceinline__ void f8_store_row(const float *v, uint32_t c0, uint32
                     codes_row[c0 + b * 128 + q * 32 + lane] = (uint8_t)(code >> (8 * q));
             }
         }
-        if (lane == 0)
-            *(uint32_t *)scales_tile = bytes;
+        if (lane < N / 4)
+            scales[lane] = (uint8_t)(bytes >> (8 * lane));
     }
 }
 
@@ -274,15 +269,18 @@ __device__ __forceinline__ float norm_value(float h, float w, float r)
 template <int N>
 __device__ __forceinline__ void norm_values(float *v, const float *w, float r)
 {
+    static_assert(N % 4 == 0, "");
     float y[N];
-    uint32_t near = 0xFFFFFFFFu;
+    uint32_t near = 0xFFFFFFFFu;   // (shifted, so that what is above the 19 bits falls off)
+    const uint64_t root = pair_of(r, r);
 #pragma unroll
-    for (int q = 0; q < N; ++q) {
-        y[q] = __fmul_rn(__fmul_rn(v[q], r), w[q]);
-        const uint32_t b = __float_as_uint(y[q]);
-        near = min(near, b == 0u ? 0xFFFFFFFFu : (b + 4u) & 0x7FFFFu);   // (zeros, as behind a row's end, are exact)
+    for (int q = 0; q < N; q += 2) {
+        y[q] = v[q], y[q + 1] = v[q + 1];
+        mul2(y[q], y[q + 1], root);
+        mul2(y[q], y[q + 1], pair_of(w[q], w[q + 1]));
+        near = __vimin3_u32(near, __float_as_uint(y[q]) * 8192u + 4u * 8192u, __float_as_uint(y[q + 1]) * 8192u + 4u * 8192u);
     }
-    if (near <= 8u) {
+    if (near <= 8u * 8192u) {
 #pragma unroll
         for (int q = 0; q < N; ++q)
             y[q] = v[q] == 0.f ? y[q] : norm_value(v[q], w[q], r);

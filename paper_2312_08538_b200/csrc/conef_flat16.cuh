@@ -438,8 +438,8 @@ __global__ void __launch_bounds__(kF16Threads, f16_ctas(ICO)) k_flat16(const __g
         for (int x = 0; x < NS; ++x) {
             float amax = 0.f;
             if constexpr (MX4) {
-                amax = mx4_absmax<16>(r);
-                amax = mx4_absmax2(amax, __shfl_xor_sync(0xffffffffu, amax, 1));
+                amax = absmax<16>(r);
+                amax = absmax2(amax, __shfl_xor_sync(0xffffffffu, amax, 1));
             } else {
 #pragma unroll
                 for (int q = 0; q < 16; ++q)

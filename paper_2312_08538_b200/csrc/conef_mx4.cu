@@ -75,10 +75,10 @@ __global__ void __launch_bounds__(kQThreads) k_mx4_rows(const T *x, const __grid
         for (int g = 0; g < E / 4; ++g)
             drop4(v + 4 * g, mix64(z + kDrawStep * g), A.drop);
     }
-    float most = mx4_absmax<E>(v);
+    float most = absmax<E>(v);
 #pragma unroll
     for (int o = 1; o < LANES; o *= 2)
-        most = mx4_absmax2(most, __shfl_xor_sync(0xffffffffu, most, o));
+        most = absmax2(most, __shfl_xor_sync(0xffffffffu, most, o));
     const uint32_t byte = mx4_scale(__float_as_uint(most));
     const float inv = mx4_inv(byte);
 #pragma unroll
@@ -155,7 +155,7 @@ __global__ void __launch_bounds__(kBothWarps * 32, STOCH ? 4 : 5) k_mx4_both(con
     float v[32];
     // scales 32 elements; the scale
     auto scaled = [&](float (&v)[32]) {
-        float most = mx4_absmax<32>(v);
+        float most = absmax<32>(v);
         if (SHORT && DROP)   // (the largest product is that of the largest element)
             most = __fmul_rn(most, A.drop.scale);
         const uint32_t byte = mx4_scale(__float_as_uint(most));

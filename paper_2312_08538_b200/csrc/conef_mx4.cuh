@@ -7,6 +7,7 @@
 #include <cuda_fp16.h>
 
 #include "conef_draw.cuh"
+#include "conef_elem.cuh"
 
 namespace conef {
 
@@ -74,27 +75,6 @@ __device__ __forceinline__ uint32_t mx4_stochastic8(const float *v, uint64_t w0,
     for (int i = 0; i < 4; ++i)
         noise[2 * i] = mx4_noise_lo(w[i]), noise[2 * i + 1] = mx4_noise_hi(w[i]);
     return mx4_stochastic8(v, noise);
-}
-// the largest of the sizes of three, NaN where one is
-__device__ __forceinline__ float mx4_absmax3(float a, float b, float c)
-{
-    float r;
-    asm("max.NaN.abs.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
-    return r;
-}
-__device__ __forceinline__ float mx4_absmax2(float a, float b) { return mx4_absmax3(a, b, b); }
-// ... of n elements, a multiple of 8, in four chains
-template <int N>
-__device__ __forceinline__ float mx4_absmax(const float *v)
-{
-    float m[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-        m[i] = mx4_absmax2(v[2 * i], v[2 * i + 1]);
-#pragma unroll
-    for (int i = 8; i < N; i += 2)
-        m[i / 2 % 4] = mx4_absmax3(m[i / 2 % 4], v[i], v[i + 1]);
-    return mx4_absmax2(mx4_absmax3(m[0], m[1], m[2]), m[3]);
 }
 // values of two codes (low four bits first), still to be scaled
 __device__ __forceinline__ float2 mx4_values2(uint32_t byte)

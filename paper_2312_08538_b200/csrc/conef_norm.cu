@@ -11,105 +11,116 @@ struct NormArgs {
     uint8_t *codes, *scales;
     float *rstd;
     int64_t rows, cols, x_ld, add_ld, h_ld, y_ld;
-    double eps;
+    double eps, share;   // share: of a column in the mean
     int kind;
-    uint32_t groups;
     bool w32, aligned32, aligned_w;
 };
 
-// the weights of a lane's 16 columns (aligned: 16 of them are)
+// ------------------------------------------------------------------ rows by blocks
+// A lane has 8 elements of a row and a block all of it, 256 elements to a warp (rows of up to 256: a warp has all of it); blocks stay and take rows a grid apart.  So
+// little to a lane leaves room for 32 warps on an SM, which hide what is done once per row: sums across lanes and warps, a barrier, the root.  The rows ahead
+// are copied into shared memory meanwhile, DEPTH of them, each lane what it will read: 6.5 TB/s are 44 KB on their way to each SM at a latency of a microsecond.
+// Elements of 16 bits on odd addresses, which no copy takes, are read when they are wanted.
+// 8192 x 1600 in bf16 with a residual, and the gradient: 16 elements to a lane 37 and 39 us, 32 elements 35 and 51, 8 with one row ahead in registers 27 and 32.
+constexpr int kNormPer = 8, kNormWarp = 32 * kNormPer;   // elements of a lane and of a warp
+constexpr int64_t kNormWidest = 32 * kNormWarp;
+template <class T, bool VEC>
+using NormPiece = Piece<T, VEC, kNormPer>;
+
+template <class T, bool VEC, int ARRAYS>
+struct Ahead {
+    static constexpr bool ON = VEC || sizeof(T) == 4;
+    static constexpr int CHUNK = VEC ? 16 : 4, PER = CHUNK / (int)sizeof(T), CHUNKS = kNormPer / PER;   // bytes and elements of a copy; copies per array
+    static constexpr int STAGE = ARRAYS * kNormWarp * (int)sizeof(T), FIT = 6144 / STAGE, DEPTH = FIT < 4 ? FIT : 4;   // (6 KB to each of 32 warps)
+    static constexpr int BYTES = ON ? STAGE * DEPTH : 0;                                                               // of a warp
+
+    uint8_t *at;   // the lane's place
+    uint32_t c0, cols;
+    int lane, now, next;
+
+    __device__ __forceinline__ Ahead(uint8_t *smem, int warp, int lane, uint32_t c0, uint32_t cols)
+        : at(smem + warp * BYTES + lane * CHUNK), c0(c0), cols(cols), lane(lane), now(0), next(0)
+    {
+    }
+    __device__ __forceinline__ uint32_t first(int i) const { return VEC ? c0 + lane * kNormPer + i * PER : lane_col<VEC, kNormPer>(c0, lane, i); }
+    // asks for a row's elements; then close(), once for all arrays (also where there is no row any more)
+    __device__ __forceinline__ void ask(int array, const T *row) const
+    {
+        if constexpr (ON) {
+#pragma unroll
+            for (int i = 0; i < CHUNKS; ++i) {
+                const uint32_t c = first(i), to = (uint32_t)__cvta_generic_to_shared(at + next * STAGE + (array * CHUNKS + i) * (32 * CHUNK));
+                if (c < cols) {
+                    if constexpr (VEC)   // (zeros behind the row's end)
+                        asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(row + c), "r"(min((cols - c) * (uint32_t)sizeof(T), 16u)) : "memory");
+                    else
+                        asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(to), "l"(row + c) : "memory");
+                }
+            }
+        }
+    }
+    __device__ __forceinline__ void close()
+    {
+        if constexpr (ON) {
+            asm volatile("cp.async.commit_group;" ::: "memory");
+            next = next + 1 == DEPTH ? 0 : next + 1;
+        }
+    }
+    // waits for the oldest row asked for, DEPTH being; take()s of its arrays follow, then done()
+    static __device__ __forceinline__ void wait()
+    {
+        if constexpr (ON)
+            asm volatile("cp.async.wait_group %0;" ::"n"(DEPTH - 1) : "memory");
+    }
+    __device__ __forceinline__ void take(int array, const T *row, NormPiece<T, VEC> &p) const
+    {
+        if constexpr (ON) {
+#pragma unroll
+            for (int i = 0; i < CHUNKS; ++i) {
+                const uint8_t *const from = at + now * STAGE + (array * CHUNKS + i) * (32 * CHUNK);
+                const bool there = first(i) < cols;
+                if constexpr (VEC) {
+                    const uint4 w = there ? *(const uint4 *)from : make_uint4(0u, 0u, 0u, 0u);
+                    p.w[4 * i] = w.x, p.w[4 * i + 1] = w.y, p.w[4 * i + 2] = w.z, p.w[4 * i + 3] = w.w;
+                } else {
+                    p.w[i] = there ? *(const uint32_t *)from : 0u;
+                }
+            }
+        } else {
+            p.load(row, c0, cols, lane, false);
+        }
+    }
+    __device__ __forceinline__ void done()
+    {
+        if constexpr (ON)
+            now = now + 1 == DEPTH ? 0 : now + 1;
+    }
+};
+
+// the weights of a lane's columns (aligned: 16 bytes of them are)
 template <class T, bool VEC>
 __device__ __forceinline__ void load_weights(const void *w, bool w32, bool aligned, uint32_t c0, uint32_t cols, int lane, float *v)
 {
-    const uint32_t c = c0 + lane * 16;
-    if (VEC && aligned && c + 16 <= cols) {
+    constexpr int N = kNormPer;
+    const uint32_t c = c0 + lane * N;
+    if (VEC && aligned && c + N <= cols) {
         if (w32) {
 #pragma unroll
-            for (int q = 0; q < 16; q += 4)
+            for (int q = 0; q < N; q += 4)
                 Vec16<float>::unpack(*(const uint4 *)((const float *)w + c + q), *(float(*)[4])(v + q));
         } else {
 #pragma unroll
-            for (int q = 0; q < 16; q += Vec16<T>::N)
+            for (int q = 0; q < N; q += Vec16<T>::N)
                 Vec16<T>::unpack(*(const uint4 *)((const T *)w + c + q), *(float(*)[Vec16<T>::N])(v + q));
         }
         return;
     }
 #pragma unroll
-    for (int q = 0; q < 16; ++q) {
-        const uint32_t i = lane_col<T, VEC>(c0, lane, q);
+    for (int q = 0; q < N; ++q) {
+        const uint32_t i = lane_col<VEC, N>(c0, lane, q);
         v[q] = i >= cols ? 0.f : w32 ? ((const float *)w)[i] : to_f32(((const T *)w)[i]);
     }
 }
-
-// ------------------------------------------------------------------ rows on their way
-// Groups of W warps walk over rows, a piece of 512 elements to a warp, and have those ahead copied into shared memory meanwhile, each lane what it will read: DEPTH rows
-// of ARRAYS matrices.  (A row at a time without that waits for memory once per row: norm-and-gradient of 8192 x 1600 in bf16 with two rows in registers 30 + 30 us.)
-// Elements of 16 bits on odd addresses, which no copy takes, are read when they are wanted.
-template <class T, bool VEC, int ARRAYS>
-struct Rows {
-    static constexpr bool AHEAD = VEC || sizeof(T) == 4;
-    static constexpr int CHUNK = VEC ? 16 : 4, PER = CHUNK / (int)sizeof(T), CHUNKS = 16 / PER;   // bytes and elements of a copy; copies per piece
-    static constexpr int STAGE = ARRAYS * (int)sizeof(T) * 512, DEPTH = sizeof(T) == 2 ? 4 : 2, BYTES = AHEAD ? STAGE * DEPTH : 16;   // of a warp
-
-    uint32_t at;   // the warp's shared memory, and the lane's place in it
-    uint32_t c0, cols;
-    int lane;
-
-    __device__ __forceinline__ Rows(const uint8_t *smem, uint32_t c0, uint32_t cols, int lane) : c0(c0), cols(cols), lane(lane)
-    {
-        at = (uint32_t)__cvta_generic_to_shared(smem) + lane * CHUNK;
-    }
-    __device__ __forceinline__ uint32_t first(int i) const { return VEC ? c0 + lane * 16 + i * PER : lane_col<T, VEC>(c0, lane, i); }
-    __device__ __forceinline__ uint32_t slot(int stage, int array, int i) const { return at + stage * STAGE + (array * CHUNKS + i) * (32 * CHUNK); }
-    __device__ __forceinline__ void ask(int stage, int array, const T *row) const
-    {
-        if constexpr (AHEAD) {
-#pragma unroll
-            for (int i = 0; i < CHUNKS; ++i) {
-                const uint32_t c = first(i);
-                if (c >= cols)
-                    continue;
-                if constexpr (VEC) {
-                    const uint32_t bytes = min((cols - c) * (uint32_t)sizeof(T), 16u);   // (zeros behind the row's end)
-                    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(slot(stage, array, i)), "l"(row + c), "r"(bytes) : "memory");
-                } else {
-                    asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(slot(stage, array, i)), "l"(row + c) : "memory");
-                }
-            }
-        }
-    }
-    static __device__ __forceinline__ void close() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-    static __device__ __forceinline__ void wait() { asm volatile("cp.async.wait_group %0;" ::"n"(DEPTH - 1) : "memory"); }   // (for the oldest of DEPTH)
-    __device__ __forceinline__ void take(int stage, int array, const T *row, Piece<T, VEC> &p) const
-    {
-        if constexpr (!AHEAD) {
-            p.load(row, c0, cols, lane, false);
-        } else {
-#pragma unroll
-            for (int i = 0; i < CHUNKS; ++i) {
-                const bool there = first(i) < cols;
-                if constexpr (VEC) {
-                    uint32_t x = 0, y = 0, z = 0, w = 0;
-                    if (there)
-                        asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(x), "=r"(y), "=r"(z), "=r"(w) : "r"(slot(stage, array, i)) : "memory");
-                    p.w[4 * i] = x, p.w[4 * i + 1] = y, p.w[4 * i + 2] = z, p.w[4 * i + 3] = w;
-                } else {
-                    uint32_t x = 0;
-                    if (there)
-                        asm volatile("ld.shared.b32 %0, [%1];" : "=r"(x) : "r"(slot(stage, array, i)) : "memory");
-                    p.w[i] = x;
-                }
-            }
-        }
-    }
-};
-template <int W>
-__device__ __forceinline__ void group_sync(int group)   // the W warps of a group
-{
-    asm volatile("bar.sync %0, %1;" ::"r"(group + 1), "n"(W * 32) : "memory");
-}
-__host__ __device__ constexpr int norm_threads(int w) { return w > 4 ? w * 32 : 128; }
-__host__ __device__ constexpr int norm_groups(int w) { return w > 4 ? 1 : 4 / w; }   // of a block
 
 // 1 / sqrt(m) to 64 bits' precision: two steps of Newton's iteration from fp32's estimate, whose relative error of 2^-22 each squares (times 3/2).  (Divided and
 // rooted by the 64-bit functions, which are long, a row took a microsecond more.)
@@ -122,135 +133,146 @@ __device__ __forceinline__ double root_of(double m)
     r = r * __fma_rn(-half * r, r, 1.5);
     return r * __fma_rn(-half * r, r, 1.5);
 }
+// what a lane's elements become behind the norm
 template <class T, bool VEC>
-__device__ __forceinline__ void norm_finish(const NormArgs &A, const Piece<T, VEC> &p, const float *w, float root, uint32_t c0, int lane, int64_t row)
+__device__ __forceinline__ void norm_finish(const NormArgs &A, const NormPiece<T, VEC> &p, const float *w, float root, uint32_t c0, int lane, int64_t row)
 {
-    float v[16];
+    constexpr int N = kNormPer;
+    float v[N];
     p.unpack(v);
     if (A.codes) {
         const uint32_t blocks = (uint32_t)f8_blocks(A.cols);
-        norm_values<16>(v, w, root);
-        f8_store_row<T, VEC>(v, c0, blocks, lane, A.kind, true, A.codes + row * blocks * 128, A.scales + f8_scale_at(row, c0 / 128, f8_scale_tiles(A.cols)));
+        uint8_t *const scales = A.scales + f8_scale_at(row, c0 / 128, f8_scale_tiles(A.cols));
+        if (lane_col<VEC, N>(c0, lane, 0) < (uint32_t)A.cols)
+            norm_values<N>(v, w, root);
+        f8_store_row<T, VEC, N>(v, c0, blocks, lane, A.kind, true, A.codes + row * blocks * 128, scales);
+        if (c0 % 512 == 0 && c0 + kNormWarp >= (uint32_t)A.cols && lane < 2)   // (the last tile's second half)
+            scales[2 + lane] = 0;
     } else {
 #pragma unroll
-        for (int q = 0; q < 16; ++q)
+        for (int q = 0; q < N; ++q)
             v[q] = __fmul_rn(__fmul_rn(v[q], root), w[q]);
-        Piece<T, VEC> o;
+        NormPiece<T, VEC> o;
         o.pack(v);
         o.store((T *)A.y + row * A.y_ld, c0, (uint32_t)A.cols, lane, A.aligned32);
     }
 }
 // h, rounded to its type
 template <class T, bool VEC>
-__device__ __forceinline__ void norm_join(Piece<T, VEC> &p, const Piece<T, VEC> &o)
+__device__ __forceinline__ void norm_join(NormPiece<T, VEC> &p, const NormPiece<T, VEC> &o)
 {
-    float a[16], b[16];
+    float a[kNormPer], b[kNormPer];
     p.unpack(a), o.unpack(b);
 #pragma unroll
-    for (int q = 0; q < 16; ++q)
+    for (int q = 0; q < kNormPer; ++q)
         a[q] = __fadd_rn(a[q], b[q]);
     p.pack(a);
 }
 // Squares are summed in 64 bits, which fp32's rounding of the root then does not show: a row's values, and so the codes, do not depend on how it is cut.
 template <class T, bool VEC>
-__device__ __forceinline__ double norm_squares(const Piece<T, VEC> &p)
+__device__ __forceinline__ double norm_squares(const NormPiece<T, VEC> &p)
 {
-    float v[16];
+    float v[kNormPer];
     p.unpack(v);
     double a = 0, b = 0;
 #pragma unroll
-    for (int q = 0; q < 16; q += 2) {
+    for (int q = 0; q < kNormPer; q += 2) {
         a = __fma_rn((double)v[q], (double)v[q], a);
         b = __fma_rn((double)v[q + 1], (double)v[q + 1], b);
     }
     return a + b;
 }
-template <class T, bool VEC, int W>
-__global__ void __launch_bounds__(norm_threads(W)) k_rms_norm(const __grid_constant__ NormArgs A)
+template <class V>
+__device__ __forceinline__ V warp_sum(V v)
 {
-    using R = Rows<T, VEC, 2>;
-    constexpr int G = norm_groups(W);
+#pragma unroll
+    for (int o = 16; o; o /= 2)
+        v += __shfl_xor_sync(0xffffffffu, v, o);
+    return v;
+}
+// scales of rows that do not exist, from `row` on
+__device__ __forceinline__ void norm_no_rows(const NormArgs &A, int64_t row, int64_t step, uint32_t thread, uint32_t threads)
+{
+    const int64_t tiles = f8_scale_tiles(A.cols);
+    for (; row < (A.rows + 127) / 128 * 128; row += step)
+        for (uint32_t t = thread; t < (uint32_t)tiles; t += threads)
+            *(uint32_t *)(A.scales + f8_scale_at(row, t * 4, tiles)) = 0u;
+}
+// ALONE: a warp has a row
+template <class T, bool VEC, bool ALONE>
+__global__ void __launch_bounds__(ALONE ? 256 : 1024, ALONE ? 4 : 1) k_rms_norm(const __grid_constant__ NormArgs A)
+{
     extern __shared__ __align__(16) uint8_t norm_smem[];
-    __shared__ double part[2][G][W];
+    __shared__ double part[2][32];
     grid_release();
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = warp / W, wq = warp % W;
-    const uint32_t c0 = wq * 512u;
-    const R rows(norm_smem + warp * R::BYTES, c0, (uint32_t)A.cols, lane);
-    const int64_t first = (int64_t)blockIdx.x * G + g, step = A.groups;
-    const T *const x = (const T *)A.x, *const add = (const T *)A.add;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, warps = blockDim.x >> 5;
+    const uint32_t cols = (uint32_t)A.cols, c0 = ALONE ? 0u : warp * kNormWarp;
+    int64_t row = ALONE ? (int64_t)blockIdx.x * 8 + warp : blockIdx.x;
+    const int64_t step = ALONE ? (int64_t)gridDim.x * 8 : gridDim.x;
     grid_wait();
-    float w[16];
-    load_weights<T, VEC>(A.w, A.w32, A.aligned_w, c0, (uint32_t)A.cols, lane, w);
-    auto ask = [&](int stage, int64_t row) {
+    float w[kNormPer];
+    load_weights<T, VEC>(A.w, A.w32, A.aligned_w, c0, cols, lane, w);
+    Ahead<T, VEC, 2> rows(norm_smem, warp, lane, c0, cols);
+    const T *const x = (const T *)A.x, *const add = (const T *)A.add;
+    auto ask = [&](int64_t row) {
         if (row < A.rows) {
-            rows.ask(stage, 0, x + row * A.x_ld);
+            rows.ask(0, x + row * A.x_ld);
             if (add)
-                rows.ask(stage, 1, add + row * A.add_ld);
+                rows.ask(1, add + row * A.add_ld);
         }
-        R::close();
+        rows.close();
     };
 #pragma unroll
-    for (int d = 0; d < R::DEPTH - 1; ++d)
-        ask(d, first + d * step);
-    int stage = 0, turn = 0;
-    int64_t row = first;
-    for (; row < A.rows; row += step) {
-        ask((stage + R::DEPTH - 1) % R::DEPTH, row + (R::DEPTH - 1) * step);
-        R::wait();
-        Piece<T, VEC> p;
-        rows.take(stage, 0, x + row * A.x_ld, p);
+    for (int d = 0; d < rows.DEPTH - 1; ++d)
+        ask(row + d * step);
+    for (int turn = 0; row < A.rows; row += step, turn ^= 1) {
+        ask(row + (rows.DEPTH - 1) * step);
+        rows.wait();
+        NormPiece<T, VEC> p;
+        rows.take(0, x + row * A.x_ld, p);
         if (add) {
-            Piece<T, VEC> o;
-            rows.take(stage, 1, add + row * A.add_ld, o);
-            norm_join(p, o);
-            p.store((T *)A.h + row * A.h_ld, c0, (uint32_t)A.cols, lane, A.aligned32);
+            NormPiece<T, VEC> a;
+            rows.take(1, add + row * A.add_ld, a);
+            norm_join(p, a);
+            p.store((T *)A.h + row * A.h_ld, c0, cols, lane, A.aligned32);
         }
-        double sum = norm_squares(p);
-#pragma unroll
-        for (int o = 16; o; o /= 2)
-            sum += __shfl_xor_sync(0xffffffffu, sum, o);
-        if constexpr (W > 1) {
+        rows.done();
+        double sum = warp_sum(norm_squares(p));
+        if constexpr (!ALONE) {
             if (lane == 0)
-                part[turn][g][wq] = sum;
-            group_sync<W>(g);
-            sum = 0;
-#pragma unroll
-            for (int i = 0; i < W; ++i)
-                sum += part[turn][g][i];
-            turn ^= 1;
+                part[turn][warp] = sum;
+            __syncthreads();
+            sum = warp_sum(lane < warps ? part[turn][lane] : 0.0);
         }
-        const float root = (float)root_of(sum / (double)A.cols + A.eps);
-        if (wq == 0 && lane == 0)
+        const float root = (float)root_of(__fma_rn(sum, A.share, A.eps));
+        if ((ALONE || warp == 0) && lane == 0)
             A.rstd[row] = root;
-        if ((A.y || A.codes) && c0 < (uint32_t)A.cols)
+        if (A.y || A.codes)
             norm_finish<T, VEC>(A, p, w, root, c0, lane, row);
-        stage = (stage + 1) % R::DEPTH;
     }
-    if (A.codes && c0 < (uint32_t)A.cols && lane == 0)   // scales of rows that do not exist
-        for (; row < (A.rows + 127) / 128 * 128; row += step)
-            *(uint32_t *)(A.scales + f8_scale_at(row, c0 / 128, f8_scale_tiles(A.cols))) = 0u;
+    if (A.codes)
+        norm_no_rows(A, row, step, ALONE ? lane : threadIdx.x, ALONE ? 32 : blockDim.x);
 }
-// ... of any length: a CTA per row, the second reading from h or x (a lane reads what it wrote)
+// ... of any length, a row per block: the second reading is from h or x (a lane reads what it wrote)
 template <class T, bool VEC>
-__global__ void __launch_bounds__(512) k_rms_norm_long(const __grid_constant__ NormArgs A)
+__global__ void __launch_bounds__(1024) k_rms_norm_long(const __grid_constant__ NormArgs A)
 {
-    constexpr int W = 16;
-    __shared__ double part[W];
+    __shared__ double part[32];
     grid_release();
-    const int wq = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int64_t row = blockIdx.x;
-    const uint32_t cols = (uint32_t)A.cols;
+    const uint32_t cols = (uint32_t)A.cols, step = 32 * kNormWarp;
     const T *const x = (const T *)A.x + row * A.x_ld;
     T *const h = (T *)A.h + row * A.h_ld;
     grid_wait();
-    if (row >= A.rows) {   // scales of rows that do not exist
-        for (uint32_t t = threadIdx.x; t < (uint32_t)f8_scale_tiles(A.cols); t += 512)
-            *(uint32_t *)(A.scales + f8_scale_at(row, t * 4, f8_scale_tiles(A.cols))) = 0u;
+    if (row >= A.rows) {
+        norm_no_rows(A, row, 1ll << 40, threadIdx.x, 1024);
         return;
     }
     double sum = 0;
-    Piece<T, VEC> p, o;
-    for (uint32_t c0 = wq * 512u; c0 < cols; c0 += W * 512u) {
+    NormPiece<T, VEC> p, o;
+#pragma unroll 2
+    for (uint32_t c0 = warp * kNormWarp; c0 < cols; c0 += step) {
         p.load(x, c0, cols, lane, A.aligned32);
         if (A.add) {
             o.load((const T *)A.add + row * A.add_ld, c0, cols, lane, A.aligned32);
@@ -259,23 +281,19 @@ __global__ void __launch_bounds__(512) k_rms_norm_long(const __grid_constant__ N
         }
         sum += norm_squares(p);
     }
-#pragma unroll
-    for (int o = 16; o; o /= 2)
-        sum += __shfl_xor_sync(0xffffffffu, sum, o);
+    sum = warp_sum(sum);
     if (lane == 0)
-        part[wq] = sum;
+        part[warp] = sum;
     __syncthreads();
-    sum = 0;
-#pragma unroll
-    for (int i = 0; i < W; ++i)
-        sum += part[i];
-    const float root = (float)root_of(sum / (double)A.cols + A.eps);
+    sum = warp_sum(part[lane]);
+    const float root = (float)root_of(__fma_rn(sum, A.share, A.eps));
     if (threadIdx.x == 0)
         A.rstd[row] = root;
     if (!A.y && !A.codes)
         return;
-    for (uint32_t c0 = wq * 512u; c0 < cols; c0 += W * 512u) {
-        float w[16];
+#pragma unroll 2
+    for (uint32_t c0 = warp * kNormWarp; c0 < cols; c0 += step) {
+        float w[kNormPer];
         load_weights<T, VEC>(A.w, A.w32, A.aligned_w, c0, cols, lane, w);
         p.load(A.add ? h : x, c0, cols, lane, A.aligned32);
         norm_finish<T, VEC>(A, p, w, root, c0, lane, row);
@@ -284,145 +302,149 @@ __global__ void __launch_bounds__(512) k_rms_norm_long(const __grid_constant__ N
 
 // ------------------------------------------------------------------ the gradient
 // With n = h r and g = dy w: dx = r (g - n mean(g n)) + add, dw = the sum over rows of dy n.  The columns' sums stay in registers (in 32 bits: rows of a group are
-// few) and are written once per group, to be added in 64 bits and in their order by k_norm_columns: results do not depend on which group is done first.
+// few) and are written once per block, to be added in 64 bits and in their order by k_norm_columns: results do not depend on which block is done first.
 struct NormGradArgs {
     const void *dy, *h, *w, *add;
     void *dx;
     const float *rstd;
     const float *means;     // per row, where a row has more columns than a group
-    float *partial;         // per group and column, or NULL
+    float *partial;         // per block and column, or NULL
     int64_t rows, cols, dy_ld, h_ld, add_ld, dx_ld;
-    uint32_t groups;
+    float share;
     bool w32, aligned32, aligned_w;
 };
-template <class T, bool VEC, int W, bool GIVEN>
-__global__ void __launch_bounds__(norm_threads(W)) k_norm_grad(const __grid_constant__ NormGradArgs A)
+// GIVEN: the means are; a block has every gridDim.y-th 8192 columns
+template <class T, bool VEC, bool ALONE, bool GIVEN>
+__global__ void __launch_bounds__(ALONE ? 256 : 1024, ALONE ? 4 : 1) k_norm_grad(const __grid_constant__ NormGradArgs A)
 {
-    using R = Rows<T, VEC, 3>;
-    constexpr int G = norm_groups(W);
+    constexpr int N = kNormPer;
     extern __shared__ __align__(16) uint8_t norm_smem[];
-    __shared__ float part[2][G][W];
+    __shared__ float part[2][32];
+    __shared__ float other[ALONE ? 8 * kNormWarp : 1];
     grid_release();
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = warp / W, wq = warp % W;
-    const uint32_t c0 = (blockIdx.y * W + wq) * 512u, group = blockIdx.x * G + g;
-    const R rows(norm_smem + warp * R::BYTES, c0, (uint32_t)A.cols, lane);
-    const T *const dy = (const T *)A.dy, *const h = (const T *)A.h, *const add = (const T *)A.add;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, warps = blockDim.x >> 5;
+    const uint32_t cols = (uint32_t)A.cols, c0 = ALONE ? 0u : (blockIdx.y * 32 + warp) * kNormWarp;
+    int64_t row = ALONE ? (int64_t)blockIdx.x * 8 + warp : blockIdx.x;
+    const int64_t step = ALONE ? (int64_t)gridDim.x * 8 : gridDim.x;
     grid_wait();
-    float w[16], sums[16];
-    load_weights<T, VEC>(A.w, A.w32, A.aligned_w, c0, (uint32_t)A.cols, lane, w);
+    float w[N], sums[N];
+    load_weights<T, VEC>(A.w, A.w32, A.aligned_w, c0, cols, lane, w);
 #pragma unroll
-    for (int q = 0; q < 16; ++q)
+    for (int q = 0; q < N; ++q)
         sums[q] = 0.f;
-    auto ask = [&](int stage, int64_t row) {
+    Ahead<T, VEC, 3> rows(norm_smem, warp, lane, c0, cols);
+    const T *const dy = (const T *)A.dy, *const h = (const T *)A.h, *const add = (const T *)A.add;
+    auto ask = [&](int64_t row) {
         if (row < A.rows) {
-            rows.ask(stage, 0, dy + row * A.dy_ld);
-            rows.ask(stage, 1, h + row * A.h_ld);
+            rows.ask(0, dy + row * A.dy_ld);
+            rows.ask(1, h + row * A.h_ld);
             if (add)
-                rows.ask(stage, 2, add + row * A.add_ld);
+                rows.ask(2, add + row * A.add_ld);
         }
-        R::close();
+        rows.close();
     };
 #pragma unroll
-    for (int d = 0; d < R::DEPTH - 1; ++d)
-        ask(d, group + (int64_t)d * A.groups);
-    const float share = 1.f / (float)A.cols;
-    int stage = 0, turn = 0;
-    for (int64_t row = group; row < A.rows; row += A.groups) {
-        ask((stage + R::DEPTH - 1) % R::DEPTH, row + (int64_t)(R::DEPTH - 1) * A.groups);
-        const float root = A.rstd[row];
-        R::wait();
-        float d[16], n[16];
-        Piece<T, VEC> p;
-        rows.take(stage, 0, dy + row * A.dy_ld, p);
-        p.unpack(d);
-        rows.take(stage, 1, h + row * A.h_ld, p);
-        p.unpack(n);
-        float m = 0.f;
+    for (int k = 0; k < rows.DEPTH - 1; ++k)
+        ask(row + k * step);
+    float r = row < A.rows ? A.rstd[row] : 0.f;
+    for (int turn = 0; row < A.rows; row += step, turn ^= 1) {
+        ask(row + (rows.DEPTH - 1) * step);
+        const float root = r;
+        r = row + step < A.rows ? A.rstd[row + step] : 0.f;
+        float m = GIVEN ? A.means[row] : 0.f;
+        rows.wait();
+        float d[N], n[N];
+        NormPiece<T, VEC> a;
+        rows.take(0, dy + row * A.dy_ld, a);
+        a.unpack(d);
+        rows.take(1, h + row * A.h_ld, a);
+        a.unpack(n);
 #pragma unroll
-        for (int q = 0; q < 16; ++q) {
+        for (int q = 0; q < N; ++q) {
             n[q] = __fmul_rn(n[q], root);
             sums[q] = __fmaf_rn(d[q], n[q], sums[q]);
             d[q] = __fmul_rn(d[q], w[q]);
-            m = __fmaf_rn(d[q], n[q], m);
+            if (!GIVEN)
+                m = __fmaf_rn(d[q], n[q], m);
         }
-        if constexpr (GIVEN) {
-            m = A.means[row];
-        } else {
-#pragma unroll
-            for (int s = 16; s; s /= 2)
-                m += __shfl_xor_sync(0xffffffffu, m, s);
-            if constexpr (W > 1) {
+        if constexpr (!GIVEN) {
+            m = warp_sum(m);
+            if constexpr (!ALONE) {
                 if (lane == 0)
-                    part[turn][g][wq] = m;
-                group_sync<W>(g);
-                m = 0.f;
-#pragma unroll
-                for (int i = 0; i < W; ++i)
-                    m += part[turn][g][i];
-                turn ^= 1;
+                    part[turn][warp] = m;
+                __syncthreads();
+                m = warp_sum(lane < warps ? part[turn][lane] : 0.f);
             }
-            m *= share;
+            m *= A.share;
         }
 #pragma unroll
-        for (int q = 0; q < 16; ++q)
+        for (int q = 0; q < N; ++q)
             d[q] = __fmul_rn(__fmaf_rn(-n[q], m, d[q]), root);
         if (add) {
-            rows.take(stage, 2, add + row * A.add_ld, p);
-            p.unpack(n);
+            rows.take(2, add + row * A.add_ld, a);
+            a.unpack(n);
 #pragma unroll
-            for (int q = 0; q < 16; ++q)
+            for (int q = 0; q < N; ++q)
                 d[q] = __fadd_rn(d[q], n[q]);
         }
-        p.pack(d);
-        p.store((T *)A.dx + row * A.dx_ld, c0, (uint32_t)A.cols, lane, A.aligned32);
-        stage = (stage + 1) % R::DEPTH;
+        rows.done();
+        a.pack(d);
+        a.store((T *)A.dx + row * A.dx_ld, c0, cols, lane, A.aligned32);
     }
-    if (A.partial) {
+    if (!A.partial)
+        return;
+    if constexpr (ALONE) {   // a block's warps one after the other
 #pragma unroll
-        for (int q = 0; q < 16; ++q) {
-            const uint32_t c = lane_col<T, VEC>(c0, lane, q);
-            if (c < (uint32_t)A.cols)
-                A.partial[(int64_t)group * A.cols + c] = sums[q];
-        }
+        for (int q = 0; q < N; ++q)
+            other[(warp * N + q) * 32 + lane] = sums[q];
+        __syncthreads();
+        if (warp > 0)
+            return;
+        for (int i = 1; i < 8; ++i)
+#pragma unroll
+            for (int q = 0; q < N; ++q)
+                sums[q] += other[(i * N + q) * 32 + lane];
+    }
+#pragma unroll
+    for (int q = 0; q < N; ++q) {
+        const uint32_t c = lane_col<VEC, N>(c0, lane, q);
+        if (c < cols)
+            A.partial[(int64_t)blockIdx.x * A.cols + c] = sums[q];
     }
 }
-// ... the rows' means alone, a CTA each
+// ... the rows' means alone, a block each
 template <class T, bool VEC>
-__global__ void __launch_bounds__(256) k_norm_means(const __grid_constant__ NormGradArgs A, float *means)
+__global__ void __launch_bounds__(1024) k_norm_means(const __grid_constant__ NormGradArgs A, float *means)
 {
-    __shared__ float part[8];
+    __shared__ float part[32];
     grid_release();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int64_t row = blockIdx.x;
     grid_wait();
     const float root = A.rstd[row];
     float m = 0.f;
-    for (uint32_t c0 = warp * 512u; c0 < (uint32_t)A.cols; c0 += 8 * 512u) {
-        Piece<T, VEC> a, b;
+#pragma unroll 2
+    for (uint32_t c0 = warp * kNormWarp; c0 < (uint32_t)A.cols; c0 += 32 * kNormWarp) {
+        NormPiece<T, VEC> a, b;
         a.load((const T *)A.dy + row * A.dy_ld, c0, (uint32_t)A.cols, lane, A.aligned32);
         b.load((const T *)A.h + row * A.h_ld, c0, (uint32_t)A.cols, lane, A.aligned32);
-        float dy[16], n[16], w[16], s = 0.f;
-        a.unpack(dy), b.unpack(n);
+        float d[kNormPer], n[kNormPer], w[kNormPer], s = 0.f;
+        a.unpack(d), b.unpack(n);
         load_weights<T, VEC>(A.w, A.w32, A.aligned_w, c0, (uint32_t)A.cols, lane, w);
 #pragma unroll
-        for (int q = 0; q < 16; ++q)
-            s = __fmaf_rn(__fmul_rn(dy[q], w[q]), __fmul_rn(n[q], root), s);
+        for (int q = 0; q < kNormPer; ++q)
+            s = __fmaf_rn(__fmul_rn(d[q], w[q]), __fmul_rn(n[q], root), s);
         m += s;
     }
-#pragma unroll
-    for (int s = 16; s; s /= 2)
-        m += __shfl_xor_sync(0xffffffffu, m, s);
+    m = warp_sum(m);
     if (lane == 0)
         part[warp] = m;
     __syncthreads();
-    if (threadIdx.x == 0) {
-        m = 0.f;
-        for (int i = 0; i < 8; ++i)
-            m += part[i];
-        means[row] = m / (float)A.cols;
-    }
+    m = warp_sum(part[lane]);
+    if (threadIdx.x == 0)
+        means[row] = m * A.share;
 }
-// the groups' sums of 32 columns
+// the blocks' sums of 32 columns
 __global__ void __launch_bounds__(1024) k_norm_columns(const float *partial, uint32_t groups, int64_t cols, float *dw)
 {
     __shared__ double part[32][33];
@@ -448,66 +470,53 @@ __global__ void __launch_bounds__(1024) k_norm_columns(const float *partial, uin
 
 // ------------------------------------------------------------------ host
 
-// warps per row, and the groups that share the rows: as many as there are warps for, `per_sm` to an SM
-static int norm_warps(int64_t cols) { return cols <= 512 ? 1 : cols <= 1024 ? 2 : cols <= 2048 ? 4 : cols <= 4096 ? 8 : 16; }
-constexpr int64_t kNormWidest = 16 * 512;
-static uint32_t row_groups(int64_t rows, int64_t cols, int per_sm)
+// warps of a block: one with a row of its own each, or as many as a row has (beyond the widest: with as many of its columns)
+static int norm_warps(int64_t cols) { return cols <= kNormWarp ? 8 : (int)((std::min(cols, kNormWidest) + kNormWarp - 1) / kNormWarp); }
+// blocks that share the rows: 32 warps to an SM
+static uint32_t norm_blocks(int64_t rows, int64_t cols)
 {
-    const int w = norm_warps(cols), g = norm_groups(w);
-    return (uint32_t)std::min<int64_t>(kPlanSMs * per_sm / w, (rows + g - 1) / g * g);
+    return (uint32_t)std::min<int64_t>((int64_t)kPlanSMs * (32 / norm_warps(cols)), cols <= kNormWarp ? (rows + 7) / 8 : rows);
 }
-static uint32_t grad_groups(int64_t rows, int64_t cols) { return row_groups(rows, cols, 16); }
-// f by the warps that a row takes
-template <class F>
-static cudaError_t by_warps(int64_t cols, F f)
+
+template <auto KERNEL, int BYTES, class A>   // BYTES: of a warp
+static cudaError_t launch_norm(dim3 grid, int warps, cudaStream_t s, const A &args)
 {
-    switch (norm_warps(cols)) {
-    case 1: return f(std::integral_constant<int, 1>());
-    case 2: return f(std::integral_constant<int, 2>());
-    case 4: return f(std::integral_constant<int, 4>());
-    case 8: return f(std::integral_constant<int, 8>());
-    }
-    return f(std::integral_constant<int, 16>());
+    static int done[64];
+    const size_t smem = (size_t)warps * BYTES;
+    const cudaError_t e = opt_in_smem(KERNEL, smem + 10240, done);   // (48 KB hold what the kernel declares, too)
+    return e != cudaSuccess ? e : launch(KERNEL, grid, warps * 32, smem, s, args);
 }
 
 template <class T, bool VEC>
-static cudaError_t norm(NormArgs A, cudaStream_t s)
+static cudaError_t norm(const NormArgs &A, cudaStream_t s)
 {
+    const int64_t rows = A.codes ? (A.rows + 127) / 128 * 128 : A.rows;   // (scales of rows that do not exist are zero)
     if (A.cols > kNormWidest)
-        return launch(k_rms_norm_long<T, VEC>, dim3((unsigned)(A.codes ? (A.rows + 127) / 128 * 128 : A.rows)), 512, 0, s, A);
-    A.groups = row_groups(A.codes ? (A.rows + 127) / 128 * 128 : A.rows, A.cols, 24);   // (scales of rows that do not exist are zero)
-    return by_warps(A.cols, [&](auto w) {
-        constexpr int W = decltype(w)::value;
-        constexpr size_t smem = (size_t)Rows<T, VEC, 2>::BYTES * norm_threads(W) / 32;
-        static int done[64];
-        const cudaError_t e = opt_in_smem(k_rms_norm<T, VEC, W>, smem + 1024, done);
-        return e != cudaSuccess ? e : launch(k_rms_norm<T, VEC, W>, dim3(A.groups / norm_groups(W)), norm_threads(W), smem, s, A);
-    });
+        return launch(k_rms_norm_long<T, VEC>, dim3((unsigned)rows), 1024, 0, s, A);
+    constexpr int bytes = Ahead<T, VEC, 2>::BYTES;
+    const dim3 grid(norm_blocks(rows, A.cols));
+    return A.cols <= kNormWarp ? launch_norm<k_rms_norm<T, VEC, true>, bytes>(grid, norm_warps(A.cols), s, A)
+                               : launch_norm<k_rms_norm<T, VEC, false>, bytes>(grid, norm_warps(A.cols), s, A);
 }
 
 template <class T, bool VEC>
 static cudaError_t norm_grad(NormGradArgs A, float *means, float *dw, cudaStream_t s)
 {
-    auto go = [&](auto w, auto given) {
-        constexpr int W = decltype(w)::value;
-        constexpr bool GIVEN = decltype(given)::value;
-        constexpr size_t smem = (size_t)Rows<T, VEC, 3>::BYTES * norm_threads(W) / 32;
-        static int done[64];
-        const cudaError_t e = opt_in_smem(k_norm_grad<T, VEC, W, GIVEN>, smem + 1024, done);   // (48 KB hold what the kernel declares, too)
-        const dim3 grid(A.groups / norm_groups(W), (unsigned)((A.cols + W * 512 - 1) / (W * 512)));
-        return e != cudaSuccess ? e : launch(k_norm_grad<T, VEC, W, GIVEN>, grid, norm_threads(W), smem, s, A);
-    };
+    const unsigned blocks = norm_blocks(A.rows, A.cols);
+    const int warps = norm_warps(A.cols);
+    constexpr int bytes = Ahead<T, VEC, 3>::BYTES;
     cudaError_t e;
     if (A.cols > kNormWidest) {
-        e = launch(k_norm_means<T, VEC>, dim3((unsigned)A.rows), 256, 0, s, A, means);
+        e = launch(k_norm_means<T, VEC>, dim3((unsigned)A.rows), 1024, 0, s, A, means);
         A.means = means;
         if (e == cudaSuccess)
-            e = go(std::integral_constant<int, 16>(), std::true_type());
+            e = launch_norm<k_norm_grad<T, VEC, false, true>, bytes>(dim3(blocks, (unsigned)((A.cols + kNormWidest - 1) / kNormWidest)), warps, s, A);
     } else {
-        e = by_warps(A.cols, [&](auto w) { return go(w, std::false_type()); });
+        e = A.cols <= kNormWarp ? launch_norm<k_norm_grad<T, VEC, true, false>, bytes>(dim3(blocks), warps, s, A)
+                                : launch_norm<k_norm_grad<T, VEC, false, false>, bytes>(dim3(blocks), warps, s, A);
     }
     if (e == cudaSuccess && dw)
-        e = launch(k_norm_columns, dim3((unsigned)((A.cols + 31) / 32)), 1024, 0, s, (const float *)A.partial, A.groups, A.cols, dw);
+        e = launch(k_norm_columns, dim3((unsigned)((A.cols + 31) / 32)), 1024, 0, s, (const float *)A.partial, (uint32_t)blocks, A.cols, dw);
     return e;
 }
 
@@ -549,8 +558,8 @@ int conef_rms_norm(const void *x, const void *add, const void *weight, int dtype
         return CONEF_ERR_UNSUPPORTED;
     // (with the transpose's form both are made by the second kernel, which needs the rows' roots first)
     const bool second = codes_t != nullptr;
-    NormArgs A = {x, add, weight, h, y, second ? nullptr : (uint8_t *)codes, second ? nullptr : (uint8_t *)scales, rstd, rows, cols, x_ld, add_ld, h_ld, y_ld, eps,
-                  kind, 0, weight_dtype == CONEF_F32, false, ((uintptr_t)weight & 15) == 0};
+    NormArgs A = {x, add, weight, h, y, second ? nullptr : (uint8_t *)codes, second ? nullptr : (uint8_t *)scales, rstd, rows, cols, x_ld, add_ld, h_ld, y_ld, eps, 1.0 / (double)cols,
+                  kind, weight_dtype == CONEF_F32, false, ((uintptr_t)weight & 15) == 0};
     return with_elem(dtype, [&](auto t) {
         using T = decltype(t);
         auto on = [&](uintptr_t bytes) {
@@ -572,7 +581,7 @@ int conef_rms_norm_grad_bytes(int64_t rows, int64_t cols, size_t *bytes)
         return CONEF_ERR_INVALID_ARG;
     if (rows >= (1ll << 31) || cols >= (1ll << 31))
         return CONEF_ERR_UNSUPPORTED;
-    *bytes = rows && cols ? ((size_t)grad_groups(rows, cols) * (size_t)cols + (cols > kNormWidest ? (size_t)rows : 0)) * sizeof(float) : 0;
+    *bytes = rows && cols ? ((size_t)norm_blocks(rows, cols) * (size_t)cols + (cols > kNormWidest ? (size_t)rows : 0)) * sizeof(float) : 0;
     return CONEF_OK;
 }
 
@@ -602,9 +611,9 @@ int conef_rms_norm_grad(const void *dy, const void *h, const void *weight, const
     if (!workspace || workspace_bytes < need)
         return CONEF_ERR_WORKSPACE_TOO_SMALL;
     float *const partial = (float *)workspace;
-    NormGradArgs A = {dy, h, weight, add, dx, rstd, nullptr, dweight ? partial : nullptr, rows, cols, dy_ld, h_ld, add_ld, dx_ld, grad_groups(rows, cols),
+    NormGradArgs A = {dy, h, weight, add, dx, rstd, nullptr, dweight ? partial : nullptr, rows, cols, dy_ld, h_ld, add_ld, dx_ld, 1.f / (float)cols,
                       weight_dtype == CONEF_F32, false, ((uintptr_t)weight & 15) == 0};
-    float *const means = partial + (size_t)A.groups * cols;
+    float *const means = partial + (size_t)norm_blocks(rows, cols) * cols;
     return with_elem(dtype, [&](auto t) {
         using T = decltype(t);
         auto on = [&](uintptr_t bytes) {
