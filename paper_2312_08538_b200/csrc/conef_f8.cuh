@@ -20,6 +20,11 @@ __host__ __device__ inline int64_t f8_scale_at(int64_t row, int64_t block, int64
 {
     return ((row >> 7) * tiles + (block >> 2)) * 512 + (row & 31) * 16 + ((row >> 5) & 3) * 4 + (block & 3);
 }
+// ... by one multiplication
+__device__ __forceinline__ uint64_t f8_scale_at32(uint32_t row, uint32_t block, uint32_t tiles)
+{
+    return (uint64_t)(row >> 7) * (tiles * 512u) + ((block >> 2) * 512u + (row & 31u) * 16u + ((row >> 5) & 3u) * 4u + (block & 3u));
+}
 
 __device__ __forceinline__ float absmax4(const float *v) { return absmax3(absmax2(v[0], v[1]), v[2], v[3]); }
 // scale byte of a block from the largest |x| in it as bits (as integers NaN > infinity > every finite value)
@@ -265,9 +270,9 @@ __device__ __forceinline__ float norm_value(float h, float w, float r)
 }
 // ... of N elements.  Ties of the 8-bit types, and 1.75 times powers of two, are multiples of 2^19 units of fp32's last place; two ordinary roundings are off by three
 // units at most, so a value further from those than that is on the right side as it is.  One in 2^16 is not, and its thread's are formed exactly.
-// (In the transpose's form and the rows' of 8192 x 1600 31.5 -> 23 us.)
+// All lanes of a warp call; elements that are not `real` become zero.
 template <int N>
-__device__ __forceinline__ void norm_values(float *v, const float *w, float r)
+__device__ __forceinline__ void norm_values(float *v, const float *w, float r, bool real)
 {
     static_assert(N % 4 == 0, "");
     float y[N];
@@ -280,14 +285,14 @@ __device__ __forceinline__ void norm_values(float *v, const float *w, float r)
         mul2(y[q], y[q + 1], pair_of(w[q], w[q + 1]));
         near = __vimin3_u32(near, __float_as_uint(y[q]) * 8192u + 4u * 8192u, __float_as_uint(y[q + 1]) * 8192u + 4u * 8192u);
     }
-    if (near <= 8u * 8192u) {
+    if (__any_sync(0xffffffffu, real && near <= 8u * 8192u)) {
 #pragma unroll
         for (int q = 0; q < N; ++q)
             y[q] = v[q] == 0.f ? y[q] : norm_value(v[q], w[q], r);
     }
 #pragma unroll
     for (int q = 0; q < N; ++q)
-        v[q] = y[q];
+        v[q] = real ? y[q] : 0.f;
 }
 
 // a form that a launch writes, or its transpose's

@@ -10,7 +10,8 @@ struct NormArgs {
     void *h, *y;
     uint8_t *codes, *scales;
     float *rstd;
-    int64_t rows, cols, x_ld, add_ld, h_ld, y_ld;
+    int64_t rows, cols;
+    uint32_t x_ld, add_ld, h_ld, y_ld;
     double eps, share;   // share: of a column in the mean
     int kind;
     bool w32, aligned32, aligned_w;
@@ -20,7 +21,8 @@ struct NormArgs {
 // A lane has 8 elements of a row and a block all of it, 256 elements to a warp (rows of up to 256: a warp has all of it); blocks stay and take rows a grid apart.  So
 // little to a lane leaves room for 32 warps on an SM, which hide what is done once per row: sums across lanes and warps, a barrier, the root.  The rows ahead
 // are copied into shared memory meanwhile, DEPTH of them, each lane what it will read: 6.5 TB/s are 44 KB on their way to each SM at a latency of a microsecond.
-// Elements of 16 bits on odd addresses, which no copy takes, are read when they are wanted.
+// Rows on odd addresses, which copies would take four bytes at a time or not at all, are read when they are wanted, by the norm one row ahead (30011 x 1301
+// in fp32 and its gradient by copies of four bytes 73 and 111 us, as they are wanted 71 and 85, ahead in registers 61 and 129).
 // 8192 x 1600 in bf16 with a residual, and the gradient: 16 elements to a lane 37 and 39 us, 32 elements 35 and 51, 8 with one row ahead in registers 27 and 32.
 constexpr int kNormPer = 8, kNormWarp = 32 * kNormPer;   // elements of a lane and of a warp
 constexpr int64_t kNormWidest = 32 * kNormWarp;
@@ -29,9 +31,9 @@ using NormPiece = Piece<T, VEC, kNormPer>;
 
 template <class T, bool VEC, int ARRAYS>
 struct Ahead {
-    static constexpr bool ON = VEC || sizeof(T) == 4;
-    static constexpr int CHUNK = VEC ? 16 : 4, PER = CHUNK / (int)sizeof(T), CHUNKS = kNormPer / PER;   // bytes and elements of a copy; copies per array
-    static constexpr int STAGE = ARRAYS * kNormWarp * (int)sizeof(T), FIT = 6144 / STAGE, DEPTH = FIT < 4 ? FIT : 4;   // (6 KB to each of 32 warps)
+    static constexpr bool ON = VEC;
+    static constexpr int CHUNK = 16, PER = CHUNK / (int)sizeof(T), CHUNKS = kNormPer / PER;   // bytes and elements of a copy; copies per array
+    static constexpr int STAGE = ARRAYS * kNormWarp * (int)sizeof(T), FIT = 6144 / STAGE, DEPTH = !ON ? 1 : FIT < 4 ? FIT : 4;   // (6 KB to each of 32 warps)
     static constexpr int BYTES = ON ? STAGE * DEPTH : 0;                                                               // of a warp
 
     uint8_t *at;   // the lane's place
@@ -42,7 +44,7 @@ struct Ahead {
         : at(smem + warp * BYTES + lane * CHUNK), c0(c0), cols(cols), lane(lane), now(0), next(0)
     {
     }
-    __device__ __forceinline__ uint32_t first(int i) const { return VEC ? c0 + lane * kNormPer + i * PER : lane_col<VEC, kNormPer>(c0, lane, i); }
+    __device__ __forceinline__ uint32_t first(int i) const { return c0 + lane * kNormPer + i * PER; }
     // asks for a row's elements; then close(), once for all arrays (also where there is no row any more)
     __device__ __forceinline__ void ask(int array, const T *row) const
     {
@@ -50,12 +52,8 @@ struct Ahead {
 #pragma unroll
             for (int i = 0; i < CHUNKS; ++i) {
                 const uint32_t c = first(i), to = (uint32_t)__cvta_generic_to_shared(at + next * STAGE + (array * CHUNKS + i) * (32 * CHUNK));
-                if (c < cols) {
-                    if constexpr (VEC)   // (zeros behind the row's end)
-                        asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(row + c), "r"(min((cols - c) * (uint32_t)sizeof(T), 16u)) : "memory");
-                    else
-                        asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(to), "l"(row + c) : "memory");
-                }
+                if (c < cols)   // (zeros behind the row's end)
+                    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(row + c), "r"(min((cols - c) * (uint32_t)sizeof(T), 16u)) : "memory");
             }
         }
     }
@@ -78,13 +76,8 @@ struct Ahead {
 #pragma unroll
             for (int i = 0; i < CHUNKS; ++i) {
                 const uint8_t *const from = at + now * STAGE + (array * CHUNKS + i) * (32 * CHUNK);
-                const bool there = first(i) < cols;
-                if constexpr (VEC) {
-                    const uint4 w = there ? *(const uint4 *)from : make_uint4(0u, 0u, 0u, 0u);
-                    p.w[4 * i] = w.x, p.w[4 * i + 1] = w.y, p.w[4 * i + 2] = w.z, p.w[4 * i + 3] = w.w;
-                } else {
-                    p.w[i] = there ? *(const uint32_t *)from : 0u;
-                }
+                const uint4 w = first(i) < cols ? *(const uint4 *)from : make_uint4(0u, 0u, 0u, 0u);
+                p.w[4 * i] = w.x, p.w[4 * i + 1] = w.y, p.w[4 * i + 2] = w.z, p.w[4 * i + 3] = w.w;
             }
         } else {
             p.load(row, c0, cols, lane, false);
@@ -135,17 +128,16 @@ __device__ __forceinline__ double root_of(double m)
 }
 // what a lane's elements become behind the norm
 template <class T, bool VEC>
-__device__ __forceinline__ void norm_finish(const NormArgs &A, const NormPiece<T, VEC> &p, const float *w, float root, uint32_t c0, int lane, int64_t row)
+__device__ __forceinline__ void norm_finish(const NormArgs &A, const NormPiece<T, VEC> &p, const float *w, float root, uint32_t c0, int lane, uint32_t row)
 {
     constexpr int N = kNormPer;
     float v[N];
     p.unpack(v);
     if (A.codes) {
-        const uint32_t blocks = (uint32_t)f8_blocks(A.cols);
-        uint8_t *const scales = A.scales + f8_scale_at(row, c0 / 128, f8_scale_tiles(A.cols));
-        if (lane_col<VEC, N>(c0, lane, 0) < (uint32_t)A.cols)
-            norm_values<N>(v, w, root);
-        f8_store_row<T, VEC, N>(v, c0, blocks, lane, A.kind, true, A.codes + row * blocks * 128, scales);
+        const uint32_t blocks = ((uint32_t)A.cols + 127u) / 128u;
+        uint8_t *const scales = A.scales + f8_scale_at32(row, c0 / 128u, ((uint32_t)A.cols + 511u) / 512u);
+        norm_values<N>(v, w, root, lane_col<VEC, N>(c0, lane, 0) < (uint32_t)A.cols);
+        f8_store_row<T, VEC, N>(v, c0, blocks, lane, A.kind, true, A.codes + (uint64_t)row * (blocks * 128u), scales);
         if (c0 % 512 == 0 && c0 + kNormWarp >= (uint32_t)A.cols && lane < 2)   // (the last tile's second half)
             scales[2 + lane] = 0;
     } else {
@@ -154,7 +146,7 @@ __device__ __forceinline__ void norm_finish(const NormArgs &A, const NormPiece<T
             v[q] = __fmul_rn(__fmul_rn(v[q], root), w[q]);
         NormPiece<T, VEC> o;
         o.pack(v);
-        o.store((T *)A.y + row * A.y_ld, c0, (uint32_t)A.cols, lane, A.aligned32);
+        o.store((T *)A.y + (uint64_t)row * A.y_ld, c0, (uint32_t)A.cols, lane, A.aligned32);
     }
 }
 // h, rounded to its type
@@ -207,34 +199,44 @@ __global__ void __launch_bounds__(ALONE ? 256 : 1024, ALONE ? 4 : 1) k_rms_norm(
     grid_release();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, warps = blockDim.x >> 5;
     const uint32_t cols = (uint32_t)A.cols, c0 = ALONE ? 0u : warp * kNormWarp;
-    int64_t row = ALONE ? (int64_t)blockIdx.x * 8 + warp : blockIdx.x;
-    const int64_t step = ALONE ? (int64_t)gridDim.x * 8 : gridDim.x;
+    uint32_t row = ALONE ? blockIdx.x * 8 + warp : blockIdx.x;   // (rows are fewer than 2^31)
+    const uint32_t step = ALONE ? gridDim.x * 8 : gridDim.x;
     grid_wait();
     float w[kNormPer];
     load_weights<T, VEC>(A.w, A.w32, A.aligned_w, c0, cols, lane, w);
     Ahead<T, VEC, 2> rows(norm_smem, warp, lane, c0, cols);
     const T *const x = (const T *)A.x, *const add = (const T *)A.add;
-    auto ask = [&](int64_t row) {
-        if (row < A.rows) {
-            rows.ask(0, x + row * A.x_ld);
-            if (add)
-                rows.ask(1, add + row * A.add_ld);
+    NormPiece<T, VEC> x_next, a_next;   // (where copies are not ON)
+    auto ask = [&](uint32_t row) {
+        if (row < (uint32_t)A.rows) {
+            if constexpr (rows.ON) {
+                rows.ask(0, x + (uint64_t)row * A.x_ld);
+                if (add)
+                    rows.ask(1, add + (uint64_t)row * A.add_ld);
+            } else {
+                x_next.load(x + (uint64_t)row * A.x_ld, c0, cols, lane, false);
+                if (add)
+                    a_next.load(add + (uint64_t)row * A.add_ld, c0, cols, lane, false);
+            }
         }
         rows.close();
     };
+    if constexpr (!rows.ON)
+        ask(row);
 #pragma unroll
     for (int d = 0; d < rows.DEPTH - 1; ++d)
         ask(row + d * step);
-    for (int turn = 0; row < A.rows; row += step, turn ^= 1) {
-        ask(row + (rows.DEPTH - 1) * step);
+    for (int turn = 0; row < (uint32_t)A.rows; row += step, turn ^= 1) {
+        NormPiece<T, VEC> p = x_next, a = a_next;
+        ask(row + (rows.ON ? rows.DEPTH - 1 : 1) * step);
         rows.wait();
-        NormPiece<T, VEC> p;
-        rows.take(0, x + row * A.x_ld, p);
+        if constexpr (rows.ON)
+            rows.take(0, x + (uint64_t)row * A.x_ld, p);
         if (add) {
-            NormPiece<T, VEC> a;
-            rows.take(1, add + row * A.add_ld, a);
+            if constexpr (rows.ON)
+                rows.take(1, add + (uint64_t)row * A.add_ld, a);
             norm_join(p, a);
-            p.store((T *)A.h + row * A.h_ld, c0, cols, lane, A.aligned32);
+            p.store((T *)A.h + (uint64_t)row * A.h_ld, c0, cols, lane, A.aligned32);
         }
         rows.done();
         double sum = warp_sum(norm_squares(p));
@@ -260,12 +262,12 @@ __global__ void __launch_bounds__(1024) k_rms_norm_long(const __grid_constant__ 
     __shared__ double part[32];
     grid_release();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int64_t row = blockIdx.x;
+    const uint32_t row = blockIdx.x;
     const uint32_t cols = (uint32_t)A.cols, step = 32 * kNormWarp;
-    const T *const x = (const T *)A.x + row * A.x_ld;
-    T *const h = (T *)A.h + row * A.h_ld;
+    const T *const x = (const T *)A.x + (uint64_t)row * A.x_ld;
+    T *const h = (T *)A.h + (uint64_t)row * A.h_ld;
     grid_wait();
-    if (row >= A.rows) {
+    if (row >= (uint32_t)A.rows) {
         norm_no_rows(A, row, 1ll << 40, threadIdx.x, 1024);
         return;
     }
@@ -275,7 +277,7 @@ __global__ void __launch_bounds__(1024) k_rms_norm_long(const __grid_constant__ 
     for (uint32_t c0 = warp * kNormWarp; c0 < cols; c0 += step) {
         p.load(x, c0, cols, lane, A.aligned32);
         if (A.add) {
-            o.load((const T *)A.add + row * A.add_ld, c0, cols, lane, A.aligned32);
+            o.load((const T *)A.add + (uint64_t)row * A.add_ld, c0, cols, lane, A.aligned32);
             norm_join(p, o);
             p.store(h, c0, cols, lane, A.aligned32);
         }
@@ -309,7 +311,8 @@ struct NormGradArgs {
     const float *rstd;
     const float *means;     // per row, where a row has more columns than a group
     float *partial;         // per block and column, or NULL
-    int64_t rows, cols, dy_ld, h_ld, add_ld, dx_ld;
+    int64_t rows, cols;
+    uint32_t dy_ld, h_ld, add_ld, dx_ld;
     float share;
     bool w32, aligned32, aligned_w;
 };
@@ -324,8 +327,8 @@ __global__ void __launch_bounds__(ALONE ? 256 : 1024, ALONE ? 4 : 1) k_norm_grad
     grid_release();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, warps = blockDim.x >> 5;
     const uint32_t cols = (uint32_t)A.cols, c0 = ALONE ? 0u : (blockIdx.y * 32 + warp) * kNormWarp;
-    int64_t row = ALONE ? (int64_t)blockIdx.x * 8 + warp : blockIdx.x;
-    const int64_t step = ALONE ? (int64_t)gridDim.x * 8 : gridDim.x;
+    uint32_t row = ALONE ? blockIdx.x * 8 + warp : blockIdx.x;   // (rows are fewer than 2^31)
+    const uint32_t step = ALONE ? gridDim.x * 8 : gridDim.x;
     grid_wait();
     float w[N], sums[N];
     load_weights<T, VEC>(A.w, A.w32, A.aligned_w, c0, cols, lane, w);
@@ -334,30 +337,30 @@ __global__ void __launch_bounds__(ALONE ? 256 : 1024, ALONE ? 4 : 1) k_norm_grad
         sums[q] = 0.f;
     Ahead<T, VEC, 3> rows(norm_smem, warp, lane, c0, cols);
     const T *const dy = (const T *)A.dy, *const h = (const T *)A.h, *const add = (const T *)A.add;
-    auto ask = [&](int64_t row) {
-        if (row < A.rows) {
-            rows.ask(0, dy + row * A.dy_ld);
-            rows.ask(1, h + row * A.h_ld);
+    auto ask = [&](uint32_t row) {
+        if (row < (uint32_t)A.rows) {
+            rows.ask(0, dy + (uint64_t)row * A.dy_ld);
+            rows.ask(1, h + (uint64_t)row * A.h_ld);
             if (add)
-                rows.ask(2, add + row * A.add_ld);
+                rows.ask(2, add + (uint64_t)row * A.add_ld);
         }
         rows.close();
     };
 #pragma unroll
     for (int k = 0; k < rows.DEPTH - 1; ++k)
         ask(row + k * step);
-    float r = row < A.rows ? A.rstd[row] : 0.f;
-    for (int turn = 0; row < A.rows; row += step, turn ^= 1) {
+    float r = row < (uint32_t)A.rows ? A.rstd[row] : 0.f;
+    for (int turn = 0; row < (uint32_t)A.rows; row += step, turn ^= 1) {
         ask(row + (rows.DEPTH - 1) * step);
         const float root = r;
-        r = row + step < A.rows ? A.rstd[row + step] : 0.f;
+        r = row + step < (uint32_t)A.rows ? A.rstd[row + step] : 0.f;
         float m = GIVEN ? A.means[row] : 0.f;
         rows.wait();
         float d[N], n[N];
         NormPiece<T, VEC> a;
-        rows.take(0, dy + row * A.dy_ld, a);
+        rows.take(0, dy + (uint64_t)row * A.dy_ld, a);
         a.unpack(d);
-        rows.take(1, h + row * A.h_ld, a);
+        rows.take(1, h + (uint64_t)row * A.h_ld, a);
         a.unpack(n);
 #pragma unroll
         for (int q = 0; q < N; ++q) {
@@ -381,7 +384,7 @@ __global__ void __launch_bounds__(ALONE ? 256 : 1024, ALONE ? 4 : 1) k_norm_grad
         for (int q = 0; q < N; ++q)
             d[q] = __fmul_rn(__fmaf_rn(-n[q], m, d[q]), root);
         if (add) {
-            rows.take(2, add + row * A.add_ld, a);
+            rows.take(2, add + (uint64_t)row * A.add_ld, a);
             a.unpack(n);
 #pragma unroll
             for (int q = 0; q < N; ++q)
@@ -389,7 +392,7 @@ __global__ void __launch_bounds__(ALONE ? 256 : 1024, ALONE ? 4 : 1) k_norm_grad
         }
         rows.done();
         a.pack(d);
-        a.store((T *)A.dx + row * A.dx_ld, c0, cols, lane, A.aligned32);
+        a.store((T *)A.dx + (uint64_t)row * A.dx_ld, c0, cols, lane, A.aligned32);
     }
     if (!A.partial)
         return;
@@ -409,7 +412,7 @@ __global__ void __launch_bounds__(ALONE ? 256 : 1024, ALONE ? 4 : 1) k_norm_grad
     for (int q = 0; q < N; ++q) {
         const uint32_t c = lane_col<VEC, N>(c0, lane, q);
         if (c < cols)
-            A.partial[(int64_t)blockIdx.x * A.cols + c] = sums[q];
+            A.partial[(uint64_t)blockIdx.x * (uint32_t)A.cols + c] = sums[q];
     }
 }
 // ... the rows' means alone, a block each
@@ -426,8 +429,8 @@ __global__ void __launch_bounds__(1024) k_norm_means(const __grid_constant__ Nor
 #pragma unroll 2
     for (uint32_t c0 = warp * kNormWarp; c0 < (uint32_t)A.cols; c0 += 32 * kNormWarp) {
         NormPiece<T, VEC> a, b;
-        a.load((const T *)A.dy + row * A.dy_ld, c0, (uint32_t)A.cols, lane, A.aligned32);
-        b.load((const T *)A.h + row * A.h_ld, c0, (uint32_t)A.cols, lane, A.aligned32);
+        a.load((const T *)A.dy + (uint64_t)row * A.dy_ld, c0, (uint32_t)A.cols, lane, A.aligned32);
+        b.load((const T *)A.h + (uint64_t)row * A.h_ld, c0, (uint32_t)A.cols, lane, A.aligned32);
         float d[kNormPer], n[kNormPer], w[kNormPer], s = 0.f;
         a.unpack(d), b.unpack(n);
         load_weights<T, VEC>(A.w, A.w32, A.aligned_w, c0, (uint32_t)A.cols, lane, w);
@@ -558,7 +561,7 @@ int conef_rms_norm(const void *x, const void *add, const void *weight, int dtype
         return CONEF_ERR_UNSUPPORTED;
     // (with the transpose's form both are made by the second kernel, which needs the rows' roots first)
     const bool second = codes_t != nullptr;
-    NormArgs A = {x, add, weight, h, y, second ? nullptr : (uint8_t *)codes, second ? nullptr : (uint8_t *)scales, rstd, rows, cols, x_ld, add_ld, h_ld, y_ld, eps, 1.0 / (double)cols,
+    NormArgs A = {x, add, weight, h, y, second ? nullptr : (uint8_t *)codes, second ? nullptr : (uint8_t *)scales, rstd, rows, cols, (uint32_t)x_ld, (uint32_t)add_ld, (uint32_t)h_ld, (uint32_t)y_ld, eps, 1.0 / (double)cols,
                   kind, weight_dtype == CONEF_F32, false, ((uintptr_t)weight & 15) == 0};
     return with_elem(dtype, [&](auto t) {
         using T = decltype(t);
@@ -611,7 +614,7 @@ int conef_rms_norm_grad(const void *dy, const void *h, const void *weight, const
     if (!workspace || workspace_bytes < need)
         return CONEF_ERR_WORKSPACE_TOO_SMALL;
     float *const partial = (float *)workspace;
-    NormGradArgs A = {dy, h, weight, add, dx, rstd, nullptr, dweight ? partial : nullptr, rows, cols, dy_ld, h_ld, add_ld, dx_ld, 1.f / (float)cols,
+    NormGradArgs A = {dy, h, weight, add, dx, rstd, nullptr, dweight ? partial : nullptr, rows, cols, (uint32_t)dy_ld, (uint32_t)h_ld, (uint32_t)add_ld, (uint32_t)dx_ld, 1.f / (float)cols,
                       weight_dtype == CONEF_F32, false, ((uintptr_t)weight & 15) == 0};
     float *const means = partial + (size_t)norm_blocks(rows, cols) * cols;
     return with_elem(dtype, [&](auto t) {
