@@ -199,17 +199,17 @@ __device__ __forceinline__ NsTile ns_tile(const A &P, uint32_t tile)
     return t;
 }
 
-// 32 columns of a lane's row, rounded to the result
-__device__ __forceinline__ void ns_result(const NsArgs &P, uint32_t batch, uint32_t row, uint32_t col, uint32_t have, int lane, bool there, const float (&f)[32])
+// 16 columns of a lane's row, rounded to the result
+__device__ __forceinline__ void ns_result(const NsArgs &P, uint32_t batch, uint32_t row, uint32_t col, uint32_t have, int lane, const float (&f)[16])
 {
-    uint32_t w[16];   // two columns each
+    uint32_t w[8];   // two columns each
 #pragma unroll
-    for (int i = 0; i < 16; ++i)
+    for (int i = 0; i < 8; ++i)
         w[i] = P.dtype == CONEF_BF16 ? Vec16<__nv_bfloat16>::pack2(f[2 * i], f[2 * i + 1]) : Vec16<__half>::pack2(f[2 * i], f[2 * i + 1]);
     uint16_t *const out = (uint16_t *)P.result + (int64_t)batch * P.result_stride;
     if (P.flip) {
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
+        for (int i = 0; i < 8; ++i) {
             // two rows of a column to a lane
             const uint32_t other = __shfl_xor_sync(0xffffffffu, w[i], 1), c = 2 * i + (lane & 1);
             const uint32_t both = lane & 1 ? __byte_perm(other, w[i], 0x7632) : __byte_perm(w[i], other, 0x5410);
@@ -225,15 +225,15 @@ __device__ __forceinline__ void ns_result(const NsArgs &P, uint32_t batch, uint3
                 }
             }
         }
-    } else if (there) {
+    } else if (row < P.n) {
         uint16_t *const to = out + (int64_t)row * P.result_ld + col;
-        if (P.wide && have == 32) {
+        if (P.wide && have == 16) {
 #pragma unroll
-            for (int i = 0; i < 16; i += 4)
+            for (int i = 0; i < 8; i += 4)
                 *(uint4 *)(to + 2 * i) = make_uint4(w[i], w[i + 1], w[i + 2], w[i + 3]);
         } else {
 #pragma unroll
-            for (int i = 0; i < 32; ++i)
+            for (int i = 0; i < 16; ++i)
                 if ((uint32_t)i < have)
                     to[i] = (uint16_t)(w[i / 2] >> (16 * (i & 1)));
         }
@@ -368,7 +368,7 @@ __global__ void __launch_bounds__(kMmThreads, 1) k_ns_product(const __grid_const
         }
         __syncwarp();
     } else {
-        // sums of 32 rows (a lane each) and 64 columns, 32 at a time
+        // Sums of 32 rows (a lane each) and 64 columns, 16 at a time.  E's next 16 are on their way meanwhile, the first while the sums are formed.
         uint32_t set = 0, turn = 0;
         bool ok = true;
         const uint32_t c0 = (uint32_t)(warp >> 2) * 64;
@@ -376,18 +376,29 @@ __global__ void __launch_bounds__(kMmThreads, 1) k_ns_product(const __grid_const
             const NsTile t = ns_tile(P, tile);
             const uint32_t row = t.i * BM + rank * 128 + (warp & 3) * 32 + lane, col0 = t.j * BN + c0;
             const bool mirror = P.symmetric && t.i != t.j;
+            const __half *const eh = P.add.hi + ((int64_t)t.batch * P.add.rows + row) * P.add.pitch + col0,
+                         *const el = P.add.lo + ((int64_t)t.batch * P.add.rows + row) * P.add.pitch + col0;   // (rows are padded to 64 elements)
+            uint32_t h[8] = {}, l[8] = {};
+            auto ask = [&](uint32_t q) {
+                if (P.add.hi && row < P.n && col0 + q * 16 < P.m) {
+                    load32_keep(eh + q * 16, h);
+                    if (P.add.lo)
+                        load32_keep(el + q * 16, l);
+                }
+            };
+            ask(0);
             ok = ok && tc::bar_wait(&S.sums[set], turn, waits, P.sums_limit);
             if (ok)
                 tc::fence_after();
 #pragma unroll
-            for (uint32_t half = 0; half < 2; ++half) {
-                uint32_t v[32];
-                const uint32_t col = col0 + half * 32;
+            for (uint32_t q = 0; q < 4; ++q) {
+                const uint32_t col = col0 + q * 16;
+                uint32_t v[16];
                 __syncwarp();
                 if (ok) {
-                    tc::tmem_load32(((uint32_t)(warp & 3) << 21) + set * BN + c0 + half * 32, v);
+                    tc::tmem_load16(((uint32_t)(warp & 3) << 21) + set * BN + c0 + q * 16, v);
                     tc::tmem_load_wait();
-                    if (half == 1) {
+                    if (q == 3) {
                         tc::fence_before();
                         __syncwarp();
                         if (lane == 0) {
@@ -399,68 +410,62 @@ __global__ void __launch_bounds__(kMmThreads, 1) k_ns_product(const __grid_const
                     }
                 } else {   // a wait ran out: what was not computed is NaN
 #pragma unroll
-                    for (int i = 0; i < 32; ++i)
+                    for (int i = 0; i < 16; ++i)
                         v[i] = 0x7FFFFFFFu;
                 }
                 if (col >= P.m)   // (the same for all lanes)
                     continue;
-                const bool there = row < P.n;
-                const uint32_t have = min(32u, P.m - col);
-                float f[32];
+                float f[16];
 #pragma unroll
-                for (int i = 0; i < 32; ++i)
+                for (int i = 0; i < 16; ++i)
                     f[i] = __fmul_rn(__uint_as_float(v[i]), P.f_sum);
-                if (P.add.hi && there) {
-                    const int64_t at = ((int64_t)t.batch * P.add.rows + row) * P.add.pitch + col;   // (rows are padded to 64 elements)
+                if (P.add.hi) {
 #pragma unroll
-                    for (int i = 0; i < 32; i += 16) {
-                        uint32_t h[8], l[8] = {};
-                        load32_keep(P.add.hi + at + i, h);
-                        if (P.add.lo)
-                            load32_keep(P.add.lo + at + i, l);
+                    for (int i = 0; i < 8; ++i) {
+                        const float2 a = __half22float2(*(const __half2 *)&h[i]), b = __half22float2(*(const __half2 *)&l[i]);
+                        f[2 * i] = __fmaf_rn(__fadd_rn(a.x, b.x), P.f_add, f[2 * i]);
+                        f[2 * i + 1] = __fmaf_rn(__fadd_rn(a.y, b.y), P.f_add, f[2 * i + 1]);
+                    }
+                    if (q < 3)
+                        ask(q + 1);
+                }
+                const uint32_t have = min(16u, P.m - col);
+                if (P.result) {
+                    ns_result(P, t.batch, row, col, have, lane, f);
+                    continue;
+                }
+                const int64_t base = (int64_t)t.batch * P.out.rows * P.out.pitch, at = base + (int64_t)row * P.out.pitch + col;
+                uint32_t w[16];   // hi, lo
 #pragma unroll
-                        for (int q = 0; q < 8; ++q) {
-                            const float2 a = __half22float2(*(const __half2 *)&h[q]), b = __half22float2(*(const __half2 *)&l[q]);
-                            f[i + 2 * q] = __fmaf_rn(__fadd_rn(a.x, b.x), P.f_add, f[i + 2 * q]);
-                            f[i + 2 * q + 1] = __fmaf_rn(__fadd_rn(a.y, b.y), P.f_add, f[i + 2 * q + 1]);
-                        }
+                for (int i = 0; i < 16; ++i) {
+                    __half hi, lo;
+                    split(f[i], hi, lo);
+                    w[i] = (uint32_t)__half_as_ushort(hi) | (uint32_t)__half_as_ushort(lo) << 16;
+                }
+                if (row < P.n) {   // (what lies past a row's end is not read)
+                    uint32_t o[8];
+#pragma unroll
+                    for (int i = 0; i < 8; ++i)
+                        o[i] = __byte_perm(w[2 * i], w[2 * i + 1], 0x5410);
+                    store32_keep(P.out.hi + at, o);
+                    if (P.out.lo) {
+#pragma unroll
+                        for (int i = 0; i < 8; ++i)
+                            o[i] = __byte_perm(w[2 * i], w[2 * i + 1], 0x7632);
+                        store32_keep(P.out.lo + at, o);
                     }
                 }
-                if (P.result) {
-                    ns_result(P, t.batch, row, col, have, lane, there, f);
-                } else {
-                    const int64_t base = (int64_t)t.batch * P.out.rows * P.out.pitch, at = base + (int64_t)row * P.out.pitch + col;
-                    uint32_t w[32];   // hi, lo
+                if (mirror) {
+                    // two rows of a column to a lane: even lanes take even columns, odd ones odd columns, of both rows
 #pragma unroll
-                    for (int i = 0; i < 32; ++i) {
-                        __half h, l;
-                        split(f[i], h, l);
-                        w[i] = (uint32_t)__half_as_ushort(h) | (uint32_t)__half_as_ushort(l) << 16;
-                    }
-                    if (there) {
-#pragma unroll
-                        for (int i = 0; i < 32; i += 16) {   // (what lies past a row's end is not read)
-                            uint32_t h[8], l[8];
-#pragma unroll
-                            for (int q = 0; q < 8; ++q)
-                                h[q] = __byte_perm(w[i + 2 * q], w[i + 2 * q + 1], 0x5410), l[q] = __byte_perm(w[i + 2 * q], w[i + 2 * q + 1], 0x7632);
-                            store32_keep(P.out.hi + at + i, h);
+                    for (int i = 0; i < 16; i += 2) {
+                        const uint32_t other = __shfl_xor_sync(0xffffffffu, lane & 1 ? w[i] : w[i + 1], 1);
+                        const uint32_t upper = lane & 1 ? other : w[i], lower = lane & 1 ? w[i + 1] : other, c = i + (lane & 1);
+                        if ((row & ~1u) < P.n && c < have) {
+                            const int64_t to = base + (int64_t)(col + c) * P.out.pitch + (row & ~1u);
+                            *(uint32_t *)(P.out.hi + to) = __byte_perm(upper, lower, 0x5410);
                             if (P.out.lo)
-                                store32_keep(P.out.lo + at + i, l);
-                        }
-                    }
-                    if (mirror) {
-                        // two rows of a column to a lane: even lanes take even columns, odd ones odd columns, of both rows
-#pragma unroll
-                        for (int i = 0; i < 32; i += 2) {
-                            const uint32_t other = __shfl_xor_sync(0xffffffffu, lane & 1 ? w[i] : w[i + 1], 1);
-                            const uint32_t upper = lane & 1 ? other : w[i], lower = lane & 1 ? w[i + 1] : other, c = i + (lane & 1);
-                            if ((row & ~1u) < P.n && c < have) {
-                                const int64_t to = base + (int64_t)(col + c) * P.out.pitch + (row & ~1u);
-                                *(uint32_t *)(P.out.hi + to) = __byte_perm(upper, lower, 0x5410);
-                                if (P.out.lo)
-                                    *(uint32_t *)(P.out.lo + to) = __byte_perm(upper, lower, 0x7632);
-                            }
+                                *(uint32_t *)(P.out.lo + to) = __byte_perm(upper, lower, 0x7632);
                         }
                     }
                 }
