@@ -158,30 +158,37 @@ __global__ void __launch_bounds__(256) k_ns_start(const __grid_constant__ NsIn A
 }
 
 // ------------------------------------------------------------------ products
-// D = f_sum (L R) + f_add E for stacks of matrices; R along k like L (A = X X^T, A A), or (CROSS) as it is multiplied, along D's columns (B X).
-// The kernel is that of conef_mm.cuh with another stage and another way out.  A stage has 64 elements of k of L's and R's hi and lo, or 128 of hi alone; what
-// leaves is split again, or rounded to the result.
+// D = f_sum (L R) + f_add E for stacks of matrices; R along k like L (A = X X^T, A A), or (CROSS) as it is multiplied, along D's columns (C X).
+// The kernel is that of conef_mm.cuh with another ring and another way out.  A stage has 64 elements of k of L and R, their hi parts or their lo parts; without the
+// lo parts (`single`) each is a product, with them two in a row are three.  What leaves is split again, or rounded to the result; it goes through shared memory
+// and tiled copies, and so does E: a row to a lane, straight to memory, 16 accesses to 32 lines each made 12000 cycles of a tile of 256 x 256, whose
+// products take 13000 (hi parts, k = 1600).
 struct NsArgs {
-    Split out, add;              // (add.hi: NULL without E; lo: NULL where hi alone is written or added)
-    void *result;                // the last product's, instead of out
+    void *result;                // the last product's, instead of the outputs
     int64_t result_ld, result_stride;
     float f_sum, f_add;
     uint32_t n, m, k;            // of D = n x m
-    uint32_t k_steps, stages_k, per_matrix, tiles_m, n_tiles, stages;
+    uint32_t k_steps, stages_k, per_matrix, tiles_m, n_tiles;
     uint32_t symmetric, flip, dtype, single;
-    uint32_t wide;               // the result's rows (flip: columns in pairs) can be stored 16 (4) bytes at a time
+    uint32_t add, add_lo, out_lo;   // E, and the lo parts of E and of what is written
+    uint32_t wide;                  // the result goes by tiled copies
     uint64_t limit, sums_limit;
     uint32_t loads[2];
 };
 struct NsMaps {
-    CUtensorMap lh, ll, rh, rl;
+    CUtensorMap lh, ll, rh, rl;     // tiles of 64 elements by 128 rows (CROSS, R: 64)
+    CUtensorMap eh, el, oh, ol;     // of 64 by 32: E, outputs or (oh) the result
+    CUtensorMap th, tl;             // of 32 by 64: the outputs' or the result's transpose
 };
-constexpr uint32_t kNsPart = 128 * 128;   // bytes: 128 rows (CROSS: of k's 64, two columns of 64 elements) of hi or lo
+constexpr uint32_t kNsPart = 128 * 128, kNsStage = 2 * kNsPart, kNsStages = 5, kNsStaging = 4096;   // bytes: 128 rows of L or R (CROSS: of k's 64, two columns of 64 elements); a warp's 32 x 64 elements
+struct NsShared {
+    MmShared mm;
+    uint64_t added[kMmEpilogue];
+};
 struct NsTile {
     uint32_t batch, i, j;
 };
-template <class A>
-__device__ __forceinline__ NsTile ns_tile(const A &P, uint32_t tile)
+__device__ __forceinline__ NsTile ns_tile(const NsArgs &P, uint32_t tile)
 {
     NsTile t;
     t.batch = tile / P.per_matrix;
@@ -198,46 +205,53 @@ __device__ __forceinline__ NsTile ns_tile(const A &P, uint32_t tile)
     }
     return t;
 }
-
-// 16 columns of a lane's row, rounded to the result
-__device__ __forceinline__ void ns_result(const NsArgs &P, uint32_t batch, uint32_t row, uint32_t col, uint32_t have, int lane, const float (&f)[16])
+// a lane's row of 64 elements (32 words) in a warp's staging memory, 16-byte pieces exchanged as tiled copies do
+__device__ __forceinline__ void staging_read(uint32_t staging, int lane, uint32_t (&w)[32])
 {
-    uint32_t w[8];   // two columns each
 #pragma unroll
     for (int i = 0; i < 8; ++i)
-        w[i] = P.dtype == CONEF_BF16 ? Vec16<__nv_bfloat16>::pack2(f[2 * i], f[2 * i + 1]) : Vec16<__half>::pack2(f[2 * i], f[2 * i + 1]);
-    uint16_t *const out = (uint16_t *)P.result + (int64_t)batch * P.result_stride;
-    if (P.flip) {
+        asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];"
+                     : "=r"(w[4 * i]), "=r"(w[4 * i + 1]), "=r"(w[4 * i + 2]), "=r"(w[4 * i + 3])
+                     : "r"(staging + lane * 128 + ((i ^ (lane & 7)) << 4))
+                     : "memory");
+}
+// Tiles of it to memory, as they are and (mirror) transposed: 64 rows of 32 elements.  The warp's earlier stores from that memory have been read.
+template <bool TURNED>
+__device__ __forceinline__ void staging_store(uint32_t staging, int lane, const uint32_t (&w)[32], const void *map, uint32_t x, uint32_t y, uint32_t z)
+{
+    if (lane == 0)
+        tc::store_wait_read();
+    __syncwarp();
+    if constexpr (TURNED) {
+        // two rows of a column to a lane: even lanes take even columns, odd ones odd columns, of both rows
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            // two rows of a column to a lane
+        for (int i = 0; i < 32; ++i) {
             const uint32_t other = __shfl_xor_sync(0xffffffffu, w[i], 1), c = 2 * i + (lane & 1);
             const uint32_t both = lane & 1 ? __byte_perm(other, w[i], 0x7632) : __byte_perm(w[i], other, 0x5410);
-            const int64_t to = (int64_t)(col + c) * P.result_ld + (row & ~1u);
-            if (c < have) {
-                if (P.wide && (row | 1u) < P.n) {
-                    *(uint32_t *)(out + to) = both;
-                } else {
-                    if ((row & ~1u) < P.n)
-                        out[to] = (uint16_t)both;
-                    if ((row | 1u) < P.n)
-                        out[to + 1] = (uint16_t)(both >> 16);
-                }
-            }
+            asm volatile("st.shared.b32 [%0], %1;" ::"r"(staging + c * 64 + (lane & ~1) * 2), "r"(both) : "memory");
         }
-    } else if (row < P.n) {
-        uint16_t *const to = out + (int64_t)row * P.result_ld + col;
-        if (P.wide && have == 16) {
+    } else {
 #pragma unroll
-            for (int i = 0; i < 8; i += 4)
-                *(uint4 *)(to + 2 * i) = make_uint4(w[i], w[i + 1], w[i + 2], w[i + 3]);
-        } else {
-#pragma unroll
-            for (int i = 0; i < 16; ++i)
-                if ((uint32_t)i < have)
-                    to[i] = (uint16_t)(w[i / 2] >> (16 * (i & 1)));
-        }
+        for (int i = 0; i < 8; ++i)
+            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(staging + lane * 128 + ((i ^ (lane & 7)) << 4)), "r"(w[4 * i]), "r"(w[4 * i + 1]), "r"(w[4 * i + 2]),
+                         "r"(w[4 * i + 3])
+                         : "memory");
     }
+    tc::store_fence();
+    __syncwarp();
+    if (lane == 0)
+        tc::tile_store3(map, staging, x, y, z);
+}
+// 64 columns of a lane's row of the result, two to a word, element by element
+__device__ __forceinline__ void ns_result(const NsArgs &P, uint32_t batch, uint32_t row, uint32_t col, const uint32_t (&w)[32])
+{
+    if (row >= P.n)
+        return;
+    uint16_t *const out = (uint16_t *)P.result + (int64_t)batch * P.result_stride;
+#pragma unroll
+    for (int i = 0; i < 64; ++i)
+        if (col + i < P.m)
+            out[P.flip ? (int64_t)(col + i) * P.result_ld + row : (int64_t)row * P.result_ld + col + i] = (uint16_t)(w[i / 2] >> (16 * (i & 1)));
 }
 
 // A tile is 128 x 128, or of a pair of CTAs 256 x 256: with 128 x 128 a product reads as many bytes of shared memory per cycle as there are, so that the copies into it
@@ -246,9 +260,9 @@ template <bool PAIR, bool CROSS>
 __global__ void __launch_bounds__(kMmThreads, 1) k_ns_product(const __grid_constant__ NsMaps maps, const __grid_constant__ NsArgs P)
 {
     constexpr uint32_t BN = PAIR ? 256 : 128, BM = PAIR ? 256 : 128;
-    constexpr uint32_t stage_bytes = 4 * kNsPart;
     extern __shared__ __align__(1024) uint8_t mm_smem[];
-    __shared__ MmShared S;
+    __shared__ NsShared N;
+    MmShared &S = N.mm;
     const int warp = __shfl_sync(0xffffffffu, (int)(threadIdx.x >> 5), 0), lane = threadIdx.x & 31;
     const uint32_t rank = PAIR ? blockIdx.x & 1u : 0u, first = PAIR ? blockIdx.x / 2 : blockIdx.x, step = PAIR ? gridDim.x / 2 : gridDim.x;
     uint8_t *const ring = mm_smem + ((1024u - (tc::saddr(mm_smem) & 1023u)) & 1023u);
@@ -264,6 +278,8 @@ __global__ void __launch_bounds__(kMmThreads, 1) k_ns_product(const __grid_const
                 tc::bar_init(&S.sums[i], 1);
                 tc::bar_init(&S.taken[i], BN / 16 * (PAIR ? 2 : 1));
             }
+            for (int i = 0; i < kMmEpilogue; ++i)
+                tc::bar_init(&N.added[i], 1);
             tc::bar_init(&S.drain, 1);
             S.dead = 0;
             asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -280,10 +296,9 @@ __global__ void __launch_bounds__(kMmThreads, 1) k_ns_product(const __grid_const
     asm volatile("fence.proxy.async;" ::: "memory");   // (what the launch before stored, ordinary stores, is read by copies)
 
     auto load = [&](uint32_t s, uint32_t ks, const NsTile &t) {
-        // parts of a stage: L's hi and lo, or hi and the next 64 of k; R's
-        const uint32_t st = tc::saddr(ring) + s * stage_bytes, k0 = ks * (P.single ? 128 : 64), k1 = P.single ? k0 + 64 : k0;
-        const uint32_t i0 = t.i * BM + rank * 128, j0 = t.j * BN + rank * (BN / 2);
-        const void *const l1 = P.single ? &maps.lh : &maps.ll, *const r1 = P.single ? &maps.rh : &maps.rl;
+        const uint32_t st = tc::saddr(ring) + s * kNsStage, k0 = (P.single ? ks : ks / 2) * 64, i0 = t.i * BM + rank * 128, j0 = t.j * BN + rank * (BN / 2);
+        const bool low = !P.single && (ks & 1);
+        const void *const l = low ? &maps.ll : &maps.lh, *const r = low ? &maps.rl : &maps.rh;
         auto part = [&](uint32_t dst, const void *map, uint32_t x, uint32_t y) {
             if constexpr (PAIR)
                 tc::tile_load3_pair(dst, map, x, y, t.batch, tc::leaders(&S.full[s]));
@@ -291,17 +306,13 @@ __global__ void __launch_bounds__(kMmThreads, 1) k_ns_product(const __grid_const
                 tc::tile_load3(dst, map, x, y, t.batch, &S.full[s]);
         };
         if (rank == 0)
-            tc::bar_expect(&S.full[s], (PAIR ? 2 : 1) * stage_bytes);
-        part(st, &maps.lh, k0, i0);
-        part(st + kNsPart, l1, k1, i0);
+            tc::bar_expect(&S.full[s], (PAIR ? 2 : 1) * kNsStage);
+        part(st, l, k0, i0);
         if constexpr (CROSS) {
-            part(st + 2 * kNsPart, &maps.rh, j0, k0);
-            part(st + 2 * kNsPart + kNsPart / 2, &maps.rh, j0 + 64, k0);
-            part(st + 3 * kNsPart, r1, j0, k1);
-            part(st + 3 * kNsPart + kNsPart / 2, r1, j0 + 64, k1);
+            part(st + kNsPart, r, j0, k0);
+            part(st + kNsPart + kNsPart / 2, r, j0 + 64, k0);
         } else {
-            part(st + 2 * kNsPart, &maps.rh, k0, j0);
-            part(st + 3 * kNsPart, r1, k1, j0);
+            part(st + kNsPart, r, k0, j0);
         }
     };
     uint32_t armed = 0;
@@ -316,7 +327,7 @@ __global__ void __launch_bounds__(kMmThreads, 1) k_ns_product(const __grid_const
                 if (tc::elect())
                     load(s, ks, t);
                 ++armed;
-                if (++s == P.stages)
+                if (++s == kNsStages)
                     s = 0, phase ^= 1u;
             }
         }
@@ -325,8 +336,8 @@ __global__ void __launch_bounds__(kMmThreads, 1) k_ns_product(const __grid_const
         __syncwarp();
     } else if (warp == kMmEpilogue + 1) {
         const uint32_t instruction = tc::f16_instruction<PAIR, CROSS>(BN);
-        constexpr uint32_t part16 = kNsPart / 16, k_step = CROSS ? 128 : 2;   // (16 of k: 32 bytes of a row, or two groups of eight rows)
-        const uint32_t a0 = tc::desc_low(ring), b0 = CROSS ? tc::desc_low_across(tc::saddr(ring) + 2 * kNsPart, kNsPart / 2) : a0 + 2 * part16;
+        constexpr uint32_t k_step = CROSS ? 128 : 2;   // (16 of k: 32 bytes of a row, or two groups of eight rows)
+        const uint32_t a0 = tc::desc_low(ring), b0 = CROSS ? tc::desc_low_across(tc::saddr(ring) + kNsPart, kNsPart / 2) : a0 + kNsPart / 16;
         uint32_t s = 0, phase = 0, set = 0, turn = 0;
         bool ok = true;
         for (uint32_t tile = rank ? P.n_tiles : first; ok && tile < P.n_tiles; tile += step) {
@@ -334,31 +345,35 @@ __global__ void __launch_bounds__(kMmThreads, 1) k_ns_product(const __grid_const
             if (!(ok = tc::bar_wait(&S.taken[set], turn ^ 1u, waits, P.limit)))
                 break;
             tc::fence_after();
+            uint32_t high = 0;   // the stage before, where that has the hi parts
             for (uint32_t ks = 0; ks < P.stages_k; ++ks) {
                 if (!(ok = tc::bar_wait(&S.full[s], phase, waits, P.limit)))
                     break;
                 tc::fence_after();
                 if (tc::elect()) {
-                    const uint32_t a = a0 + s * (stage_bytes / 16), b = b0 + s * (stage_bytes / 16);
-                    if (P.single) {
-                        const uint32_t steps = P.k_steps - ks * 8u;
+                    const uint32_t a = a0 + s * (kNsStage / 16), b = b0 + s * (kNsStage / 16);
+                    if (P.single || !(ks & 1)) {
+                        const uint32_t steps = P.k_steps - (P.single ? ks : ks / 2) * 4u;
 #pragma unroll
-                        for (uint32_t t = 0; t < 8; ++t)
+                        for (uint32_t t = 0; t < 4; ++t)
                             if (t < steps)
-                                tc::f16_product<PAIR>(d, a + part16 * (t / 4) + 2 * (t % 4), b + part16 * (t / 4) + k_step * (t % 4), instruction, ks + t);
+                                tc::f16_product<PAIR>(d, a + 2 * t, b + k_step * t, instruction, ks + t);
+                        if (P.single)
+                            tc::commit<PAIR>(&S.empty[s]);
                     } else {
-                        const uint32_t steps = P.k_steps - ks * 4u;
+                        const uint32_t steps = P.k_steps - ks / 2 * 4u, ah = a0 + high * (kNsStage / 16), bh = b0 + high * (kNsStage / 16);
 #pragma unroll
                         for (uint32_t t = 0; t < 4; ++t)
                             if (t < steps) {
-                                tc::f16_product<PAIR>(d, a + 2 * t, b + k_step * t, instruction, ks + t);
-                                tc::f16_product<PAIR>(d, a + 2 * t, b + part16 + k_step * t, instruction, 1);
-                                tc::f16_product<PAIR>(d, a + part16 + 2 * t, b + k_step * t, instruction, 1);
+                                tc::f16_product<PAIR>(d, ah + 2 * t, b + k_step * t, instruction, 1);
+                                tc::f16_product<PAIR>(d, a + 2 * t, bh + k_step * t, instruction, 1);
                             }
+                        tc::commit<PAIR>(&S.empty[high]);
+                        tc::commit<PAIR>(&S.empty[s]);
                     }
-                    tc::commit<PAIR>(&S.empty[s]);
                 }
-                if (++s == P.stages)
+                high = s;
+                if (++s == kNsStages)
                     s = 0, phase ^= 1u;
             }
             if (ok && tc::elect())
@@ -368,111 +383,100 @@ __global__ void __launch_bounds__(kMmThreads, 1) k_ns_product(const __grid_const
         }
         __syncwarp();
     } else {
-        // Sums of 32 rows (a lane each) and 64 columns, 16 at a time.  E's next 16 are on their way meanwhile, the first while the sums are formed.
-        uint32_t set = 0, turn = 0;
+        // Sums of 32 rows (a lane each) and 64 columns.  E comes while they are formed.
+        uint32_t set = 0, turn = 0, asked = 0;
         bool ok = true;
-        const uint32_t c0 = (uint32_t)(warp >> 2) * 64;
+        const uint32_t c0 = (uint32_t)(warp >> 2) * 64, staging = tc::saddr(ring) + kNsStages * kNsStage + warp * kNsStaging;
         for (uint32_t tile = c0 < BN ? first : P.n_tiles; tile < P.n_tiles; tile += step) {
             const NsTile t = ns_tile(P, tile);
-            const uint32_t row = t.i * BM + rank * 128 + (warp & 3) * 32 + lane, col0 = t.j * BN + c0;
-            const bool mirror = P.symmetric && t.i != t.j;
-            const __half *const eh = P.add.hi + ((int64_t)t.batch * P.add.rows + row) * P.add.pitch + col0,
-                         *const el = P.add.lo + ((int64_t)t.batch * P.add.rows + row) * P.add.pitch + col0;   // (rows are padded to 64 elements)
-            uint32_t h[8] = {}, l[8] = {};
-            auto ask = [&](uint32_t q) {
-                if (P.add.hi && row < P.n && col0 + q * 16 < P.m) {
-                    load32_keep(eh + q * 16, h);
-                    if (P.add.lo)
-                        load32_keep(el + q * 16, l);
+            const uint32_t row0 = t.i * BM + rank * 128 + (warp & 3) * 32, row = row0 + lane, col = t.j * BN + c0;
+            const bool there = row0 < P.n && col < P.m;
+            uint32_t h[32] = {}, l[32] = {};
+            auto fetch = [&](const void *map, uint32_t (&w)[32]) {
+                if (lane == 0) {
+                    tc::store_wait_read();
+                    tc::bar_expect(&N.added[warp], kNsStaging);
+                    tc::tile_load3(staging, map, col, row0, t.batch, &N.added[warp]);
                 }
+                __syncwarp();
+                if (!tc::bar_wait(&N.added[warp], asked & 1u, waits, P.limit)) {   // (it comes all the same, and before this block ends)
+                    ok = false;
+                    tc::bar_drain(&N.added[warp], asked & 1u, tc::nanoseconds());
+                }
+                ++asked;
+                staging_read(staging, lane, w);
+                tc::store_fence();   // (the reads come before the next copy into that memory, however long the queue of other warps' accesses)
+                __syncwarp();
             };
-            ask(0);
+            if (P.add && there) {
+                fetch(&maps.eh, h);
+                if (P.add_lo)
+                    fetch(&maps.el, l);
+            }
             ok = ok && tc::bar_wait(&S.sums[set], turn, waits, P.sums_limit);
             if (ok)
                 tc::fence_after();
 #pragma unroll
             for (uint32_t q = 0; q < 4; ++q) {
-                const uint32_t col = col0 + q * 16;
                 uint32_t v[16];
-                __syncwarp();
                 if (ok) {
                     tc::tmem_load16(((uint32_t)(warp & 3) << 21) + set * BN + c0 + q * 16, v);
                     tc::tmem_load_wait();
-                    if (q == 3) {
-                        tc::fence_before();
-                        __syncwarp();
-                        if (lane == 0) {
-                            if (PAIR)
-                                tc::bar_arrive_at(tc::leaders(&S.taken[set]));
-                            else
-                                tc::bar_arrive(&S.taken[set]);
-                        }
-                    }
                 } else {   // a wait ran out: what was not computed is NaN
 #pragma unroll
                     for (int i = 0; i < 16; ++i)
                         v[i] = 0x7FFFFFFFu;
                 }
-                if (col >= P.m)   // (the same for all lanes)
-                    continue;
-                float f[16];
 #pragma unroll
-                for (int i = 0; i < 16; ++i)
-                    f[i] = __fmul_rn(__uint_as_float(v[i]), P.f_sum);
-                if (P.add.hi) {
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        const float2 a = __half22float2(*(const __half2 *)&h[i]), b = __half22float2(*(const __half2 *)&l[i]);
-                        f[2 * i] = __fmaf_rn(__fadd_rn(a.x, b.x), P.f_add, f[2 * i]);
-                        f[2 * i + 1] = __fmaf_rn(__fadd_rn(a.y, b.y), P.f_add, f[2 * i + 1]);
-                    }
-                    if (q < 3)
-                        ask(q + 1);
-                }
-                const uint32_t have = min(16u, P.m - col);
-                if (P.result) {
-                    ns_result(P, t.batch, row, col, have, lane, f);
-                    continue;
-                }
-                const int64_t base = (int64_t)t.batch * P.out.rows * P.out.pitch, at = base + (int64_t)row * P.out.pitch + col;
-                uint32_t w[16];   // hi, lo
-#pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    __half hi, lo;
-                    split(f[i], hi, lo);
-                    w[i] = (uint32_t)__half_as_ushort(hi) | (uint32_t)__half_as_ushort(lo) << 16;
-                }
-                if (row < P.n) {   // (what lies past a row's end is not read)
-                    uint32_t o[8];
-#pragma unroll
-                    for (int i = 0; i < 8; ++i)
-                        o[i] = __byte_perm(w[2 * i], w[2 * i + 1], 0x5410);
-                    store32_keep(P.out.hi + at, o);
-                    if (P.out.lo) {
-#pragma unroll
-                        for (int i = 0; i < 8; ++i)
-                            o[i] = __byte_perm(w[2 * i], w[2 * i + 1], 0x7632);
-                        store32_keep(P.out.lo + at, o);
+                for (int i = 0; i < 8; ++i) {
+                    uint32_t &hw = h[8 * q + i], &lw = l[8 * q + i];
+                    const float2 a = __half22float2(*(const __half2 *)&hw), b = __half22float2(*(const __half2 *)&lw);
+                    const float x = __fmaf_rn(__fadd_rn(a.x, b.x), P.f_add, __fmul_rn(__uint_as_float(v[2 * i]), P.f_sum));
+                    const float y = __fmaf_rn(__fadd_rn(a.y, b.y), P.f_add, __fmul_rn(__uint_as_float(v[2 * i + 1]), P.f_sum));
+                    if (P.result) {
+                        hw = P.dtype == CONEF_BF16 ? Vec16<__nv_bfloat16>::pack2(x, y) : Vec16<__half>::pack2(x, y);
+                    } else {
+                        hw = Vec16<__half>::pack2(x, y);
+                        const float2 r = __half22float2(*(const __half2 *)&hw);
+                        lw = Vec16<__half>::pack2(__fsub_rn(x, r.x), __fsub_rn(y, r.y));
                     }
                 }
-                if (mirror) {
-                    // two rows of a column to a lane: even lanes take even columns, odd ones odd columns, of both rows
-#pragma unroll
-                    for (int i = 0; i < 16; i += 2) {
-                        const uint32_t other = __shfl_xor_sync(0xffffffffu, lane & 1 ? w[i] : w[i + 1], 1);
-                        const uint32_t upper = lane & 1 ? other : w[i], lower = lane & 1 ? w[i + 1] : other, c = i + (lane & 1);
-                        if ((row & ~1u) < P.n && c < have) {
-                            const int64_t to = base + (int64_t)(col + c) * P.out.pitch + (row & ~1u);
-                            *(uint32_t *)(P.out.hi + to) = __byte_perm(upper, lower, 0x5410);
-                            if (P.out.lo)
-                                *(uint32_t *)(P.out.lo + to) = __byte_perm(upper, lower, 0x7632);
-                        }
-                    }
+            }
+            if (ok) {
+                tc::fence_before();
+                __syncwarp();
+                if (lane == 0) {
+                    if (PAIR)
+                        tc::bar_arrive_at(tc::leaders(&S.taken[set]));
+                    else
+                        tc::bar_arrive(&S.taken[set]);
                 }
             }
             if (++set == 2)
                 set = 0, turn ^= 1u;
+            if (!there)
+                continue;
+            if (P.result) {
+                if (!P.wide)
+                    ns_result(P, t.batch, row, col, h);
+                else if (P.flip)
+                    staging_store<true>(staging, lane, h, &maps.th, row0, col, t.batch);
+                else
+                    staging_store<false>(staging, lane, h, &maps.oh, col, row0, t.batch);
+                continue;
+            }
+            const bool mirror = P.symmetric && t.i != t.j;
+            staging_store<false>(staging, lane, h, &maps.oh, col, row0, t.batch);
+            if (P.out_lo)
+                staging_store<false>(staging, lane, l, &maps.ol, col, row0, t.batch);
+            if (mirror) {
+                staging_store<true>(staging, lane, h, &maps.th, row0, col, t.batch);
+                if (P.out_lo)
+                    staging_store<true>(staging, lane, l, &maps.tl, row0, col, t.batch);
+            }
         }
+        if (lane == 0)
+            tc::store_wait();
         __syncwarp();
     }
     tc::fence_before();
@@ -488,12 +492,12 @@ __global__ void __launch_bounds__(kMmThreads, 1) k_ns_product(const __grid_const
                 const uint32_t nth = armed / P.stages_k;
                 const NsTile t = ns_tile(P, first + nth * step);
                 if (tc::elect())
-                    load(armed % P.stages, armed - nth * P.stages_k, t);
+                    load(armed % kNsStages, armed - nth * P.stages_k, t);
                 __syncwarp();
             }
             if (rank == 0)
-                for (uint32_t i = 0; i < P.stages && i < all; ++i)
-                    tc::bar_drain(&S.full[(all - 1 - i) % P.stages], ((all - 1 - i) / P.stages) & 1u, t0);
+                for (uint32_t i = 0; i < kNsStages && i < all; ++i)
+                    tc::bar_drain(&S.full[(all - 1 - i) % kNsStages], ((all - 1 - i) / kNsStages) & 1u, t0);
         } else if (warp == kMmEpilogue + 1 && rank == 0) {
             if (tc::elect())
                 tc::commit<PAIR>(&S.drain);
@@ -511,41 +515,60 @@ __global__ void __launch_bounds__(kMmThreads, 1) k_ns_product(const __grid_const
 
 // ------------------------------------------------------------------ host
 
-// tiles of `box` rows of 64 elements
-static bool encode_split(CUtensorMap *map, const __half *p, int64_t rows, int64_t cols, int64_t pitch, int64_t batch, uint32_t box)
+// tiles of `width` elements (64, or 32 unpermuted) by `box` rows of a stack of matrices of 16-bit elements, `ld` and `stride` apart
+static bool encode_stack(CUtensorMap *map, const void *p, int64_t rows, int64_t cols, int64_t ld, int64_t stride, int64_t batch, uint32_t width, uint32_t box)
 {
-    const cuuint64_t dims[3] = {(cuuint64_t)cols, (cuuint64_t)rows, (cuuint64_t)batch}, strides[2] = {(cuuint64_t)pitch * 2, (cuuint64_t)(pitch * rows) * 2};
-    const cuuint32_t tile[3] = {64, box, 1}, steps[3] = {1, 1, 1};
-    return encode_tiled() && encode_tiled()(map, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 3, (void *)p, dims, strides, tile, steps, CU_TENSOR_MAP_INTERLEAVE_NONE,
-                                            CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+    const cuuint64_t dims[3] = {(cuuint64_t)cols, (cuuint64_t)rows, (cuuint64_t)batch}, strides[2] = {(cuuint64_t)ld * 2, (cuuint64_t)stride * 2};
+    const cuuint32_t tile[3] = {width, box, 1}, steps[3] = {1, 1, 1};
+    return encode_tiled() && encode_tiled()(map, CU_TENSOR_MAP_DATA_TYPE_UINT16, 3, (void *)p, dims, strides, tile, steps, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                                            width == 64 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                                            CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+static bool encode_split(CUtensorMap *map, const __half *p, const Split &s, int64_t batch, uint32_t width, uint32_t box)
+{
+    return encode_stack(map, p, s.rows, s.cols, s.pitch, s.pitch * s.rows, batch, width, box);
 }
 
-constexpr uint32_t kNsStages = 3;
-constexpr size_t kNsSmem = 1024 + kNsStages * 4 * kNsPart;
+constexpr size_t kNsSmem = 1024 + kNsStages * kNsStage + kMmEpilogue * kNsStaging;
+static_assert(kNsSmem <= kMmSmem && kNsStages <= kMmMaxStages, "");
 
+// E, out: NULL without; P has the factors, the parts and the result
 template <bool CROSS>
-static cudaError_t ns_product(const Split &L, const Split &R, int64_t batch, NsArgs P, bool pair, cudaStream_t s)
+static cudaError_t ns_product(const Split &L, const Split &R, const Split *E, const Split *out, int64_t batch, NsArgs P, bool pair, cudaStream_t s)
 {
     const uint32_t side = pair ? 256 : 128;
     P.n = (uint32_t)L.rows;
     P.m = (uint32_t)(CROSS ? R.cols : R.rows);
     P.k = (uint32_t)L.cols;
     P.k_steps = (P.k + 15) / 16;
-    P.stages_k = P.single ? (P.k + 127) / 128 : (P.k + 63) / 64;
+    P.stages_k = (P.k + 63) / 64 * (P.single ? 1 : 2);
     P.tiles_m = (P.n + side - 1) / side;
+    P.add = E != nullptr;
     const int64_t per = P.symmetric ? (int64_t)P.tiles_m * (P.tiles_m + 1) / 2 : (int64_t)P.tiles_m * ((P.m + side - 1) / side);
     if (per * batch >= (1ll << 31))
         return cudaErrorInvalidValue;
     P.per_matrix = (uint32_t)per;
     P.n_tiles = (uint32_t)(per * batch);
-    P.stages = kNsStages;
     P.limit = (uint64_t)mm_limit.nanoseconds.load();
     P.sums_limit = P.limit + 4096ull * P.stages_k;
     P.loads[0] = mm_limit.loads[0].load();
     P.loads[1] = mm_limit.loads[1].load();
-    NsMaps maps;
-    if (!encode_split(&maps.lh, L.hi, L.rows, L.cols, L.pitch, batch, 128) || !encode_split(&maps.ll, L.lo, L.rows, L.cols, L.pitch, batch, 128) ||
-        !encode_split(&maps.rh, R.hi, R.rows, R.cols, R.pitch, batch, CROSS ? 64 : 128) || !encode_split(&maps.rl, R.lo, R.rows, R.cols, R.pitch, batch, CROSS ? 64 : 128))
+    NsMaps maps = {};
+    const uint32_t r_box = CROSS ? 64 : 128;
+    bool ok = encode_split(&maps.lh, L.hi, L, batch, 64, 128) && encode_split(&maps.ll, L.lo, L, batch, 64, 128) && encode_split(&maps.rh, R.hi, R, batch, 64, r_box) &&
+              encode_split(&maps.rl, R.lo, R, batch, 64, r_box);
+    if (E)
+        ok = ok && encode_split(&maps.eh, E->hi, *E, batch, 64, 32) && encode_split(&maps.el, E->lo, *E, batch, 64, 32);
+    if (out)
+        ok = ok && encode_split(&maps.oh, out->hi, *out, batch, 64, 32) && encode_split(&maps.ol, out->lo, *out, batch, 64, 32) &&
+             (!P.symmetric || (encode_split(&maps.th, out->hi, *out, batch, 32, 64) && encode_split(&maps.tl, out->lo, *out, batch, 32, 64)));
+    if (P.result && P.wide) {
+        // (a matrix alone: any distance to the next)
+        const int64_t stride = batch > 1 ? P.result_stride : 8;
+        ok = ok && (P.flip ? encode_stack(&maps.th, P.result, P.m, P.n, P.result_ld, stride, batch, 32, 64)
+                           : encode_stack(&maps.oh, P.result, P.n, P.m, P.result_ld, stride, batch, 64, 32));
+    }
+    if (!ok)
         return cudaErrorInvalidValue;
     static int done[2][64];
     cudaError_t e = pair ? opt_in_smem(k_ns_product<true, CROSS>, kMmSmem, done[1]) : opt_in_smem(k_ns_product<false, CROSS>, kMmSmem, done[0]);
@@ -692,39 +715,36 @@ int conef_orthogonalise(const void *x, int dtype, int64_t batch, int64_t rows, i
         NsArgs P = {};
         P.symmetric = 1;
         P.single = one;
-        P.out = A;
-        if (one_c)
-            P.out.lo = nullptr;
+        P.out_lo = !one_c;
         P.f_sum = (float)(sa / (sx * sx));
-        e = ns_product<false>(X, X, batch, P, pair_a, s);
+        e = ns_product<false>(X, X, nullptr, &A, batch, P, pair_a, s);
         if (e != cudaSuccess)
             break;
         P.single = one_c;
-        P.add = P.out;
-        P.out = C;
-        if (one)
-            P.out.lo = nullptr;
+        P.add_lo = !one_c;
+        P.out_lo = !one;
         P.f_sum = (float)(c * sc / (sa * sa));
         P.f_add = (float)(b * sc / sa);
-        e = ns_product<false>(A, A, batch, P, pair_a, s);
+        e = ns_product<false>(A, A, &A, &C, batch, P, pair_a, s);
         if (e != cudaSuccess)
             break;
+        const bool last = t + 1 == steps;
+        const double to = last ? scale : sy;
         NsArgs U = {};
         U.single = one;
-        U.add = X;
-        U.out = Y;
-        if (t + 1 == steps) {
+        U.add_lo = U.out_lo = 1;
+        U.f_sum = (float)(to / (sc * sx));
+        U.f_add = (float)(a * to / sx);
+        if (last) {
             U.result = out;
             U.result_ld = rows > 1 ? out_ld : cols;
             U.result_stride = batch > 1 ? out_stride : 0;
             U.flip = z.flip;
             U.dtype = (uint32_t)out_dtype;
-            U.wide = (((uintptr_t)out | (uint64_t)(U.result_ld | U.result_stride) * 2) & (z.flip ? 3 : 15)) == 0;
+            // (a tiled copy writes a row's last 16 bytes whole, whatever the map says of its end)
+            U.wide = (((uintptr_t)out | (uint64_t)(U.result_ld | U.result_stride | cols) * 2) & 15) == 0;
         }
-        const double to = t + 1 == steps ? scale : sy;
-        U.f_sum = (float)(to / (sc * sx));
-        U.f_add = (float)(a * to / sx);
-        e = ns_product<true>(C, X, batch, U, pair_x, s);
+        e = ns_product<true>(C, X, &X, last ? nullptr : &Y, batch, U, pair_x, s);
         std::swap(X, Y);
         sx = sy;
     }
