@@ -169,7 +169,9 @@ struct NsArgs {
     float f_sum, f_add;
     uint32_t n, m, k;            // of D = n x m
     uint32_t k_steps, stages_k, per_matrix, tiles_m, n_tiles;
+    uint32_t tiles_wide;            // (symmetric) tiles are 256 x 128
     uint32_t symmetric, flip, dtype, single;
+    uint32_t bn, stage_bytes, stages;   // columns of a tile; the ring
     uint32_t add, add_lo, out_lo;   // E, and the lo parts of E and of what is written
     uint32_t wide;                  // the result goes by tiled copies
     uint64_t limit, sums_limit;
@@ -180,7 +182,13 @@ struct NsMaps {
     CUtensorMap eh, el, oh, ol;     // of 64 by 32: E, outputs or (oh) the result
     CUtensorMap th, tl;             // of 32 by 64: the outputs' or the result's transpose
 };
-constexpr uint32_t kNsPart = 128 * 128, kNsStage = 2 * kNsPart, kNsStages = 5, kNsStaging = 4096;   // bytes: 128 rows of L or R (CROSS: of k's 64, two columns of 64 elements); a warp's 32 x 64 elements
+constexpr uint32_t kNsLeft = 128 * 128, kNsStaging = 4096;   // bytes: 128 rows of L; a warp's 32 x 64 elements of what leaves
+// ... of R: 128 per row, or (CROSS) for each of k's 64, columns of 64 elements
+__host__ __device__ inline uint32_t ns_right(uint32_t bn, bool pair, bool cross)
+{
+    const uint32_t rows = pair ? bn / 2 : bn;
+    return cross ? (rows + 63) / 64 * 8192 : rows * 128;
+}
 struct NsShared {
     MmShared mm;
     uint64_t added[kMmEpilogue];
@@ -193,7 +201,16 @@ __device__ __forceinline__ NsTile ns_tile(const NsArgs &P, uint32_t tile)
     NsTile t;
     t.batch = tile / P.per_matrix;
     uint32_t in = tile - t.batch * P.per_matrix;
-    if (P.symmetric) {   // columns of a triangle
+    if (P.symmetric && P.tiles_wide) {   // tiles twice as high as wide on and above the diagonal: columns 2 p and 2 p + 1 have p + 1 each
+        uint32_t p = (uint32_t)((sqrtf(4.f * (float)in + 1.f) - 1.f) * 0.5f);
+        while (p * (p + 1) > in)
+            --p;
+        while ((p + 1) * (p + 2) <= in)
+            ++p;
+        in -= p * (p + 1);
+        const uint32_t second = in > p ? 1u : 0u;
+        t.j = 2 * p + second, t.i = in - second * (p + 1);
+    } else if (P.symmetric) {   // columns of a triangle
         uint32_t j = (uint32_t)((sqrtf(8.f * (float)in + 1.f) - 1.f) * 0.5f);
         while (j * (j + 1) / 2 > in)
             --j;
@@ -254,12 +271,13 @@ __device__ __forceinline__ void ns_result(const NsArgs &P, uint32_t batch, uint3
             out[P.flip ? (int64_t)(col + i) * P.result_ld + row : (int64_t)row * P.result_ld + col + i] = (uint16_t)(w[i / 2] >> (16 * (i & 1)));
 }
 
-// A tile is 128 x 128, or of a pair of CTAs 256 x 256: with 128 x 128 a product reads as many bytes of shared memory per cycle as there are, so that the copies into it
-// have to wait; a pair's CTA has half of R for twice the outputs.
+// A tile is 128 x 128, or of a pair of CTAs 256 by 128, 192 (not symmetric) or 256: with 128 x 128 a product reads as many bytes of shared memory per cycle as there
+// are, so that the copies into it have to wait; a pair's CTA has half of R for as many rows of L.
 template <bool PAIR, bool CROSS>
 __global__ void __launch_bounds__(kMmThreads, 1) k_ns_product(const __grid_constant__ NsMaps maps, const __grid_constant__ NsArgs P)
 {
-    constexpr uint32_t BN = PAIR ? 256 : 128, BM = PAIR ? 256 : 128;
+    constexpr uint32_t BM = PAIR ? 256 : 128;
+    const uint32_t BN = P.bn, right = ns_right(BN, PAIR, CROSS);
     extern __shared__ __align__(1024) uint8_t mm_smem[];
     __shared__ NsShared N;
     MmShared &S = N.mm;
@@ -296,7 +314,7 @@ __global__ void __launch_bounds__(kMmThreads, 1) k_ns_product(const __grid_const
     asm volatile("fence.proxy.async;" ::: "memory");   // (what the launch before stored, ordinary stores, is read by copies)
 
     auto load = [&](uint32_t s, uint32_t ks, const NsTile &t) {
-        const uint32_t st = tc::saddr(ring) + s * kNsStage, k0 = (P.single ? ks : ks / 2) * 64, i0 = t.i * BM + rank * 128, j0 = t.j * BN + rank * (BN / 2);
+        const uint32_t st = tc::saddr(ring) + s * P.stage_bytes, k0 = (P.single ? ks : ks / 2) * 64, i0 = t.i * BM + rank * 128, j0 = t.j * BN + rank * (BN / 2);
         const bool low = !P.single && (ks & 1);
         const void *const l = low ? &maps.ll : &maps.lh, *const r = low ? &maps.rl : &maps.rh;
         auto part = [&](uint32_t dst, const void *map, uint32_t x, uint32_t y) {
@@ -306,13 +324,14 @@ __global__ void __launch_bounds__(kMmThreads, 1) k_ns_product(const __grid_const
                 tc::tile_load3(dst, map, x, y, t.batch, &S.full[s]);
         };
         if (rank == 0)
-            tc::bar_expect(&S.full[s], (PAIR ? 2 : 1) * kNsStage);
+            tc::bar_expect(&S.full[s], (PAIR ? 2 : 1) * (kNsLeft + right));
         part(st, l, k0, i0);
         if constexpr (CROSS) {
-            part(st + kNsPart, r, j0, k0);
-            part(st + kNsPart + kNsPart / 2, r, j0 + 64, k0);
+            part(st + kNsLeft, r, j0, k0);
+            if (right > 8192)
+                part(st + kNsLeft + 8192, r, j0 + 64, k0);
         } else {
-            part(st + kNsPart, r, k0, j0);
+            part(st + kNsLeft, r, k0, j0);
         }
     };
     uint32_t armed = 0;
@@ -327,7 +346,7 @@ __global__ void __launch_bounds__(kMmThreads, 1) k_ns_product(const __grid_const
                 if (tc::elect())
                     load(s, ks, t);
                 ++armed;
-                if (++s == kNsStages)
+                if (++s == P.stages)
                     s = 0, phase ^= 1u;
             }
         }
@@ -337,7 +356,7 @@ __global__ void __launch_bounds__(kMmThreads, 1) k_ns_product(const __grid_const
     } else if (warp == kMmEpilogue + 1) {
         const uint32_t instruction = tc::f16_instruction<PAIR, CROSS>(BN);
         constexpr uint32_t k_step = CROSS ? 128 : 2;   // (16 of k: 32 bytes of a row, or two groups of eight rows)
-        const uint32_t a0 = tc::desc_low(ring), b0 = CROSS ? tc::desc_low_across(tc::saddr(ring) + kNsPart, kNsPart / 2) : a0 + kNsPart / 16;
+        const uint32_t a0 = tc::desc_low(ring), b0 = CROSS ? tc::desc_low_across(tc::saddr(ring) + kNsLeft, 8192) : a0 + kNsLeft / 16, step16 = P.stage_bytes / 16;
         uint32_t s = 0, phase = 0, set = 0, turn = 0;
         bool ok = true;
         for (uint32_t tile = rank ? P.n_tiles : first; ok && tile < P.n_tiles; tile += step) {
@@ -351,7 +370,7 @@ __global__ void __launch_bounds__(kMmThreads, 1) k_ns_product(const __grid_const
                     break;
                 tc::fence_after();
                 if (tc::elect()) {
-                    const uint32_t a = a0 + s * (kNsStage / 16), b = b0 + s * (kNsStage / 16);
+                    const uint32_t a = a0 + s * step16, b = b0 + s * step16;
                     if (P.single || !(ks & 1)) {
                         const uint32_t steps = P.k_steps - (P.single ? ks : ks / 2) * 4u;
 #pragma unroll
@@ -361,7 +380,7 @@ __global__ void __launch_bounds__(kMmThreads, 1) k_ns_product(const __grid_const
                         if (P.single)
                             tc::commit<PAIR>(&S.empty[s]);
                     } else {
-                        const uint32_t steps = P.k_steps - ks / 2 * 4u, ah = a0 + high * (kNsStage / 16), bh = b0 + high * (kNsStage / 16);
+                        const uint32_t steps = P.k_steps - ks / 2 * 4u, ah = a0 + high * step16, bh = b0 + high * step16;
 #pragma unroll
                         for (uint32_t t = 0; t < 4; ++t)
                             if (t < steps) {
@@ -373,7 +392,7 @@ __global__ void __launch_bounds__(kMmThreads, 1) k_ns_product(const __grid_const
                     }
                 }
                 high = s;
-                if (++s == kNsStages)
+                if (++s == P.stages)
                     s = 0, phase ^= 1u;
             }
             if (ok && tc::elect())
@@ -386,7 +405,7 @@ __global__ void __launch_bounds__(kMmThreads, 1) k_ns_product(const __grid_const
         // Sums of 32 rows (a lane each) and 64 columns.  E comes while they are formed.
         uint32_t set = 0, turn = 0, asked = 0;
         bool ok = true;
-        const uint32_t c0 = (uint32_t)(warp >> 2) * 64, staging = tc::saddr(ring) + kNsStages * kNsStage + warp * kNsStaging;
+        const uint32_t c0 = (uint32_t)(warp >> 2) * 64, staging = tc::saddr(ring) + P.stages * P.stage_bytes + warp * kNsStaging;
         for (uint32_t tile = c0 < BN ? first : P.n_tiles; tile < P.n_tiles; tile += step) {
             const NsTile t = ns_tile(P, tile);
             const uint32_t row0 = t.i * BM + rank * 128 + (warp & 3) * 32, row = row0 + lane, col = t.j * BN + c0;
@@ -465,7 +484,7 @@ __global__ void __launch_bounds__(kMmThreads, 1) k_ns_product(const __grid_const
                     staging_store<false>(staging, lane, h, &maps.oh, col, row0, t.batch);
                 continue;
             }
-            const bool mirror = P.symmetric && t.i != t.j;
+            const bool mirror = P.symmetric && t.i != (P.tiles_wide ? t.j / 2 : t.j);
             staging_store<false>(staging, lane, h, &maps.oh, col, row0, t.batch);
             if (P.out_lo)
                 staging_store<false>(staging, lane, l, &maps.ol, col, row0, t.batch);
@@ -492,12 +511,12 @@ __global__ void __launch_bounds__(kMmThreads, 1) k_ns_product(const __grid_const
                 const uint32_t nth = armed / P.stages_k;
                 const NsTile t = ns_tile(P, first + nth * step);
                 if (tc::elect())
-                    load(armed % kNsStages, armed - nth * P.stages_k, t);
+                    load(armed % P.stages, armed - nth * P.stages_k, t);
                 __syncwarp();
             }
             if (rank == 0)
-                for (uint32_t i = 0; i < kNsStages && i < all; ++i)
-                    tc::bar_drain(&S.full[(all - 1 - i) % kNsStages], ((all - 1 - i) / kNsStages) & 1u, t0);
+                for (uint32_t i = 0; i < P.stages && i < all; ++i)
+                    tc::bar_drain(&S.full[(all - 1 - i) % P.stages], ((all - 1 - i) / P.stages) & 1u, t0);
         } else if (warp == kMmEpilogue + 1 && rank == 0) {
             if (tc::elect())
                 tc::commit<PAIR>(&S.drain);
@@ -529,22 +548,55 @@ static bool encode_split(CUtensorMap *map, const __half *p, const Split &s, int6
     return encode_stack(map, p, s.rows, s.cols, s.pitch, s.pitch * s.rows, batch, width, box);
 }
 
-constexpr size_t kNsSmem = 1024 + kNsStages * kNsStage + kMmEpilogue * kNsStaging;
-static_assert(kNsSmem <= kMmSmem && kNsStages <= kMmMaxStages, "");
+// The tile whose waves over the SMs take least.  Nanoseconds per wave: of 64 elements along k, hi parts alone and all three products, and of what does not
+// depend on k, from 1600 x 1600 and 2 x 1600 x 6400.  At full rate they would be 133, 133, 200, 266 and 400, 400, 600, 800; a stage's copies, up to 32 KB to each
+// CTA, take 260 at 64 bytes a cycle, so hi parts alone gain nothing by less than 256 columns but in the number of tiles.
+struct NsTiles {
+    bool pair;
+    uint32_t bn;
+    int one, three, fixed;
+};
+static NsTiles ns_tiles(int64_t n, int64_t m, int64_t k, int64_t batch, bool symmetric, bool single)
+{
+    static const NsTiles kinds[] = {{false, 128, 270, 740, 4500}, {true, 128, 300, 600, 5500}, {true, 192, 340, 880, 6000}, {true, 256, 305, 980, 7000}};
+    NsTiles best = {};
+    int64_t least = -1;
+    for (const NsTiles &c : kinds) {
+        if (symmetric && c.bn == 192)
+            continue;
+        const int64_t high = c.pair ? 256 : 128, ti = (n + high - 1) / high, tj = (m + c.bn - 1) / c.bn, sets = c.pair ? kPlanSMs / 2 : kPlanSMs;
+        int64_t tiles = ti * tj;
+        if (symmetric)
+            tiles = c.bn == high ? ti * (ti + 1) / 2 : tj / 2 * (tj / 2 + 1) + (tj & 1 ? tj / 2 + 1 : 0);
+        // (what a tile leaves goes out while the next one's sums are formed)
+        const int64_t waves = (tiles * batch + sets - 1) / sets, cost = waves * ((k + 63) / 64) * (single ? c.one : c.three) + c.fixed;
+        if (least < 0 || cost < least)
+            best = c, least = cost;
+    }
+    return best;
+}
 
 // E, out: NULL without; P has the factors, the parts and the result
 template <bool CROSS>
-static cudaError_t ns_product(const Split &L, const Split &R, const Split *E, const Split *out, int64_t batch, NsArgs P, bool pair, cudaStream_t s)
+static cudaError_t ns_product(const Split &L, const Split &R, const Split *E, const Split *out, int64_t batch, NsArgs P, cudaStream_t s)
 {
-    const uint32_t side = pair ? 256 : 128;
     P.n = (uint32_t)L.rows;
     P.m = (uint32_t)(CROSS ? R.cols : R.rows);
     P.k = (uint32_t)L.cols;
     P.k_steps = (P.k + 15) / 16;
     P.stages_k = (P.k + 63) / 64 * (P.single ? 1 : 2);
-    P.tiles_m = (P.n + side - 1) / side;
+    const NsTiles kind = ns_tiles(P.n, P.m, P.k, batch, P.symmetric, P.single);
+    const bool pair = kind.pair;
+    const uint32_t high = pair ? 256 : 128;
+    P.bn = kind.bn;
+    P.tiles_wide = pair && P.bn == 128;
+    P.tiles_m = (P.n + high - 1) / high;
     P.add = E != nullptr;
-    const int64_t per = P.symmetric ? (int64_t)P.tiles_m * (P.tiles_m + 1) / 2 : (int64_t)P.tiles_m * ((P.m + side - 1) / side);
+    const int64_t tj = (P.m + P.bn - 1) / P.bn;
+    const int64_t per = !P.symmetric ? P.tiles_m * tj : P.tiles_wide ? tj / 2 * (tj / 2 + 1) + (tj & 1 ? tj / 2 + 1 : 0) : (int64_t)P.tiles_m * (P.tiles_m + 1) / 2;
+    const uint32_t staging = P.bn / 16 * kNsStaging;
+    P.stage_bytes = kNsLeft + ns_right(P.bn, pair, CROSS);
+    P.stages = std::min<uint32_t>(kMmMaxStages, (kMmSmem - 1024 - staging) / P.stage_bytes);
     if (per * batch >= (1ll << 31))
         return cudaErrorInvalidValue;
     P.per_matrix = (uint32_t)per;
@@ -554,7 +606,7 @@ static cudaError_t ns_product(const Split &L, const Split &R, const Split *E, co
     P.loads[0] = mm_limit.loads[0].load();
     P.loads[1] = mm_limit.loads[1].load();
     NsMaps maps = {};
-    const uint32_t r_box = CROSS ? 64 : 128;
+    const uint32_t r_box = CROSS ? 64 : pair ? P.bn / 2 : P.bn;
     bool ok = encode_split(&maps.lh, L.hi, L, batch, 64, 128) && encode_split(&maps.ll, L.lo, L, batch, 64, 128) && encode_split(&maps.rh, R.hi, R, batch, 64, r_box) &&
               encode_split(&maps.rl, R.lo, R, batch, 64, r_box);
     if (E)
@@ -576,7 +628,7 @@ static cudaError_t ns_product(const Split &L, const Split &R, const Split *E, co
         return e;
     // (a pair leaves no shared memory on its SMs: conef_mm.cuh)
     return pair ? launch_cluster(k_ns_product<true, CROSS>, (int)std::min<uint32_t>(P.n_tiles, kPlanSMs / 2), 2, kMmThreads, s, (size_t)kMmSmem, maps, P)
-                : launch(k_ns_product<false, CROSS>, dim3(std::min<uint32_t>(P.n_tiles, kPlanSMs)), kMmThreads, kNsSmem, s, maps, P);
+                : launch(k_ns_product<false, CROSS>, dim3(std::min<uint32_t>(P.n_tiles, kPlanSMs)), kMmThreads, 1024 + (size_t)P.stages * P.stage_bytes + staging, s, maps, P);
 }
 
 // the largest |b t + c t^2| for 0 <= t <= top, and the largest |s (a + b s^2 + c s^4)| for 0 <= s <= top
@@ -705,9 +757,6 @@ int conef_orthogonalise(const void *x, int dtype, int64_t batch, int64_t rows, i
                        dim3((unsigned)tiles, (unsigned)batch), 256, 0, s, in, X, (uint32_t)tiles_c, sx);
         return 0;
     });
-    // tiles of pairs where there are enough of them
-    const int64_t sides = (z.n + 255) / 256;
-    const bool pair_a = sides * (sides + 1) / 2 * batch >= kPlanSMs / 4, pair_x = sides * ((z.m + 255) / 256) * batch >= kPlanSMs / 4;
     const int single = single_steps(z.n, out_dtype, a, b, c);
     for (int t = 0; t < steps && e == cudaSuccess; ++t) {
         const double sa = fp16_scale(top[t] * top[t]), sc = fp16_scale(largest_factor(b, c, top[t] * top[t])), sy = fp16_scale(top[t + 1]);
@@ -717,7 +766,7 @@ int conef_orthogonalise(const void *x, int dtype, int64_t batch, int64_t rows, i
         P.single = one;
         P.out_lo = !one_c;
         P.f_sum = (float)(sa / (sx * sx));
-        e = ns_product<false>(X, X, nullptr, &A, batch, P, pair_a, s);
+        e = ns_product<false>(X, X, nullptr, &A, batch, P, s);
         if (e != cudaSuccess)
             break;
         P.single = one_c;
@@ -725,7 +774,7 @@ int conef_orthogonalise(const void *x, int dtype, int64_t batch, int64_t rows, i
         P.out_lo = !one;
         P.f_sum = (float)(c * sc / (sa * sa));
         P.f_add = (float)(b * sc / sa);
-        e = ns_product<false>(A, A, &A, &C, batch, P, pair_a, s);
+        e = ns_product<false>(A, A, &A, &C, batch, P, s);
         if (e != cudaSuccess)
             break;
         const bool last = t + 1 == steps;
@@ -744,7 +793,7 @@ int conef_orthogonalise(const void *x, int dtype, int64_t batch, int64_t rows, i
             // (a tiled copy writes a row's last 16 bytes whole, whatever the map says of its end)
             U.wide = (((uintptr_t)out | (uint64_t)(U.result_ld | U.result_stride | cols) * 2) & 15) == 0;
         }
-        e = ns_product<true>(C, X, &X, last ? nullptr : &Y, batch, U, pair_x, s);
+        e = ns_product<true>(C, X, &X, last ? nullptr : &Y, batch, U, s);
         std::swap(X, Y);
         sx = sy;
     }
