@@ -10,7 +10,7 @@
 //    of small singular values is as small as A has them.
 //  - A and C are kept likewise, and a product is the sum of hi hi, hi lo and lo hi in one set of fp32 sums on the tensor cores: as exact as 32-bit
 //    arithmetic at three times 16-bit's cost, not at the 20 times that 32-bit units take.
-//  - The first steps' products are hi hi alone (single_steps()).
+//  - Some products, most of them in the first steps, are hi hi alone (ns_single()).
 //
 // Per step three launches: A (symmetric: tiles on and above the diagonal, stored twice), C (likewise, A added on the way out), C X (a X added).
 #include <cuda.h>
@@ -660,16 +660,24 @@ static double largest_value(double a, double b, double c, double top)
 // a power of two that brings `bound` below 2^15, half of fp16's range
 static double fp16_scale(double bound) { return std::ldexp(1.0, 14 - std::ilogb(std::max(bound, 1e-30))); }
 
-// Steps, from the first on, whose products are of fp16's 11 bits alone.  Singular values are small then (at most 1 in all, in squares), so C, and what a rounding adds to C X, is
-// small, and falls off with the singular value as A does; it counts less the more elements it is averaged over.  Errors of the result relative to its size, the largest of
-// spectra that are flat, fall off as 1/i or exponentially, and of 1 to 128 directions with and without noise, 128 to 512 rows and one to four times the columns: one
-// step 3.7e-4 (256 rows; 512: 0.9e-4), two 3.0e-4 (2.1e-4), three 6.2e-4 (4.7e-4 and, flat with more columns, 7.6e-4) where the third step's A A is not, four
-// 1.5e-3.  Rounding to bf16 loses 1.7e-3, to fp16 2.1e-4: three steps for bf16 from 256 rows on, one for fp16 from 512.  For coefficients beyond 5 none.
-static int single_steps(int64_t n, int out_dtype, double a, double b, double c)
+// Where products are of hi parts, fp16's 11 bits, alone.  Singular values are small in the first steps (their squares add up to 1), so C is, and what a rounding adds to
+// C X falls off with the singular value as A does; it counts less the more elements it is averaged over; and what the last step adds no other raises.
+// Errors of the result relative to its size, the largest of spectra that are flat, fall off as 1/i or exponentially, and of 1 to 128 directions with and without
+// noise, five steps, 256 to 1024 rows and one to four times the columns (simulated):
+//   all of the first step 2.7e-4 (from 512 rows on, but for a few directions without any noise 1.1e-4), of the first two 3.0e-4, of the first three 7.9e-4 but for the
+//   third's A A (with it, and in the steps behind, 1e-3 to 2.5e-3 each); A in all steps with those 8.8e-4, and the last step's C X 1.2e-3.
+// Rounding to bf16 loses 1.7e-3, with the last of these 2.0e-3; rounding to fp16 2.1e-4.  More steps raise all of it (ten to 2e-3), so that holds for five.  For
+// coefficients beyond 5, and for few rows, whose products take no time, all parts are taken.
+struct NsSingle {
+    int steps;   // the first ones: all products but, from the third on, A A
+    int gram;    // ... A
+    bool last;   // the last one's C X
+};
+static NsSingle ns_single(int64_t n, int out_dtype, int steps, double a, double b, double c)
 {
-    if (std::max({std::fabs(a), std::fabs(b), std::fabs(c)}) > 5)
-        return 0;
-    return out_dtype == CONEF_BF16 ? (n >= 256 ? 3 : 0) : (n >= 512 ? 1 : 0);
+    if (std::max({std::fabs(a), std::fabs(b), std::fabs(c)}) > 5 || n < (out_dtype == CONEF_BF16 ? 256 : 512))
+        return {0, 0, false};
+    return out_dtype == CONEF_BF16 ? NsSingle{3, 5, steps <= 5} : NsSingle{1, 2, false};
 }
 
 struct NsSizes {
@@ -757,13 +765,14 @@ int conef_orthogonalise(const void *x, int dtype, int64_t batch, int64_t rows, i
                        dim3((unsigned)tiles, (unsigned)batch), 256, 0, s, in, X, (uint32_t)tiles_c, sx);
         return 0;
     });
-    const int single = single_steps(z.n, out_dtype, a, b, c);
+    const NsSingle single = ns_single(z.n, out_dtype, steps, a, b, c);
     for (int t = 0; t < steps && e == cudaSuccess; ++t) {
         const double sa = fp16_scale(top[t] * top[t]), sc = fp16_scale(largest_factor(b, c, top[t] * top[t])), sy = fp16_scale(top[t + 1]);
-        const bool one = t < single, one_c = one && t < 2;
+        const bool last = t + 1 == steps;
+        const bool one_a = t < single.gram, one_c = t < std::min(2, single.steps), one_x = t < single.steps || (last && single.last);
         NsArgs P = {};
         P.symmetric = 1;
-        P.single = one;
+        P.single = one_a;
         P.out_lo = !one_c;
         P.f_sum = (float)(sa / (sx * sx));
         e = ns_product<false>(X, X, nullptr, &A, batch, P, s);
@@ -771,16 +780,15 @@ int conef_orthogonalise(const void *x, int dtype, int64_t batch, int64_t rows, i
             break;
         P.single = one_c;
         P.add_lo = !one_c;
-        P.out_lo = !one;
+        P.out_lo = !one_x;
         P.f_sum = (float)(c * sc / (sa * sa));
         P.f_add = (float)(b * sc / sa);
         e = ns_product<false>(A, A, &A, &C, batch, P, s);
         if (e != cudaSuccess)
             break;
-        const bool last = t + 1 == steps;
         const double to = last ? scale : sy;
         NsArgs U = {};
-        U.single = one;
+        U.single = one_x;
         U.add_lo = U.out_lo = 1;
         U.f_sum = (float)(to / (sc * sx));
         U.f_add = (float)(a * to / sx);

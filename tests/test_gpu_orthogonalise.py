@@ -23,7 +23,9 @@ def update(rows, cols, dtype, seed=0, rank=None, noise=0.1):
 
 def check(got, x, steps=5, coefficients=QUINTIC, scale=1.0):
     """Rounding to the type is off by half a step at most.  Operands are kept to 2^-23 of their size (the half of fp16's lower part) and
-    sums in fp32: each step's X is off by 2^-20 relative at most, and the steps behind raise that by their slope at zero each, which is the largest."""
+    sums in fp32: each step's X is off by 2^-20 relative at most, and the steps behind raise that by their slope at zero each, which is the largest.  (From 256 rows on
+    some products take 11 bits, which adds 1.2e-3 at most; in the norm rounding loses 2^-8 / sqrt(3) / 1.4 = 1.7e-3, their root of squares is 2.0e-3, and 2^-8 is 3.9e-3.  For
+    float16, from 512 rows on, 2.7e-4 and 2.1e-4 are 3.4e-4 of 4.9e-4.)"""
     want = fo.orthogonalise(f64(x), steps, coefficients, scale)
     tol = EPS[got.dtype] + 2.0 ** -20 * sum(abs(coefficients[0]) ** i for i in range(1, steps + 1))
     far = np.linalg.norm(f64(got) - want) / max(np.linalg.norm(want), 1e-300)
