@@ -286,9 +286,15 @@ __device__ __forceinline__ void norm_values(float *v, const float *w, float r, b
         near = __vimin3_u32(near, __float_as_uint(y[q]) * 8192u + 4u * 8192u, __float_as_uint(y[q + 1]) * 8192u + 4u * 8192u);
     }
     if (__any_sync(0xffffffffu, real && near <= 8u * 8192u)) {
+        bool some = false;   // (zeros, which sums of few bits often are, look the same and are exact)
 #pragma unroll
         for (int q = 0; q < N; ++q)
-            y[q] = v[q] == 0.f ? y[q] : norm_value(v[q], w[q], r);
+            some = some || (__float_as_uint(y[q]) * 8192u + 4u * 8192u <= 8u * 8192u && v[q] != 0.f);
+        if (__any_sync(0xffffffffu, real && some)) {
+#pragma unroll
+            for (int q = 0; q < N; ++q)
+                y[q] = v[q] == 0.f ? y[q] : norm_value(v[q], w[q], r);
+        }
     }
 #pragma unroll
     for (int q = 0; q < N; ++q)

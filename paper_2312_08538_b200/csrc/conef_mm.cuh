@@ -128,6 +128,8 @@ __global__ void __launch_bounds__(kMmThreads, 1) k_matmul(const __grid_constant_
     const uint32_t rank = PAIR ? blockIdx.x & 1u : 0u, first = PAIR ? blockIdx.x / 2 : blockIdx.x, step = PAIR ? gridDim.x / 2 : gridDim.x;
     uint8_t *const ring = mm_smem + ((1024u - (tc::saddr(mm_smem) & 1023u)) & 1023u);
     const tc::Waits waits = {&S.dead, PAIR ? tc::address_in(&S.dead, rank ^ 1u) : 0u, &g_mm_ran_out};
+    if (warp == 1 && lane < (int)(sizeof maps / sizeof maps.a))
+        tc::prefetch_map(&maps.a + lane);
     if (warp == 0) {
         tc::tmem_alloc<PAIR>(&S.tmem, kMmColumns);
         if (lane == 0) {
@@ -425,7 +427,7 @@ static int matmul(const uint8_t *a, const uint8_t *as, int64_t m, const uint8_t 
     P.stages = std::min<uint32_t>({(uint32_t)kMmMaxStages, (kMmColumns - P.scale_column) / F::kScaleColumns, room / stage_bytes, std::max(2u, P.stages_k)});
     // (a tiled copy writes a row's last 16 bytes whole, whatever the map says of its end)
     P.tiled = (((uint64_t)ld * sizeof(T)) | ((uint64_t)n * sizeof(T)) | (uintptr_t)out) % 16 == 0;
-    MmMaps maps;
+    MmMaps maps = {};
     const int64_t row_bytes = F::row_bytes(k), scale_bytes = (int64_t)P.tiles * 512;
     bool ok = encode(&maps.a, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, a, m, row_bytes, row_bytes, 128, kMmM) &&
               encode(&maps.b, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, b, n, row_bytes, row_bytes, 128, PAIR ? bn / 2 : bn);

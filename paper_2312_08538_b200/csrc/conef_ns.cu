@@ -232,13 +232,15 @@ __device__ __forceinline__ void staging_read(uint32_t staging, int lane, uint32_
                      : "r"(staging + lane * 128 + ((i ^ (lane & 7)) << 4))
                      : "memory");
 }
-// Tiles of it to memory, as they are and (mirror) transposed: 64 rows of 32 elements.  The warp's earlier stores from that memory have been read.
+// Tiles of it to memory, as they are and (mirror) transposed: 64 rows of 32 elements.  `again`: an earlier store reads that memory, perhaps still.
 template <bool TURNED>
-__device__ __forceinline__ void staging_store(uint32_t staging, int lane, const uint32_t (&w)[32], const void *map, uint32_t x, uint32_t y, uint32_t z)
+__device__ __forceinline__ void staging_store(uint32_t staging, bool again, int lane, const uint32_t (&w)[32], const void *map, uint32_t x, uint32_t y, uint32_t z)
 {
-    if (lane == 0)
-        tc::store_wait_read();
-    __syncwarp();
+    if (again) {
+        if (lane == 0)
+            tc::store_wait_read();
+        __syncwarp();
+    }
     if constexpr (TURNED) {
         // two rows of a column to a lane: even lanes take even columns, odd ones odd columns, of both rows
 #pragma unroll
@@ -285,6 +287,8 @@ __global__ void __launch_bounds__(kMmThreads, 1) k_ns_product(const __grid_const
     const uint32_t rank = PAIR ? blockIdx.x & 1u : 0u, first = PAIR ? blockIdx.x / 2 : blockIdx.x, step = PAIR ? gridDim.x / 2 : gridDim.x;
     uint8_t *const ring = mm_smem + ((1024u - (tc::saddr(mm_smem) & 1023u)) & 1023u);
     const tc::Waits waits = {&S.dead, PAIR ? tc::address_in(&S.dead, rank ^ 1u) : 0u, &g_mm_ran_out};
+    if (warp == 1 && lane < (int)(sizeof maps / sizeof maps.lh))
+        tc::prefetch_map(&maps.lh + lane);
     if (warp == 0) {
         tc::tmem_alloc<PAIR>(&S.tmem, kMmColumns);
         if (lane == 0) {
@@ -446,18 +450,35 @@ __global__ void __launch_bounds__(kMmThreads, 1) k_ns_product(const __grid_const
                     for (int i = 0; i < 16; ++i)
                         v[i] = 0x7FFFFFFFu;
                 }
+                float f[16];
 #pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    uint32_t &hw = h[8 * q + i], &lw = l[8 * q + i];
-                    const float2 a = __half22float2(*(const __half2 *)&hw), b = __half22float2(*(const __half2 *)&lw);
-                    const float x = __fmaf_rn(__fadd_rn(a.x, b.x), P.f_add, __fmul_rn(__uint_as_float(v[2 * i]), P.f_sum));
-                    const float y = __fmaf_rn(__fadd_rn(a.y, b.y), P.f_add, __fmul_rn(__uint_as_float(v[2 * i + 1]), P.f_sum));
-                    if (P.result) {
-                        hw = P.dtype == CONEF_BF16 ? Vec16<__nv_bfloat16>::pack2(x, y) : Vec16<__half>::pack2(x, y);
-                    } else {
-                        hw = Vec16<__half>::pack2(x, y);
-                        const float2 r = __half22float2(*(const __half2 *)&hw);
-                        lw = Vec16<__half>::pack2(__fsub_rn(x, r.x), __fsub_rn(y, r.y));
+                for (int i = 0; i < 16; ++i)
+                    f[i] = __fmul_rn(__uint_as_float(v[i]), P.f_sum);
+                if (P.add) {
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        float2 a = __half22float2(*(const __half2 *)&h[8 * q + i]);
+                        if (P.add_lo) {
+                            const float2 b = __half22float2(*(const __half2 *)&l[8 * q + i]);
+                            a.x = __fadd_rn(a.x, b.x), a.y = __fadd_rn(a.y, b.y);
+                        }
+                        f[2 * i] = __fmaf_rn(a.x, P.f_add, f[2 * i]), f[2 * i + 1] = __fmaf_rn(a.y, P.f_add, f[2 * i + 1]);
+                    }
+                }
+                if (P.result && P.dtype == CONEF_BF16) {
+#pragma unroll
+                    for (int i = 0; i < 8; ++i)
+                        h[8 * q + i] = Vec16<__nv_bfloat16>::pack2(f[2 * i], f[2 * i + 1]);
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 8; ++i)
+                        h[8 * q + i] = Vec16<__half>::pack2(f[2 * i], f[2 * i + 1]);
+                    if (P.out_lo) {
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) {
+                            const float2 r = __half22float2(*(const __half2 *)&h[8 * q + i]);
+                            l[8 * q + i] = Vec16<__half>::pack2(__fsub_rn(f[2 * i], r.x), __fsub_rn(f[2 * i + 1], r.y));
+                        }
                     }
                 }
             }
@@ -479,23 +500,33 @@ __global__ void __launch_bounds__(kMmThreads, 1) k_ns_product(const __grid_const
                 if (!P.wide)
                     ns_result(P, t.batch, row, col, h);
                 else if (P.flip)
-                    staging_store<true>(staging, lane, h, &maps.th, row0, col, t.batch);
+                    staging_store<true>(staging, true, lane, h, &maps.th, row0, col, t.batch);
                 else
-                    staging_store<false>(staging, lane, h, &maps.oh, col, row0, t.batch);
+                    staging_store<false>(staging, true, lane, h, &maps.oh, col, row0, t.batch);
                 continue;
             }
+            // Up to four stores.  Behind the last tile's sums the ring is free, and they need not wait for one another.
+            const uint32_t more = ok && tile + step >= P.n_tiles ? min(3u, P.stages * P.stage_bytes / (BN / 16 * kNsStaging)) : 0u;
             const bool mirror = P.symmetric && t.i != (P.tiles_wide ? t.j / 2 : t.j);
-            staging_store<false>(staging, lane, h, &maps.oh, col, row0, t.batch);
-            if (P.out_lo)
-                staging_store<false>(staging, lane, l, &maps.ol, col, row0, t.batch);
+            uint32_t nth = 0;
+            auto place = [&](uint32_t n) { return n && n <= more ? tc::saddr(ring) + (warp * more + n - 1) * kNsStaging : staging; };
+            auto again = [&](uint32_t n) { return n == 0 || n > more; };
+            staging_store<false>(staging, true, lane, h, &maps.oh, col, row0, t.batch);
+            if (P.out_lo) {
+                ++nth;
+                staging_store<false>(place(nth), again(nth), lane, l, &maps.ol, col, row0, t.batch);
+            }
             if (mirror) {
-                staging_store<true>(staging, lane, h, &maps.th, row0, col, t.batch);
-                if (P.out_lo)
-                    staging_store<true>(staging, lane, l, &maps.tl, row0, col, t.batch);
+                ++nth;
+                staging_store<true>(place(nth), again(nth), lane, h, &maps.th, row0, col, t.batch);
+                if (P.out_lo) {
+                    ++nth;
+                    staging_store<true>(place(nth), again(nth), lane, l, &maps.tl, row0, col, t.batch);
+                }
             }
         }
         if (lane == 0)
-            tc::store_wait();
+            tc::store_wait_read();   // (what the launch behind waits for is the whole grid's end)
         __syncwarp();
     }
     tc::fence_before();

@@ -95,6 +95,8 @@ __device__ __forceinline__ uint32_t load_at(uint32_t at)
 __device__ __forceinline__ void bar_arrive_at(uint32_t bar) { asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory"); }
 
 // ------------------------------------------------------------------ asynchronous copies into shared memory
+// (a map is a parameter of the kernel: it may be looked up before what the launch ahead writes is there)
+__device__ __forceinline__ void prefetch_map(const void *map) { asm volatile("prefetch.tensormap [%0];" ::"l"(map) : "memory"); }
 __device__ __forceinline__ void tile_load(uint32_t dst, const void *map, uint32_t x, uint32_t y, uint64_t *bar)
 {
     asm volatile("cp.async.bulk.tensor.2d.shared::cta.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(dst), "l"(map), "r"(x), "r"(y),
