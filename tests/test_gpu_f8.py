@@ -250,5 +250,8 @@ def test_refusals(b):
         assert e.value.code == b.ERR_INVALID_ARG
 
 
-def test_nothing_ran_out(b):
-    assert b.f8_timeouts() == 0
+def test_nothing_runs_out(b):
+    before = b.f8_timeouts()
+    a, c = b.f8_quantise(matrix(3330, 2100, torch.bfloat16)), b.f8_quantise(matrix(4113, 2100, torch.bfloat16, 1))
+    assert not torch.isnan(b.f8_matmul(a, c)).any()
+    assert b.f8_timeouts() == before

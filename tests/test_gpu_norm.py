@@ -1,4 +1,6 @@
 """Root-mean-square norms with the residual's addition, their 8-bit forms and their gradient, against the plain statement in 64 bits."""
+import ctypes as C
+
 import numpy as np
 import pytest
 import torch
@@ -218,6 +220,42 @@ def test_any_leading_dimensions_streams_and_graphs(b):
         again = b.rms_norm(x, w, add=r, forms="both")
         assert torch.equal(out.y[0].codes, again.y[0].codes) and torch.equal(out.y[1].codes, again.y[1].codes)
         assert all(torch.equal(p, q) for p, q in zip(got, b.rms_norm_grad(x, again.h, w, again.rstd, add=r)))
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("rows,cols", [(40, 100), (300, 1600), (37, 1301), (5, 20001)])
+def test_in_place(b, rows, cols, dtype):
+    """h in x's or the residual's place, y in any of theirs, dx in dy's or the other gradient's."""
+    x, r, w = matrix(rows, cols, dtype), matrix(rows, cols, dtype, 1), weight(cols, dtype)
+    want = b.rms_norm(x, w, 1e-5, add=r)
+    kind = {torch.float32: b.F32, torch.bfloat16: b.BF16, torch.float16: b.F16}[dtype]
+
+    def norm(x, add, h, y):
+        rstd = torch.empty(rows, device="cuda")
+        rc = b.lib.conef_rms_norm(x.data_ptr(), add.data_ptr() if add is not None else None, w.data_ptr(), kind, kind, rows, cols, cols, cols, 1e-5,
+                                  h.data_ptr() if h is not None else None, cols, rstd.data_ptr(), y.data_ptr(), cols, 0, None, None, None, None, None)
+        assert rc == b.OK
+        return rstd
+
+    for places in (("x", "r"), ("r", "x"), ("x", "x"), ("r", "r")):
+        t = dict(x=x.clone(), r=r.clone())
+        rstd = norm(t["x"], t["r"], t[places[0]], t[places[1]])
+        assert torch.equal(t[places[1]], want.y) and torch.equal(rstd, want.rstd)
+        if places[0] != places[1]:
+            assert torch.equal(t[places[0]], want.h)
+    alone = x.clone()
+    norm(alone, None, None, alone)
+    assert torch.equal(alone, b.rms_norm(x, w, 1e-5).y)
+    dx, dw = b.rms_norm_grad(r, want.h, w, want.rstd, add=x)
+    for place in ("dy", "add"):
+        t, got = dict(dy=r.clone(), add=x.clone()), torch.empty(cols, device="cuda")
+        size = C.c_size_t()
+        assert b.lib.conef_rms_norm_grad_bytes(rows, cols, C.byref(size)) == b.OK
+        space = torch.empty(size.value, dtype=torch.uint8, device="cuda")
+        rc = b.lib.conef_rms_norm_grad(t["dy"].data_ptr(), want.h.data_ptr(), w.data_ptr(), want.rstd.data_ptr(), t["add"].data_ptr(), kind, kind, rows, cols, cols, cols, cols,
+                                       t[place].data_ptr(), cols, got.data_ptr(), space.data_ptr(), size.value, None)
+        assert rc == b.OK
+        assert torch.equal(t[place], dx) and torch.equal(got, dw)
 
 
 def test_in_an_autograd_function(b):

@@ -156,5 +156,7 @@ def test_refusals(b):
         assert e.value.code == b.ERR_INVALID_ARG
 
 
-def test_nothing_ran_out(b):
-    assert b.orthogonalise_timeouts() == 0
+def test_nothing_runs_out(b):
+    before = b.orthogonalise_timeouts()
+    assert not torch.isnan(b.orthogonalise(update(700, 1300, torch.bfloat16))).any()
+    assert b.orthogonalise_timeouts() == before

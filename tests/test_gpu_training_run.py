@@ -24,6 +24,7 @@ def test_a_layer_trains(b):
     ctx = b.ConEF([(OUT, IN, 1)], WORKERS, dict(kind="randk", k_num=1, k_den=2, seed=3), dict(kind="int8", block=256), 1.0)
     w, gain = matrix(OUT, IN, torch.float32, 1, 0.02), torch.ones(IN, device="cuda") * 1.25
     momentum = torch.zeros(OUT, IN, device="cuda")
+    before = b.f8_timeouts()
     for t in range(2):
         grads = []
         w_rows, w_cols = b.f8_quantise(w, "both", square=True)
@@ -60,4 +61,4 @@ def test_a_layer_trains(b):
         step = b.orthogonalise(momentum, scale=-0.02)
         assert far(step, fo.orthogonalise(f64(momentum), 5, (3.4445, -4.7750, 2.0315), -0.02)) <= 2.0 ** -8 + 5e-4
         w += step
-    assert torch.isfinite(w).all() and ctx.last_status() == 0 and b.f8_timeouts() == 0
+    assert torch.isfinite(w).all() and ctx.last_status() == 0 and b.f8_timeouts() == before
