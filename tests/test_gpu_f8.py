@@ -184,6 +184,32 @@ def test_product_scales_and_single_elements(b):
     check_product(b.f8_matmul(fa, fc, torch.float32), values(fa), values(fc), torch.float32)
 
 
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("m", [1, 2, 7, 8, 9, 15, 16, 17])
+def test_product_of_few_rows(b, m, dtype):
+    """... of either side."""
+    for n, k in ((1, 1), (17, 33), (100, 1300), (640, 128), (301, 4100)):
+        a, c = b.f8_quantise(matrix(m, k, torch.float32), kind="e5m2"), b.f8_quantise(matrix(n, k, torch.float32, 1, 0.02))
+        got = b.f8_matmul(a, c, dtype)
+        check_product(got, values(a), values(c), dtype)
+        turned = b.f8_matmul(c, a, dtype)
+        check_product(turned, values(c), values(a), dtype)
+
+
+def test_product_of_few_rows_with_nan_blocks_and_far_scales(b):
+    for m in (3, 12):
+        x, w = matrix(m, 640, torch.bfloat16), matrix(70, 640, torch.bfloat16, 1)
+        x[1, 200] = float("nan")
+        w[66, 639] = float("inf")
+        out = b.f8_matmul(b.f8_quantise(x), b.f8_quantise(w))
+        bad = torch.zeros_like(out, dtype=torch.bool)
+        bad[1], bad[:, 66] = True, True
+        assert torch.equal(torch.isnan(out), bad)
+        for up, down in ((2.0 ** 118, 2.0 ** -118), (2.0 ** -120, 2.0 ** 119), (2.0 ** 60, 2.0 ** -100)):
+            a, c = b.f8_quantise(matrix(m, 300, torch.float32).clamp(-200, 200) * up), b.f8_quantise(matrix(40, 300, torch.float32, 1).clamp(-200, 200) * down)
+            check_product(b.f8_matmul(a, c, torch.float32), values(a), values(c), torch.float32)
+
+
 def test_product_with_nan_blocks(b):
     x, w = matrix(140, 640, torch.bfloat16), matrix(70, 640, torch.bfloat16, 1)
     x[5, 200] = float("nan")
