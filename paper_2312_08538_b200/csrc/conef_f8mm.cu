@@ -43,24 +43,29 @@ struct F8Format {
 };
 
 // ------------------------------------------------------------------ few rows against many
-// Up to 16 rows of one side (tokens) against all of the other's (a weight's), which are read once: 1 x 6400 x 1600 are 10 MB, 1.6 us.  A tile of tcgen05.mma would have
-// 128 rows with one used, and a chain of copies and barriers for each (9.5 us); here a warp takes 16 rows of the weight and a share of the blocks along k, eight
-// warps a row group, straight from memory to registers, where codes become fp16 (exactly) for mma.m16n8k16.  A lane has 16 bytes of two rows
-// and of a token at a time: the instruction's order of k is any that both sides share.  Sums of a block are fp32, times its two scales' power of two, and added in fp32.
+// Up to eight rows of one side (tokens) against all of the other's (a weight's), which are read once: 1 x 6400 x 1600 are 10 MB, 1.6 us.  A tile of tcgen05.mma would have
+// 128 rows with one used, and a chain of copies and barriers for each (9.5 us; here 5.3); here a warp takes 16 rows of the weight and a share
+// of the blocks along k, straight from memory to the registers of mma.m16n8k32.  A lane has 16 bytes of two rows and of a
+// token at a time: the instruction's order of k is any that both sides share.  Sums of a block are fp32, times its two scales' power of two, and added in fp32.
 constexpr int kFewWarps = 8;
-// four codes to two pairs of fp16
-__device__ __forceinline__ void few_halves(uint32_t w, uint32_t kind, uint32_t &lo, uint32_t &hi)
+constexpr uint32_t kFewAhead = 4;
+// 16 rows of the weight by eight tokens and 32 of k; KINDS: 0 to 3, the weight's kind and twice the tokens'
+template <int KINDS>
+__device__ __forceinline__ void few_product(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1)
 {
-    if (kind == CONEF_E4M3)
-        asm("{\n\t.reg .b16 a, b;\n\tmov.b32 {a, b}, %2;\n\tcvt.rn.f16x2.e4m3x2 %0, a;\n\tcvt.rn.f16x2.e4m3x2 %1, b;\n\t}" : "=r"(lo), "=r"(hi) : "r"(w));
+#define FEW_PRODUCT(KW, KT)                                                                                                                                              \
+    asm("mma.sync.aligned.m16n8k32.row.col.f32." KW "." KT ".f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"                                        \
+        : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])                                                                                                                 \
+        : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1))
+    if constexpr (KINDS == 0)
+        FEW_PRODUCT("e4m3", "e4m3");
+    else if constexpr (KINDS == 1)
+        FEW_PRODUCT("e5m2", "e4m3");
+    else if constexpr (KINDS == 2)
+        FEW_PRODUCT("e4m3", "e5m2");
     else
-        asm("{\n\t.reg .b16 a, b;\n\tmov.b32 {a, b}, %2;\n\tcvt.rn.f16x2.e5m2x2 %0, a;\n\tcvt.rn.f16x2.e5m2x2 %1, b;\n\t}" : "=r"(lo), "=r"(hi) : "r"(w));
-}
-__device__ __forceinline__ void few_product(float (&d)[4], const uint32_t (&a)[4], const uint32_t (&b)[2])
-{
-    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
-        : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
-        : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b[0]), "r"(b[1]));
+        FEW_PRODUCT("e5m2", "e5m2");
+#undef FEW_PRODUCT
 }
 // v 2^(E + F) for scale bytes e and f, in two steps, neither of which leaves the range where the result does not
 __device__ __forceinline__ float few_scaled(float v, uint32_t e, uint32_t f)
@@ -72,82 +77,109 @@ __device__ __forceinline__ float few_scaled(float v, uint32_t e, uint32_t f)
 struct FewArgs {
     const uint8_t *w, *ws, *t, *ts;   // codes and scales: the weight's, the tokens'
     uint32_t rows, tokens, blocks, tiles;
-    uint32_t kind_w, kind_t;
+    uint32_t share;                   // warps that share a row group's blocks: 1, 2, 4 or 8
     int64_t row_step, token_step;     // of the output, in elements
 };
-template <class T, int NT>   // NT: groups of eight tokens
-__global__ void __launch_bounds__(kFewWarps * 32) k_f8_few(const __grid_constant__ FewArgs P, T *out)
+template <class T, int KINDS>
+__global__ void __launch_bounds__(kFewWarps * 32, 3) k_f8_few(const FewArgs P, T *out)
 {
-    __shared__ float part[kFewWarps][NT * 8][17];
+    extern __shared__ __align__(16) uint8_t few_smem[];
+    __shared__ float part[kFewWarps][8][17];
     grid_release();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, q = lane & 3, g = lane >> 2;
     const uint64_t pitch = (uint64_t)P.blocks * 128u;
-    const uint32_t row0 = blockIdx.x * 16 + g, row1 = row0 + 8;
-    const uint8_t *const w0 = P.w + min(row0, P.rows - 1) * pitch + q * 16, *const w1 = P.w + min(row1, P.rows - 1) * pitch + q * 16;   // (what does not exist is not stored)
-    const uint8_t *t[NT];
-#pragma unroll
-    for (int n = 0; n < NT; ++n)
-        t[n] = P.t + min((uint32_t)(n * 8 + g), P.tokens - 1) * pitch + q * 16;
-    float sum[NT][4] = {};
+    const uint32_t first = blockIdx.x * (kFewWarps / P.share) * 16, row0 = first + warp / P.share * 16 + g, row1 = row0 + 8;
+    const uint32_t have0 = min(row0, P.rows - 1), have1 = min(row1, P.rows - 1);   // (what does not exist is not stored)
+    const uint8_t *const w0 = P.w + have0 * pitch + q * 16, *const w1 = P.w + have1 * pitch + q * 16, *const t = P.t + min((uint32_t)g, P.tokens - 1) * pitch + q * 16;
+    const uint8_t *const s0 = P.ws + f8_scale_at32(have0, 0, P.tiles), *const s1 = P.ws + f8_scale_at32(have1, 0, P.tiles), *const ts = P.ts + f8_scale_at32(2 * q, 0, P.tiles);
+    float sum[4] = {};
     grid_wait();
-#pragma unroll 2
-    for (uint32_t b = warp; b < P.blocks; b += kFewWarps) {
-        uint4 x[2], y[2], z[NT][2];
+    // The weight's blocks ahead are copied into shared memory, each lane what it will read, kFewAhead of 2 KB to a warp; scales and tokens, which L1 has after a while, come one
+    // block ahead in registers.  (Tokens by copies that pass L1 by are the same lines of L2 for all SMs: 1 x 50257 x 1600 23 -> 74 us.)
+    uint8_t *const mine = few_smem + (warp * kFewAhead * 4 * 32 + lane) * 16;
+    auto copy16 = [](uint8_t *to, const uint8_t *from) {
+        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"((uint32_t)__cvta_generic_to_shared(to)), "l"(from) : "memory");
+    };
+    auto ask = [&](uint32_t b, uint32_t stage) {
+        if (b < P.blocks) {
+            uint8_t *const to = mine + stage * 2048;
+            const uint64_t at = b * 128ull;
+            copy16(to, w0 + at), copy16(to + 512, w0 + at + 64), copy16(to + 1024, w1 + at), copy16(to + 1536, w1 + at + 64);
+        }
+        asm volatile("cp.async.commit_group;" ::: "memory");
+    };
+    struct Rest {
+        uint4 z[2];
+        uint32_t e0, e1, f0, f1;
+    } now, next;
+    auto ask_rest = [&](uint32_t b) {
+        const uint64_t at = (uint64_t)(b >> 2) * 512u + (b & 3u);
+        next.z[0] = *(const uint4 *)(t + b * 128ull), next.z[1] = *(const uint4 *)(t + b * 128ull + 64);
+        next.e0 = s0[at], next.e1 = s1[at], next.f0 = ts[at], next.f1 = ts[at + 16];   // (token 2 q + 1: 16 bytes on)
+    };
+    uint32_t b = warp % P.share, stage = 0;
+#pragma unroll
+    for (uint32_t i = 0; i < kFewAhead - 1; ++i)
+        ask(b + i * P.share, i);
+    if (b < P.blocks)
+        ask_rest(b);
+    for (; b < P.blocks; b += P.share) {
+        ask(b + (kFewAhead - 1) * P.share, (stage + kFewAhead - 1) % kFewAhead);
+        now = next;
+        if (b + P.share < P.blocks)
+            ask_rest(b + P.share);
+        asm volatile("cp.async.wait_group %0;" ::"n"(kFewAhead - 1) : "memory");
+        const uint8_t *const from = mine + stage * 2048;
+        stage = (stage + 1) % kFewAhead;
+        uint4 x[2], y[2];
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+            x[h] = *(const uint4 *)(from + h * 512), y[h] = *(const uint4 *)(from + 1024 + h * 512);
+        const uint4(&z)[2] = now.z;
+        const uint32_t e0 = now.e0, e1 = now.e1, f0 = now.f0, f1 = now.f1;
+        float d[4] = {};
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-            x[h] = __ldcs((const uint4 *)(w0 + b * 128ull + h * 64));
-            y[h] = __ldcs((const uint4 *)(w1 + b * 128ull + h * 64));
-#pragma unroll
-            for (int n = 0; n < NT; ++n)
-                z[n][h] = *(const uint4 *)(t[n] + b * 128ull + h * 64);
+            few_product<KINDS>(d, x[h].x, y[h].x, x[h].y, y[h].y, z[h].x, z[h].y);
+            few_product<KINDS>(d, x[h].z, y[h].z, x[h].w, y[h].w, z[h].z, z[h].w);
         }
-        const uint32_t e0 = P.ws[f8_scale_at32(row0, b, P.tiles)], e1 = P.ws[f8_scale_at32(row1, b, P.tiles)];   // (scales of rows that do not exist do)
-        float d[NT][4] = {};
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            const uint32_t xw[4] = {x[h].x, x[h].y, x[h].z, x[h].w}, yw[4] = {y[h].x, y[h].y, y[h].z, y[h].w};
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                uint32_t a[4];
-                few_halves(xw[i], P.kind_w, a[0], a[2]);
-                few_halves(yw[i], P.kind_w, a[1], a[3]);
-#pragma unroll
-                for (int n = 0; n < NT; ++n) {
-                    const uint32_t zw[4] = {z[n][h].x, z[n][h].y, z[n][h].z, z[n][h].w};
-                    uint32_t c[2];
-                    few_halves(zw[i], P.kind_t, c[0], c[1]);
-                    few_product(d[n], a, c);
-                }
-            }
-        }
-#pragma unroll
-        for (int n = 0; n < NT; ++n) {
-            const uint32_t f0 = P.ts[f8_scale_at32(n * 8 + 2 * q, b, P.tiles)], f1 = P.ts[f8_scale_at32(n * 8 + 2 * q + 1, b, P.tiles)];
-            sum[n][0] = __fadd_rn(sum[n][0], few_scaled(d[n][0], e0, f0)), sum[n][1] = __fadd_rn(sum[n][1], few_scaled(d[n][1], e0, f1));
-            sum[n][2] = __fadd_rn(sum[n][2], few_scaled(d[n][2], e1, f0)), sum[n][3] = __fadd_rn(sum[n][3], few_scaled(d[n][3], e1, f1));
+        // the two scales' product, where it is a normal number (and neither of them NaN: 255 and 127 or more are not)
+        const uint32_t least = min(e0, e1) + min(f0, f1), most = max(e0, e1) + max(f0, f1);
+        if (__all_sync(0xffffffffu, least > 127u && most < 382u && max(max(e0, e1), max(f0, f1)) < kF8Nan)) {
+            sum[0] = __fmaf_rn(d[0], __uint_as_float((e0 + f0 - 127u) << 23), sum[0]), sum[1] = __fmaf_rn(d[1], __uint_as_float((e0 + f1 - 127u) << 23), sum[1]);
+            sum[2] = __fmaf_rn(d[2], __uint_as_float((e1 + f0 - 127u) << 23), sum[2]), sum[3] = __fmaf_rn(d[3], __uint_as_float((e1 + f1 - 127u) << 23), sum[3]);
+        } else {
+            sum[0] = __fadd_rn(sum[0], few_scaled(d[0], e0, f0)), sum[1] = __fadd_rn(sum[1], few_scaled(d[1], e0, f1));
+            sum[2] = __fadd_rn(sum[2], few_scaled(d[2], e1, f0)), sum[3] = __fadd_rn(sum[3], few_scaled(d[3], e1, f1));
         }
     }
-#pragma unroll
-    for (int n = 0; n < NT; ++n) {
-        part[warp][n * 8 + 2 * q][g] = sum[n][0], part[warp][n * 8 + 2 * q + 1][g] = sum[n][1];
-        part[warp][n * 8 + 2 * q][g + 8] = sum[n][2], part[warp][n * 8 + 2 * q + 1][g + 8] = sum[n][3];
-    }
+    part[warp][2 * q][g] = sum[0], part[warp][2 * q + 1][g] = sum[1];
+    part[warp][2 * q][g + 8] = sum[2], part[warp][2 * q + 1][g + 8] = sum[3];
     __syncthreads();
-    if (threadIdx.x < NT * 128) {
-        const uint32_t token = threadIdx.x >> 4, r = threadIdx.x & 15, row = blockIdx.x * 16 + r;
-        float s = part[0][token][r];
-#pragma unroll
-        for (int i = 1; i < kFewWarps; ++i)
-            s = __fadd_rn(s, part[i][token][r]);
+    for (uint32_t i = threadIdx.x; i < (kFewWarps / P.share) * 128u; i += kFewWarps * 32) {
+        const uint32_t group = i >> 7, token = i >> 4 & 7u, r = i & 15u, row = first + group * 16 + r;
+        float s = part[group * P.share][token][r];
+        for (uint32_t k = 1; k < P.share; ++k)
+            s = __fadd_rn(s, part[group * P.share + k][token][r]);
         if (token < P.tokens && row < P.rows)
             out[token * P.token_step + row * P.row_step] = from_f32<T>(s);
     }
 }
 template <class T>
-static cudaError_t few(const FewArgs &P, T *out, cudaStream_t s)
+static cudaError_t few(FewArgs P, int kind_w, int kind_t, T *out, cudaStream_t s)
 {
-    const dim3 grid((P.rows + 15) / 16);
-    return P.tokens <= 8 ? launch(k_f8_few<T, 1>, grid, kFewWarps * 32, 0, s, P, out) : launch(k_f8_few<T, 2>, grid, kFewWarps * 32, 0, s, P, out);
+    // as many warps as the SMs hold, 24 each, with as many blocks as that leaves (1 x 6400 x 1600 with 12 to an SM 6.4, with 24 5.3 us)
+    const int64_t groups = ((int64_t)P.rows + 15) / 16;
+    P.share = kFewWarps;
+    while (P.share > 1 && groups * P.share > kPlanSMs * 24)
+        P.share /= 2;
+    const int64_t per_cta = kFewWarps / P.share;
+    static void (*const kernels[4])(FewArgs, T *) = {k_f8_few<T, 0>, k_f8_few<T, 1>, k_f8_few<T, 2>, k_f8_few<T, 3>};
+    constexpr size_t smem = kFewWarps * kFewAhead * 2048;
+    static int done[4][64];
+    const int kinds = kind_w + 2 * kind_t;
+    const cudaError_t e = opt_in_smem(kernels[kinds], smem, done[kinds]);
+    return e != cudaSuccess ? e : launch(kernels[kinds], dim3((unsigned)((groups + per_cta - 1) / per_cta)), kFewWarps * 32, smem, s, P, out);
 }
 
 }  // namespace conef
@@ -177,14 +209,14 @@ int conef_f8_matmul(const void *a_codes, const void *a_scales, int a_kind, int64
                         "conef_f8_matmul");
     return with_elem(dtype, [&](auto t) {
         using T = decltype(t);
-        if (std::min(m, n) <= 16) {
+        if (std::min(m, n) <= 8) {
             const bool turned = n < m;   // (the weight's rows are A's)
             FewArgs P = {(const uint8_t *)b_codes, (const uint8_t *)b_scales, (const uint8_t *)a_codes, (const uint8_t *)a_scales, (uint32_t)n, (uint32_t)m, (uint32_t)f8_blocks(k),
-                         (uint32_t)f8_scale_tiles(k), (uint32_t)b_kind, (uint32_t)a_kind, 1, ld};
+                         (uint32_t)f8_scale_tiles(k), 0, 1, ld};
             if (turned)
                 P = {(const uint8_t *)a_codes, (const uint8_t *)a_scales, (const uint8_t *)b_codes, (const uint8_t *)b_scales, (uint32_t)m, (uint32_t)n, P.blocks, P.tiles,
-                     (uint32_t)a_kind, (uint32_t)b_kind, ld, 1};
-            return launched(few(P, (T *)out, (cudaStream_t)stream), "conef_f8_matmul");
+                     0, ld, 1};
+            return launched(few(P, turned ? a_kind : b_kind, turned ? b_kind : a_kind, (T *)out, (cudaStream_t)stream), "conef_f8_matmul");
         }
         const MmChoice c = mm_choice<F8Format>(m, n, k);
         return (c.pair ? matmul<F8Format, T, true> : matmul<F8Format, T, false>)((const uint8_t *)a_codes, (const uint8_t *)a_scales, m, (const uint8_t *)b_codes,
