@@ -57,7 +57,7 @@ struct TileArgs {
     const void *w;
     F8Out out;
     uint32_t tiles_c;
-    bool w32, square, aligned32;
+    bool w32, square, aligned32, whole;   // whole: the transpose's codes begin on 32 bytes
 };
 template <class T, bool NORM>
 __host__ __device__ constexpr int tile_threads() { return NORM || sizeof(T) == 4 ? 512 : 256; }
@@ -171,11 +171,9 @@ __global__ void __launch_bounds__((tile_threads<T, NORM>()), NORM || sizeof(T) =
             const uint32_t byte = f8_scale(most, kind);
             uint32_t code;
             f8_encode<4>(v, byte, kind, &code);
-            if (row < A.rows) {
-#pragma unroll
-                for (int q = 0; q < 4; ++q)
-                    A.out.codes[(row * blocks + c0 / 128) * 128 + q * 32 + lane] = (uint8_t)(code >> (8 * q));
-            }
+            code = bytes_turned(code, lane);
+            if (row < A.rows)
+                *(uint32_t *)(A.out.codes + (row * blocks + c0 / 128) * 128 + (lane & 3) * 32 + (lane >> 2) * 4) = code;
             if (lane == 0)
                 A.out.scales[f8_scale_at(row, c0 / 128, scale_tiles)] = (uint8_t)(row < A.rows ? byte : 0u);
         };
@@ -278,8 +276,12 @@ __global__ void __launch_bounds__((tile_threads<T, NORM>()), NORM || sizeof(T) =
     auto store = [&](int64_t column, uint32_t byte, const uint32_t *code) {
         if (column < A.cols) {
             uint4 *const to = (uint4 *)(A.out.codes_t + (column * blocks_t + r0 / 128) * 128 + quarter * 32);
-            to[0] = make_uint4(code[0], code[1], code[2], code[3]);
-            to[1] = make_uint4(code[4], code[5], code[6], code[7]);
+            if (A.whole) {   // (a sector at once)
+                store32_keep(to, *(const uint32_t(*)[8])code);
+            } else {
+                to[0] = make_uint4(code[0], code[1], code[2], code[3]);
+                to[1] = make_uint4(code[4], code[5], code[6], code[7]);
+            }
         }
         if (quarter == 0)
             A.out.scales_t[f8_scale_at(column, r0 / 128, scale_tiles_t)] = (uint8_t)(column < A.cols ? byte : 0u);
@@ -334,13 +336,8 @@ __global__ void __launch_bounds__(kF8Threads) k_f8_dequantise(const uint8_t *cod
         const uint32_t bytes = *(const uint32_t *)s;
 #pragma unroll
         for (int b = 0; b < 4; ++b) {
-            uint32_t w = 0;
-#pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                const uint32_t c = c0 + b * 128 + q * 32 + lane;
-                w |= c < cols ? (uint32_t)from[c] << (8 * q) : 0u;
-            }
-            f8_values4(w, kind, v + 4 * b);
+            const uint32_t c = c0 + b * 128 + (lane & 3) * 32 + (lane >> 2) * 4;   // (rows are padded to blocks)
+            f8_values4(bytes_turned(c0 / 128 + b < blocks ? *(const uint32_t *)(from + c) : 0u, lane), kind, v + 4 * b);
             const float f = f8_pow(bytes >> (8 * b) & 255u);
 #pragma unroll
             for (int q = 0; q < 4; ++q)
@@ -383,7 +380,7 @@ static cudaError_t tiles_form(const T *x, const TileArgs &A, int64_t n_tiles, cu
 cudaError_t f8_tiles(const void *x, int dtype, int64_t rows, int64_t cols, int64_t ld, const float *rstd, const void *w, bool w32, bool square, const F8Out &out,
                      cudaStream_t s)
 {
-    TileArgs A = {rows, cols, ld, rstd, w, out, (uint32_t)(f8_scale_tiles(cols) * 4), w32, square, false};
+    TileArgs A = {rows, cols, ld, rstd, w, out, (uint32_t)(f8_scale_tiles(cols) * 4), w32, square, false, ((uintptr_t)out.codes_t & 31) == 0};
     const int64_t tiles_r = out.codes_t ? f8_scale_tiles(rows) * 4 : (rows + 127) / 128;
     cudaError_t e = cudaErrorInvalidValue;
     with_elem(dtype, [&](auto t) {

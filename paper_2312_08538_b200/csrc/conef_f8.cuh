@@ -84,6 +84,16 @@ __device__ __forceinline__ void f8_values4(uint32_t w, int kind, float *v)
 template <bool VEC, int N>
 __device__ __forceinline__ uint32_t lane_col(uint32_t c0, int lane, int q) { return VEC ? c0 + lane * N + q : c0 + (q >> 2) * 128 + (q & 3) * 32 + lane; }
 
+// Bytes 0 to 3 of four neighbouring lanes, turned: lane i has byte i of each.  So codes of every 32nd element of a block leave, and come, as words (8192 x 1601 in bf16
+// to codes byte by byte 14.7 us, values of codes 20.8).
+__device__ __forceinline__ uint32_t bytes_turned(uint32_t w, int lane)
+{
+    uint32_t o = __shfl_xor_sync(0xffffffffu, w, 1);
+    w = __byte_perm(w, o, lane & 1 ? 0x3715 : 0x6240);
+    o = __shfl_xor_sync(0xffffffffu, w, 2);
+    return __byte_perm(w, o, lane & 2 ? 0x3276 : 0x5410);
+}
+
 // 32 bytes that other kernels may read again
 __device__ __forceinline__ void load32_keep(const void *p, uint32_t (&w)[8])
 {
@@ -240,11 +250,10 @@ __device__ __forceinline__ void f8_store_row(const float *v, uint32_t c0, uint32
             const uint32_t byte = f8_scale(most, kind);
             uint32_t code;
             f8_encode<4>(v + 4 * b, byte, kind, &code);
+            code = bytes_turned(code, lane);
             if (there && c0 / 128 + b < blocks) {
                 bytes |= byte << (8 * b);
-#pragma unroll
-                for (int q = 0; q < 4; ++q)
-                    codes_row[c0 + b * 128 + q * 32 + lane] = (uint8_t)(code >> (8 * q));
+                *(uint32_t *)(codes_row + c0 + b * 128 + (lane & 3) * 32 + (lane >> 2) * 4) = code;
             }
         }
         if (lane < N / 4)
