@@ -56,25 +56,48 @@ __global__ void __launch_bounds__(256) k_ns_squares(const __grid_constant__ NsIn
     const T *const x = (const T *)A.x + blockIdx.y * A.stride;
     grid_wait();
     double sum = 0;
-    for (int64_t row = (int64_t)blockIdx.x * 8 + warp; row < A.rows; row += (int64_t)A.n_parts * 8)
-#pragma unroll 4
-        for (int64_t c = (int64_t)lane * N; c < A.cols; c += 32 * N) {
-            float v[N];
-            if constexpr (VEC) {
-                if (c + N <= A.cols) {
-                    Vec16<T>::unpack(*(const uint4 *)(x + row * A.ld + c), v);
-                } else {
+    auto add = [&](const float *v) {
 #pragma unroll
-                    for (int q = 0; q < N; ++q)
-                        v[q] = c + q < A.cols ? to_f32(x[row * A.ld + c + q]) : 0.f;
-                }
-            } else {
-                v[0] = to_f32(x[row * A.ld + c]);
-            }
+        for (int q = 0; q < N; ++q)
+            sum = __fma_rn((double)v[q], (double)v[q], sum);
+    };
+    // N elements of a row's, or fewer at its end
+    auto piece = [&](const T *p, int64_t have) {
+        float v[N];
+        if (VEC && have >= N) {
+            if constexpr (VEC)
+                Vec16<T>::unpack(*(const uint4 *)p, v);
+        } else {
 #pragma unroll
             for (int q = 0; q < N; ++q)
-                sum = __fma_rn((double)v[q], (double)v[q], sum);
+                v[q] = q < have ? to_f32(p[q]) : 0.f;
         }
+        add(v);
+    };
+    if (VEC && A.ld == A.cols) {   // one array: four pieces of each thread's on their way
+        const int64_t all = A.rows * A.cols, step = (int64_t)A.n_parts * 256 * N;
+        int64_t at = ((int64_t)blockIdx.x * 256 + threadIdx.x) * N;
+        for (; at + 3 * step + N <= all; at += 4 * step) {
+            uint4 w[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                w[i] = *(const uint4 *)(x + at + i * step);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                float v[N];
+                if constexpr (VEC)
+                    Vec16<T>::unpack(w[i], v);
+                add(v);
+            }
+        }
+        for (; at < all; at += step)
+            piece(x + at, all - at);
+    } else {
+        for (int64_t row = (int64_t)blockIdx.x * 8 + warp; row < A.rows; row += (int64_t)A.n_parts * 8)
+#pragma unroll 4
+            for (int64_t c = (int64_t)lane * N; c < A.cols; c += 32 * N)
+                piece(x + row * A.ld + c, A.cols - c);
+    }
 #pragma unroll
     for (int o = 16; o; o /= 2)
         sum += __shfl_xor_sync(0xffffffffu, sum, o);
@@ -781,7 +804,7 @@ int conef_orthogonalise(const void *x, int dtype, int64_t batch, int64_t rows, i
         return m;
     };
     Split X = take(z.m, z.pitch_x), Y = take(z.m, z.pitch_x), A = take(z.n, z.pitch_a), C = take(z.n, z.pitch_a);
-    NsIn in = {x, rows, cols, ld, stride, (double *)at, (uint32_t)std::min<int64_t>(kNsParts, (rows + 7) / 8)};
+    NsIn in = {x, rows, cols, ld, stride, (double *)at, (uint32_t)std::min<int64_t>(kNsParts, (rows * cols + 8191) / 8192)};
     double sx = fp16_scale(top[0]);
     cudaError_t e = cudaErrorInvalidValue;
     const int64_t tiles_c = (cols + 63) / 64, tiles = (rows + 63) / 64 * tiles_c;
