@@ -316,7 +316,7 @@ struct NormGradArgs {
     float share;
     bool w32, aligned32, aligned_w;
 };
-// GIVEN: the means are; a block has every gridDim.y-th 8192 columns
+// GIVEN: the means are; a block has 8192 columns (the grid's first dimension, of which there may be more than 65535) of its rows (the second)
 template <class T, bool VEC, bool ALONE, bool GIVEN>
 __global__ void __launch_bounds__(ALONE ? 256 : 1024, ALONE ? 4 : 1) k_norm_grad(const __grid_constant__ NormGradArgs A)
 {
@@ -326,9 +326,9 @@ __global__ void __launch_bounds__(ALONE ? 256 : 1024, ALONE ? 4 : 1) k_norm_grad
     __shared__ float other[ALONE ? 8 * kNormWarp : 1];
     grid_release();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, warps = blockDim.x >> 5;
-    const uint32_t cols = (uint32_t)A.cols, c0 = ALONE ? 0u : (blockIdx.y * 32 + warp) * kNormWarp;
-    uint32_t row = ALONE ? blockIdx.x * 8 + warp : blockIdx.x;   // (rows are fewer than 2^31)
-    const uint32_t step = ALONE ? gridDim.x * 8 : gridDim.x;
+    const uint32_t cols = (uint32_t)A.cols, c0 = ALONE ? 0u : ((GIVEN ? blockIdx.x * 32 : 0u) + warp) * kNormWarp, block = GIVEN ? blockIdx.y : blockIdx.x, blocks = GIVEN ? gridDim.y : gridDim.x;
+    uint32_t row = ALONE ? block * 8 + warp : block;   // (rows are fewer than 2^31)
+    const uint32_t step = ALONE ? blocks * 8 : blocks;
     grid_wait();
     float w[N], sums[N];
     load_weights<T, VEC>(A.w, A.w32, A.aligned_w, c0, cols, lane, w);
@@ -412,20 +412,20 @@ __global__ void __launch_bounds__(ALONE ? 256 : 1024, ALONE ? 4 : 1) k_norm_grad
     for (int q = 0; q < N; ++q) {
         const uint32_t c = lane_col<VEC, N>(c0, lane, q);
         if (c < cols)
-            A.partial[(uint64_t)blockIdx.x * (uint32_t)A.cols + c] = sums[q];
+            A.partial[(uint64_t)block * (uint32_t)A.cols + c] = sums[q];
     }
 }
 // ... the rows' means alone, a block each
 template <class T, bool VEC>
 __global__ void __launch_bounds__(1024) k_norm_means(const __grid_constant__ NormGradArgs A, float *means)
 {
-    __shared__ float part[32];
+    __shared__ double part[32];
     grid_release();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int64_t row = blockIdx.x;
     grid_wait();
     const float root = A.rstd[row];
-    float m = 0.f;
+    double m = 0;   // (of up to 2^21 lanes' parts)
 #pragma unroll 2
     for (uint32_t c0 = warp * kNormWarp; c0 < (uint32_t)A.cols; c0 += 32 * kNormWarp) {
         NormPiece<T, VEC> a, b;
@@ -437,7 +437,7 @@ __global__ void __launch_bounds__(1024) k_norm_means(const __grid_constant__ Nor
 #pragma unroll
         for (int q = 0; q < kNormPer; ++q)
             s = __fmaf_rn(__fmul_rn(d[q], w[q]), __fmul_rn(n[q], root), s);
-        m += s;
+        m += (double)s;
     }
     m = warp_sum(m);
     if (lane == 0)
@@ -445,7 +445,7 @@ __global__ void __launch_bounds__(1024) k_norm_means(const __grid_constant__ Nor
     __syncthreads();
     m = warp_sum(part[lane]);
     if (threadIdx.x == 0)
-        means[row] = m * A.share;
+        means[row] = (float)m * A.share;
 }
 // the blocks' sums of 32 columns
 __global__ void __launch_bounds__(1024) k_norm_columns(const float *partial, uint32_t groups, int64_t cols, float *dw)
@@ -513,7 +513,7 @@ static cudaError_t norm_grad(NormGradArgs A, float *means, float *dw, cudaStream
         e = launch(k_norm_means<T, VEC>, dim3((unsigned)A.rows), 1024, 0, s, A, means);
         A.means = means;
         if (e == cudaSuccess)
-            e = launch_norm<k_norm_grad<T, VEC, false, true>, bytes>(dim3(blocks, (unsigned)((A.cols + kNormWidest - 1) / kNormWidest)), warps, s, A);
+            e = launch_norm<k_norm_grad<T, VEC, false, true>, bytes>(dim3((unsigned)((A.cols + kNormWidest - 1) / kNormWidest), blocks), warps, s, A);
     } else {
         e = A.cols <= kNormWarp ? launch_norm<k_norm_grad<T, VEC, true, false>, bytes>(dim3(blocks), warps, s, A)
                                 : launch_norm<k_norm_grad<T, VEC, false, false>, bytes>(dim3(blocks), warps, s, A);

@@ -67,3 +67,22 @@ def test_product(b, x):
     fa, fc = b.f8_quantise(a), b.f8_quantise(c)
     out = b.f8_matmul(fa, fc)
     assert torch.equal(out[-LAST:], b.f8_matmul(b.f8_quantise(a[-LAST:].contiguous()), fc))
+
+
+def test_gradient_of_a_row_with_more_than_2_29_columns(b):
+    """More groups of columns than a grid's second dimension has blocks.  The row repeats a pattern, so the formula's mean is the pattern's."""
+    period, repeats = 1 << 16, 8194   # 65552 groups of 8192 columns
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(6)
+    dy, h, w = ((torch.randn(period, generator=gen, device="cuda") + 0.5).bfloat16() for _ in range(3))
+    rstd = torch.full((1,), 0.75, device="cuda")
+    dx, dw = b.rms_norm_grad(dy.repeat(repeats)[None], h.repeat(repeats)[None], w.repeat(repeats), rstd)
+    n, g = h.double() * 0.75, dy.double() * w.double()
+    mean, size = (g * n).mean(), (g * n).abs().mean()
+    want = 0.75 * (g - n * mean)
+    # the mean: 8 terms of three roundings each in 32 bits, the rest in 64; two more to multiply it, three of the difference, and dx's own to 8 bits
+    loose = 0.75 * (n.abs() * size * 14 + (g.abs() + n.abs() * mean.abs()) * 4) * 2.0**-24
+    for part in (dx[0, :period], dx[0, period * 4097:period * 4098], dx[0, -period:]):
+        assert ((part.double() - want).abs() <= want.abs() * 2.0**-8 + loose * (1 + 2.0**-8)).all()
+    for part in (dw[:period], dw[-period:]):
+        assert ((part.double() - dy.double() * n).abs() <= (dy.double() * n).abs() * 2.0**-23).all()
