@@ -44,7 +44,7 @@ struct F8Format {
 
 // ------------------------------------------------------------------ few rows against many
 // Up to eight rows of one side (tokens) against all of the other's (a weight's), which are read once: 1 x 6400 x 1600 are 10 MB, 1.6 us.  A tile of tcgen05.mma would have
-// 128 rows with one used, and a chain of copies and barriers for each (9.5 us; here 5.3); here a warp takes 16 rows of the weight and a share
+// 128 rows with one used, and a chain of copies and barriers for each (9.5 us; here 4.9); here a warp takes 16 rows of the weight and a share
 // of the blocks along k, straight from memory to the registers of mma.m16n8k32.  A lane has 16 bytes of two rows and of a
 // token at a time: the instruction's order of k is any that both sides share.  Sums of a block are fp32, times its two scales' power of two, and added in fp32.
 constexpr int kFewWarps = 8;
@@ -91,7 +91,9 @@ __global__ void __launch_bounds__(kFewWarps * 32, 3) k_f8_few(const FewArgs P, T
     const uint32_t first = blockIdx.x * (kFewWarps / P.share) * 16, row0 = first + warp / P.share * 16 + g, row1 = row0 + 8;
     const uint32_t have0 = min(row0, P.rows - 1), have1 = min(row1, P.rows - 1);   // (what does not exist is not stored)
     const uint8_t *const w0 = P.w + have0 * pitch + q * 16, *const w1 = P.w + have1 * pitch + q * 16, *const t = P.t + min((uint32_t)g, P.tokens - 1) * pitch + q * 16;
-    const uint8_t *const s0 = P.ws + f8_scale_at32(have0, 0, P.tiles), *const s1 = P.ws + f8_scale_at32(have1, 0, P.tiles), *const ts = P.ts + f8_scale_at32(2 * q, 0, P.tiles);
+    const uint8_t *const s0 = P.ws + f8_scale_at32(have0, 0, P.tiles), *const s1 = P.ws + f8_scale_at32(have1, 0, P.tiles), *const ts = P.ts + f8_scale_at32(min(2u * q, P.tokens - 1), 0, P.tiles);
+    // (the second token's scales: 16 bytes on; tokens that do not exist have others', whose product stays a normal number)
+    const uint32_t ts_next = 2u * q + 1 < P.tokens ? 16u : 0u;
     float sum[4] = {};
     grid_wait();
     // The weight's blocks ahead are copied into shared memory, each lane what it will read, kFewAhead of 2 KB to a warp; scales and tokens, which L1 has after a while, come one
@@ -115,7 +117,7 @@ __global__ void __launch_bounds__(kFewWarps * 32, 3) k_f8_few(const FewArgs P, T
     auto ask_rest = [&](uint32_t b) {
         const uint64_t at = (uint64_t)(b >> 2) * 512u + (b & 3u);
         next.z[0] = *(const uint4 *)(t + b * 128ull), next.z[1] = *(const uint4 *)(t + b * 128ull + 64);
-        next.e0 = s0[at], next.e1 = s1[at], next.f0 = ts[at], next.f1 = ts[at + 16];   // (token 2 q + 1: 16 bytes on)
+        next.e0 = s0[at], next.e1 = s1[at], next.f0 = ts[at], next.f1 = ts[at + ts_next];
     };
     uint32_t b = warp % P.share, stage = 0;
 #pragma unroll
@@ -168,7 +170,7 @@ __global__ void __launch_bounds__(kFewWarps * 32, 3) k_f8_few(const FewArgs P, T
 template <class T>
 static cudaError_t few(FewArgs P, int kind_w, int kind_t, T *out, cudaStream_t s)
 {
-    // as many warps as the SMs hold, 24 each, with as many blocks as that leaves (1 x 6400 x 1600 with 12 to an SM 6.4, with 24 5.3 us)
+    // as many warps as the SMs hold, 24 each, with as many blocks as that leaves (1 x 6400 x 1600 with 12 to an SM 6.4, with 24 5.3 us then)
     const int64_t groups = ((int64_t)P.rows + 15) / 16;
     P.share = kFewWarps;
     while (P.share > 1 && groups * P.share > kPlanSMs * 24)
