@@ -43,12 +43,12 @@ struct F8Format {
 };
 
 // ------------------------------------------------------------------ few rows against many
-// Up to eight rows of one side (tokens) against all of the other's (a weight's), which are read once: 1 x 6400 x 1600 are 10 MB, 1.6 us.  A tile of tcgen05.mma would have
-// 128 rows with one used, and a chain of copies and barriers for each (9.5 us; here 4.9); here a warp takes 16 rows of the weight and a share
+// Few rows of one side (tokens) against all of the other's (a weight's), which are read once for eight: 1 x 6400 x 1600 are 10 MB, 1.6 us.  A tile of tcgen05.mma would have
+// 128 rows with one used, and a chain of copies and barriers for each (9.5 us; here 4.9); here a warp takes eight tokens, 16 rows of the weight and a share
 // of the blocks along k, straight from memory to the registers of mma.m16n8k32.  A lane has 16 bytes of two rows and of a
 // token at a time: the instruction's order of k is any that both sides share.  Sums of a block are fp32, times its two scales' power of two, and added in fp32.
 constexpr int kFewWarps = 8;
-constexpr uint32_t kFewAhead = 4;
+constexpr uint32_t kFewAhead = 4, kFewStage = 2048 + 128;
 // 16 rows of the weight by eight tokens and 32 of k; KINDS: 0 to 3, the weight's kind and twice the tokens'
 template <int KINDS>
 __device__ __forceinline__ void few_product(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1)
@@ -77,6 +77,7 @@ __device__ __forceinline__ float few_scaled(float v, uint32_t e, uint32_t f)
 struct FewArgs {
     const uint8_t *w, *ws, *t, *ts;   // codes and scales: the weight's, the tokens'
     uint32_t rows, tokens, blocks, tiles;
+    uint32_t groups;                  // of eight tokens: neighbouring CTAs, which find the weight in L2
     uint32_t share;                   // warps that share a row group's blocks: 1, 2, 4 or 8
     int64_t row_step, token_step;     // of the output, in elements
 };
@@ -88,57 +89,55 @@ __global__ void __launch_bounds__(kFewWarps * 32, 3) k_f8_few(const FewArgs P, T
     grid_release();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, q = lane & 3, g = lane >> 2;
     const uint64_t pitch = (uint64_t)P.blocks * 128u;
-    const uint32_t first = blockIdx.x * (kFewWarps / P.share) * 16, row0 = first + warp / P.share * 16 + g, row1 = row0 + 8;
+    const uint32_t at = blockIdx.x / P.groups, token0 = (blockIdx.x - at * P.groups) * 8, tokens = min(8u, P.tokens - token0);
+    const uint32_t first = at * (kFewWarps / P.share) * 16, row0 = first + warp / P.share * 16 + g, row1 = row0 + 8;
     const uint32_t have0 = min(row0, P.rows - 1), have1 = min(row1, P.rows - 1);   // (what does not exist is not stored)
-    const uint8_t *const w0 = P.w + have0 * pitch + q * 16, *const w1 = P.w + have1 * pitch + q * 16, *const t = P.t + min((uint32_t)g, P.tokens - 1) * pitch + q * 16;
-    const uint8_t *const s0 = P.ws + f8_scale_at32(have0, 0, P.tiles), *const s1 = P.ws + f8_scale_at32(have1, 0, P.tiles), *const ts = P.ts + f8_scale_at32(min(2u * q, P.tokens - 1), 0, P.tiles);
-    // (the second token's scales: 16 bytes on; tokens that do not exist have others', whose product stays a normal number)
-    const uint32_t ts_next = 2u * q + 1 < P.tokens ? 16u : 0u;
+    const uint8_t *const w0 = P.w + have0 * pitch + q * 16, *const w1 = P.w + have1 * pitch + q * 16, *const t = P.t + (token0 + min((uint32_t)g, tokens - 1)) * pitch + q * 16;
+    // Scales come as words, four blocks of a row: of four lanes one has the weight's row, the next the row eight on, the third a token (one that does not exist is
+    // another again: its products with the weight stay normal numbers).
+    const uint8_t *const scales = q == 0 ? P.ws + f8_scale_at32(have0, 0, P.tiles) : q == 1 ? P.ws + f8_scale_at32(have1, 0, P.tiles)
+                                                                                      : P.ts + f8_scale_at32(token0 + min((uint32_t)g, tokens - 1), 0, P.tiles);
     float sum[4] = {};
     grid_wait();
-    // The weight's blocks ahead are copied into shared memory, each lane what it will read, kFewAhead of 2 KB to a warp; scales and tokens, which L1 has after a while, come one
-    // block ahead in registers.  (Tokens by copies that pass L1 by are the same lines of L2 for all SMs: 1 x 50257 x 1600 23 -> 74 us.)
-    uint8_t *const mine = few_smem + (warp * kFewAhead * 4 * 32 + lane) * 16;
+    // The weight's blocks ahead and scales are copied into shared memory, kFewAhead of 2 KB to a warp, of which a lane reads what it has copied; tokens, which L1 has after a while, come one
+    // block ahead in registers (two and three ahead: nothing).  (Tokens by copies that pass L1 by are the same lines of L2 for all SMs: 1 x 50257 x 1600 23 -> 74 us.)
+    uint8_t *const ring = few_smem + warp * kFewAhead * kFewStage, *const mine = ring + lane * 16;
     auto copy16 = [](uint8_t *to, const uint8_t *from) {
         asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"((uint32_t)__cvta_generic_to_shared(to)), "l"(from) : "memory");
     };
     auto ask = [&](uint32_t b, uint32_t stage) {
         if (b < P.blocks) {
-            uint8_t *const to = mine + stage * 2048;
+            uint8_t *const to = mine + stage * kFewStage;
             const uint64_t at = b * 128ull;
+            asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"((uint32_t)__cvta_generic_to_shared(ring + stage * kFewStage + 2048 + lane * 4)), "l"(scales + (uint64_t)(b >> 2) * 512u)
+                         : "memory");
             copy16(to, w0 + at), copy16(to + 512, w0 + at + 64), copy16(to + 1024, w1 + at), copy16(to + 1536, w1 + at + 64);
         }
         asm volatile("cp.async.commit_group;" ::: "memory");
     };
-    struct Rest {
-        uint4 z[2];
-        uint32_t e0, e1, f0, f1;
-    } now, next;
-    auto ask_rest = [&](uint32_t b) {
-        const uint64_t at = (uint64_t)(b >> 2) * 512u + (b & 3u);
-        next.z[0] = *(const uint4 *)(t + b * 128ull), next.z[1] = *(const uint4 *)(t + b * 128ull + 64);
-        next.e0 = s0[at], next.e1 = s1[at], next.f0 = ts[at], next.f1 = ts[at + ts_next];
+    uint4 z[2], next[2];
+    auto ask_tokens = [&](uint32_t b) {
+        if (b < P.blocks)
+            next[0] = *(const uint4 *)(t + b * 128ull), next[1] = *(const uint4 *)(t + b * 128ull + 64);
     };
     uint32_t b = warp % P.share, stage = 0;
 #pragma unroll
     for (uint32_t i = 0; i < kFewAhead - 1; ++i)
         ask(b + i * P.share, i);
-    if (b < P.blocks)
-        ask_rest(b);
+    ask_tokens(b);
     for (; b < P.blocks; b += P.share) {
         ask(b + (kFewAhead - 1) * P.share, (stage + kFewAhead - 1) % kFewAhead);
-        now = next;
-        if (b + P.share < P.blocks)
-            ask_rest(b + P.share);
+        z[0] = next[0], z[1] = next[1];
+        ask_tokens(b + P.share);
         asm volatile("cp.async.wait_group %0;" ::"n"(kFewAhead - 1) : "memory");
-        const uint8_t *const from = mine + stage * 2048;
+        __syncwarp();
+        const uint8_t *const from = mine + stage * kFewStage, *const bytes = ring + stage * kFewStage + 2048 + (b & 3u);
         stage = (stage + 1) % kFewAhead;
         uint4 x[2], y[2];
 #pragma unroll
         for (int h = 0; h < 2; ++h)
             x[h] = *(const uint4 *)(from + h * 512), y[h] = *(const uint4 *)(from + 1024 + h * 512);
-        const uint4(&z)[2] = now.z;
-        const uint32_t e0 = now.e0, e1 = now.e1, f0 = now.f0, f1 = now.f1;
+        const uint32_t e0 = bytes[g * 16], e1 = bytes[g * 16 + 4], f0 = bytes[q * 32 + 8], f1 = bytes[q * 32 + 24];
         float d[4] = {};
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
@@ -147,6 +146,7 @@ __global__ void __launch_bounds__(kFewWarps * 32, 3) k_f8_few(const FewArgs P, T
         }
         // the two scales' product, where it is a normal number (and neither of them NaN: 255 and 127 or more are not)
         const uint32_t least = min(e0, e1) + min(f0, f1), most = max(e0, e1) + max(f0, f1);
+        // (... and all lanes have the scales by now, into whose place the next ones go)
         if (__all_sync(0xffffffffu, least > 127u && most < 382u && max(max(e0, e1), max(f0, f1)) < kF8Nan)) {
             sum[0] = __fmaf_rn(d[0], __uint_as_float((e0 + f0 - 127u) << 23), sum[0]), sum[1] = __fmaf_rn(d[1], __uint_as_float((e0 + f1 - 127u) << 23), sum[1]);
             sum[2] = __fmaf_rn(d[2], __uint_as_float((e1 + f0 - 127u) << 23), sum[2]), sum[3] = __fmaf_rn(d[3], __uint_as_float((e1 + f1 - 127u) << 23), sum[3]);
@@ -163,8 +163,8 @@ __global__ void __launch_bounds__(kFewWarps * 32, 3) k_f8_few(const FewArgs P, T
         float s = part[group * P.share][token][r];
         for (uint32_t k = 1; k < P.share; ++k)
             s = __fadd_rn(s, part[group * P.share + k][token][r]);
-        if (token < P.tokens && row < P.rows)
-            out[token * P.token_step + row * P.row_step] = from_f32<T>(s);
+        if (token < tokens && row < P.rows)
+            out[(token0 + token) * P.token_step + row * P.row_step] = from_f32<T>(s);
     }
 }
 template <class T>
@@ -172,16 +172,24 @@ static cudaError_t few(FewArgs P, int kind_w, int kind_t, T *out, cudaStream_t s
 {
     // as many warps as the SMs hold, 24 each, with as many blocks as that leaves (1 x 6400 x 1600 with 12 to an SM 6.4, with 24 5.3 us then)
     const int64_t groups = ((int64_t)P.rows + 15) / 16;
+    P.groups = (P.tokens + 7) / 8;
     P.share = kFewWarps;
-    while (P.share > 1 && groups * P.share > kPlanSMs * 24)
+    while (P.share > 1 && groups * P.groups * P.share > kPlanSMs * 24)
         P.share /= 2;
     const int64_t per_cta = kFewWarps / P.share;
     static void (*const kernels[4])(FewArgs, T *) = {k_f8_few<T, 0>, k_f8_few<T, 1>, k_f8_few<T, 2>, k_f8_few<T, 3>};
-    constexpr size_t smem = kFewWarps * kFewAhead * 2048;
+    constexpr size_t smem = kFewWarps * kFewAhead * kFewStage;
     static int done[4][64];
     const int kinds = kind_w + 2 * kind_t;
     const cudaError_t e = opt_in_smem(kernels[kinds], smem, done[kinds]);
-    return e != cudaSuccess ? e : launch(kernels[kinds], dim3((unsigned)((groups + per_cta - 1) / per_cta)), kFewWarps * 32, smem, s, P, out);
+    return e != cudaSuccess ? e : launch(kernels[kinds], dim3((unsigned)((groups + per_cta - 1) / per_cta * P.groups)), kFewWarps * 32, smem, s, P, out);
+}
+// Whether that takes less: up to eight tokens always; then the weight once per eight tokens at 5 TB/s, and 2 us less than tiles of tcgen05.mma
+// to begin and end with (mm_cost: theirs beside that, which is long where k is long and the weight's rows are few).  Tiles and this, us: 16 x 6400 x 1600 8.8 and 6.7, 17 rows
+// 8.7 and 10.2; 32 x 1600 x 6400 13.4 and 9.7, 64 rows 13.3 and 15.3; 16 x 4096 x 4096 12.8 and 8.6, 32 rows 10.3 and 13.8; 16 x 8192 x 8192 19 and 27.
+static bool few_rows(int64_t tokens, int64_t rows, int64_t k, int64_t mm_cost)
+{
+    return tokens <= 8 || (tokens <= 64 && (double)((tokens + 7) / 8) * (double)rows * (double)k / 5000 < (double)mm_cost + 2000);
 }
 
 }  // namespace conef
@@ -211,16 +219,16 @@ int conef_f8_matmul(const void *a_codes, const void *a_scales, int a_kind, int64
                         "conef_f8_matmul");
     return with_elem(dtype, [&](auto t) {
         using T = decltype(t);
-        if (std::min(m, n) <= 8) {
+        const MmChoice c = mm_choice<F8Format>(m, n, k);
+        if (few_rows(std::min(m, n), std::max(m, n), k, c.cost)) {
             const bool turned = n < m;   // (the weight's rows are A's)
             FewArgs P = {(const uint8_t *)b_codes, (const uint8_t *)b_scales, (const uint8_t *)a_codes, (const uint8_t *)a_scales, (uint32_t)n, (uint32_t)m, (uint32_t)f8_blocks(k),
-                         (uint32_t)f8_scale_tiles(k), 0, 1, ld};
+                         (uint32_t)f8_scale_tiles(k), 0, 0, 1, ld};
             if (turned)
                 P = {(const uint8_t *)a_codes, (const uint8_t *)a_scales, (const uint8_t *)b_codes, (const uint8_t *)b_scales, (uint32_t)m, (uint32_t)n, P.blocks, P.tiles,
-                     0, ld, 1};
+                     0, 0, ld, 1};
             return launched(few(P, turned ? a_kind : b_kind, turned ? b_kind : a_kind, (T *)out, (cudaStream_t)stream), "conef_f8_matmul");
         }
-        const MmChoice c = mm_choice<F8Format>(m, n, k);
         return (c.pair ? matmul<F8Format, T, true> : matmul<F8Format, T, false>)((const uint8_t *)a_codes, (const uint8_t *)a_scales, m, (const uint8_t *)b_codes,
                                                                                  (const uint8_t *)b_scales, n, k, (T *)out, ld, c.bn, a_kind, b_kind, "conef_f8_matmul",
                                                                                  (cudaStream_t)stream);

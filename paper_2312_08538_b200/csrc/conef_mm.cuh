@@ -364,20 +364,20 @@ static bool encode(CUtensorMap *map, CUtensorMapDataType type, int elem, const v
 struct MmChoice {
     uint32_t bn;
     bool pair;
+    int64_t cost;
 };
 template <class F>
 static MmChoice mm_choice(int64_t m, int64_t n, int64_t k)
 {
     const int64_t k_steps = (k + F::kStepK - 1) / F::kStepK;
-    MmChoice best = {0, false};
-    int64_t least = 0;
+    MmChoice best = {0, false, 0};
     for (int pair = 0; pair < 2; ++pair)
         for (uint32_t bn = pair ? 128 : 64; bn <= 256; bn += 64) {
             const int64_t rows = pair ? 2 * kMmM : kMmM, sets = pair ? kPlanSMs / 2 : kPlanSMs;
             const int64_t waves = ((m + rows - 1) / rows * ((n + bn - 1) / bn) + sets - 1) / sets;
             const int64_t cost = waves * (k_steps * F::per_step(pair, bn / 64 - 1) + F::per_tile(bn / 64 - 1)) + pair * 1000;
-            if (!best.bn || cost < least)
-                best = {bn, pair != 0}, least = cost;
+            if (!best.bn || cost < best.cost)
+                best = {bn, pair != 0, cost};
         }
     return best;
 }

@@ -281,3 +281,32 @@ def test_nothing_runs_out(b):
     a, c = b.f8_quantise(matrix(3330, 2100, torch.bfloat16)), b.f8_quantise(matrix(4113, 2100, torch.bfloat16, 1))
     assert not torch.isnan(b.f8_matmul(a, c)).any()
     assert b.f8_timeouts() == before
+
+
+@pytest.mark.parametrize("m,n,k", [(24, 200, 6400), (33, 129, 6400), (64, 100, 4100), (65, 100, 4100), (64, 64, 20000), (19, 777, 1300), (9, 60, 33)])
+def test_product_of_some_rows(b, m, n, k):
+    """... by groups of eight against a long k, and either side's."""
+    for kinds in (("e4m3", "e5m2"), ("e5m2", "e4m3")):
+        a, c = b.f8_quantise(matrix(m, k, torch.float32), kind=kinds[0]), b.f8_quantise(matrix(n, k, torch.float32, 1, 0.02), kind=kinds[1])
+        for got, x, y in ((b.f8_matmul(a, c, torch.float32), a, c), (b.f8_matmul(c, a, torch.float32), c, a)):
+            check_product(got, values(x), values(y), torch.float32)
+
+
+def test_product_of_some_rows_into_a_wider_matrix(b):
+    a, c = b.f8_quantise(matrix(27, 2000, torch.bfloat16)), b.f8_quantise(matrix(90, 2000, torch.bfloat16, 1))
+    for p, q in ((a, c), (c, a)):
+        wide = torch.full((p.rows + 2, q.rows + 3), 7.0, device="cuda")
+        assert b.lib.conef_f8_matmul(p.codes.data_ptr(), p.scales.data_ptr(), b.E4M3, p.rows, q.codes.data_ptr(), q.scales.data_ptr(), b.E4M3, q.rows, 2000, wide[1:, 1:].data_ptr(),
+                                     b.F32, wide.shape[1], b._stream_handle(None)) == b.OK
+        assert torch.equal(wide[1:-1, 1:-2], b.f8_matmul(p, q, torch.float32))
+        wide[1:-1, 1:-2] = 7.0
+        assert (wide == 7.0).all()
+
+
+def test_product_of_some_rows_with_a_nan_block(b):
+    x, w = matrix(30, 3000, torch.bfloat16), matrix(70, 3000, torch.bfloat16, 1)
+    x[29, 2999], w[66, 639] = float("nan"), float("inf")
+    for out, i, j in ((b.f8_matmul(b.f8_quantise(x), b.f8_quantise(w)), 29, 66), (b.f8_matmul(b.f8_quantise(w), b.f8_quantise(x)), 66, 29)):
+        bad = torch.zeros_like(out, dtype=torch.bool)
+        bad[i], bad[:, j] = True, True
+        assert torch.equal(torch.isnan(out), bad)
