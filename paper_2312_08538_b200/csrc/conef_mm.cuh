@@ -45,6 +45,7 @@ struct MmArgs {
     uint32_t sums, scale_column; // sets of sums in tensor memory, and the first column of scales
     uint64_t limit, sums_limit;  // nanoseconds that a wait takes at most, and the one for a tile's sums, which lasts for all of k
     uint32_t loads[2];           // stages that the CTA(s) of a pair bring at most (tests)
+    uint32_t copied;             // bytes of codes that fill a stage (a single CTA's)
     uint32_t kind_a, kind_b;     // types of elements, where the format has several
 };
 // CTAs in which a wait has run out, since the library was loaded (a count per format, whose file includes this)
@@ -169,7 +170,7 @@ __global__ void __launch_bounds__(kMmThreads, 1) k_matmul(const __grid_constant_
             tc::tile_load_pair(sc + F::kTiles * 512, &maps.bs, ks / F::kTileStages * (F::kTiles * 128), n0 / 128, bar);
         } else {
             const uint32_t tile = ks / F::kTileStages * F::kTiles, scale_bytes = min(P.tiles - tile, (uint32_t)F::kTiles) * 512u;
-            tc::bar_expect(&S.full[s], kMmM * 128 + b_bytes + scale_bytes * (1 + scale_rows));
+            tc::bar_expect(&S.full[s], P.copied + scale_bytes * (1 + scale_rows));
             tc::tile_load(st, &maps.a, ks * 128, tm * kMmM, &S.full[s]);
             tc::tile_load(st + kMmM * 128, &maps.b, ks * 128, n0, &S.full[s]);
             tc::bulk_load(sc, P.as + ((size_t)tm * P.tiles + tile) * 512, scale_bytes, &S.full[s]);
@@ -408,6 +409,10 @@ static int matmul(const uint8_t *a, const uint8_t *as, int64_t m, const uint8_t 
     P.sums_limit = P.limit + 4096ull * P.stages_k;
     P.loads[0] = mm_limit.loads[0].load();
     P.loads[1] = mm_limit.loads[1].load();
+    // Rows that a copy brings: of a matrix with fewer than a tile's, in eights; behind them a product has whatever the stage held, in sums that nobody stores.  (Filled with
+    // zeros to a tile's 128, matrices of less than 128 KB took up to twice as long: 9 x 8192 x 8192 32 us, 16 rows 19.)
+    const uint32_t a_box = PAIR ? kMmM : (uint32_t)std::min<int64_t>(kMmM, (m + 7) / 8 * 8), b_box = PAIR ? bn / 2 : (uint32_t)std::min<int64_t>(bn, (n + 7) / 8 * 8);
+    P.copied = (a_box + b_box) * 128;
     P.tiles = (uint32_t)F::scale_tiles(k);
     P.b_rows = (uint32_t)((n + 127) / 128);
     P.bn = bn;
@@ -429,8 +434,8 @@ static int matmul(const uint8_t *a, const uint8_t *as, int64_t m, const uint8_t 
     P.tiled = (((uint64_t)ld * sizeof(T)) | ((uint64_t)n * sizeof(T)) | (uintptr_t)out) % 16 == 0;
     MmMaps maps = {};
     const int64_t row_bytes = F::row_bytes(k), scale_bytes = (int64_t)P.tiles * 512;
-    bool ok = encode(&maps.a, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, a, m, row_bytes, row_bytes, 128, kMmM) &&
-              encode(&maps.b, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, b, n, row_bytes, row_bytes, 128, PAIR ? bn / 2 : bn);
+    bool ok = encode(&maps.a, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, a, m, row_bytes, row_bytes, 128, a_box) &&
+              encode(&maps.b, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, b, n, row_bytes, row_bytes, 128, b_box);
     if (P.tiled)
         ok = ok && encode(&maps.out, sizeof(T) == 4 ? CU_TENSOR_MAP_DATA_TYPE_UINT32 : CU_TENSOR_MAP_DATA_TYPE_UINT16, sizeof(T), out, m, n * (int64_t)sizeof(T),
                           (m > 1 ? ld : n) * (int64_t)sizeof(T), 128 / sizeof(T), 32);
