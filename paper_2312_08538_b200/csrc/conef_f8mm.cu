@@ -184,12 +184,12 @@ static cudaError_t few(FewArgs P, int kind_w, int kind_t, T *out, cudaStream_t s
     const cudaError_t e = opt_in_smem(kernels[kinds], smem, done[kinds]);
     return e != cudaSuccess ? e : launch(kernels[kinds], dim3((unsigned)((groups + per_cta - 1) / per_cta * P.groups)), kFewWarps * 32, smem, s, P, out);
 }
-// Whether that takes less: up to eight tokens always; then the weight once per eight tokens at 5 TB/s, and 2 us less than tiles of tcgen05.mma
-// to begin and end with (mm_cost: theirs beside that, which is long where k is long and the weight's rows are few).  Tiles and this, us: 16 x 6400 x 1600 8.8 and 6.7, 17 rows
-// 8.7 and 10.2; 32 x 1600 x 6400 13.4 and 9.7, 64 rows 13.3 and 15.3; 16 x 4096 x 4096 12.8 and 8.6, 32 rows 10.3 and 13.8; 16 x 8192 x 8192 19 and 27.
+// Whether that takes less: up to eight tokens always; then the weight once per eight tokens at 5 TB/s, and 0.7 us less than tiles of tcgen05.mma
+// to begin and end with (mm_cost: theirs beside that, which is long where k is long and the weight's rows are few).  Tiles and this, us: 16 x 6400 x 1600 6.5 and 6.8;
+// 32 x 1600 x 6400 13.4 and 9.7, 64 rows 13.3 and 15.3; 16 x 4096 x 4096 10.5 and 8.8, 32 rows 10.5 and 13.8; 16 x 8192 x 8192 19 and 27.
 static bool few_rows(int64_t tokens, int64_t rows, int64_t k, int64_t mm_cost)
 {
-    return tokens <= 8 || (tokens <= 64 && (double)((tokens + 7) / 8) * (double)rows * (double)k / 5000 < (double)mm_cost + 2000);
+    return tokens <= 8 || (tokens <= 64 && (double)((tokens + 7) / 8) * (double)rows * (double)k / 5000 < (double)mm_cost + 700);
 }
 
 }  // namespace conef
