@@ -44,7 +44,7 @@ struct F8Format {
 
 // ------------------------------------------------------------------ few rows against many
 // Few rows of one side (tokens) against all of the other's (a weight's), which are read once for eight: 1 x 6400 x 1600 are 10 MB, 1.6 us.  A tile of tcgen05.mma would have
-// 128 rows with one used, and a chain of copies and barriers for each (9.5 us; here 4.9); here a warp takes eight tokens, 16 rows of the weight and a share
+// 128 rows with one used, and a chain of copies and barriers for each (16 rows 6.5 us; here one 4.8); here a warp takes eight tokens, 16 rows of the weight and a share
 // of the blocks along k, straight from memory to the registers of mma.m16n8k32.  A lane has 16 bytes of two rows and of a
 // token at a time: the instruction's order of k is any that both sides share.  Sums of a block are fp32, times its two scales' power of two, and added in fp32.
 constexpr int kFewWarps = 8;
