@@ -10,6 +10,7 @@ namespace conef {
 
 struct F8Format {
     static constexpr uint32_t kStageK = 128, kStepK = 32, kTiles = 1, kTileStages = 4, kScaleColumns = 12;
+    static constexpr bool kSplits = true;
     static int64_t row_bytes(int64_t k) { return f8_blocks(k) * 128; }
     static int64_t scale_tiles(int64_t k) { return f8_scale_tiles(k); }
     static int per_step(int pair, int width)
@@ -27,7 +28,7 @@ struct F8Format {
     // stage ks: its scales to tensor memory, then the products
     template <bool PAIR>
     static __device__ __forceinline__ void issue(const MmArgs &P, uint32_t d, uint32_t a, uint32_t b, uint32_t sc, uint32_t instruction, uint32_t sa, uint32_t sb, uint32_t shift,
-                                                 uint32_t scale_rows, uint32_t ks)
+                                                 uint32_t scale_rows, uint32_t ks, uint32_t ks0)
     {
         const uint32_t steps = P.k_steps - ks * 4u, number = ks & 3u;
         tc::scales_copy<PAIR>(sa, sc);
@@ -38,7 +39,7 @@ struct F8Format {
 #pragma unroll
         for (uint32_t t = 0; t < 4; ++t)
             if (t < steps)
-                tc::f8_product<PAIR>(d, a + 2 * t, b + 2 * t, instruction, sa, sb + shift, ks + t);
+                tc::f8_product<PAIR>(d, a + 2 * t, b + 2 * t, instruction, sa, sb + shift, ks - ks0 + t);
     }
 };
 
@@ -167,15 +168,20 @@ __global__ void __launch_bounds__(kFewWarps * 32, 3) k_f8_few(const FewArgs P, T
             out[(token0 + token) * P.token_step + row * P.row_step] = from_f32<T>(s);
     }
 }
+// warps that share a row group's blocks: as many as the SMs hold, 24 each, with as many blocks as that leaves (1 x 6400 x 1600 with 12 to an SM 6.4, with 24 5.3 us then)
+static uint32_t few_share(int64_t rows, int64_t tokens)
+{
+    uint32_t share = kFewWarps;
+    while (share > 1 && (rows + 15) / 16 * ((tokens + 7) / 8) * share > kPlanSMs * 24)
+        share /= 2;
+    return share;
+}
 template <class T>
 static cudaError_t few(FewArgs P, int kind_w, int kind_t, T *out, cudaStream_t s)
 {
-    // as many warps as the SMs hold, 24 each, with as many blocks as that leaves (1 x 6400 x 1600 with 12 to an SM 6.4, with 24 5.3 us then)
     const int64_t groups = ((int64_t)P.rows + 15) / 16;
     P.groups = (P.tokens + 7) / 8;
-    P.share = kFewWarps;
-    while (P.share > 1 && groups * P.groups * P.share > kPlanSMs * 24)
-        P.share /= 2;
+    P.share = few_share(P.rows, P.tokens);
     const int64_t per_cta = kFewWarps / P.share;
     static void (*const kernels[4])(FewArgs, T *) = {k_f8_few<T, 0>, k_f8_few<T, 1>, k_f8_few<T, 2>, k_f8_few<T, 3>};
     constexpr size_t smem = kFewWarps * kFewAhead * kFewStage;
@@ -184,12 +190,15 @@ static cudaError_t few(FewArgs P, int kind_w, int kind_t, T *out, cudaStream_t s
     const cudaError_t e = opt_in_smem(kernels[kinds], smem, done[kinds]);
     return e != cudaSuccess ? e : launch(kernels[kinds], dim3((unsigned)((groups + per_cta - 1) / per_cta * P.groups)), kFewWarps * 32, smem, s, P, out);
 }
-// Whether that takes less: up to eight tokens always; then the weight once per eight tokens at 5 TB/s, and 0.7 us less than tiles of tcgen05.mma
-// to begin and end with (mm_cost: theirs beside that, which is long where k is long and the weight's rows are few).  Tiles and this, us: 16 x 6400 x 1600 6.5 and 6.8;
-// 32 x 1600 x 6400 13.4 and 9.7, 64 rows 13.3 and 15.3; 16 x 4096 x 4096 10.5 and 8.8, 32 rows 10.5 and 13.8; 16 x 8192 x 8192 19 and 27.
+// Whether that takes less: up to eight tokens always; then the weight once per eight tokens at 5 TB/s, or 0.4 us for each of a warp's blocks, and 0.7 us less than
+// tiles of tcgen05.mma to begin and end with (mm_cost: theirs beside that).  Tiles and this, us: 16 x 6400 x 1600 6.5 and 6.8; 16 x 1600 x 1600 6.1 and 4.1;
+// 16 x 4096 x 4096 9 and 8.8, 32 rows 9 and 13.8; 16 x 8192 x 8192 19 and 27; 64 x 64 x 65536 16 and 26.
 static bool few_rows(int64_t tokens, int64_t rows, int64_t k, int64_t mm_cost)
 {
-    return tokens <= 8 || (tokens <= 64 && (double)((tokens + 7) / 8) * (double)rows * (double)k / 5000 < (double)mm_cost + 700);
+    if (tokens <= 8 || tokens > 64)
+        return tokens <= 8;
+    const int64_t share = few_share(rows, tokens), bytes = (tokens + 7) / 8 * rows * f8_blocks(k) * 128, alone = (f8_blocks(k) + share - 1) / share * 400;
+    return std::max(bytes / 5000, alone) < mm_cost + 700;
 }
 
 }  // namespace conef
@@ -229,9 +238,9 @@ int conef_f8_matmul(const void *a_codes, const void *a_scales, int a_kind, int64
                      0, 0, ld, 1};
             return launched(few(P, turned ? a_kind : b_kind, turned ? b_kind : a_kind, (T *)out, (cudaStream_t)stream), "conef_f8_matmul");
         }
-        return (c.pair ? matmul<F8Format, T, true> : matmul<F8Format, T, false>)((const uint8_t *)a_codes, (const uint8_t *)a_scales, m, (const uint8_t *)b_codes,
-                                                                                 (const uint8_t *)b_scales, n, k, (T *)out, ld, c.bn, a_kind, b_kind, "conef_f8_matmul",
-                                                                                 (cudaStream_t)stream);
+        const auto product = c.pair ? matmul<F8Format, T, true, false> : c.split > 1 ? matmul<F8Format, T, false, true> : matmul<F8Format, T, false, false>;
+        return product((const uint8_t *)a_codes, (const uint8_t *)a_scales, m, (const uint8_t *)b_codes, (const uint8_t *)b_scales, n, k, (T *)out, ld, c, a_kind, b_kind,
+                       "conef_f8_matmul", (cudaStream_t)stream);
     });
 }
 

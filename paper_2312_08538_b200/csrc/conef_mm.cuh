@@ -30,6 +30,7 @@ constexpr uint32_t kMmColumns = 512;                     // tensor memory, all o
 //   kTileStages        stages that one tile serves (one after the other)
 //   row_bytes(k), scale_tiles(k)
 //   instruction<PAIR>(n, P), issue<PAIR>(...)
+//   kSplits            whether few tiles may be shared along k
 
 struct MmArgs {
     const uint8_t *as, *bs;      // scales (a single CTA's)
@@ -47,6 +48,7 @@ struct MmArgs {
     uint32_t loads[2];           // stages that the CTA(s) of a pair bring at most (tests)
     uint32_t copied;             // bytes of codes that fill a stage (a single CTA's)
     uint32_t kind_a, kind_b;     // types of elements, where the format has several
+    uint32_t split, split_stages;   // CTAs of a cluster that share a tile's k, and stages of each (the last one's may be fewer)
 };
 // CTAs in which a wait has run out, since the library was loaded (a count per format, whose file includes this)
 static __device__ unsigned long long g_mm_ran_out;
@@ -119,14 +121,62 @@ __device__ __forceinline__ uint4 pack16<__half>(const uint32_t *v)
     });
 }
 
-template <class F, class T, bool PAIR>
+// The sums of a tile whose k the CTAs of a cluster share: each CTA adds up its columns, of all, in the CTAs' order, four columns to a thread
+template <int SPLIT, class T>
+__device__ __forceinline__ void mm_join(const MmArgs &P, const float *sums, const int &dead, const MmTile &at, uint32_t part, T *out)
+{
+    const uint32_t width = P.bn / SPLIT, quads = width / 4, shift = 31 - __clz(quads);   // (a power of two)
+    const int64_t row0 = (int64_t)at.m * kMmM, col0 = (int64_t)at.n * P.bn;
+    uint32_t any = 0;
+#pragma unroll
+    for (int i = 0; i < SPLIT; ++i)
+        any |= tc::load_at(tc::address_in(&dead, i));
+    const uint32_t all = (uint32_t)min((int64_t)kMmM, P.m - row0) << shift;
+    for (uint32_t e = threadIdx.x; e < all; e += kMmThreads) {
+        const uint32_t r = e >> shift, c = part * width + (e & (quads - 1)) * 4;
+        const int64_t col = col0 + c;
+        if (col >= P.n)
+            continue;
+        const float *const mine = sums + r * (P.bn + 4) + c;
+        float4 v[SPLIT];
+#pragma unroll
+        for (int i = 0; i < SPLIT; ++i)
+            v[i] = tc::load_at4(tc::address_in(mine, i));
+        float f[4] = {v[0].x, v[0].y, v[0].z, v[0].w};
+#pragma unroll
+        for (int i = 1; i < SPLIT; ++i)
+            f[0] = __fadd_rn(f[0], v[i].x), f[1] = __fadd_rn(f[1], v[i].y), f[2] = __fadd_rn(f[2], v[i].z), f[3] = __fadd_rn(f[3], v[i].w);
+        T *const to = out + (row0 + r) * P.ld + col;
+        T o[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            o[i] = from_f32<T>(any ? __uint_as_float(0x7FFFFFFFu) : f[i]);   // (a wait ran out: what was not computed is NaN)
+        if (P.tiled && col + 4 <= P.n) {
+            if constexpr (sizeof(T) == 4)
+                *(uint4 *)to = *(const uint4 *)o;
+            else
+                *(uint2 *)to = *(const uint2 *)o;
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (col + i < P.n)
+                    to[i] = o[i];
+        }
+    }
+}
+
+// SPLIT: the CTAs of a cluster have one tile, and each a part of k.  What they have summed goes to their own shared memory, where all stages have been used, and each
+// adds up a share of the columns, in the CTAs' order.
+template <class F, class T, bool PAIR, bool SPLIT>
 __global__ void __launch_bounds__(kMmThreads, 1) k_matmul(const __grid_constant__ MmMaps maps, const __grid_constant__ MmArgs P, T *out)
 {
     extern __shared__ __align__(1024) uint8_t mm_smem[];
     __shared__ MmShared S;
     const int warp = __shfl_sync(0xffffffffu, (int)(threadIdx.x >> 5), 0), lane = threadIdx.x & 31;   // (known to be the same in all lanes)
     const uint32_t stage_bytes = mm_stage_bytes(P.bn, PAIR), scale_rows = mm_scale_rows(P.bn), b_bytes = P.bn * (PAIR ? 64u : 128u);
-    const uint32_t rank = PAIR ? blockIdx.x & 1u : 0u, first = PAIR ? blockIdx.x / 2 : blockIdx.x, step = PAIR ? gridDim.x / 2 : gridDim.x;
+    const uint32_t rank = PAIR ? blockIdx.x & 1u : 0u, first = PAIR ? blockIdx.x / 2 : SPLIT ? blockIdx.x / P.split : blockIdx.x;
+    const uint32_t step = PAIR ? gridDim.x / 2 : gridDim.x;   // (SPLIT: beyond the tiles)
+    const uint32_t part = SPLIT ? blockIdx.x - first * P.split : 0u, ks0 = SPLIT ? part * P.split_stages : 0u, ks1 = SPLIT ? min(ks0 + P.split_stages, P.stages_k) : P.stages_k;
     uint8_t *const ring = mm_smem + ((1024u - (tc::saddr(mm_smem) & 1023u)) & 1023u);
     const tc::Waits waits = {&S.dead, PAIR ? tc::address_in(&S.dead, rank ^ 1u) : 0u, &g_mm_ran_out};
     if (warp == 1 && lane < (int)(sizeof maps / sizeof maps.a))
@@ -185,7 +235,7 @@ __global__ void __launch_bounds__(kMmThreads, 1) k_matmul(const __grid_constant_
         for (uint32_t tile = first; ok && tile < P.n_tiles; tile += step) {
             const MmTile at = mm_tile(P, tile);
             const uint32_t tm = at.m * (PAIR ? 2 : 1) + rank, n0 = at.n * P.bn;   // (tm in 128 rows)
-            for (uint32_t ks = 0; ks < P.stages_k; ++ks) {
+            for (uint32_t ks = ks0; ks < ks1; ++ks) {
                 if (!(ok = armed < P.loads[rank] && tc::bar_wait(&S.empty[s], phase ^ 1u, waits, P.limit)))
                     break;
                 if (tc::elect())
@@ -209,13 +259,13 @@ __global__ void __launch_bounds__(kMmThreads, 1) k_matmul(const __grid_constant_
             if (!(ok = tc::bar_wait(&S.taken[set], turn ^ 1u, waits, P.limit)))
                 break;
             tc::fence_after();
-            for (uint32_t ks = 0; ks < P.stages_k; ++ks) {
+            for (uint32_t ks = ks0; ks < ks1; ++ks) {
                 if (!(ok = tc::bar_wait(&S.full[s], phase, waits, P.limit)))
                     break;
                 tc::fence_after();
                 if (tc::elect()) {
                     const uint32_t sa = P.scale_column + s * F::kScaleColumns, sb = sa + F::kTiles * 4;
-                    F::template issue<PAIR>(P, d, a0 + s * step16, b0 + s * step16, sc0 + s * step16, instruction, sa, sb, shift, scale_rows, ks);
+                    F::template issue<PAIR>(P, d, a0 + s * step16, b0 + s * step16, sc0 + s * step16, instruction, sa, sb, shift, scale_rows, ks, ks0);
                     tc::commit<PAIR>(&S.empty[s]);
                 }
                 if (++s == P.stages)
@@ -225,6 +275,22 @@ __global__ void __launch_bounds__(kMmThreads, 1) k_matmul(const __grid_constant_
                 tc::commit<PAIR>(&S.sums[set]);
             if (++set == P.sums)
                 set = 0, turn ^= 1u;
+        }
+        __syncwarp();
+    } else if (SPLIT) {
+        const uint32_t c0 = (uint32_t)(warp >> 2) * 64;
+        if (c0 < P.bn && tc::bar_wait(&S.sums[0], 0, waits, P.sums_limit)) {   // (where the wait runs out, `dead` tells all CTAs)
+            tc::fence_after();
+            uint4 *const to = (uint4 *)ring + (((warp & 3) * 32 + lane) * (P.bn + 4) + c0) / 4;   // (rows 16 bytes apart: eight lanes' go to all banks)
+#pragma unroll
+            for (uint32_t q = 0; q < 64; q += 32) {
+                uint32_t v[32];
+                tc::tmem_load32(((uint32_t)(warp & 3) << 21) + c0 + q, v);
+                tc::tmem_load_wait();
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    to[q / 4 + i] = make_uint4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
+            }
         }
         __syncwarp();
     } else {
@@ -299,9 +365,19 @@ __global__ void __launch_bounds__(kMmThreads, 1) k_matmul(const __grid_constant_
     }
     tc::fence_before();
     __syncthreads();
-    if (PAIR)
+    if (PAIR || SPLIT)
         tc::cluster_sync();   // neither CTA tells a barrier of one that has ended
     tc::fence_after();
+    if constexpr (SPLIT) {
+        if (P.split == 2)
+            mm_join<2>(P, (const float *)ring, S.dead, mm_tile(P, first), part, out);
+        else if (P.split == 4)
+            mm_join<4>(P, (const float *)ring, S.dead, mm_tile(P, first), part, out);
+        else
+            mm_join<8>(P, (const float *)ring, S.dead, mm_tile(P, first), part, out);
+        __syncthreads();
+        tc::cluster_sync();   // (all have read)
+    }
     if (*waits.dead) {
         // A wait has run out (in a pair both know by now).  What is in flight ends before shared and tensor memory are given back: the copies, for whose
         // barriers to be told of all their bytes each CTA of a pair brings what the other has, and the products.
@@ -365,21 +441,35 @@ static bool encode(CUtensorMap *map, CUtensorMapDataType type, int elem, const v
 struct MmChoice {
     uint32_t bn;
     bool pair;
+    uint32_t split;
     int64_t cost;
 };
 template <class F>
 static MmChoice mm_choice(int64_t m, int64_t n, int64_t k)
 {
     const int64_t k_steps = (k + F::kStepK - 1) / F::kStepK;
-    MmChoice best = {0, false, 0};
+    MmChoice best = {0, false, 1, 0};
     for (int pair = 0; pair < 2; ++pair)
         for (uint32_t bn = pair ? 128 : 64; bn <= 256; bn += 64) {
             const int64_t rows = pair ? 2 * kMmM : kMmM, sets = pair ? kPlanSMs / 2 : kPlanSMs;
             const int64_t waves = ((m + rows - 1) / rows * ((n + bn - 1) / bn) + sets - 1) / sets;
             const int64_t cost = waves * (k_steps * F::per_step(pair, bn / 64 - 1) + F::per_tile(bn / 64 - 1)) + pair * 1000;
             if (!best.bn || cost < best.cost)
-                best = {bn, pair != 0, cost};
+                best = {bn, pair != 0, 1, cost};
         }
+    if constexpr (F::kSplits) {
+        // Clusters that share tiles along k, as many as run at once (74, 33 or 15 with a CTA to an SM, which lie in groups of 16 to 20: a second wave of one takes
+        // as long as the first; 256 x 512 x 8192 by 16 clusters 16 us, 448 columns by 14 9.2); to begin, to join the sums and to end they take 2 us more.
+        // Without and with: 64 x 1600 x 6400 13.4 and 8.7 us, 64 x 4096 x 4096 10.6 and 8.7, 768 x 768 x 8192 17 and 13, 256 x 256 x 32768 53 and 14.
+        const int64_t stages = (k + F::kStageK - 1) / F::kStageK;
+        for (uint32_t bn = 64; bn <= 128; bn += 64)
+            for (uint32_t split = 2; split <= 8; split *= 2) {
+                const int64_t tiles = (m + kMmM - 1) / kMmM * ((n + bn - 1) / bn), each = (stages + split - 1) / split;
+                const int64_t cost = each * (F::kStageK / F::kStepK) * F::per_step(0, bn / 64 - 1) + F::per_tile(bn / 64 - 1) + 2000;
+                if (tiles <= (split == 2 ? 72 : split == 4 ? 32 : 14) && each >= 4 && each * (split - 1) < stages && cost < best.cost)
+                    best = {bn, false, split, cost};
+            }
+    }
     return best;
 }
 
@@ -389,11 +479,12 @@ struct MmLimit {
 };
 inline MmLimit mm_limit;   // (of all formats)
 
-template <class F, class T, bool PAIR>
-static int matmul(const uint8_t *a, const uint8_t *as, int64_t m, const uint8_t *b, const uint8_t *bs, int64_t n, int64_t k, T *out, int64_t ld, uint32_t bn,
+template <class F, class T, bool PAIR, bool SPLIT>
+static int matmul(const uint8_t *a, const uint8_t *as, int64_t m, const uint8_t *b, const uint8_t *bs, int64_t n, int64_t k, T *out, int64_t ld, const MmChoice &choice,
                   int kind_a, int kind_b, const char *what, cudaStream_t s)
 {
     constexpr int64_t kRows = PAIR ? 2 * kMmM : kMmM;
+    const uint32_t bn = choice.bn;
     MmArgs P;
     P.as = as;
     P.bs = bs;
@@ -404,6 +495,8 @@ static int matmul(const uint8_t *a, const uint8_t *as, int64_t m, const uint8_t 
     P.stages_k = (uint32_t)((k + F::kStageK - 1) / F::kStageK);
     P.kind_a = (uint32_t)kind_a;
     P.kind_b = (uint32_t)kind_b;
+    P.split = SPLIT ? choice.split : 1;
+    P.split_stages = (P.stages_k + P.split - 1) / P.split;
     P.limit = (uint64_t)mm_limit.nanoseconds.load();
     // (a stage takes 0.4 us at most where nothing else runs)
     P.sums_limit = P.limit + 4096ull * P.stages_k;
@@ -429,7 +522,7 @@ static int matmul(const uint8_t *a, const uint8_t *as, int64_t m, const uint8_t 
     P.scale_column = P.sums * bn > 256 ? 384 : 256;
     const uint32_t stage_bytes = mm_stage_bytes(bn, PAIR);
     const uint32_t room = kMmSmem - 1024 - mm_staging(bn);
-    P.stages = std::min<uint32_t>({(uint32_t)kMmMaxStages, (kMmColumns - P.scale_column) / F::kScaleColumns, room / stage_bytes, std::max(2u, P.stages_k)});
+    P.stages = std::min<uint32_t>({(uint32_t)kMmMaxStages, (kMmColumns - P.scale_column) / F::kScaleColumns, room / stage_bytes, std::max(2u, P.split_stages)});   // (SPLIT: a tile's sums fit two)
     // (a tiled copy writes a row's last 16 bytes whole, whatever the map says of its end)
     P.tiled = (((uint64_t)ld * sizeof(T)) | ((uint64_t)n * sizeof(T)) | (uintptr_t)out) % 16 == 0;
     MmMaps maps = {};
@@ -448,12 +541,14 @@ static int matmul(const uint8_t *a, const uint8_t *as, int64_t m, const uint8_t 
     // each could hold one half.  A pair leaves no shared memory at all, since the other one could be any kernel's.
     const size_t smem = PAIR ? kMmSmem : std::max<size_t>(1024 + (size_t)P.stages * stage_bytes + mm_staging(bn), kMmAlone);
     static int done[64];
-    cudaError_t e = opt_in_smem(k_matmul<F, T, PAIR>, kMmSmem, done);
+    cudaError_t e = opt_in_smem(k_matmul<F, T, PAIR, SPLIT>, kMmSmem, done);
     if (e == cudaSuccess) {
         if (PAIR)
-            e = launch_cluster(k_matmul<F, T, PAIR>, (int)std::min<uint32_t>(P.n_tiles, kPlanSMs / 2), 2, kMmThreads, s, smem, maps, P, out);
+            e = launch_cluster(k_matmul<F, T, PAIR, SPLIT>, (int)std::min<uint32_t>(P.n_tiles, kPlanSMs / 2), 2, kMmThreads, s, smem, maps, P, out);
+        else if (SPLIT)
+            e = launch_cluster(k_matmul<F, T, PAIR, SPLIT>, (int)P.n_tiles, (int)P.split, kMmThreads, s, smem, maps, P, out);
         else
-            e = launch(k_matmul<F, T, PAIR>, dim3(std::min<uint32_t>(P.n_tiles, kPlanSMs)), kMmThreads, smem, s, maps, P, out);
+            e = launch(k_matmul<F, T, PAIR, SPLIT>, dim3(std::min<uint32_t>(P.n_tiles, kPlanSMs)), kMmThreads, smem, s, maps, P, out);
     }
     return launched(e, what);
 }

@@ -14,6 +14,7 @@ namespace conef {
 
 struct Mx4Format {
     static constexpr uint32_t kStageK = 256, kStepK = 64, kTiles = 2, kTileStages = 1, kScaleColumns = 24;
+    static constexpr bool kSplits = false;   // (which would change the order of sums)
     static int64_t row_bytes(int64_t k) { return mx4_blocks(k) * 16; }
     static int64_t scale_tiles(int64_t k) { return mx4_scale_tiles(k); }
     // Nanoseconds per wave of tiles, from 8192 x 6400 by 1600 and by 4096: what a step of 64 along k takes (full rate
@@ -37,7 +38,7 @@ struct Mx4Format {
     // stage ks: its scales to tensor memory, then the products
     template <bool PAIR>
     static __device__ __forceinline__ void issue(const MmArgs &P, uint32_t d, uint32_t a, uint32_t b, uint32_t sc, uint32_t instruction, uint32_t sa, uint32_t sb, uint32_t shift,
-                                                 uint32_t scale_rows, uint32_t ks)
+                                                 uint32_t scale_rows, uint32_t ks, uint32_t ks0)
     {
         const uint32_t steps = P.k_steps - ks * 4u;
 #pragma unroll
@@ -51,7 +52,7 @@ struct Mx4Format {
 #pragma unroll
         for (uint32_t t = 0; t < 2; ++t) {
             if (2 * t < steps)
-                tc::mx4_product<PAIR, 0>(d, a + 4 * t, b + 4 * t, instruction, sa + 4 * t, sb + 8 * t + shift, ks + t);
+                tc::mx4_product<PAIR, 0>(d, a + 4 * t, b + 4 * t, instruction, sa + 4 * t, sb + 8 * t + shift, ks - ks0 + t);
             if (2 * t + 1 < steps)
                 tc::mx4_product<PAIR, 1>(d, a + 4 * t + 2, b + 4 * t + 2, instruction, sa + 4 * t, sb + 8 * t + shift, 1);
         }
@@ -86,8 +87,8 @@ int conef_mx4_matmul(const void *a_codes, const void *a_scales, int64_t m, const
     return with_elem(dtype, [&](auto t) {
         using T = decltype(t);
         const MmChoice c = mm_choice<Mx4Format>(m, n, k);
-        return (c.pair ? matmul<Mx4Format, T, true> : matmul<Mx4Format, T, false>)((const uint8_t *)a_codes, (const uint8_t *)a_scales, m, (const uint8_t *)b_codes,
-                                                             (const uint8_t *)b_scales, n, k, (T *)out, ld, c.bn, 0, 0, "conef_mx4_matmul", (cudaStream_t)stream);
+        return (c.pair ? matmul<Mx4Format, T, true, false> : matmul<Mx4Format, T, false, false>)((const uint8_t *)a_codes, (const uint8_t *)a_scales, m, (const uint8_t *)b_codes,
+                                                             (const uint8_t *)b_scales, n, k, (T *)out, ld, c, 0, 0, "conef_mx4_matmul", (cudaStream_t)stream);
     });
 }
 

@@ -310,3 +310,27 @@ def test_product_of_some_rows_with_a_nan_block(b):
         bad = torch.zeros_like(out, dtype=torch.bool)
         bad[i], bad[:, j] = True, True
         assert torch.equal(torch.isnan(out), bad)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("m,n,k", [(100, 1600, 6400), (130, 77, 8192), (200, 130, 20000), (256, 256, 33001), (65, 65, 4097), (129, 513, 2048), (300, 700, 5000), (768, 768, 8192)])
+def test_product_of_few_tiles_against_a_long_k(b, m, n, k, dtype):
+    """... where thread blocks share a tile along k."""
+    a, c = b.f8_quantise(matrix(m, k, torch.bfloat16), kind="e5m2"), b.f8_quantise(matrix(n, k, torch.bfloat16, 1, 0.02))
+    got = b.f8_matmul(a, c, dtype)
+    check_product(got, values(a), values(c), dtype)
+    assert all(torch.equal(b.f8_matmul(a, c, dtype), got) for _ in range(3))
+
+
+def test_product_of_few_tiles_into_a_wider_matrix_with_a_nan_block(b):
+    x, w = matrix(140, 9000, torch.bfloat16), matrix(90, 9000, torch.bfloat16, 1)
+    x[139, 8999], w[66, 639] = float("nan"), float("inf")
+    p, q = b.f8_quantise(x), b.f8_quantise(w)
+    wide = torch.full((142, 93), 7.0, device="cuda")
+    assert b.lib.conef_f8_matmul(p.codes.data_ptr(), p.scales.data_ptr(), b.E4M3, 140, q.codes.data_ptr(), q.scales.data_ptr(), b.E4M3, 90, 9000, wide[1:, 1:].data_ptr(), b.F32, 93,
+                                 b._stream_handle(None)) == b.OK
+    bad = torch.zeros(140, 90, dtype=torch.bool, device="cuda")
+    bad[139], bad[:, 66] = True, True
+    assert torch.equal(torch.isnan(wide[1:-1, 1:-2]), bad)
+    wide[1:-1, 1:-2] = 7.0
+    assert (wide == 7.0).all()

@@ -70,3 +70,10 @@ def test_orthogonalise(b, short_waits, rows, cols, batch, loads, second):
     assert torch.equal(torch.where(lost, want, got), want)
     assert all(torch.equal(b.orthogonalise(x, steps=2), want) for _ in range(3))
     assert b.orthogonalise_timeouts() == after
+
+
+@pytest.mark.parametrize("shape,loads", [((100, 1600, 6400), 0), ((100, 1600, 6400), 5), ((200, 130, 20000), 17), ((256, 256, 33001), 6), ((768, 768, 8192), 31)])
+def test_blocks_that_share_a_tile_along_k(b, short_waits, shape, loads):
+    """Nothing is computed, also where the last blocks of tiles, which have fewer stages (11 of 13, 17 of 20), have all of theirs."""
+    lost, all_of_them = check(b, short_waits, shape, torch.bfloat16, loads)
+    assert lost == all_of_them
