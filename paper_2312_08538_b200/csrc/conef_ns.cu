@@ -199,6 +199,9 @@ struct NsArgs {
     uint32_t wide;                  // the result goes by tiled copies
     uint64_t limit, sums_limit;
     uint32_t loads[2];
+    uint32_t split, split_stages;   // CTAs of a cluster that share a tile's k, and stages of each (an even number; the last one's may be fewer)
+    __half *hi, *lo;                // ... which store their outputs themselves
+    int64_t out_pitch, out_stride;
 };
 struct NsMaps {
     CUtensorMap lh, ll, rh, rl;     // tiles of 64 elements by 128 rows (CROSS, R: 64)
@@ -296,9 +299,51 @@ __device__ __forceinline__ void ns_result(const NsArgs &P, uint32_t batch, uint3
             out[P.flip ? (int64_t)(col + i) * P.result_ld + row : (int64_t)row * P.result_ld + col + i] = (uint16_t)(w[i / 2] >> (16 * (i & 1)));
 }
 
+// The sums of a tile whose k the CTAs of a cluster share (conef_mm.cuh): each CTA adds up its columns, four to a thread, in the CTAs' order, and stores them, twice off the diagonal
+template <int SPLIT>
+__device__ __forceinline__ void ns_join(const NsArgs &P, const float *sums, const int &dead, const NsTile &t, uint32_t part)
+{
+    constexpr uint32_t width = 128 / SPLIT, quads = width / 4;
+    uint32_t any = 0;
+#pragma unroll
+    for (int i = 0; i < SPLIT; ++i)
+        any |= tc::load_at(tc::address_in(&dead, i));
+    __half *const hi = P.hi + (int64_t)t.batch * P.out_stride, *const lo = P.lo + (int64_t)t.batch * P.out_stride;
+    for (uint32_t e = threadIdx.x; e < 128 * quads; e += kMmThreads) {
+        const uint32_t r = e / quads, c = part * width + e % quads * 4, row = t.i * 128 + r, col = t.j * 128 + c;
+        if (row >= P.n || col >= P.m)
+            continue;
+        float4 v[SPLIT];
+#pragma unroll
+        for (int i = 0; i < SPLIT; ++i)
+            v[i] = tc::load_at4(tc::address_in(sums + r * 132 + c, i));
+        float f[4] = {v[0].x, v[0].y, v[0].z, v[0].w};
+#pragma unroll
+        for (int i = 1; i < SPLIT; ++i)
+            f[0] = __fadd_rn(f[0], v[i].x), f[1] = __fadd_rn(f[1], v[i].y), f[2] = __fadd_rn(f[2], v[i].z), f[3] = __fadd_rn(f[3], v[i].w);
+        __half h[4], l[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            split(any ? __uint_as_float(0x7FFFFFFFu) : __fmul_rn(f[i], P.f_sum), h[i], l[i]);
+        const int64_t at = (int64_t)row * P.out_pitch + col;   // (rows are padded to 64 elements)
+        *(uint2 *)(hi + at) = *(const uint2 *)h;
+        if (P.out_lo)
+            *(uint2 *)(lo + at) = *(const uint2 *)l;
+        if (t.i != t.j)
+#pragma unroll
+            for (uint32_t i = 0; i < 4; ++i)
+                if (col + i < P.m) {
+                    const int64_t turned = (int64_t)(col + i) * P.out_pitch + row;
+                    hi[turned] = h[i];
+                    if (P.out_lo)
+                        lo[turned] = l[i];
+                }
+    }
+}
+
 // A tile is 128 x 128, or of a pair of CTAs 256 by 128, 192 (not symmetric) or 256: with 128 x 128 a product reads as many bytes of shared memory per cycle as there
 // are, so that the copies into it have to wait; a pair's CTA has half of R for as many rows of L.
-template <bool PAIR, bool CROSS>
+template <bool PAIR, bool CROSS, bool SPLIT>
 __global__ void __launch_bounds__(kMmThreads, 1) k_ns_product(const __grid_constant__ NsMaps maps, const __grid_constant__ NsArgs P)
 {
     constexpr uint32_t BM = PAIR ? 256 : 128;
@@ -307,7 +352,8 @@ __global__ void __launch_bounds__(kMmThreads, 1) k_ns_product(const __grid_const
     __shared__ NsShared N;
     MmShared &S = N.mm;
     const int warp = __shfl_sync(0xffffffffu, (int)(threadIdx.x >> 5), 0), lane = threadIdx.x & 31;
-    const uint32_t rank = PAIR ? blockIdx.x & 1u : 0u, first = PAIR ? blockIdx.x / 2 : blockIdx.x, step = PAIR ? gridDim.x / 2 : gridDim.x;
+    const uint32_t rank = PAIR ? blockIdx.x & 1u : 0u, first = PAIR ? blockIdx.x / 2 : SPLIT ? blockIdx.x / P.split : blockIdx.x, step = PAIR ? gridDim.x / 2 : gridDim.x;
+    const uint32_t part = SPLIT ? blockIdx.x - first * P.split : 0u, ks0 = SPLIT ? part * P.split_stages : 0u, ks1 = SPLIT ? min(ks0 + P.split_stages, P.stages_k) : P.stages_k;
     uint8_t *const ring = mm_smem + ((1024u - (tc::saddr(mm_smem) & 1023u)) & 1023u);
     const tc::Waits waits = {&S.dead, PAIR ? tc::address_in(&S.dead, rank ^ 1u) : 0u, &g_mm_ran_out};
     if (warp == 1 && lane < (int)(sizeof maps / sizeof maps.lh))
@@ -367,7 +413,7 @@ __global__ void __launch_bounds__(kMmThreads, 1) k_ns_product(const __grid_const
         bool ok = true;
         for (uint32_t tile = first; ok && tile < P.n_tiles; tile += step) {
             const NsTile t = ns_tile(P, tile);
-            for (uint32_t ks = 0; ks < P.stages_k; ++ks) {
+            for (uint32_t ks = ks0; ks < ks1; ++ks) {
                 if (!(ok = armed < P.loads[rank] && tc::bar_wait(&S.empty[s], phase ^ 1u, waits, P.limit)))
                     break;
                 if (tc::elect())
@@ -392,7 +438,7 @@ __global__ void __launch_bounds__(kMmThreads, 1) k_ns_product(const __grid_const
                 break;
             tc::fence_after();
             uint32_t high = 0;   // the stage before, where that has the hi parts
-            for (uint32_t ks = 0; ks < P.stages_k; ++ks) {
+            for (uint32_t ks = ks0; ks < ks1; ++ks) {
                 if (!(ok = tc::bar_wait(&S.full[s], phase, waits, P.limit)))
                     break;
                 tc::fence_after();
@@ -403,7 +449,7 @@ __global__ void __launch_bounds__(kMmThreads, 1) k_ns_product(const __grid_const
 #pragma unroll
                         for (uint32_t t = 0; t < 4; ++t)
                             if (t < steps)
-                                tc::f16_product<PAIR>(d, a + 2 * t, b + k_step * t, instruction, ks + t);
+                                tc::f16_product<PAIR>(d, a + 2 * t, b + k_step * t, instruction, ks - ks0 + t);
                         if (P.single)
                             tc::commit<PAIR>(&S.empty[s]);
                     } else {
@@ -426,6 +472,22 @@ __global__ void __launch_bounds__(kMmThreads, 1) k_ns_product(const __grid_const
                 tc::commit<PAIR>(&S.sums[set]);
             if (++set == 2)
                 set = 0, turn ^= 1u;
+        }
+        __syncwarp();
+    } else if (SPLIT) {
+        const uint32_t c0 = (uint32_t)(warp >> 2) * 64;
+        if (c0 < BN && tc::bar_wait(&S.sums[0], 0, waits, P.sums_limit)) {   // (where the wait runs out, `dead` tells all CTAs)
+            tc::fence_after();
+            uint4 *const to = (uint4 *)ring + (((warp & 3) * 32 + lane) * 132 + c0) / 4;
+#pragma unroll
+            for (uint32_t q = 0; q < 4; ++q) {
+                uint32_t v[16];
+                tc::tmem_load16(((uint32_t)(warp & 3) << 21) + c0 + q * 16, v);
+                tc::tmem_load_wait();
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    to[q * 4 + i] = make_uint4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
+            }
         }
         __syncwarp();
     } else {
@@ -554,9 +616,20 @@ __global__ void __launch_bounds__(kMmThreads, 1) k_ns_product(const __grid_const
     }
     tc::fence_before();
     __syncthreads();
-    if (PAIR)
+    if (PAIR || SPLIT)
         tc::cluster_sync();   // neither CTA tells a barrier of one that has ended
     tc::fence_after();
+    if constexpr (SPLIT) {
+        const NsTile t = ns_tile(P, first);
+        if (P.split == 2)
+            ns_join<2>(P, (const float *)ring, S.dead, t, part);
+        else if (P.split == 4)
+            ns_join<4>(P, (const float *)ring, S.dead, t, part);
+        else
+            ns_join<8>(P, (const float *)ring, S.dead, t, part);
+        __syncthreads();
+        tc::cluster_sync();   // (all have read)
+    }
     if (*waits.dead) {   // as in conef_mm.cuh: what is in flight ends before shared and tensor memory are given back
         const uint64_t t0 = tc::nanoseconds();
         if (warp == kMmEpilogue) {
@@ -609,10 +682,11 @@ struct NsTiles {
     bool pair;
     uint32_t bn;
     int one, three, fixed;
+    uint32_t split;   // CTAs that share a tile along k
 };
-static NsTiles ns_tiles(int64_t n, int64_t m, int64_t k, int64_t batch, bool symmetric, bool single)
+static NsTiles ns_tiles(int64_t n, int64_t m, int64_t k, int64_t batch, bool symmetric, bool splits, bool single)
 {
-    static const NsTiles kinds[] = {{false, 128, 270, 740, 4500}, {true, 128, 300, 600, 5500}, {true, 192, 340, 880, 6000}, {true, 256, 305, 980, 7000}};
+    static const NsTiles kinds[] = {{false, 128, 270, 740, 4500, 1}, {true, 128, 300, 600, 5500, 1}, {true, 192, 340, 880, 6000, 1}, {true, 256, 305, 980, 7000, 1}};
     NsTiles best = {};
     int64_t least = -1;
     for (const NsTiles &c : kinds) {
@@ -627,6 +701,14 @@ static NsTiles ns_tiles(int64_t n, int64_t m, int64_t k, int64_t batch, bool sym
         if (least < 0 || cost < least)
             best = c, least = cost;
     }
+    // A of X with few rows: clusters, as many as run at once (conef_mm.cuh), which take 3.5 us more to begin, to join and to end.  All of five steps without and with: 64 x 4096
+    // 240 and 115 us, 100 x 1000 151 and 122.
+    for (uint32_t split = 2; splits && split <= 8; split *= 2) {
+        const int64_t ti = (n + 127) / 128, tiles = ti * (ti + 1) / 2 * batch, stages = (k + 63) / 64, each = (stages + split - 1) / split;
+        const int64_t cost = each * (single ? kinds[0].one : kinds[0].three) + kinds[0].fixed + 3500;
+        if (tiles <= (split == 2 ? 72 : split == 4 ? 32 : 14) && each * (split - 1) < stages && cost < least)
+            best = kinds[0], best.split = split, least = cost;
+    }
     return best;
 }
 
@@ -639,7 +721,7 @@ static cudaError_t ns_product(const Split &L, const Split &R, const Split *E, co
     P.k = (uint32_t)L.cols;
     P.k_steps = (P.k + 15) / 16;
     P.stages_k = (P.k + 63) / 64 * (P.single ? 1 : 2);
-    const NsTiles kind = ns_tiles(P.n, P.m, P.k, batch, P.symmetric, P.single);
+    const NsTiles kind = ns_tiles(P.n, P.m, P.k, batch, P.symmetric, !CROSS && !E, P.single);
     const bool pair = kind.pair;
     const uint32_t high = pair ? 256 : 128;
     P.bn = kind.bn;
@@ -659,6 +741,11 @@ static cudaError_t ns_product(const Split &L, const Split &R, const Split *E, co
     P.sums_limit = P.limit + 4096ull * P.stages_k;
     P.loads[0] = mm_limit.loads[0].load();
     P.loads[1] = mm_limit.loads[1].load();
+    P.split = kind.split;
+    const uint32_t stages = (P.k + 63) / 64;
+    P.split_stages = (stages + P.split - 1) / P.split * (P.single ? 1 : 2);
+    if (P.split > 1)
+        P.hi = out->hi, P.lo = out->lo, P.out_pitch = out->pitch, P.out_stride = out->pitch * out->rows;
     NsMaps maps = {};
     const uint32_t r_box = CROSS ? 64 : pair ? P.bn / 2 : P.bn;
     bool ok = encode_split(&maps.lh, L.hi, L, batch, 64, 128) && encode_split(&maps.ll, L.lo, L, batch, 64, 128) && encode_split(&maps.rh, R.hi, R, batch, 64, r_box) &&
@@ -676,13 +763,19 @@ static cudaError_t ns_product(const Split &L, const Split &R, const Split *E, co
     }
     if (!ok)
         return cudaErrorInvalidValue;
-    static int done[2][64];
-    cudaError_t e = pair ? opt_in_smem(k_ns_product<true, CROSS>, kMmSmem, done[1]) : opt_in_smem(k_ns_product<false, CROSS>, kMmSmem, done[0]);
+    static int done[3][64];
+    const size_t smem = 1024 + (size_t)P.stages * P.stage_bytes + staging;
+    if constexpr (!CROSS)
+        if (P.split > 1) {
+            const cudaError_t e = opt_in_smem(k_ns_product<false, false, true>, kMmSmem, done[2]);
+            return e != cudaSuccess ? e : launch_cluster(k_ns_product<false, false, true>, (int)P.n_tiles, (int)P.split, kMmThreads, s, smem, maps, P);
+        }
+    const cudaError_t e = pair ? opt_in_smem(k_ns_product<true, CROSS, false>, kMmSmem, done[1]) : opt_in_smem(k_ns_product<false, CROSS, false>, kMmSmem, done[0]);
     if (e != cudaSuccess)
         return e;
     // (a pair leaves no shared memory on its SMs: conef_mm.cuh)
-    return pair ? launch_cluster(k_ns_product<true, CROSS>, (int)std::min<uint32_t>(P.n_tiles, kPlanSMs / 2), 2, kMmThreads, s, (size_t)kMmSmem, maps, P)
-                : launch(k_ns_product<false, CROSS>, dim3(std::min<uint32_t>(P.n_tiles, kPlanSMs)), kMmThreads, 1024 + (size_t)P.stages * P.stage_bytes + staging, s, maps, P);
+    return pair ? launch_cluster(k_ns_product<true, CROSS, false>, (int)std::min<uint32_t>(P.n_tiles, kPlanSMs / 2), 2, kMmThreads, s, (size_t)kMmSmem, maps, P)
+                : launch(k_ns_product<false, CROSS, false>, dim3(std::min<uint32_t>(P.n_tiles, kPlanSMs)), kMmThreads, smem, s, maps, P);
 }
 
 // the largest |b t + c t^2| for 0 <= t <= top, and the largest |s (a + b s^2 + c s^4)| for 0 <= s <= top

@@ -54,7 +54,7 @@ def test_pairs_that_bring_different_numbers_of_stages(b, short_waits, loads, sec
 
 
 @pytest.mark.parametrize("rows,cols,batch", [(100, 300, 1), (600, 200, 3), (1600, 1600, 1), (700, 2500, 3)])
-@pytest.mark.parametrize("loads,second", [(0, 0), (1, 1), (0, -1), (-1, 0), (3, 5), (6, 2), (9, 9)])
+@pytest.mark.parametrize("loads,second", [(0, 0), (1, 1), (0, -1), (-1, 0), (3, 5), (6, 2), (7, 7)])   # (blocks that share a tile along its rows bring six)
 def test_orthogonalise(b, short_waits, rows, cols, batch, loads, second):
     """Few steps, so that the waits of all launches last a second at most; a product that lacks a tile leaves NaN in the next ones' sums."""
     x = torch.stack([update(rows, cols, torch.bfloat16, i) for i in range(batch)])
@@ -77,3 +77,17 @@ def test_blocks_that_share_a_tile_along_k(b, short_waits, shape, loads):
     """Nothing is computed, also where the last blocks of tiles, which have fewer stages (11 of 13, 17 of 20), have all of theirs."""
     lost, all_of_them = check(b, short_waits, shape, torch.bfloat16, loads)
     assert lost == all_of_them
+
+
+@pytest.mark.parametrize("rows,cols,loads", [(100, 4000, 0), (100, 4000, 3), (100, 4000, 13), (300, 5000, 0), (300, 5000, 3), (300, 5000, 9)])
+def test_orthogonalise_long_rows(b, short_waits, rows, cols, loads):
+    """Blocks that share a tile along its rows: of 4000 16 half stages each (the last ones 14), of 5000, from 256 rows on the hi parts alone, 10 of 79 stages (the last ones,
+    which have all of theirs with loads = 9, 9): nothing is computed."""
+    x = update(rows, cols, torch.bfloat16)
+    want = b.orthogonalise(x, steps=2)
+    before = b.orthogonalise_timeouts()
+    short_waits(loads)
+    got = b.orthogonalise(x, steps=2)
+    b.mx4_set_waits()
+    assert b.orthogonalise_timeouts() > before and torch.isnan(got).all()
+    assert all(torch.equal(b.orthogonalise(x, steps=2), want) for _ in range(3))

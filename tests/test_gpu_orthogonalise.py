@@ -56,6 +56,17 @@ def test_large_and_many(b, rows, cols, batch):
         check(b.orthogonalise(x[batch - 1]), x[batch - 1])
 
 
+@pytest.mark.parametrize("rows,cols,batch", [(1, 9000, 1), (100, 4000, 1), (40, 9001, 2), (300, 5000, 1), (128, 8192, 3), (5000, 130, 1), (3000, 200, 14), (513, 2500, 1)])
+def test_long_rows(b, rows, cols, batch):
+    """... whose products with themselves blocks share along the rows."""
+    x = torch.stack([update(rows, cols, torch.bfloat16, i) for i in range(batch)])
+    for to in (torch.bfloat16, torch.float16):
+        got = b.orthogonalise(x, dtype=to)
+        for i in {0, batch - 1}:
+            check(got[i], x[i])
+        assert all(torch.equal(b.orthogonalise(x, dtype=to), got) for _ in range(3))
+
+
 def test_singular_values(b):
     """Those of the result are the polynomial of x's: no further from it than the result is from the exact one (Weyl), by check()'s bound.  (After twelve cubic
     steps the smallest of x, times 1.5 each, are still on their way to one.)"""
