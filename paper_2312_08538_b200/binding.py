@@ -630,8 +630,8 @@ _QUINTIC = (3.4445, -4.7750, 2.0315)   # (singular values go to between 0.7 and 
 def orthogonalise(x: torch.Tensor, steps: int = 5, scale: float = 1.0, coefficients: Sequence[float] = _QUINTIC, dtype: Optional[torch.dtype] = None,
                   out: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
     """x, a matrix or a stack of them (the dimensions before the last two), brought near the orthogonal matrix next to it by `steps` Newton-Schulz products of
-    its quotient by its Frobenius norm, X <- (c0 + c1 X X^T + c2 (X X^T)^2) X, times `scale`: an update as the Muon optimiser applies it.  The result is in
-    bfloat16 or float16 (default: x's type, bfloat16 for float32); out may be x."""
+    its quotient by its Frobenius norm, X <- (c0 + c1 X X^T + c2 (X X^T)^2) X, times `scale`: an update as the Muon optimiser applies it.  Products are of 22-bit
+    operands in fp32 sums throughout; the result is rounded once, to bfloat16 or float16 (default: x's type, bfloat16 for float32); out may be x."""
     where = "orthogonalise"
     if x.dim() < 2:
         _refuse(where, "x has fewer than two dimensions")

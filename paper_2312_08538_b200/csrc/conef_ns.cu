@@ -9,8 +9,9 @@
 //    host), which is 22 bits; a X is added in fp32 and only C X, C = b A + c A^2, is a product: its share of a rounding's noise in the directions
 //    of small singular values is as small as A has them.
 //  - A and C are kept likewise, and a product is the sum of hi hi, hi lo and lo hi in one set of fp32 sums on the tensor cores: as exact as 32-bit
-//    arithmetic at three times 16-bit's cost, not at the 20 times that 32-bit units take.
-//  - Some products, most of them in the first steps, are hi hi alone (ns_single()).
+//    arithmetic at three times 16-bit's cost, not at the 20 times that 32-bit units take.  (hi hi alone in products of the first steps leaves an error of 1e-3 in five
+//    steps, 4e-3 in twenty, ahead of the rounding, whose own is 1.7e-3 in bf16 and 2e-4 in fp16: no product does so.  It would take 257 us for 1600 x 1600 in place of 350, and
+//    764 for 2 x 6400 x 1600 in place of 1436.)
 //
 // Per step three launches: A (symmetric: tiles on and above the diagonal, stored twice), C (likewise, A added on the way out), C X (a X added).
 #include <cuda.h>
@@ -182,10 +183,10 @@ __global__ void __launch_bounds__(256) k_ns_start(const __grid_constant__ NsIn A
 
 // ------------------------------------------------------------------ products
 // D = f_sum (L R) + f_add E for stacks of matrices; R along k like L (A = X X^T, A A), or (CROSS) as it is multiplied, along D's columns (C X).
-// The kernel is that of conef_mm.cuh with another ring and another way out.  A stage has 64 elements of k of L and R, their hi parts or their lo parts; without the
-// lo parts (`single`) each is a product, with them two in a row are three.  What leaves is split again, or rounded to the result; it goes through shared memory
+// The kernel is that of conef_mm.cuh with another ring and another way out.  A stage has 64 elements of k of L and R, their hi parts or their lo parts; two in a row
+// are three products.  What leaves is split again, or rounded to the result; it goes through shared memory
 // and tiled copies, and so does E: a row to a lane, straight to memory, 16 accesses to 32 lines each made 12000 cycles of a tile of 256 x 256, whose
-// products take 13000 (hi parts, k = 1600).
+// products hi hi take 13000 at k = 1600.
 struct NsArgs {
     void *result;                // the last product's, instead of the outputs
     int64_t result_ld, result_stride;
@@ -193,9 +194,9 @@ struct NsArgs {
     uint32_t n, m, k;            // of D = n x m
     uint32_t k_steps, stages_k, per_matrix, tiles_m, n_tiles;
     uint32_t tiles_wide;            // (symmetric) tiles are 256 x 128
-    uint32_t symmetric, flip, dtype, single;
+    uint32_t symmetric, flip, dtype;
     uint32_t bn, stage_bytes, stages;   // columns of a tile; the ring
-    uint32_t add, add_lo, out_lo;   // E, and the lo parts of E and of what is written
+    uint32_t add;                   // E
     uint32_t wide;                  // the result goes by tiled copies
     uint64_t limit, sums_limit;
     uint32_t loads[2];
@@ -327,16 +328,14 @@ __device__ __forceinline__ void ns_join(const NsArgs &P, const float *sums, cons
             split(any ? __uint_as_float(0x7FFFFFFFu) : __fmul_rn(f[i], P.f_sum), h[i], l[i]);
         const int64_t at = (int64_t)row * P.out_pitch + col;   // (rows are padded to 64 elements)
         *(uint2 *)(hi + at) = *(const uint2 *)h;
-        if (P.out_lo)
-            *(uint2 *)(lo + at) = *(const uint2 *)l;
+        *(uint2 *)(lo + at) = *(const uint2 *)l;
         if (t.i != t.j)
 #pragma unroll
             for (uint32_t i = 0; i < 4; ++i)
                 if (col + i < P.m) {
                     const int64_t turned = (int64_t)(col + i) * P.out_pitch + row;
                     hi[turned] = h[i];
-                    if (P.out_lo)
-                        lo[turned] = l[i];
+                    lo[turned] = l[i];
                 }
     }
 }
@@ -387,8 +386,8 @@ __global__ void __launch_bounds__(kMmThreads, 1) k_ns_product(const __grid_const
     asm volatile("fence.proxy.async;" ::: "memory");   // (what the launch before stored, ordinary stores, is read by copies)
 
     auto load = [&](uint32_t s, uint32_t ks, const NsTile &t) {
-        const uint32_t st = tc::saddr(ring) + s * P.stage_bytes, k0 = (P.single ? ks : ks / 2) * 64, i0 = t.i * BM + rank * 128, j0 = t.j * BN + rank * (BN / 2);
-        const bool low = !P.single && (ks & 1);
+        const uint32_t st = tc::saddr(ring) + s * P.stage_bytes, k0 = ks / 2 * 64, i0 = t.i * BM + rank * 128, j0 = t.j * BN + rank * (BN / 2);
+        const bool low = ks & 1;
         const void *const l = low ? &maps.ll : &maps.lh, *const r = low ? &maps.rl : &maps.rh;
         auto part = [&](uint32_t dst, const void *map, uint32_t x, uint32_t y) {
             if constexpr (PAIR)
@@ -444,16 +443,14 @@ __global__ void __launch_bounds__(kMmThreads, 1) k_ns_product(const __grid_const
                 tc::fence_after();
                 if (tc::elect()) {
                     const uint32_t a = a0 + s * step16, b = b0 + s * step16;
-                    if (P.single || !(ks & 1)) {
-                        const uint32_t steps = P.k_steps - (P.single ? ks : ks / 2) * 4u;
+                    const uint32_t steps = P.k_steps - ks / 2 * 4u;
+                    if (!(ks & 1)) {
 #pragma unroll
                         for (uint32_t t = 0; t < 4; ++t)
                             if (t < steps)
                                 tc::f16_product<PAIR>(d, a + 2 * t, b + k_step * t, instruction, ks - ks0 + t);
-                        if (P.single)
-                            tc::commit<PAIR>(&S.empty[s]);
                     } else {
-                        const uint32_t steps = P.k_steps - ks / 2 * 4u, ah = a0 + high * step16, bh = b0 + high * step16;
+                        const uint32_t ah = a0 + high * step16, bh = b0 + high * step16;
 #pragma unroll
                         for (uint32_t t = 0; t < 4; ++t)
                             if (t < steps) {
@@ -518,8 +515,7 @@ __global__ void __launch_bounds__(kMmThreads, 1) k_ns_product(const __grid_const
             };
             if (P.add && there) {
                 fetch(&maps.eh, h);
-                if (P.add_lo)
-                    fetch(&maps.el, l);
+                fetch(&maps.el, l);
             }
             ok = ok && tc::bar_wait(&S.sums[set], turn, waits, P.sums_limit);
             if (ok)
@@ -543,10 +539,8 @@ __global__ void __launch_bounds__(kMmThreads, 1) k_ns_product(const __grid_const
 #pragma unroll
                     for (int i = 0; i < 8; ++i) {
                         float2 a = __half22float2(*(const __half2 *)&h[8 * q + i]);
-                        if (P.add_lo) {
-                            const float2 b = __half22float2(*(const __half2 *)&l[8 * q + i]);
-                            a.x = __fadd_rn(a.x, b.x), a.y = __fadd_rn(a.y, b.y);
-                        }
+                        const float2 b = __half22float2(*(const __half2 *)&l[8 * q + i]);
+                        a.x = __fadd_rn(a.x, b.x), a.y = __fadd_rn(a.y, b.y);
                         f[2 * i] = __fmaf_rn(a.x, P.f_add, f[2 * i]), f[2 * i + 1] = __fmaf_rn(a.y, P.f_add, f[2 * i + 1]);
                     }
                 }
@@ -558,7 +552,7 @@ __global__ void __launch_bounds__(kMmThreads, 1) k_ns_product(const __grid_const
 #pragma unroll
                     for (int i = 0; i < 8; ++i)
                         h[8 * q + i] = Vec16<__half>::pack2(f[2 * i], f[2 * i + 1]);
-                    if (P.out_lo) {
+                    if (!P.result) {
 #pragma unroll
                         for (int i = 0; i < 8; ++i) {
                             const float2 r = __half22float2(*(const __half2 *)&h[8 * q + i]);
@@ -593,21 +587,13 @@ __global__ void __launch_bounds__(kMmThreads, 1) k_ns_product(const __grid_const
             // Up to four stores.  Behind the last tile's sums the ring is free, and they need not wait for one another.
             const uint32_t more = ok && tile + step >= P.n_tiles ? min(3u, P.stages * P.stage_bytes / (BN / 16 * kNsStaging)) : 0u;
             const bool mirror = P.symmetric && t.i != (P.tiles_wide ? t.j / 2 : t.j);
-            uint32_t nth = 0;
             auto place = [&](uint32_t n) { return n && n <= more ? tc::saddr(ring) + (warp * more + n - 1) * kNsStaging : staging; };
             auto again = [&](uint32_t n) { return n == 0 || n > more; };
             staging_store<false>(staging, true, lane, h, &maps.oh, col, row0, t.batch);
-            if (P.out_lo) {
-                ++nth;
-                staging_store<false>(place(nth), again(nth), lane, l, &maps.ol, col, row0, t.batch);
-            }
+            staging_store<false>(place(1), again(1), lane, l, &maps.ol, col, row0, t.batch);
             if (mirror) {
-                ++nth;
-                staging_store<true>(place(nth), again(nth), lane, h, &maps.th, row0, col, t.batch);
-                if (P.out_lo) {
-                    ++nth;
-                    staging_store<true>(place(nth), again(nth), lane, l, &maps.tl, row0, col, t.batch);
-                }
+                staging_store<true>(place(2), again(2), lane, h, &maps.th, row0, col, t.batch);
+                staging_store<true>(place(3), again(3), lane, l, &maps.tl, row0, col, t.batch);
             }
         }
         if (lane == 0)
@@ -675,18 +661,17 @@ static bool encode_split(CUtensorMap *map, const __half *p, const Split &s, int6
     return encode_stack(map, p, s.rows, s.cols, s.pitch, s.pitch * s.rows, batch, width, box);
 }
 
-// The tile whose waves over the SMs take least.  Nanoseconds per wave: of 64 elements along k, hi parts alone and all three products, and of what does not
-// depend on k, from 1600 x 1600 and 2 x 1600 x 6400.  At full rate they would be 133, 133, 200, 266 and 400, 400, 600, 800; a stage's copies, up to 32 KB to each
-// CTA, take 260 at 64 bytes a cycle, so hi parts alone gain nothing by less than 256 columns but in the number of tiles.
+// The tile whose waves over the SMs take least.  Nanoseconds per wave: of 64 elements along k, and of what does not depend on k, from 1600 x 1600 and
+// 2 x 1600 x 6400.  At full rate the first would be 400, 400, 600, 800.
 struct NsTiles {
     bool pair;
     uint32_t bn;
-    int one, three, fixed;
+    int step, fixed;
     uint32_t split;   // CTAs that share a tile along k
 };
-static NsTiles ns_tiles(int64_t n, int64_t m, int64_t k, int64_t batch, bool symmetric, bool splits, bool single)
+static NsTiles ns_tiles(int64_t n, int64_t m, int64_t k, int64_t batch, bool symmetric, bool splits)
 {
-    static const NsTiles kinds[] = {{false, 128, 270, 740, 4500, 1}, {true, 128, 300, 600, 5500, 1}, {true, 192, 340, 880, 6000, 1}, {true, 256, 305, 980, 7000, 1}};
+    static const NsTiles kinds[] = {{false, 128, 740, 4500, 1}, {true, 128, 600, 5500, 1}, {true, 192, 880, 6000, 1}, {true, 256, 980, 7000, 1}};
     NsTiles best = {};
     int64_t least = -1;
     for (const NsTiles &c : kinds) {
@@ -697,7 +682,7 @@ static NsTiles ns_tiles(int64_t n, int64_t m, int64_t k, int64_t batch, bool sym
         if (symmetric)
             tiles = c.bn == high ? ti * (ti + 1) / 2 : tj / 2 * (tj / 2 + 1) + (tj & 1 ? tj / 2 + 1 : 0);
         // (what a tile leaves goes out while the next one's sums are formed)
-        const int64_t waves = (tiles * batch + sets - 1) / sets, cost = waves * ((k + 63) / 64) * (single ? c.one : c.three) + c.fixed;
+        const int64_t waves = (tiles * batch + sets - 1) / sets, cost = waves * ((k + 63) / 64) * c.step + c.fixed;
         if (least < 0 || cost < least)
             best = c, least = cost;
     }
@@ -705,7 +690,7 @@ static NsTiles ns_tiles(int64_t n, int64_t m, int64_t k, int64_t batch, bool sym
     // 240 and 115 us, 100 x 1000 151 and 122.
     for (uint32_t split = 2; splits && split <= 8; split *= 2) {
         const int64_t ti = (n + 127) / 128, tiles = ti * (ti + 1) / 2 * batch, stages = (k + 63) / 64, each = (stages + split - 1) / split;
-        const int64_t cost = each * (single ? kinds[0].one : kinds[0].three) + kinds[0].fixed + 3500;
+        const int64_t cost = each * kinds[0].step + kinds[0].fixed + 3500;
         if (tiles <= (split == 2 ? 72 : split == 4 ? 32 : 14) && each * (split - 1) < stages && cost < least)
             best = kinds[0], best.split = split, least = cost;
     }
@@ -720,8 +705,8 @@ static cudaError_t ns_product(const Split &L, const Split &R, const Split *E, co
     P.m = (uint32_t)(CROSS ? R.cols : R.rows);
     P.k = (uint32_t)L.cols;
     P.k_steps = (P.k + 15) / 16;
-    P.stages_k = (P.k + 63) / 64 * (P.single ? 1 : 2);
-    const NsTiles kind = ns_tiles(P.n, P.m, P.k, batch, P.symmetric, !CROSS && !E, P.single);
+    P.stages_k = (P.k + 63) / 64 * 2;
+    const NsTiles kind = ns_tiles(P.n, P.m, P.k, batch, P.symmetric, !CROSS && !E);
     const bool pair = kind.pair;
     const uint32_t high = pair ? 256 : 128;
     P.bn = kind.bn;
@@ -743,7 +728,7 @@ static cudaError_t ns_product(const Split &L, const Split &R, const Split *E, co
     P.loads[1] = mm_limit.loads[1].load();
     P.split = kind.split;
     const uint32_t stages = (P.k + 63) / 64;
-    P.split_stages = (stages + P.split - 1) / P.split * (P.single ? 1 : 2);
+    P.split_stages = (stages + P.split - 1) / P.split * 2;
     if (P.split > 1)
         P.hi = out->hi, P.lo = out->lo, P.out_pitch = out->pitch, P.out_stride = out->pitch * out->rows;
     NsMaps maps = {};
@@ -806,26 +791,6 @@ static double largest_value(double a, double b, double c, double top)
 }
 // a power of two that brings `bound` below 2^15, half of fp16's range
 static double fp16_scale(double bound) { return std::ldexp(1.0, 14 - std::ilogb(std::max(bound, 1e-30))); }
-
-// Where products are of hi parts, fp16's 11 bits, alone.  Singular values are small in the first steps (their squares add up to 1), so C is, and what a rounding adds to
-// C X falls off with the singular value as A does; it counts less the more elements it is averaged over; and what the last step adds no other raises.
-// Errors of the result relative to its size, the largest of spectra that are flat, fall off as 1/i or exponentially, and of 1 to 128 directions with and without
-// noise, five steps, 256 to 1024 rows and one to four times the columns (simulated):
-//   all of the first step 2.7e-4 (from 512 rows on, but for a few directions without any noise 1.1e-4), of the first two 3.0e-4, of the first three 7.9e-4 but for the
-//   third's A A (with it, and in the steps behind, 1e-3 to 2.5e-3 each); A in all steps with those 8.8e-4, and the last step's C X 1.2e-3.
-// Rounding to bf16 loses 1.7e-3, with the last of these 2.0e-3; rounding to fp16 2.1e-4.  More steps raise all of it (ten to 2e-3), so that holds for five.  For
-// coefficients beyond 5, and for few rows, whose products take no time, all parts are taken.
-struct NsSingle {
-    int steps;   // the first ones: all products but, from the third on, A A
-    int gram;    // ... A
-    bool last;   // the last one's C X
-};
-static NsSingle ns_single(int64_t n, int out_dtype, int steps, double a, double b, double c)
-{
-    if (std::max({std::fabs(a), std::fabs(b), std::fabs(c)}) > 5 || n < (out_dtype == CONEF_BF16 ? 256 : 512))
-        return {0, 0, false};
-    return out_dtype == CONEF_BF16 ? NsSingle{3, 5, steps <= 5} : NsSingle{1, 2, false};
-}
 
 struct NsSizes {
     int64_t n, m, pitch_x, pitch_a;   // rows <= columns
@@ -912,22 +877,15 @@ int conef_orthogonalise(const void *x, int dtype, int64_t batch, int64_t rows, i
                        dim3((unsigned)tiles, (unsigned)batch), 256, 0, s, in, X, (uint32_t)tiles_c, sx);
         return 0;
     });
-    const NsSingle single = ns_single(z.n, out_dtype, steps, a, b, c);
     for (int t = 0; t < steps && e == cudaSuccess; ++t) {
         const double sa = fp16_scale(top[t] * top[t]), sc = fp16_scale(largest_factor(b, c, top[t] * top[t])), sy = fp16_scale(top[t + 1]);
         const bool last = t + 1 == steps;
-        const bool one_a = t < single.gram, one_c = t < std::min(2, single.steps), one_x = t < single.steps || (last && single.last);
         NsArgs P = {};
         P.symmetric = 1;
-        P.single = one_a;
-        P.out_lo = !one_c;
         P.f_sum = (float)(sa / (sx * sx));
         e = ns_product<false>(X, X, nullptr, &A, batch, P, s);
         if (e != cudaSuccess)
             break;
-        P.single = one_c;
-        P.add_lo = !one_c;
-        P.out_lo = !one_x;
         P.f_sum = (float)(c * sc / (sa * sa));
         P.f_add = (float)(b * sc / sa);
         e = ns_product<false>(A, A, &A, &C, batch, P, s);
@@ -935,8 +893,6 @@ int conef_orthogonalise(const void *x, int dtype, int64_t batch, int64_t rows, i
             break;
         const double to = last ? scale : sy;
         NsArgs U = {};
-        U.single = one_x;
-        U.add_lo = U.out_lo = 1;
         U.f_sum = (float)(to / (sc * sx));
         U.f_add = (float)(a * to / sx);
         if (last) {
