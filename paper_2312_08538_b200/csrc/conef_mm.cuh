@@ -205,6 +205,7 @@ __global__ void __launch_bounds__(kMmThreads, 1) k_matmul(const __grid_constant_
     tc::fence_after();
     grid_release();
     grid_wait();
+    asm volatile("fence.proxy.async;" ::: "memory");   // (what the launch before stored, ordinary stores, is read by copies)
 
     // step ks of a tile into stage s: row tm of scales of A (128 rows of codes), columns from n0 on
     auto load = [&](uint32_t s, uint32_t ks, uint32_t tm, uint32_t n0) {
