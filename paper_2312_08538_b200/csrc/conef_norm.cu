@@ -303,14 +303,17 @@ __global__ void __launch_bounds__(1024) k_rms_norm_long(const __grid_constant__ 
 }
 
 // ------------------------------------------------------------------ the gradient
-// With n = h r and g = dy w: dx = r (g - n mean(g n)) + add, dw = the sum over rows of dy n.  The columns' sums stay in registers (in 32 bits: rows of a group are
-// few) and are written once per block, to be added in 64 bits and in their order by k_norm_columns: results do not depend on which block is done first.
+// With n = h r and g = dy w: dx = r (g - n mean(g n)) + add, dw = the sum over rows of dy n.  The columns' sums stay in registers, in 32 bits for kNormChain rows at
+// most, and are written once per block and so many rows, to be added in 64 bits and in their order by k_norm_columns: results do not depend on which block is done first.
+// (One chain for all rows of a block loses up to 2^-24 with each: 4 columns of 20 million rows, 4223 to a warp, 6e-5.)
+constexpr uint32_t kNormChain = 256;
 struct NormGradArgs {
     const void *dy, *h, *w, *add;
     void *dx;
     const float *rstd;
     const float *means;     // per row, where a row has more columns than a group
-    float *partial;         // per block and column, or NULL
+    float *partial;         // per segment, block and column, or NULL
+    uint32_t segments;      // of kNormChain rows of a block's (a warp's)
     int64_t rows, cols;
     uint32_t dy_ld, h_ld, add_ld, dx_ld;
     float share;
@@ -350,7 +353,8 @@ __global__ void __launch_bounds__(ALONE ? 256 : 1024, ALONE ? 4 : 1) k_norm_grad
     for (int k = 0; k < rows.DEPTH - 1; ++k)
         ask(row + k * step);
     float r = row < (uint32_t)A.rows ? A.rstd[row] : 0.f;
-    for (int turn = 0; row < (uint32_t)A.rows; row += step, turn ^= 1) {
+    int turn = 0;
+    auto take = [&] {
         ask(row + (rows.DEPTH - 1) * step);
         const float root = r;
         r = row + step < (uint32_t)A.rows ? A.rstd[row + step] : 0.f;
@@ -393,26 +397,32 @@ __global__ void __launch_bounds__(ALONE ? 256 : 1024, ALONE ? 4 : 1) k_norm_grad
         rows.done();
         a.pack(d);
         a.store((T *)A.dx + (uint64_t)row * A.dx_ld, c0, cols, lane, A.aligned32);
-    }
-    if (!A.partial)
-        return;
-    if constexpr (ALONE) {   // a block's warps one after the other
-#pragma unroll
-        for (int q = 0; q < N; ++q)
-            other[(warp * N + q) * 32 + lane] = sums[q];
-        __syncthreads();
-        if (warp > 0)
-            return;
-        for (int i = 1; i < 8; ++i)
+    };
+    for (uint32_t segment = 0; segment < A.segments; ++segment) {
+        for (uint32_t i = 0; i < kNormChain && row < (uint32_t)A.rows; ++i, row += step, turn ^= 1)
+            take();
+        if (!A.partial)
+            continue;
+        if constexpr (ALONE) {   // a block's warps one after the other
 #pragma unroll
             for (int q = 0; q < N; ++q)
-                sums[q] += other[(i * N + q) * 32 + lane];
-    }
+                other[(warp * N + q) * 32 + lane] = sums[q];
+            __syncthreads();
+            if (warp == 0)
+                for (int i = 1; i < 8; ++i)
 #pragma unroll
-    for (int q = 0; q < N; ++q) {
-        const uint32_t c = lane_col<VEC, N>(c0, lane, q);
-        if (c < cols)
-            A.partial[(uint64_t)block * (uint32_t)A.cols + c] = sums[q];
+                    for (int q = 0; q < N; ++q)
+                        sums[q] += other[(i * N + q) * 32 + lane];
+            __syncthreads();
+        }
+        float *const partial = A.partial + ((uint64_t)segment * blocks + block) * cols;
+#pragma unroll
+        for (int q = 0; q < N; ++q) {
+            const uint32_t c = lane_col<VEC, N>(c0, lane, q);
+            if (c < cols && (!ALONE || warp == 0))
+                partial[c] = sums[q];
+            sums[q] = 0.f;
+        }
     }
 }
 // ... the rows' means alone, a block each
@@ -481,6 +491,14 @@ static uint32_t norm_blocks(int64_t rows, int64_t cols)
     return (uint32_t)std::min<int64_t>((int64_t)kPlanSMs * (32 / norm_warps(cols)), cols <= kNormWarp ? (rows + 7) / 8 : rows);
 }
 
+// how often a block of the gradient writes its columns' sums
+static uint32_t norm_segments(int64_t rows, int64_t cols)
+{
+    const int64_t chains = (int64_t)norm_blocks(rows, cols) * (cols <= kNormWarp ? 8 : 1);
+    return (uint32_t)(((rows + chains - 1) / chains + kNormChain - 1) / kNormChain);
+}
+static size_t norm_partials(int64_t rows, int64_t cols) { return (size_t)norm_blocks(rows, cols) * norm_segments(rows, cols) * (size_t)cols; }
+
 template <auto KERNEL, int BYTES, class A>   // BYTES: of a warp
 static cudaError_t launch_norm(dim3 grid, int warps, cudaStream_t s, const A &args)
 {
@@ -519,7 +537,7 @@ static cudaError_t norm_grad(NormGradArgs A, float *means, float *dw, cudaStream
                                 : launch_norm<k_norm_grad<T, VEC, false, false>, bytes>(dim3(blocks), warps, s, A);
     }
     if (e == cudaSuccess && dw)
-        e = launch(k_norm_columns, dim3((unsigned)((A.cols + 31) / 32)), 1024, 0, s, (const float *)A.partial, (uint32_t)blocks, A.cols, dw);
+        e = launch(k_norm_columns, dim3((unsigned)((A.cols + 31) / 32)), 1024, 0, s, (const float *)A.partial, (uint32_t)blocks * A.segments, A.cols, dw);
     return e;
 }
 
@@ -584,7 +602,7 @@ int conef_rms_norm_grad_bytes(int64_t rows, int64_t cols, size_t *bytes)
         return CONEF_ERR_INVALID_ARG;
     if (rows >= (1ll << 31) || cols >= (1ll << 31))
         return CONEF_ERR_UNSUPPORTED;
-    *bytes = rows && cols ? ((size_t)norm_blocks(rows, cols) * (size_t)cols + (cols > kNormWidest ? (size_t)rows : 0)) * sizeof(float) : 0;
+    *bytes = rows && cols ? (norm_partials(rows, cols) + (cols > kNormWidest ? (size_t)rows : 0)) * sizeof(float) : 0;
     return CONEF_OK;
 }
 
@@ -614,9 +632,9 @@ int conef_rms_norm_grad(const void *dy, const void *h, const void *weight, const
     if (!workspace || workspace_bytes < need)
         return CONEF_ERR_WORKSPACE_TOO_SMALL;
     float *const partial = (float *)workspace;
-    NormGradArgs A = {dy, h, weight, add, dx, rstd, nullptr, dweight ? partial : nullptr, rows, cols, (uint32_t)dy_ld, (uint32_t)h_ld, (uint32_t)add_ld, (uint32_t)dx_ld, 1.f / (float)cols,
+    NormGradArgs A = {dy, h, weight, add, dx, rstd, nullptr, dweight ? partial : nullptr, norm_segments(rows, cols), rows, cols, (uint32_t)dy_ld, (uint32_t)h_ld, (uint32_t)add_ld, (uint32_t)dx_ld, 1.f / (float)cols,
                       weight_dtype == CONEF_F32, false, ((uintptr_t)weight & 15) == 0};
-    float *const means = partial + (size_t)norm_blocks(rows, cols) * cols;
+    float *const means = partial + norm_partials(rows, cols);
     return with_elem(dtype, [&](auto t) {
         using T = decltype(t);
         auto on = [&](uintptr_t bytes) {
