@@ -441,7 +441,8 @@ int conef_f8_bytes(int64_t rows, int64_t cols, size_t *code_bytes /* HOST out */
  * forms then stand for the same values. */
 int conef_f8_quantise(const void *x, int dtype, int64_t rows, int64_t cols, int64_t ld, int kind, int square, void *codes, void *scales, void *codes_t, void *scales_t,
                       conef_stream stream);
-/* The values of a form, code 2^E, rounded to the type (exact in fp32 and bf16 below 2^128, and infinite there). */
+/* The values of a form, code 2^E, rounded to the type, nearest even: exact in fp32, and in bf16 where they are multiples of 2^-133 (all are where E >= -124, of
+ * CONEF_E5M2 -117, and those of 2^-126 or more); 2^128 and more is infinite. */
 int conef_f8_dequantise(const void *codes, const void *scales, int64_t rows, int64_t cols, int kind, void *out, int dtype, int64_t ld, conef_stream stream);
 /* out[i][j] = sum over c < k of A[i][c] B[j][c] for forms A (m x k) and B (n x k) of either kind, accumulated in fp32 and rounded once to the type.  What
  * conef_mx4_matmul says of bytes past a row's end, of k = 0 and of waits holds here too; conef_f8_timeouts counts these. */

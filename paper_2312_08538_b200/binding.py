@@ -483,7 +483,7 @@ def f8_quantise(x: torch.Tensor, forms: str = "rows", kind: str = "e4m3", square
 
 
 def f8_dequantise(a: F8, dtype: torch.dtype = torch.float32, stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
-    """The values of a form, rows x cols (exact in float32 and bfloat16)."""
+    """The values of a form, rows x cols, rounded to the type (exact in float32, and in bfloat16 but for multiples of less than 2^-133)."""
     _f8_check(a, "f8_dequantise")
     code = _ELEM.get(dtype)
     if code is None:
