@@ -453,7 +453,7 @@ int conef_f8_timeouts(int64_t *count /* HOST out */, conef_stream stream);
 /* Root-mean-square norm of x's rows, behind the addition of a residual where `add` is not NULL: h = x + add, rounded to the type and written (without add, h is x
  * and the argument NULL); rstd[r] = 1 / sqrt(mean over the row of h^2 + eps), computed in 64 bits and rounded to fp32 (DEVICE, one per row); and h rstd weight,
  * either rounded to the type into y, or in 8-bit floats into (codes, scales) and / or (codes_t, scales_t) as conef_f8_quantise has them: the codes and scales are
- * those of the exact products (where these are above 2^-100 in size).  y and the forms may all be NULL.  weight: `cols` elements of the matrices' type
+ * those of the exact products (where these are above 2^-100 in size; fp32's 2^128 and more counts as infinite).  y and the forms may all be NULL.  weight: `cols` elements of the matrices' type
  * or of CONEF_F32.  A row that holds an infinity or a NaN has rstd 0 or NaN, and what follows by IEEE rules.  h may be x or add, y may be x, add or h
  * (with the same ld); otherwise outputs do not overlap inputs. */
 int conef_rms_norm(const void *x, const void *add, const void *weight, int dtype, int weight_dtype, int64_t rows, int64_t cols, int64_t x_ld, int64_t add_ld, double eps,
