@@ -467,7 +467,8 @@ int conef_rms_norm_grad(const void *dy, const void *h, const void *weight, const
                         int64_t dy_ld, int64_t h_ld, int64_t add_ld, void *dx, int64_t dx_ld, float *dweight, void *workspace, size_t workspace_bytes,
                         conef_stream stream);
 
-/* Newton-Schulz orthogonalisation (Muon) of `batch` matrices of rows x cols (elements of a row are consecutive, rows `ld` apart, matrices `stride`): X_0 = x / |x|, the
+/* Newton-Schulz orthogonalisation (Muon) of `batch` matrices of rows x cols (elements of a row are consecutive, rows `ld` apart, matrices `stride`, behind one another or
+ * each between the others' rows, so that none share an element): X_0 = x / |x|, the
  * Frobenius norm (a matrix of zeros stays one), `steps` (1..32) times X <- (c0 + c1 A + c2 A^2) X with A = X X^T, the shorter side in front, and
  * out = scale X, rounded once to CONEF_BF16 or CONEF_F16.  Operands of all products are held to 22 bits under a power of two and summed in fp32: ahead of
  * that rounding the result is within 2^-14 of the exact one's size for up to ten steps of Muon's quintic.  coefficients: HOST, three; the polynomial s (c0 + c1 s^2 + c2 s^4) has to keep singular values below 10^4 in size over the steps (else

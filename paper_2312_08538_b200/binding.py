@@ -658,7 +658,8 @@ def orthogonalise(x: torch.Tensor, steps: int = 5, scale: float = 1.0, coefficie
                     _refuse(where, f"the matrices of {name} are not evenly spaced")
                 expect = gap * size
             batch *= size
-        if batch > 1 and step < (rows - 1) * ld + cols and rows and cols:
+        behind, between = step >= (rows - 1) * ld + cols, step >= cols and (batch - 1) * step + cols <= ld   # (one after the other; row by row among one another's)
+        if batch > 1 and rows and cols and not (behind or between):
             _refuse(where, f"the matrices of {name} overlap")
         return batch, ld, step
 

@@ -792,6 +792,12 @@ static double largest_value(double a, double b, double c, double top)
 // a power of two that brings `bound` below 2^15, half of fp16's range
 static double fp16_scale(double bound) { return std::ldexp(1.0, 14 - std::ilogb(std::max(bound, 1e-30))); }
 
+// whether no two matrices of a stack share an element: one behind the other, or row by row among one another's rows
+static bool ns_apart(int64_t batch, int64_t rows, int64_t cols, int64_t ld, int64_t stride)
+{
+    return stride >= (rows - 1) * ld + cols || (stride >= cols && stride <= ld && (batch - 1) * stride + cols <= ld);
+}
+
 struct NsSizes {
     int64_t n, m, pitch_x, pitch_a;   // rows <= columns
     bool flip;
@@ -833,7 +839,7 @@ int conef_orthogonalise(const void *x, int dtype, int64_t batch, int64_t rows, i
         return rc;
     if (batch < 0 || out_dtype == CONEF_F32 || steps < 1 || steps > 32 || !coefficients || !std::isfinite(scale) || std::fabs(scale) > 1e30)
         return CONEF_ERR_INVALID_ARG;
-    if (batch > 1 && rows && cols && (stride < (rows - 1) * ld + cols || out_stride < (rows - 1) * out_ld + cols))
+    if (batch > 1 && rows && cols && !(ns_apart(batch, rows, cols, ld, stride) && ns_apart(batch, rows, cols, out_ld, out_stride)))
         return CONEF_ERR_INVALID_ARG;
     // bounds of X before each step: a power of two each that keeps them within fp16
     double top[33];
@@ -901,8 +907,8 @@ int conef_orthogonalise(const void *x, int dtype, int64_t batch, int64_t rows, i
             U.result_stride = batch > 1 ? out_stride : 0;
             U.flip = z.flip;
             U.dtype = (uint32_t)out_dtype;
-            // (a tiled copy writes a row's last 16 bytes whole, whatever the map says of its end)
-            U.wide = (((uintptr_t)out | (uint64_t)(U.result_ld | U.result_stride | cols) * 2) & 15) == 0;
+            // (a tiled copy writes a row's last 16 bytes whole, whatever the map says of its end; a map's matrices follow one another)
+            U.wide = (((uintptr_t)out | (uint64_t)(U.result_ld | U.result_stride | cols) * 2) & 15) == 0 && (batch == 1 || out_stride >= out_ld);
         }
         e = ns_product<true>(C, X, &X, last ? nullptr : &Y, batch, U, s);
         std::swap(X, Y);
