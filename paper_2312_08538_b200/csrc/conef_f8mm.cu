@@ -13,6 +13,14 @@ struct F8Format {
     static constexpr bool kSplits = true;
     static int64_t row_bytes(int64_t k) { return f8_blocks(k) * 128; }
     static int64_t scale_tiles(int64_t k) { return f8_scale_tiles(k); }
+    // Nanoseconds per wave of tiles, as the 4-bit format has them (conef_mx4mm.cu): a step brings and multiplies the same 32 bytes of a row, and copies, not products, are
+    // what a wave waits for.  Microseconds into bf16, single CTAs of 64 to 256 columns and pairs of 128 to 256, the choice marked:
+    //   8192 x 6400 x 1600  126.8  84.6  77.1  76.8   79.9  69.8* 75.4        1111 x 2601 x 651   9.7  9.2  7.6*  8.9   11.0   9.3  10.1
+    //   8192 x 1600 x 6400  116.9  79.1  71.1  82.5   77.2  63.6* 76.3        4000 x 4000 x 300  19.2 14.9 14.3* 13.3   18.0  15.8  15.9
+    //   6400 x 1600 x 8192  121.2  82.3  80.5  85.1   80.6  72.4  75.4*       300 x 300 x 1600    7.1* 7.7  8.6  10.0    8.8   9.3  10.8
+    //   8192 x 1600 x 1600   37.0  27.2  24.2  29.0   26.6  23.4* 29.2        1000 x 1600 x 1600  9.8  7.7* 8.2   9.4    8.8   9.0  10.3
+    //   2048 x 6400 x 1600   37.4  27.8  25.4  27.1   26.7  23.3* 26.3        128 x 1600 x 6400  13.6 14.5 16.0  19.6   15.9  16.5  20.2 (10.7 by clusters of eight)
+    // Where it misses the fastest that costs 4 % (6400 x 1600 x 8192) and 7 % (4000 x 4000 x 300).
     static int per_step(int pair, int width)
     {
         static const int table[2][4] = {{45, 52, 67, 88}, {0, 48, 60, 73}};

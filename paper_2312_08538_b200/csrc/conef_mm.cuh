@@ -436,7 +436,7 @@ static bool encode(CUtensorMap *map, CUtensorMapDataType type, int elem, const v
                                             CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-// Columns per tile, and whether pairs of CTAs take tiles of 256 rows: the choice whose waves of tiles over the SMs take least.  F::kPerStep and F::kPerTile have
+// Columns per tile, and whether pairs of CTAs take tiles of 256 rows: the choice whose waves of tiles over the SMs take least.  F::per_step() and F::per_tile() have
 // what a wave takes in nanoseconds, by columns (64, 128, 192, 256), per instruction's step along k (single CTAs, pairs) and beside that; a launch of pairs takes a
 // microsecond more.  Pairs of 64 columns are left out: they take as many waves as single CTAs at least, none of them shorter.
 struct MmChoice {

@@ -662,7 +662,13 @@ static bool encode_split(CUtensorMap *map, const __half *p, const Split &s, int6
 }
 
 // The tile whose waves over the SMs take least.  Nanoseconds per wave: of 64 elements along k, and of what does not depend on k, from 1600 x 1600 and
-// 2 x 1600 x 6400.  At full rate the first would be 400, 400, 600, 800.
+// 2 x 1600 x 6400.  At full rate the first would be 400, 400, 600, 800.  All of five steps, us, with the choice, which is made for each of a step's three products, and with tiles
+// of one kind throughout (X X^T and A A by pairs of 128 columns in place of 192):
+//   256 x 512            140   146   145   152   197        1024 x 4096       384   442   389   435   585        1600 x 6400       761   887   762   803  1093
+//   512 x 512            174   178   178   191   257        1600 x 1600       350   409   365   351   495        2 x 6400 x 1600  1435  1623  1507  1518  1435
+//   768 x 768            199   212   209   222   312        2048 x 2048       449   508   447   518   627        4 x 1600 x 1600   933  1015   935   964  1014
+//   12 x 768 x 768       404   416   387   387   419        3 x 700 x 2500    425   441   403   415   582
+// (Where it misses the fastest, in stacks of small matrices, that costs 4 and 5 %.)
 struct NsTiles {
     bool pair;
     uint32_t bn;
