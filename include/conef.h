@@ -453,9 +453,9 @@ int conef_f8_timeouts(int64_t *count /* HOST out */, conef_stream stream);
 /* Root-mean-square norm of x's rows, behind the addition of a residual where `add` is not NULL: h = x + add, rounded to the type and written (without add, h is x
  * and the argument NULL); rstd[r] = 1 / sqrt(mean over the row of h^2 + eps), computed in 64 bits and rounded to fp32 (DEVICE, one per row); and h rstd weight,
  * either rounded to the type into y, or in 8-bit floats into (codes, scales) and / or (codes_t, scales_t) as conef_f8_quantise has them: the codes and scales are
- * those of the exact products (where these are above 2^-100 in size; fp32's 2^128 and more counts as infinite).  y and the forms may all be NULL.  weight: `cols` elements of the matrices' type
- * or of CONEF_F32.  A row that holds an infinity or a NaN has rstd 0 or NaN, and what follows by IEEE rules.  h may be x or add, y may be x, add or h
- * (with the same ld); otherwise outputs do not overlap inputs. */
+ * those of the exact products (where these are above 2^-100 in size; fp32's 2^128 and more counts as infinite).  y and the forms may all be NULL.
+ * weight: `cols` elements of the matrices' type or of CONEF_F32.  A row that holds an infinity or a NaN has rstd 0 or NaN, and what follows by IEEE rules.  h may be x or
+ * add, y may be x, add or h (with the same ld); otherwise outputs do not overlap inputs. */
 int conef_rms_norm(const void *x, const void *add, const void *weight, int dtype, int weight_dtype, int64_t rows, int64_t cols, int64_t x_ld, int64_t add_ld, double eps,
                    void *h, int64_t h_ld, float *rstd, void *y, int64_t y_ld, int kind, void *codes, void *scales, void *codes_t, void *scales_t, conef_stream stream);
 /* Its gradient: with n = h rstd and g = dy weight, dx = rstd (g - n mean(g n)) + add, the gradient of x and of the residual (add: the gradient that reaches h
@@ -468,10 +468,11 @@ int conef_rms_norm_grad(const void *dy, const void *h, const void *weight, const
                         conef_stream stream);
 
 /* Newton-Schulz orthogonalisation (Muon) of `batch` matrices of rows x cols (elements of a row are consecutive, rows `ld` apart, matrices `stride`, behind one another or
- * each between the others' rows, so that none share an element): X_0 = x / |x|, the
- * Frobenius norm (a matrix of zeros stays one), `steps` (1..32) times X <- (c0 + c1 A + c2 A^2) X with A = X X^T, the shorter side in front, and
- * out = scale X, rounded once to CONEF_BF16 or CONEF_F16.  Operands of all products are held to 22 bits under a power of two and summed in fp32: ahead of
- * that rounding the result is within 2^-14 of the exact one's size for up to ten steps of Muon's quintic.  coefficients: HOST, three; the polynomial s (c0 + c1 s^2 + c2 s^4) has to keep singular values below 10^4 in size over the steps (else
+ * each between the others' rows, so that none share an element): X_0 = x / |x|, the Frobenius norm (a matrix of zeros stays one), `steps` (1..32) times
+ * X <- (c0 + c1 A + c2 A^2) X with A = X X^T, the shorter side in front, and out = scale X, rounded once to CONEF_BF16 or CONEF_F16.  Operands of all products are held to 22 bits under a power of two and summed in fp32, which the
+ * tensor cores cut off, not round, every 16 elements: ahead of the rounding to 16 bits the result is within 2^-12 of the exact one's size for up to ten steps of Muon's quintic and
+ * sides of up to 16384 (of some hundred elements, and five steps, 1e-5).
+ * coefficients: HOST, three; the polynomial s (c0 + c1 s^2 + c2 s^4) has to keep singular values below 10^4 in size over the steps (else
  * CONEF_ERR_INVALID_ARG).  A matrix that holds an infinity or a NaN becomes NaN.  out may be x (with the same distances).  `workspace`: DEVICE, 128-byte
  * aligned, of the size that conef_orthogonalise_bytes gives; it is the call's until that has run on the stream.  Waits are bounded as conef_mx4_matmul's,
  * conef_orthogonalise_timeouts counts these. */
